@@ -174,7 +174,11 @@ def _own_norm(s):
         T, Hq, Hk, d, dt = c["T"], c["Hq"], c["Hk"], c["d"], s["q"].dtype
         s["desc"] = lib.qknorm_desc(s["q"], s["k"], rot=c["rot"], interleaved=c["inter"], n_pos=s["table"].shape[0],
                                     eps=EPS)
-        s["oq"], s["ok"] = (torch.empty((T, h, d), device=DEV, dtype=dt) for h in (Hq, Hk))
+        if c["bwd"]:                                                  # gradients lie as q and k do
+            g = torch.empty((T, Hq + 2 * Hk, d), device=DEV, dtype=dt)
+            s["oq"], s["ok"] = g[:, :Hq], g[:, Hq:Hq + Hk]
+        else:
+            s["oq"], s["ok"] = (torch.empty((T, h, d), device=DEV, dtype=dt) for h in (Hq, Hk))
         s["og"] = torch.empty((2, d), device=DEV, dtype=torch.float32)
         s["ws"] = lib.workspace(lib.paragan_qknorm_ws_size(s["desc"]))
     if not c["bwd"]:
