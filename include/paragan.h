@@ -241,6 +241,115 @@ int paragan_attn_bwd(paragan_ctx* ctx, const paragan_attn_desc* d,
                      const void* dy, void* dx, float* grads, void* ws);
 
 /* ---------------------------------------------------------------------
+ * Operators of transformer blocks, for generators and discriminators that
+ * mix tokens (image tokens, class tokens in front of them) with more than
+ * the block above: norms of query and key heads with the position rotation,
+ * and multi-head attention with a window, first tokens that stay visible,
+ * ragged lengths and a learned relative position bias.  The projections
+ * around them are the caller's.  Pointers are 16-byte aligned, strides are
+ * in elements and multiples of 8.  The current device must be the context's.
+ *
+ * Norm and rotation of every head row x (d elements) of q and k, token t:
+ *   n = x * (mean(x^2) + eps)^(-1/2) * gain    (gain_q or gain_k, [d] fp32)
+ * then each pair (a, b) of the first `rot` elements becomes
+ *   (a c - b s, a s + b c),  (c, s) = table[pos[t]][pair].
+ * Pairs are (i, i + rot/2), or (2i, 2i + 1) with interleaved.  table: fp32
+ * [n_pos][rot/2][2], any angles (for instance half of the pairs turned by a
+ * token's row and half by its column); NULL when rot is 0.  pos: [T] device,
+ * or NULL for t mod n_pos.  A token whose position is outside [0, n_pos) is
+ * padding: its rows are not read, its outputs and gradients are zero.
+ * Token t of q starts at q + t * ldq, its heads follow one another; outputs
+ * likewise with ldqo and ldko.  dq, dk (the gradients of q, k) lie as q, k
+ * do, dqo, dko (of the outputs) as the outputs do.  Outputs may be the
+ * inputs (same pointer and stride); they must not overlap otherwise.
+ * Statistics and sums are fp32.
+ * ------------------------------------------------------------------- */
+typedef struct {
+  int64_t T;                       /* tokens, 1 .. 2^31 - 1 */
+  int32_t Hq, Hk;                  /* query and key heads, >= 1 */
+  int32_t d;                       /* head width, a multiple of 8 up to 256 */
+  int32_t rot;                     /* rotated elements, a multiple of 16 up to d */
+  int32_t interleaved;             /* pair order, 0 or 1 */
+  int32_t n_pos;                   /* rows of the table, >= 1 */
+  int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: q, k, outputs, gradients */
+  float eps;                       /* > 0 */
+  int64_t ldq, ldk, ldqo, ldko;    /* >= heads * d */
+} paragan_qknorm_desc;
+
+int paragan_qknorm_check(const paragan_qknorm_desc* d);
+/* Workspace of the backward. */
+int paragan_qknorm_ws_size(const paragan_qknorm_desc* d, size_t* ws_bytes);
+int paragan_qknorm_fwd(paragan_ctx* ctx, const paragan_qknorm_desc* d,
+                       const void* q, const void* k, const float* gain_q,
+                       const float* gain_k, const float* table,
+                       const int32_t* pos, void* qo, void* ko);
+/* Writes dq, dk and the gains' gradients ([d] fp32, overwritten). */
+int paragan_qknorm_bwd(paragan_ctx* ctx, const paragan_qknorm_desc* d,
+                       const void* q, const void* k, const float* gain_q,
+                       const float* gain_k, const float* table,
+                       const int32_t* pos, const void* dqo, const void* dko,
+                       void* dq, void* dk, float* dgain_q, float* dgain_k,
+                       void* ws);
+
+/* Multi-head attention, bf16:
+ *   S = scale * q k^T + bias,  P = softmax over the visible keys,  o = P v,
+ * query head h reading key head h / (Hq / Hk).  Sequence b has len_q[b]
+ * queries and len_k[b] keys (device arrays [B], or NULL for Sq and Sk; values
+ * are clamped to [0, Sq] and [0, Sk]); query i stands at position
+ * p = i + len_k - len_q, so a few new queries are the last tokens of a cache.
+ * Key j is visible to it when j < len_k and
+ *   causal: j <= p;   window > 0: |p - j| < window or j < n_sink.
+ * A query that sees nothing gets zeros.  Rows at and past len_q of o (and
+ * of dq), rows at and past len_k of dk and dv, are written as zeros.  Keys
+ * and values at and past len_k, and keys that no query of the call sees, may
+ * hold anything; a NaN or infinity in a key or value that some query sees
+ * can reach other queries.
+ * bias (n_buckets > 0): table fp32 [Hq][n_buckets] at the bucket of j - p.
+ * With causal all buckets are for distances n = p - j >= 0; otherwise the
+ * first half is for n = p - j >= 0 and the second for n = j - p > 0.  Of the
+ * m buckets of a side, n < m/2 (rounded down) has bucket n, and above
+ *   m/2 + floor(log(n / (m/2)) / log(max_distance / (m/2)) * (m - m/2)),
+ * the last one from max_distance on.  Entries may be -infinity (such keys
+ * are not visible); the lowest finite value is a number like any other.
+ * Element (b, s, h, c) of a tensor is at b * stride[0] + s * stride[1]
+ * + h * stride[2] + c.  q, k, v may repeat through zero strides in the
+ * forward; o, and in the backward q, k and v (whose strides dq, dk and dv
+ * share), must not overlap themselves.  dout has o's strides.
+ * Softmax statistics and sums are fp32; P and dS are rounded to bf16 as
+ * matrix operands. */
+typedef struct {
+  int32_t B, Sq, Sk;               /* sequences, queries and keys of each, >= 1; Sq, Sk <= 2^30;
+                                      B * heads * ceil(S / 128) below 2^24 for either */
+  int32_t Hq, Hk;                  /* query and key heads, Hq a multiple of Hk */
+  int32_t d;                       /* head width, a multiple of 8 up to 128 */
+  int32_t causal;                  /* 0 or 1 */
+  int32_t window, n_sink;          /* 0: no window; n_sink counts with a window only; <= 2^30 */
+  int32_t n_buckets, max_distance; /* 0: no bias; up to 256 (causal >= 2, otherwise even and >= 4);
+                                      max_distance above half of a side's buckets, up to 512 */
+  float scale;                     /* > 0, finite */
+  int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+} paragan_mha_desc;
+
+int paragan_mha_check(const paragan_mha_desc* d);
+/* saved: kept from a forward to its backward; ws: scratch of either call. */
+int paragan_mha_sizes(const paragan_mha_desc* d, size_t* saved_bytes,
+                      size_t* ws_bytes);
+/* saved may be NULL when no backward follows (sampling, new tokens over a
+ * cache: the form for few queries splits the keys over the card). */
+int paragan_mha_fwd(paragan_ctx* ctx, const paragan_mha_desc* d,
+                    const void* q, const void* k, const void* v,
+                    const float* table, const int32_t* len_q,
+                    const int32_t* len_k, void* o, void* saved, void* ws);
+/* From the forward's o and saved, and dout: dq, dk, dv and dtable (fp32
+ * [Hq][n_buckets], overwritten; NULL without a bias). */
+int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d,
+                    const void* q, const void* k, const void* v,
+                    const float* table, const int32_t* len_q,
+                    const int32_t* len_k, const void* o, const void* saved,
+                    const void* dout, void* dq, void* dk, void* dv,
+                    float* dtable, void* ws);
+
+/* ---------------------------------------------------------------------
  * Generator output layer (the last generator layer of the model,
  * Evaluation "Experiment Setup"; kept in fp32 arithmetic by the paper's
  * mixed-precision placement, Design "System Optimizations"):

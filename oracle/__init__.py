@@ -18,4 +18,5 @@ layers    convolution, resampling, batch norm, spectral norm, attention,
           hinge loss, Adam (forward and backward)
 blocks    BigGAN generator / discriminator residual blocks
 biggan    parameter layout, full networks, the G+D train step
+token     head norms with rotation, multi-head attention with masks and bias
 """

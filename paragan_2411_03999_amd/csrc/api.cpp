@@ -6,6 +6,7 @@
 #include "../../include/paragan.h"
 #include "blocks.hpp"
 #include "net.hpp"
+#include "token.hpp"
 #include <cmath>
 
 using namespace pg;
@@ -444,6 +445,177 @@ extern "C" int paragan_attn_bwd(paragan_ctx* ctx, const paragan_attn_desc* d, co
     Params P{&L, "", params, nullptr, grads};
     Exec ex{ctx->stream, ctx->n_cu, ws, t.ws_size(ctx->n_cu)};
     t.bwd(ex, P, x, dy, dx, true);
+  })
+}
+
+// ------------------------------------------------------------ token attention operators
+static void on_device(const paragan_ctx* ctx, const char* what) {
+  int dev = -1;
+  PG_HIP(hipGetDevice(&dev));
+  PG_CHECK(dev == ctx->device, std::string(what) + ": the context's device is not the current one");
+}
+static void need16(const void* p, const char* what) {
+  need(p, what);
+  if (((uintptr_t)p & 15) != 0) throw Error{PARAGAN_EINVAL, std::string(what) + " is not 16-byte aligned"};
+}
+
+static QkNorm make_qk(const paragan_qknorm_desc* d) {
+  if (!d) throw Error{PARAGAN_EINVAL, "qknorm: desc is NULL"};
+  PG_CHECK(d->T >= 1 && d->T < (1LL << 31), "qknorm: T must be 1 .. 2^31 - 1");
+  PG_CHECK(d->Hq >= 1 && d->Hk >= 1 && (int64_t)d->Hq + d->Hk <= (1 << 20), "qknorm: Hq, Hk must be >= 1 (and at most 2^20 together)");
+  PG_CHECK(d->d >= 8 && d->d <= 256 && d->d % 8 == 0, "qknorm: d must be a multiple of 8 up to 256");
+  PG_CHECK(d->rot >= 0 && d->rot <= d->d && d->rot % 16 == 0, "qknorm: rot must be a multiple of 16 up to d");
+  PG_CHECK(d->interleaved == 0 || d->interleaved == 1, "qknorm: interleaved must be 0 or 1");
+  PG_CHECK(d->n_pos >= 1, "qknorm: n_pos must be >= 1");
+  PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "qknorm: dtype must be PARAGAN_BF16 or PARAGAN_F32");
+  PG_CHECK(d->eps > 0.f && std::isfinite(d->eps), "qknorm: eps must be > 0");
+  const int64_t wq = (int64_t)d->Hq * d->d, wk = (int64_t)d->Hk * d->d;
+  PG_CHECK(d->ldq >= wq && d->ldqo >= wq && d->ldk >= wk && d->ldko >= wk, "qknorm: a token stride is below heads * d");
+  PG_CHECK(d->ldq % 8 == 0 && d->ldqo % 8 == 0 && d->ldk % 8 == 0 && d->ldko % 8 == 0,
+           "qknorm: token strides must be multiples of 8");
+  for (int64_t ld : {d->ldq, d->ldqo, d->ldk, d->ldko})
+    PG_CHECK(ld < (1LL << 60) / d->T, "qknorm: a token stride is too large");
+  QkNorm a;
+  a.T = d->T; a.Hq = d->Hq; a.Hk = d->Hk; a.d = d->d; a.rot = d->rot; a.n_pos = d->n_pos;
+  a.inter = d->interleaved == 1; a.f32 = d->dtype == PARAGAN_F32; a.eps = d->eps;
+  a.ldq = d->ldq; a.ldk = d->ldk; a.ldqo = d->ldqo; a.ldko = d->ldko;
+  return a;
+}
+
+extern "C" int paragan_qknorm_check(const paragan_qknorm_desc* d) { PG_TRY(nullptr, make_qk(d)) }
+
+extern "C" int paragan_qknorm_ws_size(const paragan_qknorm_desc* d, size_t* ws_bytes) {
+  PG_TRY(nullptr, {
+    need(ws_bytes, "ws_bytes");
+    *ws_bytes = qknorm_ws_bytes(make_qk(d));
+  })
+}
+
+extern "C" int paragan_qknorm_fwd(paragan_ctx* ctx, const paragan_qknorm_desc* d, const void* q, const void* k,
+                                  const float* gain_q, const float* gain_k, const float* table, const int32_t* pos,
+                                  void* qo, void* ko) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const QkNorm a = make_qk(d);
+    need16(q, "q"); need16(k, "k"); need(gain_q, "gain_q"); need(gain_k, "gain_k");
+    if (a.rot) need16(table, "table");
+    need16(qo, "qo"); need16(ko, "ko");
+    on_device(ctx, "qknorm_fwd");
+    qknorm_fwd(ctx->stream, a, q, k, gain_q, gain_k, table, pos, qo, ko);
+  })
+}
+
+extern "C" int paragan_qknorm_bwd(paragan_ctx* ctx, const paragan_qknorm_desc* d, const void* q, const void* k,
+                                  const float* gain_q, const float* gain_k, const float* table, const int32_t* pos,
+                                  const void* dqo, const void* dko, void* dq, void* dk, float* dgain_q,
+                                  float* dgain_k, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const QkNorm a = make_qk(d);
+    need16(q, "q"); need16(k, "k"); need(gain_q, "gain_q"); need(gain_k, "gain_k");
+    if (a.rot) need16(table, "table");
+    need16(dqo, "dqo"); need16(dko, "dko"); need16(dq, "dq"); need16(dk, "dk");
+    need(dgain_q, "dgain_q"); need(dgain_k, "dgain_k"); need(ws, "ws");
+    aligned(ws, "ws");
+    on_device(ctx, "qknorm_bwd");
+    qknorm_bwd(ctx->stream, a, q, k, gain_q, gain_k, table, pos, dqo, dko, dq, dk, dgain_q, dgain_k, ws);
+  })
+}
+
+// Does (b, s, h, c) -> address hit every element of a tensor once?  Strides in
+// ascending order each have to step over all that lies inside.
+static bool distinct(const int64_t* stride, int64_t B, int64_t S, int64_t H, int64_t d) {
+  std::pair<int64_t, int64_t> e[3] = {{stride[0], B}, {stride[1], S}, {stride[2], H}};
+  std::sort(e, e + 3);
+  __int128 inner = d;
+  for (const auto& x : e) {
+    if (x.second == 1) continue;
+    if (x.first < inner) return false;
+    inner += (__int128)x.first * (x.second - 1);
+  }
+  return true;
+}
+
+static Mha make_mha(const paragan_mha_desc* d) {
+  if (!d) throw Error{PARAGAN_EINVAL, "mha: desc is NULL"};
+  const int32_t big = 1 << 30;
+  PG_CHECK(d->B >= 1 && d->Sq >= 1 && d->Sk >= 1 && d->Sq <= big && d->Sk <= big, "mha: B, Sq, Sk must be >= 1 and Sq, Sk <= 2^30");
+  PG_CHECK(d->Hq >= 1 && d->Hk >= 1 && d->Hq % d->Hk == 0, "mha: Hq must be a multiple of Hk >= 1");
+  PG_CHECK(d->d >= 8 && d->d <= 128 && d->d % 8 == 0, "mha: d must be a multiple of 8 up to 128");
+  PG_CHECK(d->causal == 0 || d->causal == 1, "mha: causal must be 0 or 1");
+  PG_CHECK(d->window >= 0 && d->window <= big && d->n_sink >= 0 && d->n_sink <= big, "mha: window, n_sink must be 0 .. 2^30");
+  if (d->n_buckets != 0) {
+    const int side = d->causal ? d->n_buckets : d->n_buckets / 2;
+    PG_CHECK(d->n_buckets > 0 && d->n_buckets <= 256 && side >= 2 && (d->causal || d->n_buckets % 2 == 0),
+             "mha: n_buckets must be 2 .. 256 (not causal: even, 4 .. 256)");
+    PG_CHECK(d->max_distance > side / 2 && d->max_distance <= kMhaMaxDist,
+             "mha: max_distance must be above half of a side's buckets and at most 512");
+  }
+  PG_CHECK(d->scale > 0.f && std::isfinite(d->scale), "mha: scale must be > 0 and finite");
+  // a launch has fewer than 2^32 threads: blocks of 256 threads, at least 128 rows of one head in each
+  PG_CHECK((int64_t)d->B * d->Hq < (1 << 24) && (int64_t)d->B * d->Hq * cdiv(d->Sq, 128) < (1 << 24) &&
+               (int64_t)d->B * d->Hk * cdiv(d->Sk, 128) < (1 << 24),
+           "mha: too many rows (B * heads * S / 128 must stay below 2^24)");
+  Mha m;
+  m.B = d->B; m.Sq = d->Sq; m.Sk = d->Sk; m.Hq = d->Hq; m.Hk = d->Hk; m.d = d->d; m.causal = d->causal == 1;
+  m.window = d->window; m.n_sink = d->n_sink; m.n_buckets = d->n_buckets; m.max_distance = d->max_distance;
+  m.scale = d->scale;
+  for (int i = 0; i < 3; ++i) {
+    m.qs[i] = d->q_stride[i]; m.ks[i] = d->k_stride[i]; m.vs[i] = d->v_stride[i]; m.os[i] = d->o_stride[i];
+    for (int64_t s : {m.qs[i], m.ks[i], m.vs[i], m.os[i]}) {
+      PG_CHECK(s >= 0 && s % 8 == 0, "mha: strides must be >= 0 and multiples of 8");
+      PG_CHECK(s < (1LL << 60) / big, "mha: a stride is too large");
+    }
+  }
+  PG_CHECK(distinct(m.os, m.B, m.Sq, m.Hq, m.d), "mha: o overlaps itself");
+  return m;
+}
+
+extern "C" int paragan_mha_check(const paragan_mha_desc* d) { PG_TRY(nullptr, make_mha(d)) }
+
+extern "C" int paragan_mha_sizes(const paragan_mha_desc* d, size_t* saved, size_t* ws) {
+  PG_TRY(nullptr, {
+    const Mha m = make_mha(d);
+    if (saved) *saved = mha_saved_bytes(m);
+    if (ws) *ws = mha_ws_bytes(m);
+  })
+}
+
+extern "C" int paragan_mha_fwd(paragan_ctx* ctx, const paragan_mha_desc* d, const void* q, const void* k,
+                               const void* v, const float* table, const int32_t* len_q, const int32_t* len_k,
+                               void* o, void* saved, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const Mha m = make_mha(d);
+    need16(q, "q"); need16(k, "k"); need16(v, "v"); need16(o, "o"); need(ws, "ws");
+    if (m.n_buckets) need(table, "table");
+    aligned(ws, "ws");
+    if (saved) aligned(saved, "saved");
+    on_device(ctx, "mha_fwd");
+    mha_fwd(ctx->stream, m, q, k, v, table, len_q, len_k, o, saved, ws);
+  })
+}
+
+extern "C" int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d, const void* q, const void* k,
+                               const void* v, const float* table, const int32_t* len_q, const int32_t* len_k,
+                               const void* o, const void* saved, const void* dout, void* dq, void* dk, void* dv,
+                               float* dtable, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const Mha m = make_mha(d);
+    PG_CHECK(distinct(m.qs, m.B, m.Sq, m.Hq, m.d) && distinct(m.ks, m.B, m.Sk, m.Hk, m.d) &&
+                 distinct(m.vs, m.B, m.Sk, m.Hk, m.d),
+             "mha_bwd: q, k or v overlaps itself (dq, dk, dv share their strides)");
+    need16(q, "q"); need16(k, "k"); need16(v, "v"); need16(o, "o"); need(saved, "saved"); need16(dout, "dout");
+    need16(dq, "dq"); need16(dk, "dk"); need16(dv, "dv"); need(ws, "ws");
+    if (m.n_buckets) { need(table, "table"); need(dtable, "dtable"); }
+    aligned(saved, "saved"); aligned(ws, "ws");
+    on_device(ctx, "mha_bwd");
+    mha_bwd(ctx->stream, m, q, k, v, table, len_q, len_k, o, saved, dout, dq, dk, dv, dtable, ws);
   })
 }
 

@@ -1,0 +1,1009 @@
+// Multi-head attention on gfx950 (bf16 MFMA 32x32x16, fp32 softmax) with
+// shared key heads, ragged lengths, causal order, a sliding window with a few
+// first tokens that stay visible, and a learned relative position bias by
+// buckets; forward, backward and the form for a few new tokens over a cache.
+//
+//   S = scale q k^T + bias[h][bucket(j - p)],  P = softmax over visible keys,
+//   o = P v;   backward: D = rowsum(do o), dS = P (do v^T - D),
+//   dq = scale dS k, dk = scale dS^T q, dv = P^T do,
+//   dbias[h][b] = sum of dS over the pairs in bucket b.
+//
+// S is never stored.  Scores are computed transposed (S^T = K Q^T), so a lane
+// owns one query (forward, dq) or one key (dk, dv); probabilities feed the
+// next product straight from the accumulator registers.  Softmax statistics,
+// all sums and the bias are fp32; the operands of the second products (P, dS)
+// are rounded to bf16 because the matrix cores take them so.  Exponentials
+// are base 2 and the running maximum is only raised when a tile's maximum
+// passes it by 2^8 (the rescale of the accumulators is then rare).
+//
+// A tile is only visited when some query of the block sees some key of it;
+// rows nobody in the block sees are not read (they may hold anything).
+#include <cfloat>
+#include <cmath>
+#include <type_traits>
+
+#include "attn_tiles.hpp"
+#include "token.hpp"
+
+namespace pg {
+
+namespace {
+
+constexpr int kMargin = 64;   // distances past max_distance that a 32 x 32 tile can reach, rounded up
+
+struct MhaArgs {
+  int B, Sq, Sk, Hq, Hk, G, d, Sqp, nblk;
+  int causal, window, n_sink, nb, maxd, half;
+  int nsplit, nrt;
+  float c, scale;               // c = scale log2(e)
+  int64_t qs[3], ks[3], vs[3], os[3];
+  const bf16_t *q, *k, *v, *dO;
+  bf16_t *o, *dq, *dk, *dv;
+  const float* table;
+  const int32_t *len_q, *len_k;
+  float *lse, *D, *part;
+  uint16_t start[257];          // smallest distance of each bucket of one side
+  uint8_t lut[kMhaMaxDist + 8]; // bucket (of one side) of each distance
+};
+
+struct Seq { int lq, lk, off; };
+PG_DEV Seq seq_of(const MhaArgs& a, int b) {
+  Seq s;
+  s.lq = a.len_q ? min(max(a.len_q[b], 0), a.Sq) : a.Sq;
+  s.lk = a.len_k ? min(max(a.len_k[b], 0), a.Sk) : a.Sk;
+  s.off = s.lk - s.lq;
+  return s;
+}
+
+// Keys that queries at positions p0 .. p1 see: [lo, hi) through the window
+// and [0, ns) of the first tokens, as nt tiles of 32: tile n is
+// n (n < st) or n - st + ws.
+struct Span {
+  int lo, hi, ns, st, ws, nt;
+  PG_DEV int key0(int n) const { return 32 * (n < st ? n : n - st + ws); }
+  PG_DEV bool row(int j) const { return (j >= lo && j < hi) || j < ns; }
+  PG_DEV bool tile(int k0) const { return (k0 + 32 > lo && k0 < hi) || k0 < ns; }
+};
+PG_DEV Span span_of(const MhaArgs& a, int lk, int p0, int p1) {
+  Span s;
+  const int top = max(a.causal ? min(lk, p1 + 1) : lk, 0);
+  s.lo = a.window ? max(p0 - a.window + 1, 0) : 0;
+  s.hi = a.window && !a.causal ? max(min(lk, p1 + a.window), 0) : top;
+  s.ns = a.window ? min(a.n_sink, top) : 0;
+  const int sink_tiles = (s.ns + 31) >> 5, w0 = s.lo >> 5, w1 = (s.hi + 31) >> 5;
+  if (sink_tiles >= w0) {
+    s.st = 0;
+    s.ws = 0;
+    s.nt = max(w1, sink_tiles);
+    if (s.lo >= s.hi) s.nt = sink_tiles;
+  } else {
+    s.st = sink_tiles;
+    s.ws = w0;
+    s.nt = sink_tiles + max(w1 - w0, 0);
+  }
+  return s;
+}
+// Does every query at positions p0 .. p1 see every key of [k0, k0 + 32)?
+PG_DEV bool all_seen(const MhaArgs& a, int lk, int k0, int p0, int p1) {
+  if (k0 + 32 > lk || (a.causal && k0 + 31 > p0)) return false;
+  return !a.window || k0 + 32 <= a.n_sink || (p1 - k0 < a.window && k0 + 31 - p0 < a.window);
+}
+// visible keys of one query: [lo, hi) and [0, ns)
+struct Row { int lo, hi, ns; };
+PG_DEV Row row_of(const MhaArgs& a, int lk, int p) {
+  Row r;
+  const int top = a.causal ? min(lk, p + 1) : lk;
+  r.lo = a.window ? p - a.window + 1 : 0;
+  r.hi = a.window ? min(top, p + a.window) : top;
+  r.ns = a.window ? min(a.n_sink, top) : 0;
+  return r;
+}
+PG_DEV bool sees(const Row& r, int j) { return (j >= r.lo && j < r.hi) || j < r.ns; }
+
+// bias in log2 units at distance index e = rel + maxd + kMargin; distances past max_distance are its own
+PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
+  const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
+  const int b = (int)a.lut[rel < 0 ? -rel : rel] + (rel > 0 ? a.half : 0);
+  const float t = a.table[(int64_t)h * a.nb + b];
+  // the lowest finite value stays finite (a row of nothing else is uniform)
+  return t < 0.f && t >= -FLT_MAX ? fmaxf(t * kL2E, -FLT_MAX) : t * kL2E;
+}
+PG_DEV int bias_len(const MhaArgs& a) { return 2 * (a.maxd + kMargin) + 1; }
+
+// Stage 32 rows x NC chunks into a swizzled tile by 256 threads: thread slots
+// i = tid + 256 j; chunks at or past d and rows that `ok` refuses are zero.
+template <int NC>
+struct Stage {
+  static constexpr int SLOTS = (32 * NC + 255) / 256;
+  uint4 v[SLOTS];
+  template <class F>
+  PG_DEV void load(const bf16_t* base, int64_t ld, int r0, int d, int tid, F ok) {
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      const int i = tid + 256 * j;
+      const int r = i / NC, c = i - (i / NC) * NC;
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (i < 32 * NC && c * 8 < d && ok(r0 + r))
+        v[j] = *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * ld + c * 8);
+    }
+  }
+  PG_DEV void store(bf16_t* t, int tid) const {
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      const int i = tid + 256 * j;
+      const int r = i / NC, c = i - (i / NC) * NC;
+      if (i < 32 * NC) *reinterpret_cast<uint4*>(t + toff<NC>(r, c * 8)) = v[j];
+    }
+  }
+};
+
+PG_DEV bf16x8 ld_frag(const bf16_t* row, int e, int d, bool ok) { return ok && e < d ? ld8g(row + e) : zero8(); }
+
+// four consecutive channels of a bf16 row; nothing past d
+PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
+  if (e < d) *reinterpret_cast<uint2*>(row + e) = make_uint2(f2bf2(a, b), f2bf2(c, f));
+}
+
+// ------------------------------------------------------------- forward
+// A wave owns 32 QT queries of one head; a block of 4 waves 128 QT.
+template <int DT, int QT, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_mha_fwd(MhaArgs a) {
+  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[2][32 * DT];
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[2][32 * DT];
+  extern __shared__ float bs[];
+  // the last queries of a causal head see the most keys: they start first
+  const int qb = a.nblk - 1 - (int)(blockIdx.x % a.nblk), bh = blockIdx.x / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
+  const Seq sq = seq_of(a, b);
+  const int qblk = qb * 128 * QT, qw = qblk + (tid >> 6) * 32 * QT;
+  const bf16_t* K = a.k + b * a.ks[0] + (h / a.G) * a.ks[2];
+  const bf16_t* V = a.v + b * a.vs[0] + (h / a.G) * a.vs[2];
+  if (BIAS)
+    for (int e = tid; e < bias_len(a); e += 256) bs[e] = bias2_at(a, h, e);
+  bf16x8 qf[QT][KF];
+  Row rw[QT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    const int q = qw + 32 * u + lq;
+    const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
+#pragma unroll
+    for (int t = 0; t < KF; ++t) qf[u][t] = ld_frag(Q, 16 * t + 8 * g, a.d, q < sq.lq);
+    rw[u] = row_of(a, sq.lk, q + sq.off);
+  }
+  f32x16 acc[QT][NT];
+  float m2[QT], l[QT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    m2[u] = -INFINITY;
+    l[u] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[u][j][r] = 0.f;
+  }
+  // a block behind the last query visits nothing and writes zeros
+  Span sp = span_of(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
+  if (qblk >= sq.lq) sp.nt = 0;
+  const Span sw = span_of(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
+  const bool mine = qw < sq.lq;
+  Stage<NC> sk, sv;
+  auto load = [&](int n) {
+    auto ok = [&](int j) { return sp.row(j); };
+    sk.load(K, a.ks[1], sp.key0(n), a.d, tid, ok);
+    sv.load(V, a.vs[1], sp.key0(n), a.d, tid, ok);
+  };
+  if (sp.nt > 0) {
+    load(0);
+    sk.store(Ks[0], tid);
+    sv.store(Vs[0], tid);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int n = 0; n < sp.nt; ++n) {
+    const bool more = n + 1 < sp.nt;
+    if (more) load(n + 1);
+    const int k0 = sp.key0(n);
+    if (mine && sw.tile(k0)) {
+      const bf16_t* ks = Ks[buf];
+      const bf16_t* vs = Vs[buf];
+      f32x16 s[QT];
+#pragma unroll
+      for (int u = 0; u < QT; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+#pragma unroll
+      for (int t = 0; t < KF; ++t) {
+        const bf16x8 ka = ld_row<NC>(ks, lq, 16 * t + 8 * g);
+#pragma unroll
+        for (int u = 0; u < QT; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[u][t], s[u], 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < QT; ++u) {
+        const int p0 = qw + 32 * u + sq.off;
+        if (BIAS) {
+          if (k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd) {
+            const float* bl = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, bl[8 * (r >> 2) + (r & 3)]);
+          } else {
+            const float far = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, far);
+          }
+        }
+        if (!all_seen(a, sq.lk, k0, p0, p0 + 31)) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!sees(rw[u], k0 + acc_row(r, g))) s[u][r] = -INFINITY;
+        }
+        float mb = s[u][0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mb = fmaxf(mb, s[u][r]);
+        mb = fmaxf(mb, __shfl_xor(mb, 32, 64));
+        if (!BIAS) mb *= a.c;
+        if (mb > m2[u] + kTau) {
+          const float alpha = exp2_(m2[u] - mb);
+          l[u] *= alpha;
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[u][j][r] *= alpha;
+          m2[u] = mb;
+        }
+        const float ms = m2[u] == -INFINITY ? 0.f : m2[u];   // nothing seen yet: every term is 2^-inf
+        float ls = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[u][r] = exp2_(BIAS ? s[u][r] - ms : fmaf(s[u][r], a.c, -ms));
+          ls += s[u][r];
+        }
+        l[u] += ls;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        bf16x8 pb[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u], t);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const bf16x8 va = ld_tr<NC>(vs, t, 32 * j, lane);
+#pragma unroll
+          for (int u = 0; u < QT; ++u)
+            acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[u], acc[u][j], 0, 0, 0);
+        }
+      }
+    }
+    if (more) {
+      sk.store(Ks[buf ^ 1], tid);
+      sv.store(Vs[buf ^ 1], tid);
+    }
+    __syncthreads();
+    buf ^= 1;
+  }
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    const int q = qw + 32 * u + lq;
+    const float lt = l[u] + __shfl_xor(l[u], 32, 64);
+    const bool any = q < sq.lq && lt > 0.f;
+    const float inv = any ? 1.f / lt : 0.f;
+    bf16_t* orow = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x16& x = acc[u][j];
+        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (any) f = make_float4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
+        if (q < a.Sq) st4(orow, 32 * j + 8 * i + 4 * g, a.d, f.x, f.y, f.z, f.w);
+      }
+    if (a.lse && g == 0 && q < a.Sqp) a.lse[(int64_t)bh * a.Sqp + q] = any ? m2[u] + __log2f(lt) : INFINITY;
+  }
+}
+
+// ------------------------------------------------------------- a few new tokens
+// The rows (query head of the group, query) of one key head form tiles of 32;
+// a block's 4 waves take key tiles in turn, each with its own running softmax,
+// joined at the end; nsplit blocks share a long cache and leave partials.
+template <int DT, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
+  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[4][32 * DT];
+  __shared__ float ml[4][32][2];
+  __shared__ __attribute__((aligned(16))) float red[3][NT * 16 * 64];
+  extern __shared__ float dyn[];   // bias of the tile's rows by bucket, [32][nb], then the distances' buckets
+  const int z = blockIdx.x % a.nsplit, rt = (blockIdx.x / a.nsplit) % a.nrt, bh = blockIdx.x / a.nsplit / a.nrt;
+  const int hk = bh % a.Hk, b = bh / a.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31, wv = tid >> 6;
+  const Seq sq = seq_of(a, b);
+  const int rho = rt * 32 + lq, R = a.G * a.Sq;
+  const int i = rho % a.Sq, h = hk * a.G + min(rho / a.Sq, a.G - 1);
+  const bool live = rho < R && i < sq.lq;
+  uint8_t* lut = reinterpret_cast<uint8_t*>(dyn + 32 * a.nb);
+  if (BIAS) {
+    for (int e = tid; e < 32 * a.nb; e += 256) {
+      const int hh = hk * a.G + min((rt * 32 + e / a.nb) / a.Sq, a.G - 1);
+      const float t = a.table[(int64_t)hh * a.nb + e % a.nb];
+      dyn[e] = t < 0.f && t >= -FLT_MAX ? fmaxf(t * kL2E, -FLT_MAX) : t * kL2E;
+    }
+    for (int e = tid; e < bias_len(a); e += 256) {
+      const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
+      lut[e] = (uint8_t)(a.lut[rel < 0 ? -rel : rel] + (rel > 0 ? a.half : 0));
+    }
+    __syncthreads();
+  }
+  const bf16_t* K = a.k + b * a.ks[0] + hk * a.ks[2];
+  const bf16_t* V = a.v + b * a.vs[0] + hk * a.vs[2];
+  const bf16_t* Q = a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
+  bf16x8 qf[KF];
+#pragma unroll
+  for (int t = 0; t < KF; ++t) qf[t] = ld_frag(Q, 16 * t + 8 * g, a.d, live);
+  const Row rw = row_of(a, sq.lk, i + sq.off);
+  f32x16 acc[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+  float m2 = -INFINITY, l = 0.f;
+  Span sp = span_of(a, sq.lk, sq.off, sq.off + sq.lq - 1);
+  if (sq.lq == 0) sp.nt = 0;
+  const int per = (sp.nt + a.nsplit - 1) / a.nsplit, n1 = min(sp.nt, (z + 1) * per);
+  for (int n = z * per + wv; n < n1; n += 4) {
+    const int k0 = sp.key0(n), kr = k0 + lq;
+    const bool kok = sp.row(kr);
+    bf16x8 kf[KF];
+    uint4 vv[NC / 2];
+#pragma unroll
+    for (int t = 0; t < KF; ++t) kf[t] = ld_frag(K + kr * a.ks[1], 16 * t + 8 * g, a.d, kok);
+#pragma unroll
+    for (int j = 0; j < NC / 2; ++j) {
+      const int x = lane + 64 * j, r = x / NC, c = x - (x / NC) * NC;
+      vv[j] = make_uint4(0, 0, 0, 0);
+      if (c * 8 < a.d && sp.row(k0 + r)) vv[j] = *reinterpret_cast<const uint4*>(V + (k0 + r) * a.vs[1] + c * 8);
+    }
+    f32x16 s;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = 0.f;
+#pragma unroll
+    for (int t = 0; t < KF; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t], qf[t], s, 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < NC / 2; ++j) {
+      const int x = lane + 64 * j, r = x / NC, c = x - (x / NC) * NC;
+      *reinterpret_cast<uint4*>(Vs[wv] + toff<NC>(r, c * 8)) = vv[j];
+    }
+    if (BIAS) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int rel = min(max(k0 + acc_row(r, g) - i - sq.off, -a.maxd), a.maxd);
+        s[r] = fmaf(s[r], a.c, dyn[lq * a.nb + lut[rel + a.maxd + kMargin]]);
+      }
+    }
+    if (!all_seen(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (!sees(rw, k0 + acc_row(r, g))) s[r] = -INFINITY;
+    }
+    float mb = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mb = fmaxf(mb, s[r]);
+    mb = fmaxf(mb, __shfl_xor(mb, 32, 64));
+    if (!BIAS) mb *= a.c;
+    if (mb > m2 + kTau) {
+      const float alpha = exp2_(m2 - mb);
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[j][r] *= alpha;
+      m2 = mb;
+    }
+    const float ms = m2 == -INFINITY ? 0.f : m2;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = exp2_(BIAS ? s[r] - ms : fmaf(s[r], a.c, -ms));
+      l += s[r];
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 pb = pack_regs(s, t);
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(Vs[wv], t, 32 * j, lane), pb, acc[j], 0, 0, 0);
+    }
+  }
+  // join the four waves
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) { ml[wv][lq][0] = m2; ml[wv][lq][1] = l; }
+  __syncthreads();
+  float M = -INFINITY, L = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) M = fmaxf(M, ml[w][lq][0]);
+  const float Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) L += ml[w][lq][1] * exp2_(ml[w][lq][0] - Ms);
+  const float f = exp2_(m2 - Ms);
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[j][r] *= f;
+  if (wv > 0)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) red[wv - 1][(j * 16 + r) * 64 + lane] = acc[j][r];
+  __syncthreads();
+  if (wv > 0) return;
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      acc[j][r] += red[0][(j * 16 + r) * 64 + lane] + red[1][(j * 16 + r) * 64 + lane] + red[2][(j * 16 + r) * 64 + lane];
+  if (a.nsplit > 1) {
+    float* slot = a.part + (int64_t)blockIdx.x * 32 * (DT + 2);
+    if (g == 0) { slot[lq] = M; slot[32 + lq] = L; }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<float4*>(slot + 64 + lq * DT + 32 * j + 8 * e + 4 * g) =
+            make_float4(acc[j][4 * e], acc[j][4 * e + 1], acc[j][4 * e + 2], acc[j][4 * e + 3]);
+    return;
+  }
+  if (rho >= R) return;
+  const bool any = live && L > 0.f;
+  const float inv = any ? 1.f / L : 0.f;
+  bf16_t* orow = a.o + b * a.os[0] + i * a.os[1] + h * a.os[2];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x16& x = acc[j];
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (any) v = make_float4(x[4 * e] * inv, x[4 * e + 1] * inv, x[4 * e + 2] * inv, x[4 * e + 3] * inv);
+      st4(orow, 32 * j + 8 * e + 4 * g, a.d, v.x, v.y, v.z, v.w);
+    }
+}
+
+// Joins the nsplit partials of a row, in split order: a thread holds 4 channels of one row.
+template <int DT>
+__global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
+  constexpr int PR = DT / 4;
+  const int x = blockIdx.x * 256 + threadIdx.x;
+  const int c = 4 * (x % PR), rr = x / PR;               // row of all row tiles
+  const int lr = rr % 32, rt = (rr / 32) % a.nrt, bh = rr / 32 / a.nrt;
+  const int hk = bh % a.Hk, b = bh / a.Hk, rho = rt * 32 + lr;
+  if (b >= a.B || rho >= a.G * a.Sq) return;
+  const float* slot = a.part + (int64_t)(bh * a.nrt + rt) * a.nsplit * 32 * (DT + 2);
+  float M = -INFINITY, L = 0.f;
+  for (int z = 0; z < a.nsplit; ++z) M = fmaxf(M, slot[(int64_t)z * 32 * (DT + 2) + lr]);
+  const float Ms = M == -INFINITY ? 0.f : M;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int z = 0; z < a.nsplit; ++z) {
+    const float* p = slot + (int64_t)z * 32 * (DT + 2);
+    const float f = exp2_(p[lr] - Ms);
+    const float4 v = *reinterpret_cast<const float4*>(p + 64 + lr * DT + c);
+    L += p[32 + lr] * f;
+    s.x += v.x * f; s.y += v.y * f; s.z += v.z * f; s.w += v.w * f;
+  }
+  const int i = rho % a.Sq, h = hk * a.G + rho / a.Sq;
+  const Seq sq = seq_of(a, b);
+  const bool any = i < sq.lq && L > 0.f;
+  const float inv = any ? 1.f / L : 0.f;
+  if (!any) s = make_float4(0.f, 0.f, 0.f, 0.f);
+  st4(a.o + b * a.os[0] + i * a.os[1] + h * a.os[2], c, a.d, s.x * inv, s.y * inv, s.z * inv, s.w * inv);
+}
+
+// ------------------------------------------------------------- dq (query-owned)
+// Also D, kept for the key-owned pass (with a bias as sum P dP in a pass of its
+// own, else as do . o), and the bias gradient:
+// dS of the tiles near the diagonal is added per distance into LDS, by each
+// wave into two arrays of its own (one per lane half), so that no two lanes of
+// one instruction meet and the order of the sums is fixed; tiles past
+// max_distance add into one register per side.
+template <int DT, int QT, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
+  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[2][32 * DT];
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[2][32 * DT];
+  extern __shared__ float bs[];   // bias by distance, then 8 arrays of dS sums by distance
+  const int qb = a.nblk - 1 - (int)(blockIdx.x % a.nblk), bh = blockIdx.x / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
+  const Seq sq = seq_of(a, b);
+  const int qblk = qb * 128 * QT, qw = qblk + (tid >> 6) * 32 * QT;
+  const bf16_t* K = a.k + b * a.ks[0] + (h / a.G) * a.ks[2];
+  const bf16_t* V = a.v + b * a.vs[0] + (h / a.G) * a.vs[2];
+  const int bl = BIAS ? bias_len(a) : 0;
+  float* const gs = bs + bl + (2 * (tid >> 6) + g) * bl;
+  if (BIAS) {
+    for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, h, e);
+    for (int e = tid; e < 8 * bl; e += 256) bs[bl + e] = 0.f;
+  }
+  bf16x8 qf[QT][KF], df[QT][KF];
+  float ls2[QT], dd[QT];
+  Row rw[QT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    const int q = qw + 32 * u + lq;
+    const bool ok = q < sq.lq;
+    const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
+    const bf16_t* DO = a.dO + b * a.os[0] + q * a.os[1] + h * a.os[2];
+    const bf16_t* O = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
+    dd[u] = 0.f;
+#pragma unroll
+    for (int t = 0; t < KF; ++t) {
+      qf[u][t] = ld_frag(Q, 16 * t + 8 * g, a.d, ok);
+      df[u][t] = ld_frag(DO, 16 * t + 8 * g, a.d, ok);
+      if (!BIAS) {
+        float x[8], o[8];
+        unpack8(__builtin_bit_cast(uint4, df[u][t]), x);
+        // from the bf16 output: off by at most 2^-8 of sum |do||o|, as much as dS loses when it becomes an operand
+        unpack8(__builtin_bit_cast(uint4, ld_frag(O, 16 * t + 8 * g, a.d, ok)), o);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dd[u] = fmaf(x[e], o[e], dd[u]);
+      }
+    }
+    dd[u] += __shfl_xor(dd[u], 32, 64);
+    ls2[u] = ok ? a.lse[(int64_t)bh * a.Sqp + q] : INFINITY;
+    if (!BIAS && g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = ok ? dd[u] : 0.f;
+    rw[u] = row_of(a, sq.lk, q + sq.off);
+  }
+  f32x16 acc[QT][NT];
+#pragma unroll
+  for (int u = 0; u < QT; ++u)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[u][j][r] = 0.f;
+  float flo = 0.f, fhi = 0.f;
+  Span sp = span_of(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
+  if (qblk >= sq.lq) sp.nt = 0;
+  const Span sw = span_of(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
+  const bool mine = qw < sq.lq;
+  Stage<NC> sk, sv;
+  auto load = [&](int n) {
+    auto ok = [&](int j) { return sp.row(j); };
+    sk.load(K, a.ks[1], sp.key0(n), a.d, tid, ok);
+    sv.load(V, a.vs[1], sp.key0(n), a.d, tid, ok);
+  };
+  // One pass over the keys.  FIRST (with a bias only): dd = sum P dP in fp32.
+  // The bias gradient sums dS over many pairs with little left over; a row
+  // term from a rounded output, or from rounded P, would dominate it.
+  auto pass = [&](auto first_c) {
+    constexpr bool FIRST = decltype(first_c)::value;
+    if (sp.nt > 0) {
+      load(0);
+      sk.store(Ks[0], tid);
+      sv.store(Vs[0], tid);
+    }
+    __syncthreads();
+    int buf = 0;
+    for (int n = 0; n < sp.nt; ++n) {
+      const bool more = n + 1 < sp.nt;
+      if (more) load(n + 1);
+      const int k0 = sp.key0(n);
+      if (mine && sw.tile(k0)) {
+        const bf16_t* ks = Ks[buf];
+        const bf16_t* vs = Vs[buf];
+        f32x16 s[QT], dp[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) { s[u][r] = 0.f; dp[u][r] = 0.f; }
+#pragma unroll
+        for (int t = 0; t < KF; ++t) {
+          const bf16x8 ka = ld_row<NC>(ks, lq, 16 * t + 8 * g), va = ld_row<NC>(vs, lq, 16 * t + 8 * g);
+#pragma unroll
+          for (int u = 0; u < QT; ++u) {
+            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[u][t], s[u], 0, 0, 0);
+            dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, df[u][t], dp[u], 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+          const int p0 = qw + 32 * u + sq.off;
+          const bool near = BIAS && k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd;
+          const int at = k0 - p0 - lq + a.maxd + kMargin + 4 * g;
+          if (BIAS) {
+            if (near) {
+#pragma unroll
+              for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, bs[at + 8 * (r >> 2) + (r & 3)] - ls2[u]);
+            } else {
+              const float far = (k0 < p0 ? bs[0] : bs[bl - 1]) - ls2[u];
+#pragma unroll
+              for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, far);
+            }
+          } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, -ls2[u]);
+          }
+          if (!all_seen(a, sq.lk, k0, p0, p0 + 31)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              if (!sees(rw[u], k0 + acc_row(r, g))) s[u][r] = -INFINITY;
+          }
+          if (FIRST) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dd[u] = fmaf(exp2_(s[u][r]), dp[u][r], dd[u]);
+            continue;
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = exp2_(s[u][r]) * (dp[u][r] - dd[u]);
+          if (BIAS) {
+            if (near) {
+#pragma unroll
+              for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(gs + at + 8 * (r >> 2) + (r & 3), s[u][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            } else {
+              float t = 0.f;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) t += s[u][r];
+              if (k0 < p0) flo += t; else fhi += t;
+            }
+          }
+        }
+        if (!FIRST)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          bf16x8 pb[QT];
+#pragma unroll
+          for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u], t);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const bf16x8 ka = ld_tr<NC>(ks, t, 32 * j, lane);
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+              acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, pb[u], acc[u][j], 0, 0, 0);
+          }
+        }
+      }
+      if (more) {
+        sk.store(Ks[buf ^ 1], tid);
+        sv.store(Vs[buf ^ 1], tid);
+      }
+      __syncthreads();
+      buf ^= 1;
+    }
+  };
+  if (BIAS) {
+    pass(std::integral_constant<bool, true>());
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      const int q = qw + 32 * u + lq;
+      dd[u] += __shfl_xor(dd[u], 32, 64);
+      if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = q < sq.lq ? dd[u] : 0.f;
+    }
+  }
+  pass(std::integral_constant<bool, false>());
+#pragma unroll
+  for (int u = 0; u < QT; ++u) {
+    const int q = qw + 32 * u + lq;
+    if (q >= a.Sq) continue;
+    bf16_t* row = a.dq + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
+    const float f = q < sq.lq ? a.scale : 0.f;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x16& x = acc[u][j];
+        st4(row, 32 * j + 8 * i + 4 * g, a.d, x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f, x[4 * i + 3] * f);
+      }
+  }
+  if (BIAS) {
+    flo = wave_sum(flo);
+    fhi = wave_sum(fhi);
+    if (lane == 0) { gs[0] += flo; gs[bl - 1] += fhi; }
+    __syncthreads();
+    for (int e = tid; e < bl; e += 256) {
+      float t = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) t += bs[bl + w * bl + e];
+      bs[e] = t;
+    }
+    __syncthreads();
+    const int mid = a.maxd + kMargin;
+    for (int k = tid; k < a.nb; k += 256) {
+      const bool up = k >= a.half;           // later keys (never with causal)
+      const int kk = up ? k - a.half : k, n0 = a.start[kk], n1 = kk + 1 < a.half ? a.start[kk + 1] : mid + 1;
+      float t = 0.f;
+      for (int n = n0; n < n1; ++n)
+        if (!(up && n == 0)) t += bs[up ? mid + n : mid - n];
+      a.part[((int64_t)bh * a.nblk + qb) * a.nb + k] = t;
+    }
+  }
+}
+
+// dbias[h][k] = sum over sequences and query blocks of their partials, in that order
+__global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int Hq, int nblk, int nb, float* out) {
+  const int x = blockIdx.x * 256 + threadIdx.x;
+  if (x >= Hq * nb) return;
+  const int h = x / nb, k = x % nb;
+  double t = 0.0;
+  for (int b = 0; b < B; ++b)
+    for (int i = 0; i < nblk; ++i) t += part[(((int64_t)b * Hq + h) * nblk + i) * nb + k];
+  out[x] = (float)t;
+}
+
+// ------------------------------------------------------------- dk, dv (key-owned)
+// A wave owns 32 keys of one key head, a block 128; the steps run over the
+// query heads of the group and their 32-query tiles, so the gradients of a
+// shared head are summed in registers.
+template <int DT, bool BIAS>
+__global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
+  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Qs[2][32 * DT];
+  __shared__ __attribute__((aligned(16))) bf16_t Ds[2][32 * DT];
+  __shared__ __attribute__((aligned(16))) float Ls[2][32], Dd[2][32];
+  extern __shared__ float bs[];   // the current head's bias by query minus key
+  const int kb = blockIdx.x % a.nblk, bh = blockIdx.x / a.nblk, hk = bh % a.Hk, b = bh / a.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lk = lane & 31;
+  const Seq sq = seq_of(a, b);
+  const int kblk = kb * 128, kw = kblk + (tid >> 6) * 32, key = kw + lk;
+  const bool kv = key < sq.lk;
+  const int bl = BIAS ? bias_len(a) : 0;
+  bf16x8 kf[KF], vf[KF];
+#pragma unroll
+  for (int t = 0; t < KF; ++t) {
+    kf[t] = ld_frag(a.k + b * a.ks[0] + key * a.ks[1] + hk * a.ks[2], 16 * t + 8 * g, a.d, kv);
+    vf[t] = ld_frag(a.v + b * a.vs[0] + key * a.vs[1] + hk * a.vs[2], 16 * t + 8 * g, a.d, kv);
+  }
+  f32x16 adk[NT], adv[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) { adk[j][r] = 0.f; adv[j][r] = 0.f; }
+  // queries [i0, i1) that see some key of [j0, j1]
+  auto seen_by = [&](int j0, int j1, int& i0, int& i1) {
+    j1 = min(j1, sq.lk - 1);
+    const bool sink = a.window && j0 < a.n_sink;
+    int lo = a.causal ? j0 : a.window && !sink ? j0 - a.window + 1 : -0x40000000;
+    int hi = a.window && !sink ? j1 + a.window - 1 : 0x40000000;
+    i0 = max(lo - sq.off, 0);
+    i1 = min(hi - sq.off + 1, sq.lq);
+    if (j1 < j0) i1 = i0;
+  };
+  int i0, i1, w0, w1;
+  seen_by(kblk, kblk + 127, i0, i1);
+  seen_by(kw, kw + 31, w0, w1);
+  const int t0 = i0 >> 5, nt = max(((i1 + 31) >> 5) - t0, 0);
+  // this lane's key is seen from positions plo .. phi
+  const bool sink = key < a.n_sink;
+  const int plo = !kv ? 0x7fffffff : a.causal ? key : a.window && !sink ? key - a.window + 1 : -0x40000000;
+  const int phi = a.window && !sink ? key + a.window - 1 : 0x7fffffff;
+  Stage<NC> st_q, st_d;
+  float sl = 0.f, sd = 0.f;
+  auto load = [&](int n) {
+    const int h = hk * a.G + n / nt, q0 = 32 * (t0 + n % nt);
+    auto ok = [&](int i) { return i >= i0 && i < i1; };
+    st_q.load(a.q + b * a.qs[0] + h * a.qs[2], a.qs[1], q0, a.d, tid, ok);
+    st_d.load(a.dO + b * a.os[0] + h * a.os[2], a.os[1], q0, a.d, tid, ok);
+    if (tid < 32) {
+      const int64_t x = ((int64_t)b * a.Hq + h) * a.Sqp + q0 + tid;
+      sl = ok(q0 + tid) ? a.lse[x] : INFINITY;
+      sd = a.D[x];
+    }
+  };
+  auto store = [&](int bf) {
+    st_q.store(Qs[bf], tid);
+    st_d.store(Ds[bf], tid);
+    if (tid < 32) { Ls[bf][tid] = sl; Dd[bf][tid] = sd; }
+  };
+  const int steps = nt * a.G;
+  if (steps > 0) {
+    load(0);
+    store(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int n = 0; n < steps; ++n) {
+    const bool more = n + 1 < steps;
+    if (more) load(n + 1);
+    const int q0 = 32 * (t0 + n % nt), p0 = q0 + sq.off;
+    if (BIAS && n % nt == 0) {   // the next head's bias; the last step's reads ended at its barrier
+      for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, hk * a.G + n / nt, bl - 1 - e);
+      __syncthreads();
+    }
+    if (q0 + 32 > w0 && q0 < w1) {
+      const bf16_t* qs = Qs[buf];
+      const bf16_t* ds = Ds[buf];
+      f32x16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) { s[r] = 0.f; dp[r] = 0.f; }
+#pragma unroll
+      for (int t = 0; t < KF; ++t) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(qs, lk, 16 * t + 8 * g), kf[t], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ds, lk, 16 * t + 8 * g), vf[t], dp, 0, 0, 0);
+      }
+      const bool near = BIAS && kw + 31 - p0 > -a.maxd && kw - p0 - 31 < a.maxd;
+      const float* bn = bs + (p0 - kw - lk + a.maxd + kMargin) + 4 * g;   // reversed: by query minus key
+      const float far = BIAS ? (kw < p0 ? bs[bl - 1] : bs[0]) : 0.f;
+      const bool full = all_seen(a, sq.lk, kw, p0, p0 + 31);
+      f32x16 p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 lv = *reinterpret_cast<const float4*>(&Ls[buf][8 * i + 4 * g]);
+        const float4 dv4 = *reinterpret_cast<const float4*>(&Dd[buf][8 * i + 4 * g]);
+        const float lsv[4] = {lv.x, lv.y, lv.z, lv.w}, ddv[4] = {dv4.x, dv4.y, dv4.z, dv4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * i + e;
+          float x = fmaf(s[r], a.c, -lsv[e]);
+          if (BIAS) x += near ? bn[8 * i + e] : far;
+          if (!full) {
+            const int pp = p0 + acc_row(r, g);
+            if (pp < plo || pp > phi) x = -INFINITY;
+          }
+          const float pr = exp2_(x);
+          p[r] = pr;
+          s[r] = pr * (dp[r] - ddv[e]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 pb = pack_regs(p, t), sb = pack_regs(s, t);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          adv[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(ds, t, 32 * j, lane), pb, adv[j], 0, 0, 0);
+          adk[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(qs, t, 32 * j, lane), sb, adk[j], 0, 0, 0);
+        }
+      }
+    }
+    if (more) store(buf ^ 1);
+    __syncthreads();
+    buf ^= 1;
+  }
+  if (key >= a.Sk) return;
+  bf16_t* dkr = a.dk + b * a.ks[0] + key * a.ks[1] + hk * a.ks[2];
+  bf16_t* dvr = a.dv + b * a.vs[0] + key * a.vs[1] + hk * a.vs[2];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x16 &x = adk[j], &y = adv[j];
+      st4(dkr, 32 * j + 8 * i + 4 * g, a.d, x[4 * i] * a.scale, x[4 * i + 1] * a.scale, x[4 * i + 2] * a.scale,
+          x[4 * i + 3] * a.scale);
+      st4(dvr, 32 * j + 8 * i + 4 * g, a.d, y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+    }
+}
+
+// ------------------------------------------------------------- launchers
+int pad_d(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
+constexpr int fwd_qt(int dt) { return dt <= 64 ? 2 : 1; }   // query tiles of a wave
+constexpr int dq_qt(int dt) { return dt <= 32 ? 2 : 1; }
+
+// bucket of distance n among the `half` buckets of a side: exact below half / 2, then
+// logarithmic up to maxd, evaluated exactly: the largest e with (n / first)^m >= (maxd / first)^e.
+int bucket_of(int n, int half, int maxd) {
+  const int first = half / 2, m = half - first;
+  if (n < first) return n;
+  if (n >= maxd) return half - 1;
+  const long double x = logl((long double)n / first) / logl((long double)maxd / first) * m;
+  const long double near = roundl(x);
+  const int e = (int)(fabsl(x - near) < 1e-12L ? near : floorl(x));
+  return std::min(first + e, half - 1);
+}
+
+MhaArgs make_args(const Mha& m) {
+  MhaArgs a{};
+  a.B = m.B; a.Sq = m.Sq; a.Sk = m.Sk; a.Hq = m.Hq; a.Hk = m.Hk; a.G = m.Hq / m.Hk; a.d = m.d;
+  a.Sqp = (int)cdiv(m.Sq, 32) * 32;
+  a.causal = m.causal; a.window = m.window; a.n_sink = m.n_sink;
+  a.nb = m.n_buckets; a.maxd = m.n_buckets ? m.max_distance : 0;
+  a.half = m.causal ? m.n_buckets : m.n_buckets / 2;
+  a.scale = m.scale; a.c = m.scale * kL2E;
+  for (int i = 0; i < 3; ++i) { a.qs[i] = m.qs[i]; a.ks[i] = m.ks[i]; a.vs[i] = m.vs[i]; a.os[i] = m.os[i]; }
+  if (m.n_buckets) {
+    int have = 0;
+    for (int n = 0; n <= m.max_distance; ++n) {
+      a.lut[n] = (uint8_t)bucket_of(n, a.half, m.max_distance);
+      while (have <= a.lut[n]) a.start[have++] = (uint16_t)n;
+    }
+    while (have <= a.half) a.start[have++] = (uint16_t)(m.max_distance + 1);
+  }
+  return a;
+}
+
+bool few_rows(const Mha& m) { return (int64_t)m.Sq * (m.Hq / m.Hk) <= 32; }
+
+// Splits of the keys: enough blocks for three on each CU, at least 8 tiles in each.
+int step_splits(const Mha& m) {
+  const int64_t tiles = m.window ? std::min<int64_t>(cdiv(m.Sk, 32), cdiv((int64_t)m.window + m.Sq, 32) + 1 + cdiv(m.n_sink, 32))
+                                 : cdiv(m.Sk, 32);
+  const int64_t blocks = (int64_t)m.B * m.Hk * cdiv((int64_t)m.Sq * (m.Hq / m.Hk), 32);
+  return (int)std::max<int64_t>(1, std::min(cdiv(768, blocks), cdiv(tiles, 8)));
+}
+
+size_t bias_bytes(const Mha& m, int arrays) {
+  return m.n_buckets ? (size_t)arrays * (2 * (m.max_distance + kMargin) + 1) * 4 : 0;
+}
+
+#define PG_DT(d, ...)                                       \
+  switch (pad_d(d)) {                                       \
+    case 32: { constexpr int DT = 32; __VA_ARGS__; break; } \
+    case 64: { constexpr int DT = 64; __VA_ARGS__; break; } \
+    case 96: { constexpr int DT = 96; __VA_ARGS__; break; } \
+    default: { constexpr int DT = 128; __VA_ARGS__; break; } \
+  }
+
+}  // namespace
+
+size_t mha_saved_bytes(const Mha& m) {
+  const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 32) * 32;
+  return align256(rows * 4);   // the rows' log2 sums
+}
+
+size_t mha_ws_bytes(const Mha& m) {
+  const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 32) * 32;
+  size_t bwd = align256(rows * 4) + align256((size_t)m.B * m.Hq * cdiv(m.Sq, 128 * dq_qt(pad_d(m.d))) * m.n_buckets * 4);
+  size_t step = 0;
+  if (few_rows(m)) step = (size_t)m.B * m.Hk * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
+  return std::max<size_t>(std::max(bwd, align256(step)), 256);
+}
+
+void mha_fwd(hipStream_t st, const Mha& m, const void* q, const void* k, const void* v, const float* table,
+             const int32_t* len_q, const int32_t* len_k, void* o, void* saved, void* ws) {
+  MhaArgs a = make_args(m);
+  a.q = (const bf16_t*)q; a.k = (const bf16_t*)k; a.v = (const bf16_t*)v; a.o = (bf16_t*)o;
+  a.table = table; a.len_q = len_q; a.len_k = len_k;
+  const double flops = 4.0 * m.B * m.Hq * (double)m.Sq * m.Sk * m.d;
+  if (!saved && few_rows(m)) {
+    a.nsplit = step_splits(m);
+    a.nrt = 1;
+    a.part = (float*)ws;
+    const dim3 grid((unsigned)((int64_t)m.B * m.Hk * a.nsplit));
+    const size_t dyn = m.n_buckets ? (size_t)32 * m.n_buckets * 4 + align256(2 * (m.max_distance + kMargin) + 1) : 0;
+    ProfScope prof(st);
+    PG_DT(m.d, {
+      if (m.n_buckets) hipLaunchKernelGGL((k_mha_step<DT, true>), grid, dim3(256), dyn, st, a);
+      else hipLaunchKernelGGL((k_mha_step<DT, false>), grid, dim3(256), 0, st, a);
+      if (a.nsplit > 1)
+        hipLaunchKernelGGL(k_mha_join<DT>, dim3((unsigned)cdiv((int64_t)m.B * m.Hk * 32 * (DT / 4), 256)), dim3(256), 0, st, a);
+    });
+    PG_LAUNCH_CHECK();
+    prof.done("k_mha_step<" + std::to_string(pad_d(m.d)) + ">", flops);
+    return;
+  }
+  a.lse = (float*)saved;
+  a.nblk = (int)cdiv(m.Sq, 128 * fwd_qt(pad_d(m.d)));
+  const dim3 grid((unsigned)((int64_t)m.B * m.Hq * a.nblk));
+  ProfScope prof(st);
+  PG_DT(m.d, {
+    constexpr int QT = fwd_qt(DT);
+    if (m.n_buckets) hipLaunchKernelGGL((k_mha_fwd<DT, QT, true>), grid, dim3(256), bias_bytes(m, 1), st, a);
+    else hipLaunchKernelGGL((k_mha_fwd<DT, QT, false>), grid, dim3(256), 0, st, a);
+  });
+  PG_LAUNCH_CHECK();
+  prof.done("k_mha_fwd<" + std::to_string(pad_d(m.d)) + ">", flops);
+}
+
+void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const void* v, const float* table,
+             const int32_t* len_q, const int32_t* len_k, const void* o, const void* saved, const void* dO, void* dq,
+             void* dk, void* dv, float* dtable, void* ws) {
+  MhaArgs a = make_args(m);
+  a.q = (const bf16_t*)q; a.k = (const bf16_t*)k; a.v = (const bf16_t*)v; a.o = (bf16_t*)const_cast<void*>(o);
+  a.table = table; a.len_q = len_q; a.len_k = len_k;
+  a.dO = (const bf16_t*)dO; a.dq = (bf16_t*)dq; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv;
+  a.lse = (float*)const_cast<void*>(saved);
+  const size_t rows = (size_t)m.B * m.Hq * a.Sqp;
+  a.D = (float*)ws;
+  a.part = (float*)((char*)ws + align256(rows * 4));
+  ProfScope prof(st);
+  PG_DT(m.d, {
+    constexpr int QT = dq_qt(DT);
+    a.nblk = (int)cdiv(m.Sq, 128 * QT);
+    const dim3 gq((unsigned)((int64_t)m.B * m.Hq * a.nblk));
+    if (m.n_buckets) {
+      hipLaunchKernelGGL((k_mha_dq<DT, QT, true>), gq, dim3(256), bias_bytes(m, 9), st, a);
+      hipLaunchKernelGGL(k_mha_dbias, dim3((unsigned)cdiv((int64_t)m.Hq * m.n_buckets, 256)), dim3(256), 0, st, a.part,
+                         m.B, m.Hq, a.nblk, m.n_buckets, dtable);
+    } else {
+      hipLaunchKernelGGL((k_mha_dq<DT, QT, false>), gq, dim3(256), 0, st, a);
+    }
+    a.nblk = (int)cdiv(m.Sk, 128);
+    const dim3 gk((unsigned)((int64_t)m.B * m.Hk * a.nblk));
+    if (m.n_buckets) hipLaunchKernelGGL((k_mha_dkv<DT, true>), gk, dim3(256), bias_bytes(m, 1), st, a);
+    else hipLaunchKernelGGL((k_mha_dkv<DT, false>), gk, dim3(256), 0, st, a);
+  });
+  PG_LAUNCH_CHECK();
+  prof.done("k_mha_bwd<" + std::to_string(pad_d(m.d)) + ">", 14.0 * m.B * m.Hq * (double)m.Sq * m.Sk * m.d);
+}
+
+}  // namespace pg

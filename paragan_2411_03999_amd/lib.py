@@ -51,6 +51,20 @@ class GoutDesc(C.Structure):
                 ("n_power_iter", C.c_int32), ("bn_eps", C.c_float), ("sn_eps", C.c_float)]
 
 
+class QkNormDesc(C.Structure):
+    _fields_ = [("T", C.c_int64), ("Hq", C.c_int32), ("Hk", C.c_int32), ("d", C.c_int32), ("rot", C.c_int32),
+                ("interleaved", C.c_int32), ("n_pos", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float),
+                ("ldq", C.c_int64), ("ldk", C.c_int64), ("ldqo", C.c_int64), ("ldko", C.c_int64)]
+
+
+class MhaDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("Sq", C.c_int32), ("Sk", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32),
+                ("d", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32), ("n_sink", C.c_int32),
+                ("n_buckets", C.c_int32), ("max_distance", C.c_int32), ("scale", C.c_float),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("o_stride", C.c_int64 * 3)]
+
+
 class Optim(C.Structure):
     _fields_ = [("kind", C.c_int32), ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float),
                 ("eps", C.c_float)]
@@ -137,6 +151,14 @@ _SIGS = {
     "paragan_attn_check": (C.c_int, [_P]),
     "paragan_attn_fwd": (C.c_int, [_P, _P, _P, _P, _P, _P, _P, _P]),
     "paragan_attn_bwd": (C.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "paragan_qknorm_check": (C.c_int, [_P]),
+    "paragan_qknorm_ws_size": (C.c_int, [_P, C.POINTER(C.c_size_t)]),
+    "paragan_qknorm_fwd": (C.c_int, [_P] * 10),
+    "paragan_qknorm_bwd": (C.c_int, [_P] * 15),
+    "paragan_mha_check": (C.c_int, [_P]),
+    "paragan_mha_sizes": (C.c_int, [_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "paragan_mha_fwd": (C.c_int, [_P] * 11),
+    "paragan_mha_bwd": (C.c_int, [_P] * 16),
     "paragan_gout_layout": (C.c_int, [_P, _P, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int64),
                                       C.POINTER(C.c_int64)]),
     "paragan_gout_sizes": (C.c_int, [_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
@@ -337,6 +359,84 @@ def paragan_attn_fwd(ctx, desc, params, u, x, y, saved, ws):
 def paragan_attn_bwd(ctx, desc, params, x, saved, dy, dx, grads, ws):
     return ctx.check(load().paragan_attn_bwd(ctx.h, C.byref(desc), _ptr(params), _ptr(x), _ptr(saved),
                                              _ptr(dy), _ptr(dx), _ptr(grads), _ptr(ws)))
+
+
+def qknorm_desc(q, k, qo=None, ko=None, *, rot, interleaved, n_pos, eps):
+    """QkNormDesc of q [T][Hq][d] and k [T][Hk][d] (heads side by side, any
+    token stride) with outputs laid out as qo and ko (None: contiguous)."""
+    import torch
+    T, hq, d = q.shape
+    hk = k.shape[1]
+    if k.shape[0] != T or k.shape[2] != d or k.dtype != q.dtype:
+        raise ParaganError(EINVAL, "qknorm: q and k differ in tokens, head width or type")
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise ParaganError(EINVAL, "qknorm: q must be bfloat16 or float32")
+    for t in (q, k, qo, ko):
+        if t is not None and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
+            raise ParaganError(EINVAL, "qknorm: the heads of a token must lie side by side")
+
+    def ld(t, h):   # a single token has no stride to speak of
+        return h * d if t is None or T == 1 else t.stride(0)
+    return QkNormDesc(T, hq, hk, d, int(rot), int(interleaved), int(n_pos),
+                      BF16 if q.dtype == torch.bfloat16 else F32, eps, ld(q, hq), ld(k, hk), ld(qo, hq), ld(ko, hk))
+
+
+def paragan_qknorm_check(desc):
+    return load().paragan_qknorm_check(C.byref(desc))
+
+
+def paragan_qknorm_ws_size(desc):
+    n = C.c_size_t()
+    _check_static(load().paragan_qknorm_ws_size(C.byref(desc), C.byref(n)))
+    return n.value
+
+
+def paragan_qknorm_fwd(ctx, desc, q, k, gain_q, gain_k, table, pos, qo, ko):
+    return ctx.check(load().paragan_qknorm_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(gain_q), _ptr(gain_k),
+                                               _ptr(table), _ptr(pos), _ptr(qo), _ptr(ko)))
+
+
+def paragan_qknorm_bwd(ctx, desc, q, k, gain_q, gain_k, table, pos, dqo, dko, dq, dk, dgain_q, dgain_k, ws):
+    return ctx.check(load().paragan_qknorm_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(gain_q), _ptr(gain_k),
+                                               _ptr(table), _ptr(pos), _ptr(dqo), _ptr(dko), _ptr(dq), _ptr(dk),
+                                               _ptr(dgain_q), _ptr(dgain_k), _ptr(ws)))
+
+
+def mha_desc(q, k, v, o, *, scale, causal=False, window=0, n_sink=0, n_buckets=0, max_distance=0):
+    """MhaDesc of q, o [B][Sq][Hq][d] and k, v [B][Sk][Hk][d] bf16 tensors or
+    views of any strides (the last dimension contiguous)."""
+    import torch
+    B, Sq, Hq, d = q.shape
+    Sk, Hk = k.shape[1], k.shape[2]
+    if tuple(o.shape) != (B, Sq, Hq, d) or tuple(k.shape) != (B, Sk, Hk, d) or tuple(v.shape) != (B, Sk, Hk, d):
+        raise ParaganError(EINVAL, "mha: the shapes of q, k, v and o do not belong together")
+    if any(t.dtype != torch.bfloat16 or t.stride(3) != 1 for t in (q, k, v, o)):
+        raise ParaganError(EINVAL, "mha: q, k, v and o must be bfloat16 with a contiguous last dimension")
+
+    def st(t):   # the stride of a dimension of one element means nothing
+        return (C.c_int64 * 3)(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
+    return MhaDesc(B, Sq, Sk, Hq, Hk, d, int(causal), int(window), int(n_sink), int(n_buckets), int(max_distance),
+                   scale, st(q), st(k), st(v), st(o))
+
+
+def paragan_mha_check(desc):
+    return load().paragan_mha_check(C.byref(desc))
+
+
+def paragan_mha_sizes(desc):
+    return _sizes(load().paragan_mha_sizes, desc)
+
+
+def paragan_mha_fwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, ws):
+    """saved: None when no backward follows."""
+    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(table),
+                                            _ptr(len_q), _ptr(len_k), _ptr(o), _ptr(saved), _ptr(ws)))
+
+
+def paragan_mha_bwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, dout, dq, dk, dv, dtable, ws):
+    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(table),
+                                            _ptr(len_q), _ptr(len_k), _ptr(o), _ptr(saved), _ptr(dout), _ptr(dq),
+                                            _ptr(dk), _ptr(dv), _ptr(dtable), _ptr(ws)))
 
 
 def paragan_gout_layout(desc):
