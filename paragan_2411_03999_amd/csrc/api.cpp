@@ -569,6 +569,8 @@ static Mha make_mha(const paragan_mha_desc* d) {
       PG_CHECK(s < (1LL << 60) / big, "mha: a stride is too large");
     }
   }
+  for (int64_t t : {m.qs[1], m.ks[1], m.vs[1], m.os[1]})   // a tile of 64 tokens is addressed in 32 bits
+    PG_CHECK(t < (1LL << 24), "mha: a token stride is 2^24 or more");
   PG_CHECK(distinct(m.os, m.B, m.Sq, m.Hq, m.d), "mha: o overlaps itself");
   return m;
 }

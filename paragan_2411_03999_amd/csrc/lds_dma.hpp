@@ -23,6 +23,12 @@ PG_DEV void lds_load16(uint32_t lds_base, uint32_t voff, uint32_t soff, __amdgpu
                : "memory", "m0");
 }
 
+// 4 bytes per lane: as lds_load16, at M0 + 4 * lane
+PG_DEV void lds_load4(uint32_t lds_base, uint32_t voff, __amdgpu_buffer_rsrc_t r) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_base), "v"(voff), "s"(r)
+               : "memory", "m0");
+}
+
 // Wait until at most N of this wave's vector-memory loads are outstanding
 // and all of its LDS reads have completed, then barrier: one statement, so
 // nothing the compiler schedules can slip between the wait and the barrier.

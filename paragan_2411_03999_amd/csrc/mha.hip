@@ -23,18 +23,47 @@
 #include <type_traits>
 
 #include "attn_tiles.hpp"
+#include "lds_dma.hpp"
 #include "token.hpp"
+#ifndef DKV_OCC
+#define DKV_OCC 1
+#endif
+#ifndef FWD_QT
+#define FWD_QT 1
+#endif
+#ifndef FWD64
+#define FWD64 1
+#endif
+#ifndef FO64
+#define FO64 3
+#endif
+#ifndef FWD_OCC
+#define FWD_OCC 2
+#endif
+#ifndef DQ_QT
+#define DQ_QT 1
+#endif
+#ifndef DO64
+#define DO64 2
+#endif
+#ifndef DQ64
+#define DQ64 2
+#endif
+#ifndef DQ_OCC
+#define DQ_OCC 2
+#endif
 
 namespace pg {
 
 namespace {
 
-constexpr int kMargin = 64;   // distances past max_distance that a 32 x 32 tile can reach, rounded up
+constexpr int kMargin = 96;   // distances past max_distance that a 64 x 32 tile can reach, rounded up
 
 struct MhaArgs {
   int B, Sq, Sk, Hq, Hk, G, d, Sqp, nblk;
   int causal, window, n_sink, nb, maxd, half;
-  int nsplit, nrt;
+  int nsplit, nrt, hset;
+  int nks, ns_sink, ns_reg, chunk;   // dk, dv: key blocks with first tokens, splits of these and of the others, steps of a split
   float c, scale;               // c = scale log2(e)
   int64_t qs[3], ks[3], vs[3], os[3];
   const bf16_t *q, *k, *v, *dO;
@@ -46,31 +75,46 @@ struct MhaArgs {
   uint8_t lut[kMhaMaxDist + 8]; // bucket (of one side) of each distance
 };
 
+// Block order.  Consecutive block numbers go round the 8 XCDs, each with an L2
+// of its own; heads that share keys and values are brought onto one XCD, in
+// sets of a.hset heads given to the XCDs in turn (0: left as they come).
+// Causal 2 x 8192 x 16 heads x 128: 784 us in plain order, 575 so.
+PG_DEV int block_no(const MhaArgs& a, int per_head) {
+  const int x = blockIdx.x;
+  if (a.hset == 0) return x;
+  const int y = x >> 3, per = per_head * a.hset, set = y / per;
+  return (set * 8 + (x & 7)) * per + y - set * per;
+}
+
 struct Seq { int lq, lk, off; };
 PG_DEV Seq seq_of(const MhaArgs& a, int b) {
   Seq s;
   s.lq = a.len_q ? min(max(a.len_q[b], 0), a.Sq) : a.Sq;
   s.lk = a.len_k ? min(max(a.len_k[b], 0), a.Sk) : a.Sk;
+  s.lq = __builtin_amdgcn_readfirstlane(s.lq);
+  s.lk = __builtin_amdgcn_readfirstlane(s.lk);
   s.off = s.lk - s.lq;
   return s;
 }
 
 // Keys that queries at positions p0 .. p1 see: [lo, hi) through the window
-// and [0, ns) of the first tokens, as nt tiles of 32: tile n is
+// and [0, ns) of the first tokens, as nt tiles of TK: tile n is
 // n (n < st) or n - st + ws.
+template <int TK>
 struct Span {
   int lo, hi, ns, st, ws, nt;
-  PG_DEV int key0(int n) const { return 32 * (n < st ? n : n - st + ws); }
+  PG_DEV int key0(int n) const { return TK * (n < st ? n : n - st + ws); }
   PG_DEV bool row(int j) const { return (j >= lo && j < hi) || j < ns; }
-  PG_DEV bool tile(int k0) const { return (k0 + 32 > lo && k0 < hi) || k0 < ns; }
+  PG_DEV bool tile(int k0) const { return (k0 + TK > lo && k0 < hi) || k0 < ns; }
 };
-PG_DEV Span span_of(const MhaArgs& a, int lk, int p0, int p1) {
-  Span s;
+template <int TK>
+PG_DEV Span<TK> span_of(const MhaArgs& a, int lk, int p0, int p1) {
+  Span<TK> s;
   const int top = max(a.causal ? min(lk, p1 + 1) : lk, 0);
   s.lo = a.window ? max(p0 - a.window + 1, 0) : 0;
   s.hi = a.window && !a.causal ? max(min(lk, p1 + a.window), 0) : top;
   s.ns = a.window ? min(a.n_sink, top) : 0;
-  const int sink_tiles = (s.ns + 31) >> 5, w0 = s.lo >> 5, w1 = (s.hi + 31) >> 5;
+  const int sink_tiles = (s.ns + TK - 1) / TK, w0 = s.lo / TK, w1 = (s.hi + TK - 1) / TK;
   if (sink_tiles >= w0) {
     s.st = 0;
     s.ws = 0;
@@ -83,10 +127,11 @@ PG_DEV Span span_of(const MhaArgs& a, int lk, int p0, int p1) {
   }
   return s;
 }
-// Does every query at positions p0 .. p1 see every key of [k0, k0 + 32)?
+// Does every query at positions p0 .. p1 see every key of [k0, k0 + TK)?
+template <int TK>
 PG_DEV bool all_seen(const MhaArgs& a, int lk, int k0, int p0, int p1) {
-  if (k0 + 32 > lk || (a.causal && k0 + 31 > p0)) return false;
-  return !a.window || k0 + 32 <= a.n_sink || (p1 - k0 < a.window && k0 + 31 - p0 < a.window);
+  if (k0 + TK > lk || (a.causal && k0 + TK - 1 > p0)) return false;
+  return !a.window || k0 + TK <= a.n_sink || (p1 - k0 < a.window && k0 + TK - 1 - p0 < a.window);
 }
 // visible keys of one query: [lo, hi) and [0, ns)
 struct Row { int lo, hi, ns; };
@@ -100,6 +145,13 @@ PG_DEV Row row_of(const MhaArgs& a, int lk, int p) {
 }
 PG_DEV bool sees(const Row& r, int j) { return (j >= r.lo && j < r.hi) || j < r.ns; }
 
+// max of three without the quieting moves that fmaxf asks for (a NaN score gives NaN through its exponential)
+PG_DEV float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // bias in log2 units at distance index e = rel + maxd + kMargin; distances past max_distance are its own
 PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
   const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
@@ -110,30 +162,31 @@ PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
 }
 PG_DEV int bias_len(const MhaArgs& a) { return 2 * (a.maxd + kMargin) + 1; }
 
-// Stage 32 rows x NC chunks into a swizzled tile by 256 threads: thread slots
-// i = tid + 256 j; chunks at or past d and rows that `ok` refuses are zero.
+// 64 rows x NC chunks from memory straight into a swizzled LDS tile by 4
+// waves: 16-byte slot i of the tile (lane order) holds chunk (i % NC) ^ swizzle
+// of row i / NC.  Chunks at or past d and rows that `ok` refuses read as zeros
+// without touching memory.
 template <int NC>
-struct Stage {
-  static constexpr int SLOTS = (32 * NC + 255) / 256;
-  uint4 v[SLOTS];
-  template <class F>
-  PG_DEV void load(const bf16_t* base, int64_t ld, int r0, int d, int tid, F ok) {
+struct Ring {
+  static constexpr int N = NC / 4;   // loads of a wave
+  uint32_t off[N];
+  int row[N];
+  PG_DEV void init(int64_t ld, int d, int tid) {
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
-      const int i = tid + 256 * j;
-      const int r = i / NC, c = i - (i / NC) * NC;
-      v[j] = make_uint4(0, 0, 0, 0);
-      if (i < 32 * NC && c * 8 < d && ok(r0 + r))
-        v[j] = *reinterpret_cast<const uint4*>(base + (int64_t)(r0 + r) * ld + c * 8);
+    for (int j = 0; j < N; ++j) {
+      const int i = ((tid >> 6) * N + j) * 64 + (tid & 63);
+      const int r = i / NC, c = (i - r * NC) ^ swz16<NC>(r);
+      row[j] = r;
+      off[j] = c * 8 < d ? (uint32_t)(r * (int)ld * 2 + c * 16) : kOOB;
     }
   }
-  PG_DEV void store(bf16_t* t, int tid) const {
+  // base: row 0 of the tile (uniform); rows r0 + r
+  template <class F>
+  PG_DEV void issue(bf16_t* tile, const bf16_t* base, int64_t ld, int r0, int wave, F ok) const {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, (63 * ld + NC * 8) * 2);
+    const uint32_t dst = lds_addr(tile) + wave * N * 1024;
 #pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
-      const int i = tid + 256 * j;
-      const int r = i / NC, c = i - (i / NC) * NC;
-      if (i < 32 * NC) *reinterpret_cast<uint4*>(t + toff<NC>(r, c * 8)) = v[j];
-    }
+    for (int j = 0; j < N; ++j) lds_load16(dst + j * 1024, ok(r0 + row[j]) ? off[j] : kOOB, 0, rs);
   }
 };
 
@@ -145,18 +198,20 @@ PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
 }
 
 // ------------------------------------------------------------- forward
-// A wave owns 32 QT queries of one head; a block of 4 waves 128 QT.
+// A wave owns 32 QT queries of one head; a block of 4 waves 128 QT.  Keys and
+// values come in tiles of 64, the next one loading while this one is used.
 template <int DT, int QT, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_mha_fwd(MhaArgs a) {
-  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
-  __shared__ __attribute__((aligned(16))) bf16_t Ks[2][32 * DT];
-  __shared__ __attribute__((aligned(16))) bf16_t Vs[2][32 * DT];
+__global__ __launch_bounds__(256, DT >= 96 ? FWD_OCC : FO64) void k_mha_fwd(MhaArgs a) {
+  constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[2][TK * DT];
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[2][TK * DT];
   extern __shared__ float bs[];
   // the last queries of a causal head see the most keys: they start first
-  const int qb = a.nblk - 1 - (int)(blockIdx.x % a.nblk), bh = blockIdx.x / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
+  const int id = block_no(a, a.nblk), qb = a.nblk - 1 - id % a.nblk, bh = id / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
-  const int qblk = qb * 128 * QT, qw = qblk + (tid >> 6) * 32 * QT;
+  const int qblk = qb * 128 * QT, qw = qblk + wv * 32 * QT;
   const bf16_t* K = a.k + b * a.ks[0] + (h / a.G) * a.ks[2];
   const bf16_t* V = a.v + b * a.vs[0] + (h / a.G) * a.vs[2];
   if (BIAS)
@@ -183,103 +238,108 @@ __global__ __launch_bounds__(256, 2) void k_mha_fwd(MhaArgs a) {
       for (int r = 0; r < 16; ++r) acc[u][j][r] = 0.f;
   }
   // a block behind the last query visits nothing and writes zeros
-  Span sp = span_of(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
+  Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
   if (qblk >= sq.lq) sp.nt = 0;
-  const Span sw = span_of(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
+  const Span<TK> sw = span_of<TK>(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
   const bool mine = qw < sq.lq;
-  Stage<NC> sk, sv;
-  auto load = [&](int n) {
-    auto ok = [&](int j) { return sp.row(j); };
-    sk.load(K, a.ks[1], sp.key0(n), a.d, tid, ok);
-    sv.load(V, a.vs[1], sp.key0(n), a.d, tid, ok);
-  };
-  if (sp.nt > 0) {
-    load(0);
-    sk.store(Ks[0], tid);
-    sv.store(Vs[0], tid);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int n = 0; n < sp.nt; ++n) {
-    const bool more = n + 1 < sp.nt;
-    if (more) load(n + 1);
+  Ring<NC> rk, rv;
+  rk.init(a.ks[1], a.d, tid);
+  rv.init(a.vs[1], a.d, tid);
+  auto load = [&](int n, int bf) {
     const int k0 = sp.key0(n);
-    if (mine && sw.tile(k0)) {
-      const bf16_t* ks = Ks[buf];
-      const bf16_t* vs = Vs[buf];
-      f32x16 s[QT];
+    auto ok = [&](int j) { return sp.row(j); };
+    rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, ok);
+    rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, ok);
+  };
+  if (sp.nt > 0) load(0, 0);
+  for (int n = 0; n < sp.nt; ++n) {
+    wait_barrier<0>();   // tile n is in LDS, and every wave has left tile n - 1
+    const int buf = n & 1, k0 = sp.key0(n);
+    if (n + 1 < sp.nt) load(n + 1, buf ^ 1);
+    if (!mine || !sw.tile(k0)) continue;
+    const bf16_t* ks = Ks[buf];
+    const bf16_t* vs = Vs[buf];
+    f32x16 s[QT][2];
 #pragma unroll
-      for (int u = 0; u < QT; ++u)
+    for (int u = 0; u < QT; ++u)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+      for (int r = 0; r < 16; ++r) s[u][0][r] = s[u][1][r] = 0.f;
 #pragma unroll
-      for (int t = 0; t < KF; ++t) {
-        const bf16x8 ka = ld_row<NC>(ks, lq, 16 * t + 8 * g);
+    for (int t = 0; t < KF; ++t)
 #pragma unroll
-        for (int u = 0; u < QT; ++u) s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[u][t], s[u], 0, 0, 0);
+      for (int x = 0; x < 2; ++x) {
+        const bf16x8 ka = ld_row<NC>(ks + 32 * DT * x, lq, 16 * t + 8 * g);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+          s[u][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[u][t], s[u][x], 0, 0, 0);
       }
 #pragma unroll
-      for (int u = 0; u < QT; ++u) {
-        const int p0 = qw + 32 * u + sq.off;
-        if (BIAS) {
-          if (k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd) {
-            const float* bl = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
+    for (int u = 0; u < QT; ++u) {
+      const int p0 = qw + 32 * u + sq.off;
+      if (BIAS) {
+        if (k0 + TK - 1 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd) {
+          const float* bl = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, bl[8 * (r >> 2) + (r & 3)]);
-          } else {
-            const float far = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, far);
-          }
+            for (int r = 0; r < 16; ++r) s[u][x][r] = fmaf(s[u][x][r], a.c, bl[32 * x + 8 * (r >> 2) + (r & 3)]);
+        } else {
+          const float far = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[u][x][r] = fmaf(s[u][x][r], a.c, far);
         }
-        if (!all_seen(a, sq.lk, k0, p0, p0 + 31)) {
+      }
+      if (!all_seen<TK>(a, sq.lk, k0, p0, p0 + 31)) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (!sees(rw[u], k0 + acc_row(r, g))) s[u][r] = -INFINITY;
-        }
-        float mb = s[u][0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) mb = fmaxf(mb, s[u][r]);
-        mb = fmaxf(mb, __shfl_xor(mb, 32, 64));
-        if (!BIAS) mb *= a.c;
-        if (mb > m2[u] + kTau) {
-          const float alpha = exp2_(m2[u] - mb);
-          l[u] *= alpha;
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[u][j][r] *= alpha;
-          m2[u] = mb;
-        }
-        const float ms = m2[u] == -INFINITY ? 0.f : m2[u];   // nothing seen yet: every term is 2^-inf
-        float ls = 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[u][r] = exp2_(BIAS ? s[u][r] - ms : fmaf(s[u][r], a.c, -ms));
-          ls += s[u][r];
-        }
-        l[u] += ls;
+            if (!sees(rw[u], k0 + 32 * x + acc_row(r, g))) s[u][x][r] = -INFINITY;
       }
+      float mb = s[u][0][0], mc = s[u][1][0];   // two chains
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        bf16x8 pb[QT];
+      for (int r = 1; r < 15; r += 2) {
+        mb = max3(mb, s[u][0][r], s[u][0][r + 1]);
+        mc = max3(mc, s[u][1][r], s[u][1][r + 1]);
+      }
+      mb = max3(max3(mb, s[u][0][15], s[u][1][15]), mc, mc);
+      mb = max3(mb, mb, __shfl_xor(mb, 32, 64));
+      if (!BIAS) mb *= a.c;
+      if (mb > m2[u] + kTau) {
+        const float alpha = exp2_(m2[u] - mb);
+        l[u] *= alpha;
 #pragma unroll
-        for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u], t);
+        for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          const bf16x8 va = ld_tr<NC>(vs, t, 32 * j, lane);
+          for (int r = 0; r < 16; ++r) acc[u][j][r] *= alpha;
+        m2[u] = mb;
+      }
+      const float ms = m2[u] == -INFINITY ? 0.f : m2[u];   // nothing seen yet: every term is 2^-inf
+      float ls[2] = {0.f, 0.f};
 #pragma unroll
-          for (int u = 0; u < QT; ++u)
-            acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[u], acc[u][j], 0, 0, 0);
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          s[u][x][r] = exp2_(BIAS ? s[u][x][r] - ms : fmaf(s[u][x][r], a.c, -ms));
+          ls[x] += s[u][x][r];
         }
+      l[u] += ls[0] + ls[1];
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      bf16x8 pb[QT];
+#pragma unroll
+      for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u][t >> 1], t & 1);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const bf16x8 va = ld_tr<NC>(vs + 32 * DT * (t >> 1), t & 1, 32 * j, lane);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+          acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[u], acc[u][j], 0, 0, 0);
       }
     }
-    if (more) {
-      sk.store(Ks[buf ^ 1], tid);
-      sv.store(Vs[buf ^ 1], tid);
-    }
-    __syncthreads();
-    buf ^= 1;
   }
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
@@ -345,7 +405,7 @@ __global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
   float m2 = -INFINITY, l = 0.f;
-  Span sp = span_of(a, sq.lk, sq.off, sq.off + sq.lq - 1);
+  Span<32> sp = span_of<32>(a, sq.lk, sq.off, sq.off + sq.lq - 1);
   if (sq.lq == 0) sp.nt = 0;
   const int per = (sp.nt + a.nsplit - 1) / a.nsplit, n1 = min(sp.nt, (z + 1) * per);
   for (int n = z * per + wv; n < n1; n += 4) {
@@ -378,7 +438,7 @@ __global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
         s[r] = fmaf(s[r], a.c, dyn[lq * a.nb + lut[rel + a.maxd + kMargin]]);
       }
     }
-    if (!all_seen(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) {
+    if (!all_seen<32>(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (!sees(rw, k0 + acc_row(r, g))) s[r] = -INFINITY;
@@ -501,19 +561,20 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 // one instruction meet and the order of the sums is fixed; tiles past
 // max_distance add into one register per side.
 template <int DT, int QT, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
-  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
-  __shared__ __attribute__((aligned(16))) bf16_t Ks[2][32 * DT];
-  __shared__ __attribute__((aligned(16))) bf16_t Vs[2][32 * DT];
+__global__ __launch_bounds__(256, DT >= 96 ? DQ_OCC : DO64) void k_mha_dq(MhaArgs a) {
+  constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Ks[2][TK * DT];
+  __shared__ __attribute__((aligned(16))) bf16_t Vs[2][TK * DT];
   extern __shared__ float bs[];   // bias by distance, then 8 arrays of dS sums by distance
-  const int qb = a.nblk - 1 - (int)(blockIdx.x % a.nblk), bh = blockIdx.x / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
+  const int id = block_no(a, a.nblk), qb = a.nblk - 1 - id % a.nblk, bh = id / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
-  const int qblk = qb * 128 * QT, qw = qblk + (tid >> 6) * 32 * QT;
+  const int qblk = qb * 128 * QT, qw = qblk + wv * 32 * QT;
   const bf16_t* K = a.k + b * a.ks[0] + (h / a.G) * a.ks[2];
   const bf16_t* V = a.v + b * a.vs[0] + (h / a.G) * a.vs[2];
   const int bl = BIAS ? bias_len(a) : 0;
-  float* const gs = bs + bl + (2 * (tid >> 6) + g) * bl;
+  float* const gs = bs + bl + (2 * wv + g) * bl;
   if (BIAS) {
     for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, h, e);
     for (int e = tid; e < 8 * bl; e += 256) bs[bl + e] = 0.f;
@@ -534,19 +595,26 @@ __global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
       qf[u][t] = ld_frag(Q, 16 * t + 8 * g, a.d, ok);
       df[u][t] = ld_frag(DO, 16 * t + 8 * g, a.d, ok);
       if (!BIAS) {
+        // from the bf16 output: off by at most 2^-8 of sum |do||o|, as much as dS loses when it becomes an operand
         float x[8], o[8];
         unpack8(__builtin_bit_cast(uint4, df[u][t]), x);
-        // from the bf16 output: off by at most 2^-8 of sum |do||o|, as much as dS loses when it becomes an operand
         unpack8(__builtin_bit_cast(uint4, ld_frag(O, 16 * t + 8 * g, a.d, ok)), o);
 #pragma unroll
         for (int e = 0; e < 8; ++e) dd[u] = fmaf(x[e], o[e], dd[u]);
       }
     }
-    dd[u] += __shfl_xor(dd[u], 32, 64);
     ls2[u] = ok ? a.lse[(int64_t)bh * a.Sqp + q] : INFINITY;
-    if (!BIAS && g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = ok ? dd[u] : 0.f;
     rw[u] = row_of(a, sq.lk, q + sq.off);
   }
+  // the rows' D, once known, to every lane and for the key-owned pass
+  auto row_terms = [&]() {
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+      const int q = qw + 32 * u + lq;
+      dd[u] += __shfl_xor(dd[u], 32, 64);
+      if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = q < sq.lq ? dd[u] : 0.f;
+    }
+  };
   f32x16 acc[QT][NT];
 #pragma unroll
   for (int u = 0; u < QT; ++u)
@@ -555,35 +623,35 @@ __global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[u][j][r] = 0.f;
   float flo = 0.f, fhi = 0.f;
-  Span sp = span_of(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
+  Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
   if (qblk >= sq.lq) sp.nt = 0;
-  const Span sw = span_of(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
+  const Span<32> sw = span_of<32>(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
   const bool mine = qw < sq.lq;
-  Stage<NC> sk, sv;
-  auto load = [&](int n) {
+  Ring<NC> rk, rv;
+  rk.init(a.ks[1], a.d, tid);
+  rv.init(a.vs[1], a.d, tid);
+  auto load = [&](int n, int bf) {
+    const int k0 = sp.key0(n);
     auto ok = [&](int j) { return sp.row(j); };
-    sk.load(K, a.ks[1], sp.key0(n), a.d, tid, ok);
-    sv.load(V, a.vs[1], sp.key0(n), a.d, tid, ok);
+    rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, ok);
+    rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, ok);
   };
   // One pass over the keys.  FIRST (with a bias only): dd = sum P dP in fp32.
   // The bias gradient sums dS over many pairs with little left over; a row
   // term from a rounded output, or from rounded P, would dominate it.
   auto pass = [&](auto first_c) {
     constexpr bool FIRST = decltype(first_c)::value;
-    if (sp.nt > 0) {
-      load(0);
-      sk.store(Ks[0], tid);
-      sv.store(Vs[0], tid);
-    }
-    __syncthreads();
-    int buf = 0;
+    if (sp.nt > 0) load(0, 0);
     for (int n = 0; n < sp.nt; ++n) {
-      const bool more = n + 1 < sp.nt;
-      if (more) load(n + 1);
-      const int k0 = sp.key0(n);
-      if (mine && sw.tile(k0)) {
-        const bf16_t* ks = Ks[buf];
-        const bf16_t* vs = Vs[buf];
+      wait_barrier<0>();   // tile n is in LDS, and every wave has left tile n - 1
+      const int buf = n & 1;
+      if (n + 1 < sp.nt) load(n + 1, buf ^ 1);
+#pragma unroll 1
+      for (int x = 0; x < 2; ++x) {
+        const int k0 = sp.key0(n) + 32 * x;
+        if (!mine || !sw.tile(k0)) continue;
+        const bf16_t* ks = Ks[buf] + 32 * DT * x;
+        const bf16_t* vs = Vs[buf] + 32 * DT * x;
         f32x16 s[QT], dp[QT];
 #pragma unroll
         for (int u = 0; u < QT; ++u)
@@ -603,20 +671,15 @@ __global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
           const int p0 = qw + 32 * u + sq.off;
           const bool near = BIAS && k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd;
           const int at = k0 - p0 - lq + a.maxd + kMargin + 4 * g;
-          if (BIAS) {
-            if (near) {
+          if (BIAS && near) {
 #pragma unroll
-              for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, bs[at + 8 * (r >> 2) + (r & 3)] - ls2[u]);
-            } else {
-              const float far = (k0 < p0 ? bs[0] : bs[bl - 1]) - ls2[u];
-#pragma unroll
-              for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, far);
-            }
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, bs[at + 8 * (r >> 2) + (r & 3)] - ls2[u]);
           } else {
+            const float far = (BIAS ? (k0 < p0 ? bs[0] : bs[bl - 1]) : 0.f) - ls2[u];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, -ls2[u]);
+            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, far);
           }
-          if (!all_seen(a, sq.lk, k0, p0, p0 + 31)) {
+          if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) {
 #pragma unroll
             for (int r = 0; r < 16; ++r)
               if (!sees(rw[u], k0 + acc_row(r, g))) s[u][r] = -INFINITY;
@@ -631,7 +694,8 @@ __global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
           if (BIAS) {
             if (near) {
 #pragma unroll
-              for (int r = 0; r < 16; ++r) __hip_atomic_fetch_add(gs + at + 8 * (r >> 2) + (r & 3), s[u][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              for (int r = 0; r < 16; ++r)
+                __hip_atomic_fetch_add(gs + at + 8 * (r >> 2) + (r & 3), s[u][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
             } else {
               float t = 0.f;
 #pragma unroll
@@ -640,38 +704,27 @@ __global__ __launch_bounds__(256, 2) void k_mha_dq(MhaArgs a) {
             }
           }
         }
-        if (!FIRST)
+        if constexpr (!FIRST) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          bf16x8 pb[QT];
+          for (int t = 0; t < 2; ++t) {
+            bf16x8 pb[QT];
 #pragma unroll
-          for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u], t);
+            for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u], t);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            const bf16x8 ka = ld_tr<NC>(ks, t, 32 * j, lane);
+            for (int j = 0; j < NT; ++j) {
+              const bf16x8 ka = ld_tr<NC>(ks, t, 32 * j, lane);
 #pragma unroll
-            for (int u = 0; u < QT; ++u)
-              acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, pb[u], acc[u][j], 0, 0, 0);
+              for (int u = 0; u < QT; ++u)
+                acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, pb[u], acc[u][j], 0, 0, 0);
+            }
           }
         }
       }
-      if (more) {
-        sk.store(Ks[buf ^ 1], tid);
-        sv.store(Vs[buf ^ 1], tid);
-      }
-      __syncthreads();
-      buf ^= 1;
     }
+    __syncthreads();   // the tiles and (BIAS) the sums are free, or whole
   };
-  if (BIAS) {
-    pass(std::integral_constant<bool, true>());
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      const int q = qw + 32 * u + lq;
-      dd[u] += __shfl_xor(dd[u], 32, 64);
-      if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = q < sq.lq ? dd[u] : 0.f;
-    }
-  }
+  if (BIAS) pass(std::integral_constant<bool, true>());
+  row_terms();
   pass(std::integral_constant<bool, false>());
 #pragma unroll
   for (int u = 0; u < QT; ++u) {
@@ -724,19 +777,61 @@ __global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int
 
 // ------------------------------------------------------------- dk, dv (key-owned)
 // A wave owns 32 keys of one key head, a block 128; the steps run over the
-// query heads of the group and their 32-query tiles, so the gradients of a
-// shared head are summed in registers.
+// query heads of the group and their 64-query tiles, so the gradients of a
+// shared head are summed in registers.  A key block that many queries see
+// (first tokens beside a window; few, long sequences) is split over blocks of
+// `chunk` steps, whose fp32 partials k_mha_dkv_join adds in split order.
+
+// the queries [i0, i1) that see some key of [j0, j1]
+PG_DEV void seen_by(const MhaArgs& a, const Seq& sq, int j0, int j1, int& i0, int& i1) {
+  j1 = min(j1, sq.lk - 1);
+  const bool sink = a.window && j0 < a.n_sink;
+  const int lo = a.causal ? j0 : a.window && !sink ? j0 - a.window + 1 : -0x40000000;
+  const int hi = a.window && !sink ? j1 + a.window - 1 : 0x40000000;
+  i0 = max(lo - sq.off, 0);
+  i1 = min(hi - sq.off + 1, sq.lq);
+  if (j1 < j0) i1 = i0;
+}
+
+// item of a launch: key block, split, and the slot of its partials
+struct KItem { int bh, kb, z; int64_t slot; };
+PG_DEV KItem item_of(const MhaArgs& a, int x) {
+  const int sinks = a.nks * a.ns_sink, per = sinks + (a.nblk - a.nks) * a.ns_reg;
+  KItem it;
+  it.bh = x / per;
+  const int y = x - it.bh * per;
+  if (y < sinks) {
+    it.kb = y / a.ns_sink;
+    it.z = y - it.kb * a.ns_sink;
+  } else {
+    it.kb = a.nks + (y - sinks) / a.ns_reg;
+    it.z = (y - sinks) % a.ns_reg;
+  }
+  // slots only for the classes that split
+  const int64_t both = (a.ns_sink > 1 ? sinks : 0) + (a.ns_reg > 1 ? per - sinks : 0);
+  it.slot = it.bh * both + (y < sinks ? y : y - sinks + (a.ns_sink > 1 ? sinks : 0));
+  return it;
+}
+
 template <int DT, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
-  constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
-  __shared__ __attribute__((aligned(16))) bf16_t Qs[2][32 * DT];
-  __shared__ __attribute__((aligned(16))) bf16_t Ds[2][32 * DT];
-  __shared__ __attribute__((aligned(16))) float Ls[2][32], Dd[2][32];
-  extern __shared__ float bs[];   // the current head's bias by query minus key
-  const int kb = blockIdx.x % a.nblk, bh = blockIdx.x / a.nblk, hk = bh % a.Hk, b = bh / a.Hk;
+__global__ __launch_bounds__(256, DT >= 96 ? DKV_OCC : 2) void k_mha_dkv(MhaArgs a) {
+  constexpr int TQ = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
+  __shared__ __attribute__((aligned(16))) bf16_t Qs[2][TQ * DT];
+  __shared__ __attribute__((aligned(16))) bf16_t Ds[2][TQ * DT];
+  extern __shared__ float ex[];   // rows' log sums and D of the two tiles, then the current head's bias by query minus key
+  float* const bs = ex + 4 * TQ;
+  const KItem it = item_of(a, block_no(a, a.nks * a.ns_sink + (a.nblk - a.nks) * a.ns_reg));
+  const int hk = it.bh % a.Hk, b = it.bh / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lk = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
-  const int kblk = kb * 128, kw = kblk + (tid >> 6) * 32, key = kw + lk;
+  const int kblk = it.kb * 128;
+  int i0, i1;
+  seen_by(a, sq, kblk, kblk + 127, i0, i1);
+  const int t0 = i0 / TQ, nt = max((i1 + TQ - 1) / TQ - t0, 0);
+  const int n0 = it.z * a.chunk, n1 = min(n0 + a.chunk, nt * a.G);
+  if (it.z > 0 && n0 >= n1) return;
+  const int kw = kblk + wv * 32, key = kw + lk;
   const bool kv = key < sq.lk;
   const int bl = BIAS ? bias_len(a) : 0;
   bf16x8 kf[KF], vf[KF];
@@ -750,60 +845,41 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) { adk[j][r] = 0.f; adv[j][r] = 0.f; }
-  // queries [i0, i1) that see some key of [j0, j1]
-  auto seen_by = [&](int j0, int j1, int& i0, int& i1) {
-    j1 = min(j1, sq.lk - 1);
-    const bool sink = a.window && j0 < a.n_sink;
-    int lo = a.causal ? j0 : a.window && !sink ? j0 - a.window + 1 : -0x40000000;
-    int hi = a.window && !sink ? j1 + a.window - 1 : 0x40000000;
-    i0 = max(lo - sq.off, 0);
-    i1 = min(hi - sq.off + 1, sq.lq);
-    if (j1 < j0) i1 = i0;
-  };
-  int i0, i1, w0, w1;
-  seen_by(kblk, kblk + 127, i0, i1);
-  seen_by(kw, kw + 31, w0, w1);
-  const int t0 = i0 >> 5, nt = max(((i1 + 31) >> 5) - t0, 0);
+  int w0, w1;
+  seen_by(a, sq, kw, kw + 31, w0, w1);
   // this lane's key is seen from positions plo .. phi
   const bool sink = key < a.n_sink;
   const int plo = !kv ? 0x7fffffff : a.causal ? key : a.window && !sink ? key - a.window + 1 : -0x40000000;
   const int phi = a.window && !sink ? key + a.window - 1 : 0x7fffffff;
-  Stage<NC> st_q, st_d;
-  float sl = 0.f, sd = 0.f;
-  auto load = [&](int n) {
-    const int h = hk * a.G + n / nt, q0 = 32 * (t0 + n % nt);
+  Ring<NC> rq, rd;
+  rq.init(a.qs[1], a.d, tid);
+  rd.init(a.os[1], a.d, tid);
+  auto load = [&](int n, int bf) {
+    const int h = hk * a.G + n / nt, q0 = TQ * (t0 + n % nt);
     auto ok = [&](int i) { return i >= i0 && i < i1; };
-    st_q.load(a.q + b * a.qs[0] + h * a.qs[2], a.qs[1], q0, a.d, tid, ok);
-    st_d.load(a.dO + b * a.os[0] + h * a.os[2], a.os[1], q0, a.d, tid, ok);
-    if (tid < 32) {
-      const int64_t x = ((int64_t)b * a.Hq + h) * a.Sqp + q0 + tid;
-      sl = ok(q0 + tid) ? a.lse[x] : INFINITY;
-      sd = a.D[x];
-    }
+    rq.issue(Qs[bf], a.q + b * a.qs[0] + h * a.qs[2] + q0 * a.qs[1], a.qs[1], q0, wv, ok);
+    rd.issue(Ds[bf], a.dO + b * a.os[0] + h * a.os[2] + q0 * a.os[1], a.os[1], q0, wv, ok);
+    // 64 rows of both: the buffers are padded to 64, rows past len_q hold +inf and 0
+    const int64_t x = ((int64_t)b * a.Hq + h) * a.Sqp + q0;
+    if (wv == 0) lds_load4(lds_addr(ex + bf * 2 * TQ), lane * 4, make_rsrc(a.lse + x, TQ * 4));
+    if (wv == 1) lds_load4(lds_addr(ex + bf * 2 * TQ + TQ), lane * 4, make_rsrc(a.D + x, TQ * 4));
   };
-  auto store = [&](int bf) {
-    st_q.store(Qs[bf], tid);
-    st_d.store(Ds[bf], tid);
-    if (tid < 32) { Ls[bf][tid] = sl; Dd[bf][tid] = sd; }
-  };
-  const int steps = nt * a.G;
-  if (steps > 0) {
-    load(0);
-    store(0);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int n = 0; n < steps; ++n) {
-    const bool more = n + 1 < steps;
-    if (more) load(n + 1);
-    const int q0 = 32 * (t0 + n % nt), p0 = q0 + sq.off;
-    if (BIAS && n % nt == 0) {   // the next head's bias; the last step's reads ended at its barrier
+  if (n0 < n1) load(n0, 0);
+  for (int n = n0; n < n1; ++n) {
+    wait_barrier<0>();   // tile n is in LDS, and every wave has left tile n - 1
+    const int buf = (n - n0) & 1;
+    if (n + 1 < n1) load(n + 1, buf ^ 1);
+    if (BIAS && (n == n0 || n % nt == 0)) {   // the next head's bias
       for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, hk * a.G + n / nt, bl - 1 - e);
       __syncthreads();
     }
-    if (q0 + 32 > w0 && q0 < w1) {
-      const bf16_t* qs = Qs[buf];
-      const bf16_t* ds = Ds[buf];
+#pragma unroll 1
+    for (int x = 0; x < 2; ++x) {
+      const int q0 = TQ * (t0 + n % nt) + 32 * x, p0 = q0 + sq.off;
+      if (q0 + 32 <= w0 || q0 >= w1) continue;
+      const bf16_t* qs = Qs[buf] + 32 * DT * x;
+      const bf16_t* ds = Ds[buf] + 32 * DT * x;
+      const float* Ls = ex + buf * 2 * TQ + 32 * x;
       f32x16 s, dp;
 #pragma unroll
       for (int r = 0; r < 16; ++r) { s[r] = 0.f; dp[r] = 0.f; }
@@ -812,28 +888,35 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(qs, lk, 16 * t + 8 * g), kf[t], s, 0, 0, 0);
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ds, lk, 16 * t + 8 * g), vf[t], dp, 0, 0, 0);
       }
-      const bool near = BIAS && kw + 31 - p0 > -a.maxd && kw - p0 - 31 < a.maxd;
-      const float* bn = bs + (p0 - kw - lk + a.maxd + kMargin) + 4 * g;   // reversed: by query minus key
-      const float far = BIAS ? (kw < p0 ? bs[bl - 1] : bs[0]) : 0.f;
-      const bool full = all_seen(a, sq.lk, kw, p0, p0 + 31);
+      if (BIAS) {
+        if (kw + 31 - p0 > -a.maxd && kw - p0 - 31 < a.maxd) {
+          const float* bn = bs + (p0 - kw - lk + a.maxd + kMargin) + 4 * g;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, bn[8 * (r >> 2) + (r & 3)]);
+        } else {
+          const float far = kw < p0 ? bs[bl - 1] : bs[0];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
+        }
+      }
+      if (!all_seen<32>(a, sq.lk, kw, p0, p0 + 31)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int pp = p0 + acc_row(r, g);
+          if (pp < plo || pp > phi) s[r] = -INFINITY;
+        }
+      }
       f32x16 p;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float4 lv = *reinterpret_cast<const float4*>(&Ls[buf][8 * i + 4 * g]);
-        const float4 dv4 = *reinterpret_cast<const float4*>(&Dd[buf][8 * i + 4 * g]);
+        const float4 lv = *reinterpret_cast<const float4*>(Ls + 8 * i + 4 * g);
+        const float4 dv4 = *reinterpret_cast<const float4*>(Ls + TQ + 8 * i + 4 * g);
         const float lsv[4] = {lv.x, lv.y, lv.z, lv.w}, ddv[4] = {dv4.x, dv4.y, dv4.z, dv4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * i + e;
-          float x = fmaf(s[r], a.c, -lsv[e]);
-          if (BIAS) x += near ? bn[8 * i + e] : far;
-          if (!full) {
-            const int pp = p0 + acc_row(r, g);
-            if (pp < plo || pp > phi) x = -INFINITY;
-          }
-          const float pr = exp2_(x);
-          p[r] = pr;
-          s[r] = pr * (dp[r] - ddv[e]);
+          p[r] = exp2_(BIAS ? s[r] - lsv[e] : fmaf(s[r], a.c, -lsv[e]));
+          s[r] = p[r] * (dp[r] - ddv[e]);
         }
       }
 #pragma unroll
@@ -846,9 +929,18 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
         }
       }
     }
-    if (more) store(buf ^ 1);
-    __syncthreads();
-    buf ^= 1;
+  }
+  if (nt * a.G > a.chunk) {   // one of several splits: partials, key rows of dk then of dv
+    float* row = a.part + ((it.slot * 128 + key - kblk) * 2) * DT;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x16 &x = adk[j], &y = adv[j];
+        *reinterpret_cast<float4*>(row + 32 * j + 8 * i + 4 * g) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        *reinterpret_cast<float4*>(row + DT + 32 * j + 8 * i + 4 * g) = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+      }
+    return;
   }
   if (key >= a.Sk) return;
   bf16_t* dkr = a.dk + b * a.ks[0] + key * a.ks[1] + hk * a.ks[2];
@@ -864,10 +956,52 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
     }
 }
 
+// Adds the partials of a split key block: a block per (16 keys, key block), a thread per 4 channels of dk or dv.
+template <int DT>
+__global__ __launch_bounds__(256) void k_mha_dkv_join(MhaArgs a) {
+  constexpr int PR = 2 * DT / 4;
+  // the key blocks of the classes that split, 8 parts of 16 keys in each
+  const int first = a.ns_sink > 1 ? 0 : a.nks, many = (a.ns_reg > 1 ? a.nblk : a.nks) - first;
+  const int part = blockIdx.x & 7, kb = first + (blockIdx.x >> 3) % many, bh = (blockIdx.x >> 3) / many;
+  const int hk = bh % a.Hk, b = bh / a.Hk;
+  const Seq sq = seq_of(a, b);
+  int i0, i1;
+  seen_by(a, sq, kb * 128, kb * 128 + 127, i0, i1);
+  const int steps = max((i1 + 63) / 64 - i0 / 64, 0) * a.G, ns = (steps + a.chunk - 1) / a.chunk;
+  if (ns <= 1) return;
+  const int sinks = a.nks * a.ns_sink, per = sinks + (a.nblk - a.nks) * a.ns_reg;
+  const KItem it = item_of(a, bh * per + (kb < a.nks ? kb * a.ns_sink : sinks + (kb - a.nks) * a.ns_reg));
+  for (int x = threadIdx.x; x < 16 * PR; x += 256) {
+    const int lr = part * 16 + x / PR, c = 4 * (x % PR), key = kb * 128 + lr;
+    if (key >= a.Sk) continue;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int z = 0; z < ns; ++z) {
+      const float4 v = *reinterpret_cast<const float4*>(a.part + (((it.slot + z) * 128 + lr) * 2) * DT + c);
+      t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    }
+    if (c < DT) {
+      const float f = a.scale;
+      st4(a.dk + b * a.ks[0] + key * a.ks[1] + hk * a.ks[2], c, a.d, t.x * f, t.y * f, t.z * f, t.w * f);
+    } else {
+      st4(a.dv + b * a.vs[0] + key * a.vs[1] + hk * a.vs[2], c - DT, a.d, t.x, t.y, t.z, t.w);
+    }
+  }
+}
+
 // ------------------------------------------------------------- launchers
+// Heads to keep together on an XCD: those of one key head where that deals
+// evenly, else an eighth of all.  Sequences of different lengths need several
+// sets on each XCD to even out (train 2 x 4096 x 16 / 4 heads x 128 through a
+// window, full and three quarters long: 783 us in plain order, 835 so).
+int head_set(int64_t heads, int group, bool ragged) {
+  if (heads % 8) return 0;
+  const int64_t m = heads / group % 8 == 0 ? group : heads / 8;
+  return ragged && heads / m < 32 ? 0 : (int)m;
+}
+
 int pad_d(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
-constexpr int fwd_qt(int dt) { return dt <= 64 ? 2 : 1; }   // query tiles of a wave
-constexpr int dq_qt(int dt) { return dt <= 32 ? 2 : 1; }
+constexpr int fwd_qt(int dt) { return dt <= 64 ? FWD64 : FWD_QT; }   // query tiles of a wave
+constexpr int dq_qt(int dt) { return dt == 64 ? DQ64 : 1; }
 
 // bucket of distance n among the `half` buckets of a side: exact below half / 2, then
 // logarithmic up to maxd, evaluated exactly: the largest e with (n / first)^m >= (maxd / first)^e.
@@ -884,7 +1018,7 @@ int bucket_of(int n, int half, int maxd) {
 MhaArgs make_args(const Mha& m) {
   MhaArgs a{};
   a.B = m.B; a.Sq = m.Sq; a.Sk = m.Sk; a.Hq = m.Hq; a.Hk = m.Hk; a.G = m.Hq / m.Hk; a.d = m.d;
-  a.Sqp = (int)cdiv(m.Sq, 32) * 32;
+  a.Sqp = (int)cdiv(m.Sq, 64) * 64;
   a.causal = m.causal; a.window = m.window; a.n_sink = m.n_sink;
   a.nb = m.n_buckets; a.maxd = m.n_buckets ? m.max_distance : 0;
   a.half = m.causal ? m.n_buckets : m.n_buckets / 2;
@@ -911,6 +1045,28 @@ int step_splits(const Mha& m) {
   return (int)std::max<int64_t>(1, std::min(cdiv(768, blocks), cdiv(tiles, 8)));
 }
 
+// How the key-owned pass is cut: blocks of 128 keys; a block's steps are
+// G x (64-query tiles that see it).  Few blocks are split until there are four
+// for each place on the card (two a CU), into 8 steps at least; blocks with
+// first tokens, which every query sees, into what the others have.
+struct KPlan { int nkb, nks, ns_sink, ns_reg, chunk; int64_t items, slots; };
+KPlan plan_keys(const Mha& m) {
+  KPlan p{};
+  const int64_t G = m.Hq / m.Hk, all = G * cdiv(m.Sq, 64);
+  p.nkb = (int)cdiv(m.Sk, 128);
+  const int64_t reg = m.window ? std::min(all, G * (cdiv((m.causal ? 1 : 2) * (int64_t)m.window + 128, 64) + 1)) : all;
+  p.nks = m.window && reg < all ? (int)std::min<int64_t>(p.nkb, cdiv(m.n_sink, 128)) : 0;
+  const int64_t bh = (int64_t)m.B * m.Hk, total = bh * (p.nks * all + (p.nkb - p.nks) * reg) / (m.causal && !m.window ? 2 : 1);
+  int64_t chunk = std::max<int64_t>(8, cdiv(total, 2048));
+  if (bh * p.nkb >= 1024) chunk = std::max(chunk, reg);   // enough blocks as they are
+  p.chunk = (int)std::min<int64_t>(chunk, 1 << 30);
+  p.ns_sink = (int)cdiv(all, chunk);
+  p.ns_reg = (int)cdiv(reg, chunk);
+  p.items = bh * ((int64_t)p.nks * p.ns_sink + (int64_t)(p.nkb - p.nks) * p.ns_reg);
+  p.slots = bh * ((p.ns_sink > 1 ? (int64_t)p.nks * p.ns_sink : 0) + (p.ns_reg > 1 ? (int64_t)(p.nkb - p.nks) * p.ns_reg : 0));
+  return p;
+}
+
 size_t bias_bytes(const Mha& m, int arrays) {
   return m.n_buckets ? (size_t)arrays * (2 * (m.max_distance + kMargin) + 1) * 4 : 0;
 }
@@ -926,13 +1082,16 @@ size_t bias_bytes(const Mha& m, int arrays) {
 }  // namespace
 
 size_t mha_saved_bytes(const Mha& m) {
-  const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 32) * 32;
+  const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 64) * 64;
   return align256(rows * 4);   // the rows' log2 sums
 }
 
 size_t mha_ws_bytes(const Mha& m) {
-  const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 32) * 32;
-  size_t bwd = align256(rows * 4) + align256((size_t)m.B * m.Hq * cdiv(m.Sq, 128 * dq_qt(pad_d(m.d))) * m.n_buckets * 4);
+  const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 64) * 64;
+  // the rows' D, then the bias partials or (after these are joined) those of dk and dv
+  const size_t bias = (size_t)m.B * m.Hq * cdiv(m.Sq, 128 * dq_qt(pad_d(m.d))) * m.n_buckets * 4;
+  const size_t keys = (size_t)plan_keys(m).slots * 128 * 2 * pad_d(m.d) * 4;
+  const size_t bwd = align256(rows * 4) + align256(std::max(bias, keys));
   size_t step = 0;
   if (few_rows(m)) step = (size_t)m.B * m.Hk * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
   return std::max<size_t>(std::max(bwd, align256(step)), 256);
@@ -963,6 +1122,7 @@ void mha_fwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   }
   a.lse = (float*)saved;
   a.nblk = (int)cdiv(m.Sq, 128 * fwd_qt(pad_d(m.d)));
+  a.hset = head_set((int64_t)m.B * m.Hq, a.G, len_k || len_q);
   const dim3 grid((unsigned)((int64_t)m.B * m.Hq * a.nblk));
   ProfScope prof(st);
   PG_DT(m.d, {
@@ -989,6 +1149,7 @@ void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   PG_DT(m.d, {
     constexpr int QT = dq_qt(DT);
     a.nblk = (int)cdiv(m.Sq, 128 * QT);
+    a.hset = head_set((int64_t)m.B * m.Hq, a.G, len_k || len_q);
     const dim3 gq((unsigned)((int64_t)m.B * m.Hq * a.nblk));
     if (m.n_buckets) {
       hipLaunchKernelGGL((k_mha_dq<DT, QT, true>), gq, dim3(256), bias_bytes(m, 9), st, a);
@@ -997,10 +1158,16 @@ void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
     } else {
       hipLaunchKernelGGL((k_mha_dq<DT, QT, false>), gq, dim3(256), 0, st, a);
     }
-    a.nblk = (int)cdiv(m.Sk, 128);
-    const dim3 gk((unsigned)((int64_t)m.B * m.Hk * a.nblk));
-    if (m.n_buckets) hipLaunchKernelGGL((k_mha_dkv<DT, true>), gk, dim3(256), bias_bytes(m, 1), st, a);
-    else hipLaunchKernelGGL((k_mha_dkv<DT, false>), gk, dim3(256), 0, st, a);
+    const KPlan p = plan_keys(m);
+    a.nblk = p.nkb; a.nks = p.nks; a.ns_sink = p.ns_sink; a.ns_reg = p.ns_reg; a.chunk = p.chunk;
+    a.hset = head_set((int64_t)m.B * m.Hk, 1, len_k || len_q);
+    const dim3 gk((unsigned)p.items);
+    if (m.n_buckets) hipLaunchKernelGGL((k_mha_dkv<DT, true>), gk, dim3(256), bias_bytes(m, 1) + 1024, st, a);
+    else hipLaunchKernelGGL((k_mha_dkv<DT, false>), gk, dim3(256), 1024, st, a);
+    if (p.slots) {
+      const int many = (p.ns_reg > 1 ? p.nkb : p.nks) - (p.ns_sink > 1 ? 0 : p.nks);
+      hipLaunchKernelGGL(k_mha_dkv_join<DT>, dim3((unsigned)((int64_t)m.B * m.Hk * many * 8)), dim3(256), 0, st, a);
+    }
   });
   PG_LAUNCH_CHECK();
   prof.done("k_mha_bwd<" + std::to_string(pad_d(m.d)) + ">", 14.0 * m.B * m.Hq * (double)m.Sq * m.Sk * m.d);

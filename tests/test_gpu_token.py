@@ -195,7 +195,8 @@ TRAIN = [
     (1, 260, 260, 2, 1, 40, 0, 20, 70), (1, 300, 300, 2, 2, 64, 0, 100, 0, 8, 20), (1, 400, 400, 1, 1, 32, 1, 64, 4, 32, 512),
     (1, 1100, 1100, 1, 1, 24, 0, 0, 0, 64, 512), (1, 70, 200, 2, 2, 64, 1), (1, 200, 70, 2, 1, 64, 1),
     (1, 65, 130, 2, 1, 32, 0, 30, 3, 12, 40), (3, 96, 96, 8, 1, 64, 1, 1, 0), (1, 96, 96, 2, 2, 16, 1, 1, 1, 2, 2),
-    (1, 513, 513, 2, 2, 128, 0, 0, 0, 32, 128), (1, 600, 600, 1, 1, 128, 1, 100, 200, 16, 50)]
+    (1, 513, 513, 2, 2, 128, 0, 0, 0, 32, 128), (1, 600, 600, 1, 1, 128, 1, 100, 200, 16, 50),
+    (1, 2100, 2100, 4, 1, 64, 1, 64, 5), (1, 1500, 1500, 2, 2, 32, 0, 90, 130)]
 
 
 @pytest.mark.parametrize("case", TRAIN, ids=[("-".join(map(str, c))) for c in TRAIN])
