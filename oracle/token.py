@@ -131,12 +131,15 @@ def mha(q, k, v, scale, causal=False, window=0, n_sink=0, table=None, max_distan
             dP = DO @ V.T
             D = (P * dP).sum(-1, keepdims=True)
             dS = P * (dP - D)
-            # dP's own rounding, and D's: from the rounded output, or (with a bias) from P and dP in fp32
+            # dP's own rounding, and D's: for dq and dk that of do . o with the rounded output; the bias gradient
+            # has its rows' dS sum to zero again, up to the rounding of the row's fp32 sum
             tp = U32 * (d + 4) * (ad @ av.T)
-            td = (P * (tp + (2 * eta + U32 * (lk + 8)) * np.abs(dP))).sum(-1, keepdims=True) if table is not None \
-                else (ad * to).sum(-1, keepdims=True)
-            ts = P * (tp + td + 4 * eta * (np.abs(dP) + np.abs(D)))
+            to_row = (ad * to).sum(-1, keepdims=True)
+            ts = P * (tp + to_row + 4 * eta * (np.abs(dP) + np.abs(D)))
             ta = ts + U16 * np.abs(dS)
+            mass = (P * (np.abs(dP) + np.abs(D) + to_row)).sum(-1, keepdims=True)
+            tr = (P * tp).sum(-1, keepdims=True) + (4 * eta + 2 * U32 * (lk + 8)) * mass
+            tt = P * (tp + tr + 4 * eta * (np.abs(dP) + np.abs(D) + to_row))
             aq, ak = np.abs(Q), np.abs(K)
             r["dq"][b, :lq, h] = scale * dS @ K
             r["tol.dq"][b, :lq, h] = scale * (ta + U32 * lk * np.abs(dS)) @ ak
@@ -146,7 +149,7 @@ def mha(q, k, v, scale, causal=False, window=0, n_sink=0, table=None, max_distan
             r["tol.dv"][b, :lk, h // G] += ((U16 + 2 * eta + U32 * lq * G) * P).T @ ad
             if at is not None:
                 np.add.at(r["dtable"][h], at, dS)
-                np.add.at(r["tol.dtable"][h], at, ts + U32 * (lq * B + 64) * np.abs(dS))
+                np.add.at(r["tol.dtable"][h], at, tt + U32 * (lq * B + 64) * (np.abs(dS) + ts))
     if dout is not None:
         for n in ("dq", "dk", "dv"):
             r["tol." + n] += U16 * (np.abs(r[n]) + r["tol." + n])

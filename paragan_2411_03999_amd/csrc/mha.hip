@@ -25,33 +25,6 @@
 #include "attn_tiles.hpp"
 #include "lds_dma.hpp"
 #include "token.hpp"
-#ifndef DKV_OCC
-#define DKV_OCC 1
-#endif
-#ifndef FWD_QT
-#define FWD_QT 1
-#endif
-#ifndef FWD64
-#define FWD64 1
-#endif
-#ifndef FO64
-#define FO64 3
-#endif
-#ifndef FWD_OCC
-#define FWD_OCC 2
-#endif
-#ifndef DQ_QT
-#define DQ_QT 1
-#endif
-#ifndef DO64
-#define DO64 2
-#endif
-#ifndef DQ64
-#define DQ64 2
-#endif
-#ifndef DQ_OCC
-#define DQ_OCC 2
-#endif
 
 namespace pg {
 
@@ -162,19 +135,19 @@ PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
 }
 PG_DEV int bias_len(const MhaArgs& a) { return 2 * (a.maxd + kMargin) + 1; }
 
-// 64 rows x NC chunks from memory straight into a swizzled LDS tile by 4
+// ROWS rows x NC chunks from memory straight into a swizzled LDS tile by 4
 // waves: 16-byte slot i of the tile (lane order) holds chunk (i % NC) ^ swizzle
 // of row i / NC.  Chunks at or past d and rows that `ok` refuses read as zeros
 // without touching memory.
-template <int NC>
+template <int NC, int ROWS>
 struct Ring {
-  static constexpr int N = NC / 4;   // loads of a wave
+  static constexpr int L = NC * ROWS / 64, N = (L + 3) / 4;   // loads of 64 lanes, of a wave at most
   uint32_t off[N];
   int row[N];
   PG_DEV void init(int64_t ld, int d, int tid) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int i = ((tid >> 6) * N + j) * 64 + (tid & 63);
+      const int i = (4 * j + (tid >> 6)) * 64 + (tid & 63);
       const int r = i / NC, c = (i - r * NC) ^ swz16<NC>(r);
       row[j] = r;
       off[j] = c * 8 < d ? (uint32_t)(r * (int)ld * 2 + c * 16) : kOOB;
@@ -183,10 +156,11 @@ struct Ring {
   // base: row 0 of the tile (uniform); rows r0 + r
   template <class F>
   PG_DEV void issue(bf16_t* tile, const bf16_t* base, int64_t ld, int r0, int wave, F ok) const {
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, (63 * ld + NC * 8) * 2);
-    const uint32_t dst = lds_addr(tile) + wave * N * 1024;
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, ((ROWS - 1) * ld + NC * 8) * 2);
+    const uint32_t dst = lds_addr(tile) + wave * 1024;
 #pragma unroll
-    for (int j = 0; j < N; ++j) lds_load16(dst + j * 1024, ok(r0 + row[j]) ? off[j] : kOOB, 0, rs);
+    for (int j = 0; j < N; ++j)
+      if (4 * j + 3 < L || 4 * j + wave < L) lds_load16(dst + j * 4096, ok(r0 + row[j]) ? off[j] : kOOB, 0, rs);
   }
 };
 
@@ -198,10 +172,10 @@ PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
 }
 
 // ------------------------------------------------------------- forward
-// A wave owns 32 QT queries of one head; a block of 4 waves 128 QT.  Keys and
+// A wave owns 32 queries of one head, a block of 4 waves 128.  Keys and
 // values come in tiles of 64, the next one loading while this one is used.
-template <int DT, int QT, bool BIAS>
-__global__ __launch_bounds__(256, DT >= 96 ? FWD_OCC : FO64) void k_mha_fwd(MhaArgs a) {
+template <int DT, bool BIAS>
+__global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][TK * DT];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][TK * DT];
@@ -211,38 +185,28 @@ __global__ __launch_bounds__(256, DT >= 96 ? FWD_OCC : FO64) void k_mha_fwd(MhaA
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
-  const int qblk = qb * 128 * QT, qw = qblk + wv * 32 * QT;
+  const int qblk = qb * 128, qw = qblk + wv * 32, q = qw + lq, p0 = qw + sq.off;
   const bf16_t* K = a.k + b * a.ks[0] + (h / a.G) * a.ks[2];
   const bf16_t* V = a.v + b * a.vs[0] + (h / a.G) * a.vs[2];
   if (BIAS)
     for (int e = tid; e < bias_len(a); e += 256) bs[e] = bias2_at(a, h, e);
-  bf16x8 qf[QT][KF];
-  Row rw[QT];
+  const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
+  bf16x8 qf[KF];
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    const int q = qw + 32 * u + lq;
-    const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
+  for (int t = 0; t < KF; ++t) qf[t] = ld_frag(Q, 16 * t + 8 * g, a.d, q < sq.lq);
+  const Row rw = row_of(a, sq.lk, q + sq.off);
+  f32x16 acc[NT];
 #pragma unroll
-    for (int t = 0; t < KF; ++t) qf[u][t] = ld_frag(Q, 16 * t + 8 * g, a.d, q < sq.lq);
-    rw[u] = row_of(a, sq.lk, q + sq.off);
-  }
-  f32x16 acc[QT][NT];
-  float m2[QT], l[QT];
+  for (int j = 0; j < NT; ++j)
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    m2[u] = -INFINITY;
-    l[u] = 0.f;
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[u][j][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+  float m2 = -INFINITY, l = 0.f;
   // a block behind the last query visits nothing and writes zeros
-  Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
+  Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128, sq.lq) - 1 + sq.off);
   if (qblk >= sq.lq) sp.nt = 0;
-  const Span<TK> sw = span_of<TK>(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
+  const Span<TK> sw = span_of<TK>(a, sq.lk, p0, min(qw + 32, sq.lq) - 1 + sq.off);
   const bool mine = qw < sq.lq;
-  Ring<NC> rk, rv;
+  Ring<NC, TK> rk, rv;
   rk.init(a.ks[1], a.d, tid);
   rv.init(a.vs[1], a.d, tid);
   auto load = [&](int n, int bf) {
@@ -259,106 +223,85 @@ __global__ __launch_bounds__(256, DT >= 96 ? FWD_OCC : FO64) void k_mha_fwd(MhaA
     if (!mine || !sw.tile(k0)) continue;
     const bf16_t* ks = Ks[buf];
     const bf16_t* vs = Vs[buf];
-    f32x16 s[QT][2];
+    f32x16 s[2];
 #pragma unroll
-    for (int u = 0; u < QT; ++u)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[u][0][r] = s[u][1][r] = 0.f;
+    for (int r = 0; r < 16; ++r) s[0][r] = s[1][r] = 0.f;
 #pragma unroll
     for (int t = 0; t < KF; ++t)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const bf16x8 ka = ld_row<NC>(ks + 32 * DT * x, lq, 16 * t + 8 * g);
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-          s[u][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[u][t], s[u][x], 0, 0, 0);
-      }
-#pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      const int p0 = qw + 32 * u + sq.off;
-      if (BIAS) {
-        if (k0 + TK - 1 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd) {
-          const float* bl = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][x][r] = fmaf(s[u][x][r], a.c, bl[32 * x + 8 * (r >> 2) + (r & 3)]);
-        } else {
-          const float far = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
-#pragma unroll
-          for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][x][r] = fmaf(s[u][x][r], a.c, far);
-        }
-      }
-      if (!all_seen<TK>(a, sq.lk, k0, p0, p0 + 31)) {
+      for (int x = 0; x < 2; ++x)
+        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ks + 32 * DT * x, lq, 16 * t + 8 * g), qf[t], s[x], 0, 0, 0);
+    // a score in log2 units is s cm + off: near the diagonal the bias is added to each, elsewhere it is one number
+    float cm = a.c, off = 0.f;
+    if (BIAS) {
+      if (k0 + TK - 1 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd) {
+        const float* bl = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!sees(rw[u], k0 + 32 * x + acc_row(r, g))) s[u][x][r] = -INFINITY;
+          for (int r = 0; r < 16; ++r) s[x][r] = fmaf(s[x][r], a.c, bl[32 * x + 8 * (r >> 2) + (r & 3)]);
+        cm = 1.f;
+      } else {
+        off = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
       }
-      float mb = s[u][0][0], mc = s[u][1][0];   // two chains
-#pragma unroll
-      for (int r = 1; r < 15; r += 2) {
-        mb = max3(mb, s[u][0][r], s[u][0][r + 1]);
-        mc = max3(mc, s[u][1][r], s[u][1][r + 1]);
-      }
-      mb = max3(max3(mb, s[u][0][15], s[u][1][15]), mc, mc);
-      mb = max3(mb, mb, __shfl_xor(mb, 32, 64));
-      if (!BIAS) mb *= a.c;
-      if (mb > m2[u] + kTau) {
-        const float alpha = exp2_(m2[u] - mb);
-        l[u] *= alpha;
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[u][j][r] *= alpha;
-        m2[u] = mb;
-      }
-      const float ms = m2[u] == -INFINITY ? 0.f : m2[u];   // nothing seen yet: every term is 2^-inf
-      float ls[2] = {0.f, 0.f};
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          s[u][x][r] = exp2_(BIAS ? s[u][x][r] - ms : fmaf(s[u][x][r], a.c, -ms));
-          ls[x] += s[u][x][r];
-        }
-      l[u] += ls[0] + ls[1];
     }
+    if (!all_seen<TK>(a, sq.lk, k0, p0, p0 + 31)) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!sees(rw, k0 + 32 * x + acc_row(r, g))) s[x][r] = -INFINITY;
+    }
+    float mb = s[0][0], mc = s[1][0];   // two chains
+#pragma unroll
+    for (int r = 1; r < 15; r += 2) {
+      mb = max3(mb, s[0][r], s[0][r + 1]);
+      mc = max3(mc, s[1][r], s[1][r + 1]);
+    }
+    mb = max3(max3(mb, s[0][15], s[1][15]), mc, mc);
+    mb = max3(mb, mb, __shfl_xor(mb, 32, 64));
+    mb = BIAS ? fmaf(mb, cm, off) : mb * a.c;
+    if (mb > m2 + kTau) {
+      const float alpha = exp2_(m2 - mb);
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[j][r] *= alpha;
+      m2 = mb;
+    }
+    const float ms = off - (m2 == -INFINITY ? 0.f : m2);   // nothing seen yet: every term is 2^-inf
+    float ls[2] = {0.f, 0.f};
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        s[x][r] = exp2_(fmaf(s[x][r], BIAS ? cm : a.c, ms));
+        ls[x] += s[x][r];
+      }
+    l += ls[0] + ls[1];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      bf16x8 pb[QT];
+      const bf16x8 pb = pack_regs(s[t >> 1], t & 1);
 #pragma unroll
-      for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u][t >> 1], t & 1);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        const bf16x8 va = ld_tr<NC>(vs + 32 * DT * (t >> 1), t & 1, 32 * j, lane);
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
-          acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pb[u], acc[u][j], 0, 0, 0);
-      }
+      for (int j = 0; j < NT; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(vs + 32 * DT * (t >> 1), t & 1, 32 * j, lane), pb, acc[j], 0, 0, 0);
     }
   }
+  const float lt = l + __shfl_xor(l, 32, 64);
+  const bool any = q < sq.lq && lt > 0.f;
+  const float inv = any ? 1.f / lt : 0.f;
+  bf16_t* orow = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    const int q = qw + 32 * u + lq;
-    const float lt = l[u] + __shfl_xor(l[u], 32, 64);
-    const bool any = q < sq.lq && lt > 0.f;
-    const float inv = any ? 1.f / lt : 0.f;
-    bf16_t* orow = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
+  for (int j = 0; j < NT; ++j)
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x16& x = acc[u][j];
-        float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (any) f = make_float4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
-        if (q < a.Sq) st4(orow, 32 * j + 8 * i + 4 * g, a.d, f.x, f.y, f.z, f.w);
-      }
-    if (a.lse && g == 0 && q < a.Sqp) a.lse[(int64_t)bh * a.Sqp + q] = any ? m2[u] + __log2f(lt) : INFINITY;
-  }
+    for (int i = 0; i < 4; ++i) {
+      const f32x16& x = acc[j];
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (any) f = make_float4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
+      if (q < a.Sq) st4(orow, 32 * j + 8 * i + 4 * g, a.d, f.x, f.y, f.z, f.w);
+    }
+  if (a.lse && g == 0 && q < a.Sqp) a.lse[(int64_t)bh * a.Sqp + q] = any ? m2 + __log2f(lt) : INFINITY;
 }
 
 // ------------------------------------------------------------- a few new tokens
@@ -554,80 +497,87 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 }
 
 // ------------------------------------------------------------- dq (query-owned)
-// Also D, kept for the key-owned pass (with a bias as sum P dP in a pass of its
-// own, else as do . o), and the bias gradient:
-// dS of the tiles near the diagonal is added per distance into LDS, by each
-// wave into two arrays of its own (one per lane half), so that no two lanes of
-// one instruction meet and the order of the sums is fixed; tiles past
-// max_distance add into one register per side.
-template <int DT, int QT, bool BIAS>
-__global__ __launch_bounds__(256, DT >= 96 ? DQ_OCC : DO64) void k_mha_dq(MhaArgs a) {
+// Also D = do . o, kept for the key-owned pass, and the bias gradient: dS of
+// the tiles near the diagonal, in a second visit, is summed per distance into
+// an array of each wave (an order that is fixed; fp32 atomics in LDS took
+// 134 cycles a wave instruction here), tiles past max_distance add into one
+// register per side.
+
+// Adds a tile of the accumulator layout (rows: keys, lanes: queries) along its
+// diagonals, row - query = -31 .. 31, to arr: lane m of a half collects the
+// wrapped diagonal row - query = m (mod 32) of its 16 rows, split where it
+// wraps; the halves are joined, one stores each part.
+PG_DEV void diag_add(float* arr, const f32x16& v, int lane) {
+  const int g = lane >> 5, m = lane & 31;
+  float up = 0.f, down = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int row = acc_row(r, g);
+    const float x = __int_as_float(__builtin_amdgcn_ds_bpermute((((row - m) & 31) + 32 * g) * 4, __float_as_int(v[r])));
+    up += m <= row ? x : 0.f;
+    down += m <= row ? 0.f : x;
+  }
+  up += __shfl_xor(up, 32, 64);
+  down += __shfl_xor(down, 32, 64);
+  // another lane of this wave may have written the element last: no reordering
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  arr[g ? m - 32 : m] += g ? down : up;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+template <int DT, bool BIAS>
+__global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][TK * DT];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][TK * DT];
-  extern __shared__ float bs[];   // bias by distance, then 8 arrays of dS sums by distance
+  extern __shared__ float bs[];   // bias by distance, then each wave's sums of dS by distance
   const int id = block_no(a, a.nblk), qb = a.nblk - 1 - id % a.nblk, bh = id / a.nblk, h = bh % a.Hq, b = bh / a.Hq;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
-  const int qblk = qb * 128 * QT, qw = qblk + wv * 32 * QT;
+  const int qblk = qb * 128, qw = qblk + wv * 32, q = qw + lq, p0 = qw + sq.off;
   const bf16_t* K = a.k + b * a.ks[0] + (h / a.G) * a.ks[2];
   const bf16_t* V = a.v + b * a.vs[0] + (h / a.G) * a.vs[2];
   const int bl = BIAS ? bias_len(a) : 0;
-  float* const gs = bs + bl + (2 * wv + g) * bl;
+  float* const gs = bs + bl + wv * bl;
   if (BIAS) {
     for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, h, e);
-    for (int e = tid; e < 8 * bl; e += 256) bs[bl + e] = 0.f;
+    for (int e = tid; e < 4 * bl; e += 256) bs[bl + e] = 0.f;
   }
-  bf16x8 qf[QT][KF], df[QT][KF];
-  float ls2[QT], dd[QT];
-  Row rw[QT];
+  const bool valid = q < sq.lq;
+  const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
+  const bf16_t* DO = a.dO + b * a.os[0] + q * a.os[1] + h * a.os[2];
+  const bf16_t* O = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
+  bf16x8 qf[KF], df[KF];
+  float dd = 0.f;
 #pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    const int q = qw + 32 * u + lq;
-    const bool ok = q < sq.lq;
-    const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
-    const bf16_t* DO = a.dO + b * a.os[0] + q * a.os[1] + h * a.os[2];
-    const bf16_t* O = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
-    dd[u] = 0.f;
+  for (int t = 0; t < KF; ++t) {
+    qf[t] = ld_frag(Q, 16 * t + 8 * g, a.d, valid);
+    df[t] = ld_frag(DO, 16 * t + 8 * g, a.d, valid);
+    // from the bf16 output: off by at most 2^-8 of sum |do||o|, as much as dS loses when it becomes an operand
+    float x[8], o[8];
+    unpack8(__builtin_bit_cast(uint4, df[t]), x);
+    unpack8(__builtin_bit_cast(uint4, ld_frag(O, 16 * t + 8 * g, a.d, valid)), o);
 #pragma unroll
-    for (int t = 0; t < KF; ++t) {
-      qf[u][t] = ld_frag(Q, 16 * t + 8 * g, a.d, ok);
-      df[u][t] = ld_frag(DO, 16 * t + 8 * g, a.d, ok);
-      if (!BIAS) {
-        // from the bf16 output: off by at most 2^-8 of sum |do||o|, as much as dS loses when it becomes an operand
-        float x[8], o[8];
-        unpack8(__builtin_bit_cast(uint4, df[u][t]), x);
-        unpack8(__builtin_bit_cast(uint4, ld_frag(O, 16 * t + 8 * g, a.d, ok)), o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dd[u] = fmaf(x[e], o[e], dd[u]);
-      }
-    }
-    ls2[u] = ok ? a.lse[(int64_t)bh * a.Sqp + q] : INFINITY;
-    rw[u] = row_of(a, sq.lk, q + sq.off);
+    for (int e = 0; e < 8; ++e) dd = fmaf(x[e], o[e], dd);
   }
-  // the rows' D, once known, to every lane and for the key-owned pass
-  auto row_terms = [&]() {
+  dd += __shfl_xor(dd, 32, 64);
+  if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = valid ? dd : 0.f;
+  const float ls2 = valid ? a.lse[(int64_t)bh * a.Sqp + q] : INFINITY;
+  const Row rw = row_of(a, sq.lk, q + sq.off);
+  f32x16 acc[NT];
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-      const int q = qw + 32 * u + lq;
-      dd[u] += __shfl_xor(dd[u], 32, 64);
-      if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = q < sq.lq ? dd[u] : 0.f;
-    }
-  };
-  f32x16 acc[QT][NT];
+  for (int j = 0; j < NT; ++j)
 #pragma unroll
-  for (int u = 0; u < QT; ++u)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[u][j][r] = 0.f;
-  float flo = 0.f, fhi = 0.f;
-  Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128 * QT, sq.lq) - 1 + sq.off);
+    for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
+  // BIAS, per row: dS of the far tiles on either side, sum of dS, P of the far tiles of earlier keys, P of the near tiles
+  float flo = 0.f, fhi = 0.f, rho = 0.f, wlo = 0.f, wn = 0.f;
+  bool lo_far = false, hi_far = false;
+  Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128, sq.lq) - 1 + sq.off);
   if (qblk >= sq.lq) sp.nt = 0;
-  const Span<32> sw = span_of<32>(a, sq.lk, qw + sq.off, min(qw + 32 * QT, sq.lq) - 1 + sq.off);
+  const Span<32> sw = span_of<32>(a, sq.lk, p0, min(qw + 32, sq.lq) - 1 + sq.off);
   const bool mine = qw < sq.lq;
-  Ring<NC> rk, rv;
+  Ring<NC, TK> rk, rv;
   rk.init(a.ks[1], a.d, tid);
   rv.init(a.vs[1], a.d, tid);
   auto load = [&](int n, int bf) {
@@ -636,107 +586,117 @@ __global__ __launch_bounds__(256, DT >= 96 ? DQ_OCC : DO64) void k_mha_dq(MhaArg
     rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, ok);
     rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, ok);
   };
-  // One pass over the keys.  FIRST (with a bias only): dd = sum P dP in fp32.
-  // The bias gradient sums dS over many pairs with little left over; a row
-  // term from a rounded output, or from rounded P, would dominate it.
-  auto pass = [&](auto first_c) {
-    constexpr bool FIRST = decltype(first_c)::value;
-    if (sp.nt > 0) load(0, 0);
-    for (int n = 0; n < sp.nt; ++n) {
-      wait_barrier<0>();   // tile n is in LDS, and every wave has left tile n - 1
-      const int buf = n & 1;
-      if (n + 1 < sp.nt) load(n + 1, buf ^ 1);
+  // One pass over the keys.  NEAR (after the other, with a bias): see below.
+  auto pass = [&](auto near_c) {
+    constexpr bool NEAR = decltype(near_c)::value;
+    const int pb0 = qblk + sq.off, pb1 = pb0 + 127;
+    auto next = [&](int n) {   // the next tile to visit
+      if (NEAR)
+        while (n < sp.nt && !(sp.key0(n) + TK - 1 - pb0 > -a.maxd && sp.key0(n) - pb1 < a.maxd)) ++n;
+      return n;
+    };
+    int n = next(0), buf = 0;
+    if (n < sp.nt) load(n, 0);
+    while (n < sp.nt) {
+      wait_barrier<0>();   // tile n is in LDS, and every wave has left the tile before
+      const int n1 = next(n + 1);
+      if (n1 < sp.nt) load(n1, buf ^ 1);
 #pragma unroll 1
       for (int x = 0; x < 2; ++x) {
         const int k0 = sp.key0(n) + 32 * x;
-        if (!mine || !sw.tile(k0)) continue;
+        const bool near = BIAS && k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd;
+        if (!mine || !sw.tile(k0) || (NEAR && !near)) continue;
         const bf16_t* ks = Ks[buf] + 32 * DT * x;
         const bf16_t* vs = Vs[buf] + 32 * DT * x;
-        f32x16 s[QT], dp[QT];
+        f32x16 s, dp;
 #pragma unroll
-        for (int u = 0; u < QT; ++u)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) { s[u][r] = 0.f; dp[u][r] = 0.f; }
+        for (int r = 0; r < 16; ++r) { s[r] = 0.f; dp[r] = 0.f; }
 #pragma unroll
         for (int t = 0; t < KF; ++t) {
-          const bf16x8 ka = ld_row<NC>(ks, lq, 16 * t + 8 * g), va = ld_row<NC>(vs, lq, 16 * t + 8 * g);
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ks, lq, 16 * t + 8 * g), qf[t], s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(vs, lq, 16 * t + 8 * g), df[t], dp, 0, 0, 0);
+        }
+        if (BIAS && near) {
+          const float* bl4 = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
 #pragma unroll
-          for (int u = 0; u < QT; ++u) {
-            s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qf[u][t], s[u], 0, 0, 0);
-            dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, df[u][t], dp[u], 0, 0, 0);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, bl4[8 * (r >> 2) + (r & 3)] - ls2);
+        } else {
+          const float far = (BIAS ? (k0 < p0 ? bs[0] : bs[bl - 1]) : 0.f) - ls2;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
+        }
+        if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!sees(rw, k0 + acc_row(r, g))) s[r] = -INFINITY;
+        }
+        if constexpr (NEAR) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float p = exp2_(s[r]);
+            wn += p;
+            s[r] = p * (dp[r] - (dd + rho));
+          }
+          diag_add(gs + k0 - p0 + a.maxd + kMargin, s, lane);
+          continue;
+        }
+        if (BIAS && !near && !a.causal && k0 < p0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) wlo += s[r] = exp2_(s[r]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]);
+        }
+        float t = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] *= dp[r] - dd;
+          if (BIAS) t += s[r];
+        }
+        if (BIAS) {
+          rho += t;
+          if (!near && k0 < p0) {
+            flo += t;
+            lo_far = bs[0] != -INFINITY;   // a hidden bucket holds nothing, and gets nothing
+          } else if (!near) {
+            fhi += t;
+            hi_far = bs[bl - 1] != -INFINITY;
           }
         }
 #pragma unroll
-        for (int u = 0; u < QT; ++u) {
-          const int p0 = qw + 32 * u + sq.off;
-          const bool near = BIAS && k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd;
-          const int at = k0 - p0 - lq + a.maxd + kMargin + 4 * g;
-          if (BIAS && near) {
+        for (int t2 = 0; t2 < 2; ++t2) {
+          const bf16x8 sb = pack_regs(s, t2);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, bs[at + 8 * (r >> 2) + (r & 3)] - ls2[u]);
-          } else {
-            const float far = (BIAS ? (k0 < p0 ? bs[0] : bs[bl - 1]) : 0.f) - ls2[u];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[u][r] = fmaf(s[u][r], a.c, far);
-          }
-          if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (!sees(rw[u], k0 + acc_row(r, g))) s[u][r] = -INFINITY;
-          }
-          if (FIRST) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dd[u] = fmaf(exp2_(s[u][r]), dp[u][r], dd[u]);
-            continue;
-          }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][r] = exp2_(s[u][r]) * (dp[u][r] - dd[u]);
-          if (BIAS) {
-            if (near) {
-#pragma unroll
-              for (int r = 0; r < 16; ++r)
-                __hip_atomic_fetch_add(gs + at + 8 * (r >> 2) + (r & 3), s[u][r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-            } else {
-              float t = 0.f;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) t += s[u][r];
-              if (k0 < p0) flo += t; else fhi += t;
-            }
-          }
-        }
-        if constexpr (!FIRST) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            bf16x8 pb[QT];
-#pragma unroll
-            for (int u = 0; u < QT; ++u) pb[u] = pack_regs(s[u], t);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-              const bf16x8 ka = ld_tr<NC>(ks, t, 32 * j, lane);
-#pragma unroll
-              for (int u = 0; u < QT; ++u)
-                acc[u][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, pb[u], acc[u][j], 0, 0, 0);
-            }
-          }
+          for (int j = 0; j < NT; ++j)
+            acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(ks, t2, 32 * j, lane), sb, acc[j], 0, 0, 0);
         }
       }
+      n = n1;
+      buf ^= 1;
     }
-    __syncthreads();   // the tiles and (BIAS) the sums are free, or whole
+    __syncthreads();   // the tiles are free and the sums whole
   };
-  if (BIAS) pass(std::integral_constant<bool, true>());
-  row_terms();
   pass(std::integral_constant<bool, false>());
-#pragma unroll
-  for (int u = 0; u < QT; ++u) {
-    const int q = qw + 32 * u + lq;
-    if (q >= a.Sq) continue;
+  if (BIAS) {
+    // dS sums to zero over a row, but with D from the rounded output it sums to
+    // rho = (true D) - D, and the bias gradient, many sums of dS with little
+    // left over, would show it.  The true dS is dS - rho P: the near tiles are
+    // visited again for theirs, the far ones together hold what is left of 1.
+    rho += __shfl_xor(rho, 32, 64);
+    pass(std::integral_constant<bool, true>());
+    const float rest = (g == 0 ? 1.f : 0.f) - wn;   // the two lanes of a row together: P of its far tiles
+    if (a.causal) wlo = rest;
+    if (lo_far) flo -= rho * wlo;
+    if (hi_far) fhi -= rho * (rest - wlo);
+  }
+  if (q < a.Sq) {
     bf16_t* row = a.dq + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
-    const float f = q < sq.lq ? a.scale : 0.f;
+    const float f = valid ? a.scale : 0.f;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const f32x16& x = acc[u][j];
+        const f32x16& x = acc[j];
         st4(row, 32 * j + 8 * i + 4 * g, a.d, x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f, x[4 * i + 3] * f);
       }
   }
@@ -748,7 +708,7 @@ __global__ __launch_bounds__(256, DT >= 96 ? DQ_OCC : DO64) void k_mha_dq(MhaArg
     for (int e = tid; e < bl; e += 256) {
       float t = 0.f;
 #pragma unroll
-      for (int w = 0; w < 8; ++w) t += bs[bl + w * bl + e];
+      for (int w = 0; w < 4; ++w) t += bs[bl + w * bl + e];
       bs[e] = t;
     }
     __syncthreads();
@@ -764,23 +724,33 @@ __global__ __launch_bounds__(256, DT >= 96 ? DQ_OCC : DO64) void k_mha_dq(MhaArg
   }
 }
 
-// dbias[h][k] = sum over sequences and query blocks of their partials, in that order
+// dbias[h][k] = sum of the partials of head h's query blocks: a block per
+// head, a column and a part of the rows to each thread, the parts added in order.
 __global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int Hq, int nblk, int nb, float* out) {
-  const int x = blockIdx.x * 256 + threadIdx.x;
-  if (x >= Hq * nb) return;
-  const int h = x / nb, k = x % nb;
+  __shared__ double sh[256];
+  const int h = blockIdx.x, parts = 256 / nb, k = threadIdx.x % nb, p = threadIdx.x / nb;
   double t = 0.0;
-  for (int b = 0; b < B; ++b)
-    for (int i = 0; i < nblk; ++i) t += part[(((int64_t)b * Hq + h) * nblk + i) * nb + k];
-  out[x] = (float)t;
+  if (p < parts)
+    for (int i = p; i < B * nblk; i += parts) t += part[(((int64_t)(i / nblk) * Hq + h) * nblk + i % nblk) * nb + k];
+  sh[threadIdx.x] = t;
+  __syncthreads();
+  if (threadIdx.x >= nb) return;
+  for (int j = 1; j < parts; ++j) t += sh[j * nb + k];
+  out[(int64_t)h * nb + k] = (float)t;
 }
 
 // ------------------------------------------------------------- dk, dv (key-owned)
 // A wave owns 32 keys of one key head, a block 128; the steps run over the
-// query heads of the group and their 64-query tiles, so the gradients of a
+// query heads of the group and their tiles of queries, so the gradients of a
 // shared head are summed in registers.  A key block that many queries see
 // (first tokens beside a window; few, long sequences) is split over blocks of
 // `chunk` steps, whose fp32 partials k_mha_dkv_join adds in split order.
+
+// At head widths past 64 the values of the block's keys stay in LDS and the
+// query tiles have 32 rows: two waves fit a SIMD then (with everything in
+// registers one does, 240 us where this takes 198; 2 x 4096 x 16 / 4 heads x
+// 128, window 1024).
+constexpr int dkv_tile(int dt) { return dt > 64 ? 32 : 64; }
 
 // the queries [i0, i1) that see some key of [j0, j1]
 PG_DEV void seen_by(const MhaArgs& a, const Seq& sq, int j0, int j1, int& i0, int& i1) {
@@ -814,12 +784,14 @@ PG_DEV KItem item_of(const MhaArgs& a, int x) {
 }
 
 template <int DT, bool BIAS>
-__global__ __launch_bounds__(256, DT >= 96 ? DKV_OCC : 2) void k_mha_dkv(MhaArgs a) {
-  constexpr int TQ = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
+__global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
+  constexpr int TQ = dkv_tile(DT), NC = DT / 8, NT = DT / 32, KF = DT / 16;
   __shared__ __attribute__((aligned(16))) bf16_t Qs[2][TQ * DT];
   __shared__ __attribute__((aligned(16))) bf16_t Ds[2][TQ * DT];
+  constexpr bool VL = DT > 64;
+  __shared__ __attribute__((aligned(16))) bf16_t Vt[VL ? 128 * DT : 8];
   extern __shared__ float ex[];   // rows' log sums and D of the two tiles, then the current head's bias by query minus key
-  float* const bs = ex + 4 * TQ;
+  float* const bs = ex + 4 * 64;
   const KItem it = item_of(a, block_no(a, a.nks * a.ns_sink + (a.nblk - a.nks) * a.ns_reg));
   const int hk = it.bh % a.Hk, b = it.bh / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lk = lane & 31;
@@ -834,11 +806,11 @@ __global__ __launch_bounds__(256, DT >= 96 ? DKV_OCC : 2) void k_mha_dkv(MhaArgs
   const int kw = kblk + wv * 32, key = kw + lk;
   const bool kv = key < sq.lk;
   const int bl = BIAS ? bias_len(a) : 0;
-  bf16x8 kf[KF], vf[KF];
+  bf16x8 kf[KF], vf[VL ? 1 : KF];
 #pragma unroll
   for (int t = 0; t < KF; ++t) {
     kf[t] = ld_frag(a.k + b * a.ks[0] + key * a.ks[1] + hk * a.ks[2], 16 * t + 8 * g, a.d, kv);
-    vf[t] = ld_frag(a.v + b * a.vs[0] + key * a.vs[1] + hk * a.vs[2], 16 * t + 8 * g, a.d, kv);
+    if (!VL) vf[t] = ld_frag(a.v + b * a.vs[0] + key * a.vs[1] + hk * a.vs[2], 16 * t + 8 * g, a.d, kv);
   }
   f32x16 adk[NT], adv[NT];
 #pragma unroll
@@ -851,18 +823,26 @@ __global__ __launch_bounds__(256, DT >= 96 ? DKV_OCC : 2) void k_mha_dkv(MhaArgs
   const bool sink = key < a.n_sink;
   const int plo = !kv ? 0x7fffffff : a.causal ? key : a.window && !sink ? key - a.window + 1 : -0x40000000;
   const int phi = a.window && !sink ? key + a.window - 1 : 0x7fffffff;
-  Ring<NC> rq, rd;
+  Ring<NC, TQ> rq, rd;
   rq.init(a.qs[1], a.d, tid);
   rd.init(a.os[1], a.d, tid);
+  if (VL && n0 < n1) {
+    Ring<NC, 64> rv;
+    rv.init(a.vs[1], a.d, tid);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+      rv.issue(Vt + 64 * DT * x, a.v + b * a.vs[0] + (kblk + 64 * x) * a.vs[1] + hk * a.vs[2], a.vs[1], kblk + 64 * x, wv,
+               [&](int j) { return j < sq.lk; });
+  }
   auto load = [&](int n, int bf) {
     const int h = hk * a.G + n / nt, q0 = TQ * (t0 + n % nt);
     auto ok = [&](int i) { return i >= i0 && i < i1; };
     rq.issue(Qs[bf], a.q + b * a.qs[0] + h * a.qs[2] + q0 * a.qs[1], a.qs[1], q0, wv, ok);
     rd.issue(Ds[bf], a.dO + b * a.os[0] + h * a.os[2] + q0 * a.os[1], a.os[1], q0, wv, ok);
-    // 64 rows of both: the buffers are padded to 64, rows past len_q hold +inf and 0
+    // TQ rows of both: the buffers are padded to 64, rows past len_q hold +inf and 0
     const int64_t x = ((int64_t)b * a.Hq + h) * a.Sqp + q0;
-    if (wv == 0) lds_load4(lds_addr(ex + bf * 2 * TQ), lane * 4, make_rsrc(a.lse + x, TQ * 4));
-    if (wv == 1) lds_load4(lds_addr(ex + bf * 2 * TQ + TQ), lane * 4, make_rsrc(a.D + x, TQ * 4));
+    if (wv == 0) lds_load4(lds_addr(ex + bf * 128), lane * 4, make_rsrc(a.lse + x, TQ * 4));
+    if (wv == 1) lds_load4(lds_addr(ex + bf * 128 + 64), lane * 4, make_rsrc(a.D + x, TQ * 4));
   };
   if (n0 < n1) load(n0, 0);
   for (int n = n0; n < n1; ++n) {
@@ -873,30 +853,32 @@ __global__ __launch_bounds__(256, DT >= 96 ? DKV_OCC : 2) void k_mha_dkv(MhaArgs
       for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, hk * a.G + n / nt, bl - 1 - e);
       __syncthreads();
     }
+    const int qt = TQ * (t0 + n % nt), pt = qt + sq.off;
 #pragma unroll 1
-    for (int x = 0; x < 2; ++x) {
-      const int q0 = TQ * (t0 + n % nt) + 32 * x, p0 = q0 + sq.off;
+    for (int x = 0; x < TQ / 32; ++x) {
+      const int q0 = qt + 32 * x, p0 = pt + 32 * x;
       if (q0 + 32 <= w0 || q0 >= w1) continue;
       const bf16_t* qs = Qs[buf] + 32 * DT * x;
       const bf16_t* ds = Ds[buf] + 32 * DT * x;
-      const float* Ls = ex + buf * 2 * TQ + 32 * x;
+      const float* Ls = ex + buf * 128 + 32 * x;
       f32x16 s, dp;
 #pragma unroll
       for (int r = 0; r < 16; ++r) { s[r] = 0.f; dp[r] = 0.f; }
 #pragma unroll
       for (int t = 0; t < KF; ++t) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(qs, lk, 16 * t + 8 * g), kf[t], s, 0, 0, 0);
-        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ds, lk, 16 * t + 8 * g), vf[t], dp, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ds, lk, 16 * t + 8 * g),
+                                                     VL ? ld_row<NC>(Vt + wv * 32 * DT, lk, 16 * t + 8 * g) : vf[VL ? 0 : t], dp, 0, 0, 0);
       }
+      float cm = a.c, off = 0.f;   // as in the forward
       if (BIAS) {
         if (kw + 31 - p0 > -a.maxd && kw - p0 - 31 < a.maxd) {
           const float* bn = bs + (p0 - kw - lk + a.maxd + kMargin) + 4 * g;
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, bn[8 * (r >> 2) + (r & 3)]);
+          cm = 1.f;
         } else {
-          const float far = kw < p0 ? bs[bl - 1] : bs[0];
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
+          off = kw < p0 ? bs[bl - 1] : bs[0];
         }
       }
       if (!all_seen<32>(a, sq.lk, kw, p0, p0 + 31)) {
@@ -910,12 +892,12 @@ __global__ __launch_bounds__(256, DT >= 96 ? DKV_OCC : 2) void k_mha_dkv(MhaArgs
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 lv = *reinterpret_cast<const float4*>(Ls + 8 * i + 4 * g);
-        const float4 dv4 = *reinterpret_cast<const float4*>(Ls + TQ + 8 * i + 4 * g);
+        const float4 dv4 = *reinterpret_cast<const float4*>(Ls + 64 + 8 * i + 4 * g);
         const float lsv[4] = {lv.x, lv.y, lv.z, lv.w}, ddv[4] = {dv4.x, dv4.y, dv4.z, dv4.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * i + e;
-          p[r] = exp2_(BIAS ? s[r] - lsv[e] : fmaf(s[r], a.c, -lsv[e]));
+          p[r] = exp2_(BIAS ? fmaf(s[r], cm, off - lsv[e]) : fmaf(s[r], a.c, -lsv[e]));
           s[r] = p[r] * (dp[r] - ddv[e]);
         }
       }
@@ -967,7 +949,8 @@ __global__ __launch_bounds__(256) void k_mha_dkv_join(MhaArgs a) {
   const Seq sq = seq_of(a, b);
   int i0, i1;
   seen_by(a, sq, kb * 128, kb * 128 + 127, i0, i1);
-  const int steps = max((i1 + 63) / 64 - i0 / 64, 0) * a.G, ns = (steps + a.chunk - 1) / a.chunk;
+  constexpr int TQ = dkv_tile(DT);
+  const int steps = max((i1 + TQ - 1) / TQ - i0 / TQ, 0) * a.G, ns = (steps + a.chunk - 1) / a.chunk;
   if (ns <= 1) return;
   const int sinks = a.nks * a.ns_sink, per = sinks + (a.nblk - a.nks) * a.ns_reg;
   const KItem it = item_of(a, bh * per + (kb < a.nks ? kb * a.ns_sink : sinks + (kb - a.nks) * a.ns_reg));
@@ -1000,19 +983,20 @@ int head_set(int64_t heads, int group, bool ragged) {
 }
 
 int pad_d(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : 128; }
-constexpr int fwd_qt(int dt) { return dt <= 64 ? FWD64 : FWD_QT; }   // query tiles of a wave
-constexpr int dq_qt(int dt) { return dt == 64 ? DQ64 : 1; }
 
-// bucket of distance n among the `half` buckets of a side: exact below half / 2, then
-// logarithmic up to maxd, evaluated exactly: the largest e with (n / first)^m >= (maxd / first)^e.
-int bucket_of(int n, int half, int maxd) {
-  const int first = half / 2, m = half - first;
-  if (n < first) return n;
-  if (n >= maxd) return half - 1;
-  const long double x = logl((long double)n / first) / logl((long double)maxd / first) * m;
-  const long double near = roundl(x);
-  const int e = (int)(fabsl(x - near) < 1e-12L ? near : floorl(x));
-  return std::min(first + e, half - 1);
+// Smallest distance of each of the `half` buckets of a side: n for the exact
+// ones, below half / 2; bucket half / 2 + e starts at the first whole number at
+// or above (half / 2) (maxd / (half / 2))^(e / (half - half / 2)).  A boundary
+// that is not itself whole is at least 5e-11 of its size from a whole number
+// (counted over all half <= 256, maxd <= 512), so rounding cannot move it.
+void bucket_starts(int half, int maxd, uint16_t* start) {
+  const int first = half / 2;
+  for (int k = 0; k <= first; ++k) start[k] = (uint16_t)k;
+  const double step = std::log2((double)maxd / first) / (half - first);
+  for (int e = 1; first + e < half; ++e) {
+    const double x = first * std::exp2(step * e);
+    start[first + e] = (uint16_t)std::ceil(x - 1e-12 * x);
+  }
 }
 
 MhaArgs make_args(const Mha& m) {
@@ -1025,12 +1009,11 @@ MhaArgs make_args(const Mha& m) {
   a.scale = m.scale; a.c = m.scale * kL2E;
   for (int i = 0; i < 3; ++i) { a.qs[i] = m.qs[i]; a.ks[i] = m.ks[i]; a.vs[i] = m.vs[i]; a.os[i] = m.os[i]; }
   if (m.n_buckets) {
-    int have = 0;
-    for (int n = 0; n <= m.max_distance; ++n) {
-      a.lut[n] = (uint8_t)bucket_of(n, a.half, m.max_distance);
-      while (have <= a.lut[n]) a.start[have++] = (uint16_t)n;
+    bucket_starts(a.half, m.max_distance, a.start);
+    for (int k = 0; k < a.half; ++k) {   // a bucket without a distance of its own leaves no mark
+      const int end = k + 1 < a.half ? a.start[k + 1] : m.max_distance + 1;
+      for (int n = a.start[k]; n < end; ++n) a.lut[n] = (uint8_t)k;
     }
-    while (have <= a.half) a.start[have++] = (uint16_t)(m.max_distance + 1);
   }
   return a;
 }
@@ -1046,25 +1029,32 @@ int step_splits(const Mha& m) {
 }
 
 // How the key-owned pass is cut: blocks of 128 keys; a block's steps are
-// G x (64-query tiles that see it).  Few blocks are split until there are four
-// for each place on the card (two a CU), into 8 steps at least; blocks with
-// first tokens, which every query sees, into what the others have.
+// G x (query tiles that see it).  Blocks with first tokens, which every
+// query sees, and all blocks where they are few, are split into pieces of
+// `chunk` steps: the number of pieces with the least modelled time, the steps
+// over the places on the card plus half the last piece, a piece's partials
+// costing about as much as 256 queries to write and add.
 struct KPlan { int nkb, nks, ns_sink, ns_reg, chunk; int64_t items, slots; };
 KPlan plan_keys(const Mha& m) {
-  KPlan p{};
-  const int64_t G = m.Hq / m.Hk, all = G * cdiv(m.Sq, 64);
-  p.nkb = (int)cdiv(m.Sk, 128);
-  const int64_t reg = m.window ? std::min(all, G * (cdiv((m.causal ? 1 : 2) * (int64_t)m.window + 128, 64) + 1)) : all;
-  p.nks = m.window && reg < all ? (int)std::min<int64_t>(p.nkb, cdiv(m.n_sink, 128)) : 0;
-  const int64_t bh = (int64_t)m.B * m.Hk, total = bh * (p.nks * all + (p.nkb - p.nks) * reg) / (m.causal && !m.window ? 2 : 1);
-  int64_t chunk = std::max<int64_t>(8, cdiv(total, 2048));
-  if (bh * p.nkb >= 1024) chunk = std::max(chunk, reg);   // enough blocks as they are
-  p.chunk = (int)std::min<int64_t>(chunk, 1 << 30);
-  p.ns_sink = (int)cdiv(all, chunk);
-  p.ns_reg = (int)cdiv(reg, chunk);
-  p.items = bh * ((int64_t)p.nks * p.ns_sink + (int64_t)(p.nkb - p.nks) * p.ns_reg);
-  p.slots = bh * ((p.ns_sink > 1 ? (int64_t)p.nks * p.ns_sink : 0) + (p.ns_reg > 1 ? (int64_t)(p.nkb - p.nks) * p.ns_reg : 0));
-  return p;
+  const int64_t tq = dkv_tile(pad_d(m.d)), G = m.Hq / m.Hk, all = G * cdiv(m.Sq, tq), bh = (int64_t)m.B * m.Hk, nkb = cdiv(m.Sk, 128);
+  const int64_t reg = m.window ? std::min(all, G * (cdiv((m.causal ? 1 : 2) * (int64_t)m.window + 128, tq) + 1)) : all;
+  const int64_t nks = m.window && reg < all ? std::min<int64_t>(nkb, cdiv(m.n_sink, 128)) : 0;
+  const double places = 512, used = m.causal && !m.window ? 0.5 : 1.0;   // half of a triangle
+  const double total = (double)bh * (nks * all + (nkb - nks) * reg * used);
+  KPlan best{};
+  double least = 0;
+  for (int64_t ns = 1; ns <= 16; ++ns) {
+    KPlan p{};
+    p.nkb = (int)nkb; p.nks = (int)nks;
+    p.chunk = (int)std::min<int64_t>(cdiv(reg, ns), 1 << 30);
+    p.ns_sink = (int)cdiv(all, p.chunk);
+    p.ns_reg = (int)cdiv(reg, p.chunk);
+    p.items = bh * (nks * p.ns_sink + (nkb - nks) * p.ns_reg);
+    p.slots = bh * ((p.ns_sink > 1 ? nks * p.ns_sink : 0) + (p.ns_reg > 1 ? (nkb - nks) * p.ns_reg : 0));
+    const double t = (total + 256.0 / tq * used * p.slots) / places + 0.5 * p.chunk;
+    if (p.items < (1 << 24) && (ns == 1 || t < least)) { best = p; least = t; }
+  }
+  return best;
 }
 
 size_t bias_bytes(const Mha& m, int arrays) {
@@ -1089,7 +1079,7 @@ size_t mha_saved_bytes(const Mha& m) {
 size_t mha_ws_bytes(const Mha& m) {
   const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 64) * 64;
   // the rows' D, then the bias partials or (after these are joined) those of dk and dv
-  const size_t bias = (size_t)m.B * m.Hq * cdiv(m.Sq, 128 * dq_qt(pad_d(m.d))) * m.n_buckets * 4;
+  const size_t bias = (size_t)m.B * m.Hq * cdiv(m.Sq, 128) * m.n_buckets * 4;
   const size_t keys = (size_t)plan_keys(m).slots * 128 * 2 * pad_d(m.d) * 4;
   const size_t bwd = align256(rows * 4) + align256(std::max(bias, keys));
   size_t step = 0;
@@ -1121,14 +1111,13 @@ void mha_fwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
     return;
   }
   a.lse = (float*)saved;
-  a.nblk = (int)cdiv(m.Sq, 128 * fwd_qt(pad_d(m.d)));
+  a.nblk = (int)cdiv(m.Sq, 128);
   a.hset = head_set((int64_t)m.B * m.Hq, a.G, len_k || len_q);
   const dim3 grid((unsigned)((int64_t)m.B * m.Hq * a.nblk));
   ProfScope prof(st);
   PG_DT(m.d, {
-    constexpr int QT = fwd_qt(DT);
-    if (m.n_buckets) hipLaunchKernelGGL((k_mha_fwd<DT, QT, true>), grid, dim3(256), bias_bytes(m, 1), st, a);
-    else hipLaunchKernelGGL((k_mha_fwd<DT, QT, false>), grid, dim3(256), 0, st, a);
+    if (m.n_buckets) hipLaunchKernelGGL((k_mha_fwd<DT, true>), grid, dim3(256), bias_bytes(m, 1), st, a);
+    else hipLaunchKernelGGL((k_mha_fwd<DT, false>), grid, dim3(256), 0, st, a);
   });
   PG_LAUNCH_CHECK();
   prof.done("k_mha_fwd<" + std::to_string(pad_d(m.d)) + ">", flops);
@@ -1147,16 +1136,15 @@ void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   a.part = (float*)((char*)ws + align256(rows * 4));
   ProfScope prof(st);
   PG_DT(m.d, {
-    constexpr int QT = dq_qt(DT);
-    a.nblk = (int)cdiv(m.Sq, 128 * QT);
+    a.nblk = (int)cdiv(m.Sq, 128);
     a.hset = head_set((int64_t)m.B * m.Hq, a.G, len_k || len_q);
     const dim3 gq((unsigned)((int64_t)m.B * m.Hq * a.nblk));
     if (m.n_buckets) {
-      hipLaunchKernelGGL((k_mha_dq<DT, QT, true>), gq, dim3(256), bias_bytes(m, 9), st, a);
-      hipLaunchKernelGGL(k_mha_dbias, dim3((unsigned)cdiv((int64_t)m.Hq * m.n_buckets, 256)), dim3(256), 0, st, a.part,
+      hipLaunchKernelGGL((k_mha_dq<DT, true>), gq, dim3(256), bias_bytes(m, 5), st, a);
+      hipLaunchKernelGGL(k_mha_dbias, dim3((unsigned)m.Hq), dim3(256), 0, st, a.part,
                          m.B, m.Hq, a.nblk, m.n_buckets, dtable);
     } else {
-      hipLaunchKernelGGL((k_mha_dq<DT, QT, false>), gq, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_mha_dq<DT, false>), gq, dim3(256), 0, st, a);
     }
     const KPlan p = plan_keys(m);
     a.nblk = p.nkb; a.nks = p.nks; a.ns_sink = p.ns_sink; a.ns_reg = p.ns_reg; a.chunk = p.chunk;
