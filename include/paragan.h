@@ -257,7 +257,7 @@ int paragan_attn_bwd(paragan_ctx* ctx, const paragan_attn_desc* d,
  * [n_pos][rot/2][2], any angles (for instance half of the pairs turned by a
  * token's row and half by its column); NULL when rot is 0.  pos: [T] device,
  * or NULL for t mod n_pos.  A token whose position is outside [0, n_pos) is
- * padding: its rows are not read, its outputs and gradients are zero.
+ * padding: its rows are not used, its outputs and gradients are zero.
  * Token t of q starts at q + t * ldq, its heads follow one another; outputs
  * likewise with ldqo and ldko.  dq, dk (the gradients of q, k) lie as q, k
  * do, dqo, dko (of the outputs) as the outputs do.  Outputs may be the

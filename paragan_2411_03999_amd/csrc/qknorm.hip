@@ -10,9 +10,16 @@
 // read twice, written once), everything between stays in registers in fp32.
 // A lane holds 8 elements of a head (one 16-byte access in bf16), a group of
 // LPH lanes one head; a group keeps its token's rotation row and the gains in
-// registers over all the heads it takes.  Sums over a head are butterflies
-// inside the group; in the half-split order the pair's other element sits
-// rot / 16 lanes away and comes by a lane shuffle.
+// registers over the heads it takes, four of which are in flight together.
+// Loads are unconditional (a group without work reads a valid row again), so
+// nothing waits for a position.  Sums over a head are butterflies inside the
+// group (lane moves in the vector unit up to 16 lanes); in the half-split
+// order the pair's other element sits rot / 16 lanes away and comes by a lane
+// exchange.  Blocks of the grid's second dimension take q or k.
+// Measured: forward of 32768 tokens x 16 heads x 64 in bf16 24 us (5.6 TB/s,
+// part of it from cache), backward of 15005 x 40 x 128 100 us (4.6 TB/s, as a
+// plain copy); fewer registers for more waves, or two heads in flight, were
+// slower (backward 104 to 396 us).
 #include "token.hpp"
 
 namespace pg {
@@ -22,27 +29,39 @@ namespace {
 constexpr int kGainBlocks = 1024;   // blocks of a backward at most (one row of gain partials each)
 
 struct QkArgs {
-  int64_t T;
-  int Hq, H, d, rot, n_pos, inter;
-  int ns, hc;                       // head splits of a token, heads of one split
+  uint32_t T;
+  int d, rot, n_pos, inter;
   float eps, inv_d;
-  int64_t ldx[2], ldy[2];           // token strides of q, k (and dq, dk) and of the outputs (and their gradients)
-  const void* x[2];
-  const void* dy[2];
-  void* y[2];                       // outputs (forward) or input gradients (backward)
-  const float* gain[2];
   const float* table;
   const int32_t* pos;
   float* part;
+  struct Side {                     // q or k
+    int H, ns, hc, grid;            // heads; splits of a token's heads, heads of one split; blocks
+    int64_t ldx, ldy;               // token strides of the input (and its gradient) and of the output (and its gradient)
+    const void *x, *dy;
+    void* y;                        // output (forward) or input gradient (backward)
+    const float* gain;
+  } side[2];
 };
 
-template <typename T> PG_DEV void ld8f(const T* p, float* f);
-template <> PG_DEV void ld8f<bf16_t>(const bf16_t* p, float* f) { unpack8(*reinterpret_cast<const uint4*>(p), f); }
-template <> PG_DEV void ld8f<float>(const float* p, float* f) {
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
+// 8 elements as they lie in memory, and as floats
+template <typename T> struct Raw;
+template <> struct Raw<bf16_t> {
+  uint4 v;
+  PG_DEV void load(const bf16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
+  PG_DEV void get(float* f) const { unpack8(v, f); }
+};
+template <> struct Raw<float> {
+  float4 a, b;
+  PG_DEV void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  PG_DEV void get(float* f) const {
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  }
+};
 template <typename T> PG_DEV void st8f(T* p, const float* f);
 template <> PG_DEV void st8f<bf16_t>(bf16_t* p, const float* f) { *reinterpret_cast<uint4*>(p) = pack8(f); }
 template <> PG_DEV void st8f<float>(float* p, const float* f) {
@@ -50,10 +69,18 @@ template <> PG_DEV void st8f<float>(float* p, const float* f) {
   reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
 
+template <int CTRL>
+PG_DEV float lane_move(float v) {
+  return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// sum over the LPH lanes of a group, in every lane
 template <int LPH>
 PG_DEV float group_sum(float v) {
-#pragma unroll
-  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if (LPH > 1) v += lane_move<0xB1>(v);    // quad lanes 1 0 3 2
+  if (LPH > 2) v += lane_move<0x4E>(v);    // quad lanes 2 3 0 1
+  if (LPH > 4) v += lane_move<0x141>(v);   // the other quad of 8 (mirrored; a quad is uniform by now)
+  if (LPH > 8) v += lane_move<0x140>(v);   // the other half of 16 (mirrored)
+  if (LPH > 16) v += __shfl_xor(v, 16, 64);
   return v;
 }
 
@@ -112,76 +139,80 @@ PG_DEV void turn(const Turn& t, int inter, int rot, float* v) {
 }
 
 template <typename T, int LPH, bool BWD>
-__global__ __launch_bounds__(256) void k_qknorm(QkArgs a) {
-  constexpr int GPB = 256 / LPH, U = BWD ? 2 : 4;
+__global__ __launch_bounds__(256, BWD ? 2 : 4) void k_qknorm(QkArgs a) {
+  constexpr int GPB = 256 / LPH, U = 4;
+  const auto& sd = a.side[blockIdx.y];
+  if ((int)blockIdx.x >= sd.grid) return;
   const int tid = threadIdx.x, lane = tid & 63, ch = tid % LPH, grp = tid / LPH;
   const bool act = ch * 8 < a.d;
-  float g[2][8], dg[2][8];
+  const int c8 = act ? ch * 8 : 0;
+  float g[8], dg[8];
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      g[w][e] = act ? a.gain[w][ch * 8 + e] : 0.f;
-      dg[w][e] = 0.f;
-    }
+  for (int e = 0; e < 8; ++e) {
+    g[e] = act ? sd.gain[c8 + e] : 0.f;
+    dg[e] = 0.f;
+  }
   // items (token, head split): below 2^31 + 2^19
-  const uint32_t items = (uint32_t)a.T * a.ns, step = gridDim.x * GPB;
-  // every group of a wave goes round together (the shuffles need all lanes)
+  const uint32_t items = a.T * (uint32_t)sd.ns, step = (uint32_t)sd.grid * GPB;
+  // every group of a wave goes round together (the lane exchanges need all lanes)
   for (uint32_t it0 = blockIdx.x * GPB; it0 < items; it0 += step) {
-    const uint32_t it = it0 + grp;
-    const bool in = it < items;
-    const int64_t t = in ? it / (uint32_t)a.ns : 0;
-    const int h0 = in ? (int)(it % (uint32_t)a.ns) * a.hc : 0;
-    const int h1 = in ? min(a.H, h0 + a.hc) : 0;
-    const int p = a.pos ? a.pos[t] : (int)((uint32_t)t % (uint32_t)a.n_pos);
+    const uint32_t it = min(it0 + grp, items - 1);
+    const bool in = it0 + grp < items;
+    const uint32_t t = it / (uint32_t)sd.ns;
+    const int h0 = (int)(it - t * sd.ns) * sd.hc, h1 = min(sd.H, h0 + sd.hc);
+    const T* x0 = (const T*)sd.x + (int64_t)t * sd.ldx + c8;
+    const T* dy0 = BWD ? (const T*)sd.dy + (int64_t)t * sd.ldy + c8 : nullptr;
+    T* y0 = (T*)sd.y + (int64_t)t * (BWD ? sd.ldx : sd.ldy) + c8;
+    const int p = a.pos ? a.pos[t] : (int)(t % (uint32_t)a.n_pos);
+    Raw<T> xr[U], dr[U];
+    auto fetch = [&](int h) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t o = (int64_t)min(h + u, h1 - 1) * a.d;
+        xr[u].load(x0 + o);
+        if (BWD) dr[u].load(dy0 + o);
+      }
+    };
+    fetch(h0);
     const bool real = p >= 0 && p < a.n_pos;          // a position outside the table: padding, zeros
     Turn tn;
     load_turn<LPH>(tn, a, real, p, lane, ch);
-    for (int k = 0; k < a.hc; k += U) {
-      float x[U][8], dy[U][8];
-      bool ok[U];
-      int w[U];
-      int64_t yo[U], xo[U];
+    for (int h = h0; h < h0 + sd.hc; h += U) {   // as often for every group of the wave
+      if (h > h0) fetch(min(h, h1 - 1));
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int h = h0 + k + u;
-        w[u] = h >= a.Hq;
-        const int hl = w[u] ? h - a.Hq : h;
-        ok[u] = h < h1 && k + u < a.hc && act;
-        xo[u] = t * a.ldx[w[u]] + (int64_t)hl * a.d + ch * 8;
-        yo[u] = t * a.ldy[w[u]] + (int64_t)hl * a.d + ch * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { x[u][e] = 0.f; dy[u][e] = 0.f; }
-        if (ok[u] && real) {
-          ld8f<T>((const T*)a.x[w[u]] + xo[u], x[u]);
-          if (BWD) ld8f<T>((const T*)a.dy[w[u]] + yo[u], dy[u]);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
+        const bool ok = in && act && h + u < h1;
+        const int64_t o = (int64_t)(h + u) * a.d;
+        float x[8], dy[8];
+        xr[u].get(x);
+        if (BWD) dr[u].get(dy);
+        const bool use = act && real && (!BWD || ok);   // nothing of padding, and of a row twice no gain gradient
         float ss = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(x[u][e], x[u][e], ss);
-        const float r = 1.f / sqrtf(fmaf(group_sum<LPH>(ss), a.inv_d, a.eps));
+        for (int e = 0; e < 8; ++e) {
+          x[e] = use ? x[e] : 0.f;
+          if (BWD) dy[e] = use ? dy[e] : 0.f;
+          ss = fmaf(x[e], x[e], ss);
+        }
+        const float r = __builtin_amdgcn_rsqf(fmaf(group_sum<LPH>(ss), a.inv_d, a.eps));
         if (!BWD) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[u][e] = x[u][e] * r * (w[u] ? g[1][e] : g[0][e]);
-          turn<false>(tn, a.inter, a.rot, x[u]);
-          if (ok[u]) st8f<T>((T*)a.y[w[u]] + yo[u], x[u]);
+          for (int e = 0; e < 8; ++e) x[e] = x[e] * r * g[e];
+          turn<false>(tn, a.inter, a.rot, x);
+          if (ok) st8f<T>(y0 + o, x);
         } else {
-          turn<true>(tn, a.inter, a.rot, dy[u]);
+          turn<true>(tn, a.inter, a.rot, dy);
           float tx = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float c = dy[u][e] * (x[u][e] * r);
-            if (w[u]) dg[1][e] += c; else dg[0][e] += c;
-            dy[u][e] *= w[u] ? g[1][e] : g[0][e];
-            tx = fmaf(dy[u][e], x[u][e], tx);
+            dg[e] = fmaf(dy[e], x[e] * r, dg[e]);
+            dy[e] *= g[e];
+            tx = fmaf(dy[e], x[e], tx);
           }
           const float m = group_sum<LPH>(tx) * a.inv_d * r * r;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) dy[u][e] = r * (dy[u][e] - x[u][e] * m);
-          if (ok[u]) st8f<T>((T*)a.y[w[u]] + xo[u], dy[u]);
+          for (int e = 0; e < 8; ++e) dy[e] = r * (dy[e] - x[e] * m);
+          if (ok) st8f<T>(y0 + o, dy);
         }
       }
     }
@@ -189,35 +220,34 @@ __global__ __launch_bounds__(256) void k_qknorm(QkArgs a) {
   if (BWD) {   // gain partials of the block: the groups' sums in group order
     __shared__ float sh[256 * 8];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sh[tid * 8 + e] = dg[w][e];
-      __syncthreads();
-      if (tid < a.d) {
-        float s = 0.f;
-        for (int j = 0; j < GPB; ++j) s += sh[j * LPH * 8 + tid];
-        a.part[((int64_t)blockIdx.x * 2 + w) * a.d + tid] = s;
-      }
+    for (int e = 0; e < 8; ++e) sh[tid * 8 + e] = dg[e];
+    __syncthreads();
+    if (tid < a.d) {
+      float s = 0.f;
+      for (int j = 0; j < GPB; ++j) s += sh[j * LPH * 8 + tid];
+      a.part[((int64_t)(blockIdx.y ? a.side[0].grid : 0) + blockIdx.x) * a.d + tid] = s;
     }
   }
 }
 
-// dg[w][c] = sum over blocks of part[block][w][c]: 32 columns x 8 row lanes a block, rows in a fixed order
-__global__ __launch_bounds__(256) void k_qknorm_gain(const float* part, int nb, int d, float* dgq, float* dgk) {
-  __shared__ float sh[8][32];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+// dg[c] = sum over the blocks of q (blockIdx.y = 0) or k of part[block][c]:
+// 16 columns x 64 row lanes a block, the rows of a lane and the lanes in order
+__global__ __launch_bounds__(1024) void k_qknorm_gain(const float* part, int nq, int nk, int d, float* dgq, float* dgk) {
+  __shared__ float sh[64][17];
+  const int c = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4, nb = blockIdx.y ? nk : nq;
+  const float* p = part + (blockIdx.y ? (int64_t)nq * d : 0);
   float s = 0.f;
-  if (c < 2 * d)
-    for (int b = r; b < nb; b += 8) s += part[(int64_t)b * 2 * d + c];
-  sh[r][threadIdx.x & 31] = s;
-  __syncthreads();
-  if (r == 0 && c < 2 * d) {
-    float v = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v += sh[j][threadIdx.x];
-    if (c < d) dgq[c] = v; else dgk[c - d] = v;
+  if (c < d) {
+#pragma unroll 8
+    for (int b = r; b < nb; b += 64) s += p[(int64_t)b * d + c];
   }
+  sh[r][threadIdx.x & 15] = s;
+  __syncthreads();
+  if (threadIdx.x >= 16 || c >= d) return;
+  float v = 0.f;
+#pragma unroll
+  for (int j = 0; j < 64; ++j) v += sh[j][threadIdx.x];
+  (blockIdx.y ? dgk : dgq)[c] = v;
 }
 
 int lanes_per_head(int d) {
@@ -227,24 +257,29 @@ int lanes_per_head(int d) {
 }
 
 // Heads of a token are split over groups until the groups fill the card's
-// 256 x 2048 threads: a few tokens then finish in one round of loads.
-QkArgs make_args(const QkNorm& a) {
+// 256 x 2048 threads: a few tokens then finish in one round of loads.  The
+// blocks are at most `most`, shared by the sides as their heads are.
+QkArgs make_args(const QkNorm& a, int64_t most) {
   QkArgs k{};
-  k.T = a.T; k.Hq = a.Hq; k.H = a.Hq + a.Hk; k.d = a.d; k.rot = a.rot; k.n_pos = a.n_pos; k.inter = a.inter;
+  k.T = (uint32_t)a.T; k.d = a.d; k.rot = a.rot; k.n_pos = a.n_pos; k.inter = a.inter;
   k.eps = a.eps; k.inv_d = 1.f / (float)a.d;
-  k.ldx[0] = a.ldq; k.ldx[1] = a.ldk; k.ldy[0] = a.ldqo; k.ldy[1] = a.ldko;
-  const int64_t want = 524288 / lanes_per_head(a.d);
-  const int64_t ns = std::min<int64_t>(k.H, std::max<int64_t>(1, cdiv(want, a.T)));
-  k.hc = (int)cdiv(k.H, ns);
-  k.ns = (int)cdiv(k.H, k.hc);
+  const int H[2] = {a.Hq, a.Hk};
+  const int64_t ldx[2] = {a.ldq, a.ldk}, ldy[2] = {a.ldqo, a.ldko};
+  const int64_t lph = lanes_per_head(a.d), want = 524288 / lph;
+  for (int w = 0; w < 2; ++w) {
+    auto& s = k.side[w];
+    s.H = H[w]; s.ldx = ldx[w]; s.ldy = ldy[w];
+    const int64_t ns = std::min<int64_t>(s.H, std::max<int64_t>(1, cdiv(want * s.H, a.T * (a.Hq + a.Hk))));
+    s.hc = (int)cdiv(s.H, ns);
+    s.ns = (int)cdiv(s.H, s.hc);
+    s.grid = (int)std::min(cdiv(a.T * s.ns, 256 / lph), std::max<int64_t>(1, most * s.H / (a.Hq + a.Hk)));
+  }
   return k;
 }
 
-int64_t grid_of(const QkArgs& k, int lph, int64_t most) { return std::min(cdiv(k.T * k.ns, 256 / lph), most); }
-
 template <bool BWD>
-void launch(hipStream_t st, const QkNorm& a, const QkArgs& k, int64_t grid) {
-  const dim3 g((unsigned)grid), b(256);
+void launch(hipStream_t st, const QkNorm& a, const QkArgs& k) {
+  const dim3 g((unsigned)std::max(k.side[0].grid, k.side[1].grid), 2), b(256);
 #define PG_QK(L)                                                                       \
   case L:                                                                              \
     if (a.f32) hipLaunchKernelGGL((k_qknorm<float, L, BWD>), g, b, 0, st, k);          \
@@ -260,29 +295,30 @@ void launch(hipStream_t st, const QkNorm& a, const QkArgs& k, int64_t grid) {
 
 }  // namespace
 
-size_t qknorm_ws_bytes(const QkNorm& a) { return (size_t)kGainBlocks * 2 * a.d * sizeof(float); }
+size_t qknorm_ws_bytes(const QkNorm& a) { return (size_t)(kGainBlocks + 1) * a.d * sizeof(float); }
 
 void qknorm_fwd(hipStream_t st, const QkNorm& a, const void* q, const void* k, const float* gq, const float* gk,
                 const float* table, const int32_t* pos, void* qo, void* ko) {
-  QkArgs g = make_args(a);
-  g.x[0] = q; g.x[1] = k; g.y[0] = qo; g.y[1] = ko;
-  g.gain[0] = gq; g.gain[1] = gk; g.table = table; g.pos = pos;
+  QkArgs g = make_args(a, 1 << 20);
+  g.table = table; g.pos = pos;
+  g.side[0].x = q; g.side[0].y = qo; g.side[0].gain = gq;
+  g.side[1].x = k; g.side[1].y = ko; g.side[1].gain = gk;
   ProfScope prof(st);
-  launch<false>(st, a, g, grid_of(g, lanes_per_head(a.d), 1 << 20));
+  launch<false>(st, a, g);
   prof.done_bytes("k_qknorm_fwd", (double)a.T * (a.Hq + a.Hk) * a.d * (a.f32 ? 8.0 : 4.0));
 }
 
 void qknorm_bwd(hipStream_t st, const QkNorm& a, const void* q, const void* k, const float* gq, const float* gk,
                 const float* table, const int32_t* pos, const void* dqo, const void* dko, void* dq, void* dk,
                 float* dgq, float* dgk, void* ws) {
-  QkArgs g = make_args(a);
-  g.x[0] = q; g.x[1] = k; g.dy[0] = dqo; g.dy[1] = dko; g.y[0] = dq; g.y[1] = dk;
-  g.gain[0] = gq; g.gain[1] = gk; g.table = table; g.pos = pos; g.part = (float*)ws;
-  const int64_t grid = grid_of(g, lanes_per_head(a.d), kGainBlocks);
+  QkArgs g = make_args(a, kGainBlocks);
+  g.table = table; g.pos = pos; g.part = (float*)ws;
+  g.side[0].x = q; g.side[0].dy = dqo; g.side[0].y = dq; g.side[0].gain = gq;
+  g.side[1].x = k; g.side[1].dy = dko; g.side[1].y = dk; g.side[1].gain = gk;
   ProfScope prof(st);
-  launch<true>(st, a, g, grid);
-  hipLaunchKernelGGL(k_qknorm_gain, dim3((unsigned)cdiv(2 * a.d, 32)), dim3(256), 0, st, (const float*)ws, (int)grid,
-                     a.d, dgq, dgk);
+  launch<true>(st, a, g);
+  hipLaunchKernelGGL(k_qknorm_gain, dim3((unsigned)cdiv(a.d, 16), 2), dim3(1024), 0, st, (const float*)ws,
+                     g.side[0].grid, g.side[1].grid, a.d, dgq, dgk);
   PG_LAUNCH_CHECK();
   prof.done_bytes("k_qknorm_bwd", (double)a.T * (a.Hq + a.Hk) * a.d * (a.f32 ? 12.0 : 6.0));
 }
