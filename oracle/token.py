@@ -131,10 +131,10 @@ def mha(q, k, v, scale, causal=False, window=0, n_sink=0, table=None, max_distan
             dP = DO @ V.T
             D = (P * dP).sum(-1, keepdims=True)
             dS = P * (dP - D)
-            # dP's own rounding, and D's: for dq and dk that of do . o with the rounded output; the bias gradient
-            # has its rows' dS sum to zero again, up to the rounding of the row's fp32 sum
+            # dP's own rounding, and D's: for dq and dk that of do . o, o of rounded probabilities and kept to twice
+            # bfloat16's digits; the bias gradient has its rows' dS sum to zero again, up to the row's fp32 sum
             tp = U32 * (d + 4) * (ad @ av.T)
-            to_row = (ad * to).sum(-1, keepdims=True)
+            to_row = (ad * (U16 * U16 * np.abs(o) + (U16 + 2 * eta) * (P @ av))).sum(-1, keepdims=True)
             ts = P * (tp + to_row + 4 * eta * (np.abs(dP) + np.abs(D)))
             ta = ts + U16 * np.abs(dS)
             mass = (P * (np.abs(dP) + np.abs(D) + to_row)).sum(-1, keepdims=True)

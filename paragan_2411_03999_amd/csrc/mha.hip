@@ -30,6 +30,7 @@ namespace pg {
 
 namespace {
 
+constexpr int kStepTable = 64;  // buckets up to which a step keeps its rows' bias in LDS (8 KB)
 constexpr int kMargin = 96;   // distances past max_distance that a 64 x 32 tile can reach, rounded up
 
 struct MhaArgs {
@@ -44,6 +45,7 @@ struct MhaArgs {
   const float* table;
   const int32_t *len_q, *len_k;
   float *lse, *D, *part;
+  uint2* olo;                   // what rounding took off the output, bf16, in register layout: [32-query tile][DT / 8][64 lanes][4]
   uint16_t start[257];          // smallest distance of each bucket of one side
   uint8_t lut[kMhaMaxDist + 8]; // bucket (of one side) of each distance
 };
@@ -125,13 +127,14 @@ PG_DEV float max3(float a, float b, float c) {
   return r;
 }
 
+// a bias in log2 units; the lowest finite value stays finite (a row of nothing else is uniform)
+PG_DEV float log2_bias(float t) { return t < 0.f && t >= -FLT_MAX ? fmaxf(t * kL2E, -FLT_MAX) : t * kL2E; }
+
 // bias in log2 units at distance index e = rel + maxd + kMargin; distances past max_distance are its own
 PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
   const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
   const int b = (int)a.lut[rel < 0 ? -rel : rel] + (rel > 0 ? a.half : 0);
-  const float t = a.table[(int64_t)h * a.nb + b];
-  // the lowest finite value stays finite (a row of nothing else is uniform)
-  return t < 0.f && t >= -FLT_MAX ? fmaxf(t * kL2E, -FLT_MAX) : t * kL2E;
+  return log2_bias(a.table[(int64_t)h * a.nb + b]);
 }
 PG_DEV int bias_len(const MhaArgs& a) { return 2 * (a.maxd + kMargin) + 1; }
 
@@ -292,55 +295,115 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
   const bool any = q < sq.lq && lt > 0.f;
   const float inv = any ? 1.f / lt : 0.f;
   bf16_t* orow = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
+  uint2* const lo = a.olo && qw < a.Sqp ? a.olo + ((int64_t)bh * (a.Sqp / 32) + qw / 32) * (DT / 8) * 64 + lane : nullptr;
 #pragma unroll
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const f32x16& x = acc[j];
-      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (any) f = make_float4(x[4 * i] * inv, x[4 * i + 1] * inv, x[4 * i + 2] * inv, x[4 * i + 3] * inv);
-      if (q < a.Sq) st4(orow, 32 * j + 8 * i + 4 * g, a.d, f.x, f.y, f.z, f.w);
+      float f[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = any ? acc[j][4 * i + e] * inv : 0.f;
+      if (q < a.Sq) st4(orow, 32 * j + 8 * i + 4 * g, a.d, f[0], f[1], f[2], f[3]);
+      if (lo) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] -= rnd<bf16_t>(f[e]);
+        lo[(4 * j + i) * 64] = make_uint2(f2bf2(f[0], f[1]), f2bf2(f[2], f[3]));
+      }
     }
   if (a.lse && g == 0 && q < a.Sqp) a.lse[(int64_t)bh * a.Sqp + q] = any ? m2 + __log2f(lt) : INFINITY;
 }
 
 // ------------------------------------------------------------- a few new tokens
 // The rows (query head of the group, query) of one key head form tiles of 32;
-// a block's 4 waves take key tiles in turn, each with its own running softmax,
-// joined at the end; nsplit blocks share a long cache and leave partials.
+// a block's 4 waves take tiles of 32 keys in turn, each with its own running
+// softmax, joined at the end; nsplit blocks share a long cache and leave
+// partials.  Bound by reading keys and values once: a wave has its next tile
+// on the way into a ring of its own in LDS while it works on one, with no
+// barrier in the loop.
+
+// 32 rows x NC chunks into a swizzled LDS tile by one wave, as Ring
+template <int NC>
+struct WaveRing {
+  static constexpr int L = NC / 2;   // loads
+  uint32_t off[L];
+  PG_DEV void init(int64_t ld, int d, int lane) {
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+      const int i = j * 64 + lane, r = i / NC, c = (i - r * NC) ^ swz16<NC>(r);
+      off[j] = c * 8 < d ? (uint32_t)(r * (int)ld * 2 + c * 16) : kOOB;
+    }
+  }
+  template <class F>
+  PG_DEV void issue(bf16_t* tile, const bf16_t* base, int64_t ld, int r0, int lane, F ok) const {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, (31 * ld + NC * 8) * 2);
+    const uint32_t dst = lds_addr(tile);
+#pragma unroll
+    for (int j = 0; j < L; ++j) lds_load16(dst + j * 1024, ok(r0 + (j * 64 + lane) / NC) ? off[j] : kOOB, 0, rs);
+  }
+};
+// at most N of this wave's loads still on their way
+template <int N>
+PG_DEV void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
 template <int DT, bool BIAS>
-__global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
+__global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
   constexpr int NC = DT / 8, NT = DT / 32, KF = DT / 16;
-  __shared__ __attribute__((aligned(16))) bf16_t Vs[4][32 * DT];
+  // [wave][buffer][keys, values]; afterwards the waves' outputs
+  constexpr int kRing = 4 * 2 * 2 * 32 * DT * 2, kRed = 3 * NT * 16 * 64 * 4;
+  __shared__ __attribute__((aligned(16))) char lds[kRing > kRed ? kRing : kRed];
   __shared__ float ml[4][32][2];
-  __shared__ __attribute__((aligned(16))) float red[3][NT * 16 * 64];
-  extern __shared__ float dyn[];   // bias of the tile's rows by bucket, [32][nb], then the distances' buckets
+  extern __shared__ float dyn[];   // BIAS: the distances' buckets, then (nb <= kStepTable) the rows' bias by bucket
   const int z = blockIdx.x % a.nsplit, rt = (blockIdx.x / a.nsplit) % a.nrt, bh = blockIdx.x / a.nsplit / a.nrt;
   const int hk = bh % a.Hk, b = bh / a.Hk;
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31, wv = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lq = lane & 31;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
   const int rho = rt * 32 + lq, R = a.G * a.Sq;
   const int i = rho % a.Sq, h = hk * a.G + min(rho / a.Sq, a.G - 1);
   const bool live = rho < R && i < sq.lq;
-  uint8_t* lut = reinterpret_cast<uint8_t*>(dyn + 32 * a.nb);
-  if (BIAS) {
-    for (int e = tid; e < 32 * a.nb; e += 256) {
-      const int hh = hk * a.G + min((rt * 32 + e / a.nb) / a.Sq, a.G - 1);
-      const float t = a.table[(int64_t)hh * a.nb + e % a.nb];
-      dyn[e] = t < 0.f && t >= -FLT_MAX ? fmaxf(t * kL2E, -FLT_MAX) : t * kL2E;
-    }
-    for (int e = tid; e < bias_len(a); e += 256) {
-      const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
-      lut[e] = (uint8_t)(a.lut[rel < 0 ? -rel : rel] + (rel > 0 ? a.half : 0));
-    }
-    __syncthreads();
-  }
+  Span<32> sp = span_of<32>(a, sq.lk, sq.off, sq.off + sq.lq - 1);
+  if (sq.lq == 0) sp.nt = 0;
+  const int per = (sp.nt + a.nsplit - 1) / a.nsplit, n1 = min(sp.nt, (z + 1) * per);
   const bf16_t* K = a.k + b * a.ks[0] + hk * a.ks[2];
   const bf16_t* V = a.v + b * a.vs[0] + hk * a.vs[2];
+  bf16_t* const ring = reinterpret_cast<bf16_t*>(lds) + wv * 4 * 32 * DT;
+  WaveRing<NC> rk, rv;
+  rk.init(a.ks[1], a.d, lane);
+  rv.init(a.vs[1], a.d, lane);
+  auto load = [&](int n, int bf) {
+    const int k0 = sp.key0(n);
+    auto ok = [&](int j) { return sp.row(j); };
+    rk.issue(ring + bf * 64 * DT, K + k0 * a.ks[1], a.ks[1], k0, lane, ok);
+    rv.issue(ring + bf * 64 * DT + 32 * DT, V + k0 * a.vs[1], a.vs[1], k0, lane, ok);
+  };
+  int n = z * per + wv, buf = 0;
+  if (n < n1) load(n, 0);
   const bf16_t* Q = a.q + b * a.qs[0] + i * a.qs[1] + h * a.qs[2];
   bf16x8 qf[KF];
 #pragma unroll
   for (int t = 0; t < KF; ++t) qf[t] = ld_frag(Q, 16 * t + 8 * g, a.d, live);
+  const uint8_t* const lut = reinterpret_cast<const uint8_t*>(dyn);
+  const float* tab = nullptr;      // this row's bias by bucket
+  float cs = a.c, flo = 0.f, fhi = 0.f;
+  if (BIAS) {
+    uint8_t* lw = reinterpret_cast<uint8_t*>(dyn);
+    for (int e = tid; e < bias_len(a); e += 256) {
+      const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
+      lw[e] = (uint8_t)(a.lut[rel < 0 ? -rel : rel] + (rel > 0 ? a.half : 0));
+    }
+    tab = a.table + (int64_t)h * a.nb;
+    if (a.nb <= kStepTable) {
+      float* tw = dyn + (bias_len(a) + 3) / 4;
+      for (int e = tid; e < 32 * a.nb; e += 256)
+        tw[e] = a.table[(int64_t)(hk * a.G + min((rt * 32 + e / a.nb) / a.Sq, a.G - 1)) * a.nb + e % a.nb];
+      tab = tw + lq * a.nb;
+    }
+    __syncthreads();
+    flo = log2_bias(tab[lut[0]]);
+    fhi = log2_bias(tab[lut[bias_len(a) - 1]]);
+  }
   const Row rw = row_of(a, sq.lk, i + sq.off);
   f32x16 acc[NT];
 #pragma unroll
@@ -348,37 +411,33 @@ __global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
   float m2 = -INFINITY, l = 0.f;
-  Span<32> sp = span_of<32>(a, sq.lk, sq.off, sq.off + sq.lq - 1);
-  if (sq.lq == 0) sp.nt = 0;
-  const int per = (sp.nt + a.nsplit - 1) / a.nsplit, n1 = min(sp.nt, (z + 1) * per);
-  for (int n = z * per + wv; n < n1; n += 4) {
-    const int k0 = sp.key0(n), kr = k0 + lq;
-    const bool kok = sp.row(kr);
-    bf16x8 kf[KF];
-    uint4 vv[NC / 2];
-#pragma unroll
-    for (int t = 0; t < KF; ++t) kf[t] = ld_frag(K + kr * a.ks[1], 16 * t + 8 * g, a.d, kok);
-#pragma unroll
-    for (int j = 0; j < NC / 2; ++j) {
-      const int x = lane + 64 * j, r = x / NC, c = x - (x / NC) * NC;
-      vv[j] = make_uint4(0, 0, 0, 0);
-      if (c * 8 < a.d && sp.row(k0 + r)) vv[j] = *reinterpret_cast<const uint4*>(V + (k0 + r) * a.vs[1] + c * 8);
+  for (; n < n1; n += 4, buf ^= 1) {
+    const int k0 = sp.key0(n);
+    const bf16_t* ks = ring + buf * 64 * DT;
+    const bf16_t* vs = ks + 32 * DT;
+    if (n + 4 < n1) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the other buffer has been read
+      load(n + 4, buf ^ 1);
+      wait_loads<2 * WaveRing<NC>::L>();
+    } else {
+      wait_loads<0>();
     }
     f32x16 s;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-    for (int t = 0; t < KF; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t], qf[t], s, 0, 0, 0);
-#pragma unroll
-    for (int j = 0; j < NC / 2; ++j) {
-      const int x = lane + 64 * j, r = x / NC, c = x - (x / NC) * NC;
-      *reinterpret_cast<uint4*>(Vs[wv] + toff<NC>(r, c * 8)) = vv[j];
-    }
+    for (int t = 0; t < KF; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ks, lq, 16 * t + 8 * g), qf[t], s, 0, 0, 0);
+    float cm = cs, off = 0.f;
     if (BIAS) {
+      if (k0 + 31 - sq.off > -a.maxd && k0 - (sq.off + sq.lq - 1) < a.maxd) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int rel = min(max(k0 + acc_row(r, g) - i - sq.off, -a.maxd), a.maxd);
-        s[r] = fmaf(s[r], a.c, dyn[lq * a.nb + lut[rel + a.maxd + kMargin]]);
+        for (int r = 0; r < 16; ++r) {
+          const int rel = min(max(k0 + acc_row(r, g) - i - sq.off, -a.maxd), a.maxd);
+          s[r] = fmaf(s[r], cs, log2_bias(tab[lut[rel + a.maxd + kMargin]]));
+        }
+        cm = 1.f;
+      } else {
+        off = k0 < sq.off ? flo : fhi;
       }
     }
     if (!all_seen<32>(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) {
@@ -388,9 +447,10 @@ __global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
     }
     float mb = s[0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mb = fmaxf(mb, s[r]);
-    mb = fmaxf(mb, __shfl_xor(mb, 32, 64));
-    if (!BIAS) mb *= a.c;
+    for (int r = 1; r < 15; r += 2) mb = max3(mb, s[r], s[r + 1]);
+    mb = max3(mb, mb, s[15]);
+    mb = max3(mb, mb, __shfl_xor(mb, 32, 64));
+    mb = BIAS ? fmaf(mb, cm, off) : mb * cs;
     if (mb > m2 + kTau) {
       const float alpha = exp2_(m2 - mb);
       l *= alpha;
@@ -400,10 +460,10 @@ __global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
         for (int r = 0; r < 16; ++r) acc[j][r] *= alpha;
       m2 = mb;
     }
-    const float ms = m2 == -INFINITY ? 0.f : m2;
+    const float ms = off - (m2 == -INFINITY ? 0.f : m2);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = exp2_(BIAS ? s[r] - ms : fmaf(s[r], a.c, -ms));
+      s[r] = exp2_(fmaf(s[r], BIAS ? cm : cs, ms));
       l += s[r];
     }
 #pragma unroll
@@ -411,9 +471,10 @@ __global__ __launch_bounds__(256, 2) void k_mha_step(MhaArgs a) {
       const bf16x8 pb = pack_regs(s, t);
 #pragma unroll
       for (int j = 0; j < NT; ++j)
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(Vs[wv], t, 32 * j, lane), pb, acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(vs, t, 32 * j, lane), pb, acc[j], 0, 0, 0);
     }
   }
+  float(*const red)[NT * 16 * 64] = reinterpret_cast<float(*)[NT * 16 * 64]>(lds);
   // join the four waves
   l += __shfl_xor(l, 32, 64);
   if (g == 0) { ml[wv][lq][0] = m2; ml[wv][lq][1] = l; }
@@ -478,9 +539,11 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
   if (b >= a.B || rho >= a.G * a.Sq) return;
   const float* slot = a.part + (int64_t)(bh * a.nrt + rt) * a.nsplit * 32 * (DT + 2);
   float M = -INFINITY, L = 0.f;
+#pragma unroll 8
   for (int z = 0; z < a.nsplit; ++z) M = fmaxf(M, slot[(int64_t)z * 32 * (DT + 2) + lr]);
   const float Ms = M == -INFINITY ? 0.f : M;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
   for (int z = 0; z < a.nsplit; ++z) {
     const float* p = slot + (int64_t)z * 32 * (DT + 2);
     const float f = exp2_(p[lr] - Ms);
@@ -548,18 +611,24 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
   const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
   const bf16_t* DO = a.dO + b * a.os[0] + q * a.os[1] + h * a.os[2];
   const bf16_t* O = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
+  const uint2* const lo = a.olo + ((int64_t)bh * (a.Sqp / 32) + qw / 32) * (DT / 8) * 64;
   bf16x8 qf[KF], df[KF];
   float dd = 0.f;
 #pragma unroll
   for (int t = 0; t < KF; ++t) {
     qf[t] = ld_frag(Q, 16 * t + 8 * g, a.d, valid);
     df[t] = ld_frag(DO, 16 * t + 8 * g, a.d, valid);
-    // from the bf16 output: off by at most 2^-8 of sum |do||o|, as much as dS loses when it becomes an operand
-    float x[8], o[8];
+    // from the output and what its rounding took off (without that D is off by 2^-8 of |do||o|, and dq by half as
+    // much again as its own rounding): left is the rounding of P as an operand, averaged over the keys
+    float x[8], o[8], e8[8];
     unpack8(__builtin_bit_cast(uint4, df[t]), x);
     unpack8(__builtin_bit_cast(uint4, ld_frag(O, 16 * t + 8 * g, a.d, valid)), o);
+    const int ji = 4 * (t / 2) + 2 * (t % 2) + g;
+    uint2 e0 = make_uint2(0, 0), e1 = e0;
+    if (valid) { e0 = lo[ji * 64 + lq]; e1 = lo[ji * 64 + 32 + lq]; }
+    unpack8(make_uint4(e0.x, e0.y, e1.x, e1.y), e8);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dd = fmaf(x[e], o[e], dd);
+    for (int e = 0; e < 8; ++e) dd = fmaf(x[e], o[e] + e8[e], dd);
   }
   dd += __shfl_xor(dd, 32, 64);
   if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = valid ? dd : 0.f;
@@ -678,7 +747,7 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
   };
   pass(std::integral_constant<bool, false>());
   if (BIAS) {
-    // dS sums to zero over a row, but with D from the rounded output it sums to
+    // dS sums to zero over a row, but with D from an output of rounded P it sums to
     // rho = (true D) - D, and the bias gradient, many sums of dS with little
     // left over, would show it.  The true dS is dS - rho P: the near tiles are
     // visited again for theirs, the far ones together hold what is left of 1.
@@ -1018,14 +1087,22 @@ MhaArgs make_args(const Mha& m) {
   return a;
 }
 
-bool few_rows(const Mha& m) { return (int64_t)m.Sq * (m.Hq / m.Hk) <= 32; }
+int64_t row_tiles(const Mha& m) { return cdiv((int64_t)m.Sq * (m.Hq / m.Hk), 32); }
+// Which calls without a backward take the form for a few new tokens: those of
+// few queries (the other form leaves three of its four waves idle: 64 x 16
+// queries of 32 / 8 heads x 128 over 1024 keys 93 us against 140; at 32
+// queries 46 against 44) and those whose row tiles leave CUs without work (128
+// queries of 8 heads over 32768 keys 58 us against 846; 512 tiles over 1024
+// keys 35 against 28).
+bool few_rows(const Mha& m) { return m.Sq <= 16 || (int64_t)m.B * m.Hk * row_tiles(m) <= 256; }
 
-// Splits of the keys: enough blocks for three on each CU, at least 8 tiles in each.
+// Splits of the keys: a block for each CU, at least 8 tiles in each (two a
+// wave): the caches are read at 5.1 TB/s then, and three blocks a CU lose 15 %
+// to the partials they leave.
 int step_splits(const Mha& m) {
-  const int64_t tiles = m.window ? std::min<int64_t>(cdiv(m.Sk, 32), cdiv((int64_t)m.window + m.Sq, 32) + 1 + cdiv(m.n_sink, 32))
+  const int64_t tiles = m.window ? std::min<int64_t>(cdiv(m.Sk, 32), cdiv((m.causal ? 1 : 2) * (int64_t)m.window + m.Sq, 32) + 1 + cdiv(m.n_sink, 32))
                                  : cdiv(m.Sk, 32);
-  const int64_t blocks = (int64_t)m.B * m.Hk * cdiv((int64_t)m.Sq * (m.Hq / m.Hk), 32);
-  return (int)std::max<int64_t>(1, std::min(cdiv(768, blocks), cdiv(tiles, 8)));
+  return (int)std::max<int64_t>(1, std::min(256 / (m.B * m.Hk * row_tiles(m)), cdiv(tiles, 8)));
 }
 
 // How the key-owned pass is cut: blocks of 128 keys; a block's steps are
@@ -1073,7 +1150,7 @@ size_t bias_bytes(const Mha& m, int arrays) {
 
 size_t mha_saved_bytes(const Mha& m) {
   const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 64) * 64;
-  return align256(rows * 4);   // the rows' log2 sums
+  return align256(rows * 4) + align256(rows * pad_d(m.d) * 2);   // the rows' log2 sums, the output's remainder
 }
 
 size_t mha_ws_bytes(const Mha& m) {
@@ -1083,7 +1160,7 @@ size_t mha_ws_bytes(const Mha& m) {
   const size_t keys = (size_t)plan_keys(m).slots * 128 * 2 * pad_d(m.d) * 4;
   const size_t bwd = align256(rows * 4) + align256(std::max(bias, keys));
   size_t step = 0;
-  if (few_rows(m)) step = (size_t)m.B * m.Hk * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
+  if (few_rows(m)) step = (size_t)m.B * m.Hk * row_tiles(m) * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
   return std::max<size_t>(std::max(bwd, align256(step)), 256);
 }
 
@@ -1095,22 +1172,23 @@ void mha_fwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   const double flops = 4.0 * m.B * m.Hq * (double)m.Sq * m.Sk * m.d;
   if (!saved && few_rows(m)) {
     a.nsplit = step_splits(m);
-    a.nrt = 1;
+    a.nrt = (int)row_tiles(m);
     a.part = (float*)ws;
-    const dim3 grid((unsigned)((int64_t)m.B * m.Hk * a.nsplit));
-    const size_t dyn = m.n_buckets ? (size_t)32 * m.n_buckets * 4 + align256(2 * (m.max_distance + kMargin) + 1) : 0;
+    const dim3 grid((unsigned)((int64_t)m.B * m.Hk * a.nrt * a.nsplit));
+    const size_t dyn = m.n_buckets ? align256(2 * (m.max_distance + kMargin) + 4) + (m.n_buckets <= kStepTable ? (size_t)128 * m.n_buckets : 0) : 0;
     ProfScope prof(st);
     PG_DT(m.d, {
       if (m.n_buckets) hipLaunchKernelGGL((k_mha_step<DT, true>), grid, dim3(256), dyn, st, a);
       else hipLaunchKernelGGL((k_mha_step<DT, false>), grid, dim3(256), 0, st, a);
       if (a.nsplit > 1)
-        hipLaunchKernelGGL(k_mha_join<DT>, dim3((unsigned)cdiv((int64_t)m.B * m.Hk * 32 * (DT / 4), 256)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(k_mha_join<DT>, dim3((unsigned)cdiv((int64_t)m.B * m.Hk * a.nrt * 32 * (DT / 4), 256)), dim3(256), 0, st, a);
     });
     PG_LAUNCH_CHECK();
     prof.done("k_mha_step<" + std::to_string(pad_d(m.d)) + ">", flops);
     return;
   }
   a.lse = (float*)saved;
+  if (saved) a.olo = (uint2*)((char*)saved + align256((size_t)m.B * m.Hq * a.Sqp * 4));
   a.nblk = (int)cdiv(m.Sq, 128);
   a.hset = head_set((int64_t)m.B * m.Hq, a.G, len_k || len_q);
   const dim3 grid((unsigned)((int64_t)m.B * m.Hq * a.nblk));
@@ -1132,6 +1210,7 @@ void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   a.dO = (const bf16_t*)dO; a.dq = (bf16_t*)dq; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv;
   a.lse = (float*)const_cast<void*>(saved);
   const size_t rows = (size_t)m.B * m.Hq * a.Sqp;
+  a.olo = (uint2*)((char*)const_cast<void*>(saved) + align256(rows * 4));
   a.D = (float*)ws;
   a.part = (float*)((char*)ws + align256(rows * 4));
   ProfScope prof(st);

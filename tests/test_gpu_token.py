@@ -220,7 +220,8 @@ def test_mha_more_queries_than_keys_leaves_empty_rows():
 STEP = [
     (1, 1, 1, 1, 1, 8, 1), (3, 1, 40, 4, 4, 64, 1), (2, 1, 1000, 32, 8, 128, 1), (2, 4, 777, 8, 1, 96, 1),
     (1, 1, 5000, 16, 2, 64, 1, 300, 4, 32, 128), (2, 3, 900, 10, 1, 32, 1, 64, 40), (1, 1, 4000, 8, 8, 128, 0, 0, 0, 16, 512),
-    (2, 2, 650, 16, 1, 64, 1, 0, 0, 256, 512), (1, 32, 333, 1, 1, 40, 1, 7, 1, 8, 16), (1, 16, 100, 2, 1, 128, 0, 5, 3)]
+    (2, 2, 650, 16, 1, 64, 1, 0, 0, 256, 512), (1, 32, 333, 1, 1, 40, 1, 7, 1, 8, 16), (1, 16, 100, 2, 1, 128, 0, 5, 3),
+    (1, 100, 2000, 4, 2, 64, 1), (2, 5, 700, 24, 2, 128, 1, 90, 2, 16, 40), (1, 130, 260, 1, 1, 32, 0, 0, 0, 200, 300)]
 
 
 @pytest.mark.parametrize("case", STEP, ids=[("-".join(map(str, c))) for c in STEP])
