@@ -119,6 +119,20 @@ PG_DEV Row row_of(const MhaArgs& a, int lk, int p) {
   return r;
 }
 PG_DEV bool sees(const Row& r, int j) { return (j >= r.lo && j < r.hi) || j < r.ns; }
+// -infinity for the keys k0 + row of a score tile that the row's query does
+// not see; one unsigned comparison each away from the first tokens
+PG_DEV void hide(f32x16& s, const Row& rw, int k0, int g) {
+  if (k0 < rw.ns) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (!sees(rw, k0 + acc_row(r, g))) s[r] = -INFINITY;
+  } else {
+    const uint32_t at = (uint32_t)(k0 + 4 * g - rw.lo), width = (uint32_t)max(rw.hi - rw.lo, 0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (at + 8 * (r >> 2) + (r & 3) >= width) s[r] = -INFINITY;
+  }
+}
 
 // max of three without the quieting moves that fmaxf asks for (a NaN score gives NaN through its exponential)
 PG_DEV float max3(float a, float b, float c) {
@@ -249,11 +263,8 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
       }
     }
     if (!all_seen<TK>(a, sq.lk, k0, p0, p0 + 31)) {
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!sees(rw, k0 + 32 * x + acc_row(r, g))) s[x][r] = -INFINITY;
+      hide(s[0], rw, k0, g);
+      hide(s[1], rw, k0 + 32, g);
     }
     float mb = s[0][0], mc = s[1][0];   // two chains
 #pragma unroll
@@ -440,11 +451,7 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
         off = k0 < sq.off ? flo : fhi;
       }
     }
-    if (!all_seen<32>(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!sees(rw, k0 + acc_row(r, g))) s[r] = -INFINITY;
-    }
+    if (!all_seen<32>(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) hide(s, rw, k0, g);
     float mb = s[0];
 #pragma unroll
     for (int r = 1; r < 15; r += 2) mb = max3(mb, s[r], s[r + 1]);
@@ -694,11 +701,7 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
         }
-        if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!sees(rw, k0 + acc_row(r, g))) s[r] = -INFINITY;
-        }
+        if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) hide(s, rw, k0, g);
         if constexpr (NEAR) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
@@ -781,14 +784,18 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
       bs[e] = t;
     }
     __syncthreads();
+    // 8 lanes a bucket
     const int mid = a.maxd + kMargin;
-    for (int k = tid; k < a.nb; k += 256) {
+    for (int k = tid >> 3; k < (a.nb + 31) / 32 * 32; k += 32) {
       const bool up = k >= a.half;           // later keys (never with causal)
-      const int kk = up ? k - a.half : k, n0 = a.start[kk], n1 = kk + 1 < a.half ? a.start[kk + 1] : mid + 1;
+      const int kk = min(up ? k - a.half : k, a.half - 1), n0 = a.start[kk], n1 = kk + 1 < a.half ? a.start[kk + 1] : mid + 1;
       float t = 0.f;
-      for (int n = n0; n < n1; ++n)
+      for (int n = n0 + (tid & 7); n < n1; n += 8)
         if (!(up && n == 0)) t += bs[up ? mid + n : mid - n];
-      a.part[((int64_t)bh * a.nblk + qb) * a.nb + k] = t;
+      t += __shfl_xor(t, 1, 64);
+      t += __shfl_xor(t, 2, 64);
+      t += __shfl_xor(t, 4, 64);
+      if ((tid & 7) == 0 && k < a.nb) a.part[((int64_t)bh * a.nblk + qb) * a.nb + k] = t;
     }
   }
 }
@@ -888,10 +895,10 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
     for (int r = 0; r < 16; ++r) { adk[j][r] = 0.f; adv[j][r] = 0.f; }
   int w0, w1;
   seen_by(a, sq, kw, kw + 31, w0, w1);
-  // this lane's key is seen from positions plo .. phi
+  // this lane's key is seen from positions plo .. plo + pspan (none is at 2^31 - 1)
   const bool sink = key < a.n_sink;
   const int plo = !kv ? 0x7fffffff : a.causal ? key : a.window && !sink ? key - a.window + 1 : -0x40000000;
-  const int phi = a.window && !sink ? key + a.window - 1 : 0x7fffffff;
+  const uint32_t pspan = !kv ? 0u : (uint32_t)((a.window && !sink ? key + a.window - 1 : 0x7fffffff) - (int64_t)plo);
   Ring<NC, TQ> rq, rd;
   rq.init(a.qs[1], a.d, tid);
   rd.init(a.os[1], a.d, tid);
@@ -951,11 +958,10 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
         }
       }
       if (!all_seen<32>(a, sq.lk, kw, p0, p0 + 31)) {
+        const uint32_t at = (uint32_t)(p0 + 4 * g - plo);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int pp = p0 + acc_row(r, g);
-          if (pp < plo || pp > phi) s[r] = -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r)
+          if (at + 8 * (r >> 2) + (r & 3) > pspan) s[r] = -INFINITY;
       }
       f32x16 p;
 #pragma unroll
