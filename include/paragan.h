@@ -314,16 +314,17 @@ int paragan_qknorm_bwd(paragan_ctx* ctx, const paragan_qknorm_desc* d,
  * Element (b, s, h, c) of a tensor is at b * stride[0] + s * stride[1]
  * + h * stride[2] + c.  q, k, v may repeat through zero strides in the
  * forward; o, and in the backward q, k and v (whose strides dq, dk and dv
- * share), must not overlap themselves.  dout has o's strides.
+ * share), must not overlap themselves.  dout has o's strides.  A stride
+ * between tokens is below 2^24.  Outputs must not overlap inputs.
  * Softmax statistics and sums are fp32; P and dS are rounded to bf16 as
  * matrix operands. */
 typedef struct {
-  int32_t B, Sq, Sk;               /* sequences, queries and keys of each, >= 1; Sq, Sk <= 2^30;
+  int32_t B, Sq, Sk;               /* sequences, queries and keys of each, >= 1; Sq, Sk <= 2^29;
                                       B * heads * ceil(S / 128) below 2^24 for either */
   int32_t Hq, Hk;                  /* query and key heads, Hq a multiple of Hk */
   int32_t d;                       /* head width, a multiple of 8 up to 128 */
   int32_t causal;                  /* 0 or 1 */
-  int32_t window, n_sink;          /* 0: no window; n_sink counts with a window only; <= 2^30 */
+  int32_t window, n_sink;          /* 0: no window; n_sink counts with a window only; <= 2^29 */
   int32_t n_buckets, max_distance; /* 0: no bias; up to 256 (causal >= 2, otherwise even and >= 4);
                                       max_distance above half of a side's buckets, up to 512 */
   float scale;                     /* > 0, finite */

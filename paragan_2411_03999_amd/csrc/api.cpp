@@ -540,12 +540,12 @@ static bool distinct(const int64_t* stride, int64_t B, int64_t S, int64_t H, int
 
 static Mha make_mha(const paragan_mha_desc* d) {
   if (!d) throw Error{PARAGAN_EINVAL, "mha: desc is NULL"};
-  const int32_t big = 1 << 30;
-  PG_CHECK(d->B >= 1 && d->Sq >= 1 && d->Sk >= 1 && d->Sq <= big && d->Sk <= big, "mha: B, Sq, Sk must be >= 1 and Sq, Sk <= 2^30");
+  const int32_t big = 1 << 29;   // sums of three positions stay in 32 bits
+  PG_CHECK(d->B >= 1 && d->Sq >= 1 && d->Sk >= 1 && d->Sq <= big && d->Sk <= big, "mha: B, Sq, Sk must be >= 1 and Sq, Sk <= 2^29");
   PG_CHECK(d->Hq >= 1 && d->Hk >= 1 && d->Hq % d->Hk == 0, "mha: Hq must be a multiple of Hk >= 1");
   PG_CHECK(d->d >= 8 && d->d <= 128 && d->d % 8 == 0, "mha: d must be a multiple of 8 up to 128");
   PG_CHECK(d->causal == 0 || d->causal == 1, "mha: causal must be 0 or 1");
-  PG_CHECK(d->window >= 0 && d->window <= big && d->n_sink >= 0 && d->n_sink <= big, "mha: window, n_sink must be 0 .. 2^30");
+  PG_CHECK(d->window >= 0 && d->window <= big && d->n_sink >= 0 && d->n_sink <= big, "mha: window, n_sink must be 0 .. 2^29");
   if (d->n_buckets != 0) {
     const int side = d->causal ? d->n_buckets : d->n_buckets / 2;
     PG_CHECK(d->n_buckets > 0 && d->n_buckets <= 256 && side >= 2 && (d->causal || d->n_buckets % 2 == 0),
@@ -564,9 +564,11 @@ static Mha make_mha(const paragan_mha_desc* d) {
   m.scale = d->scale;
   for (int i = 0; i < 3; ++i) {
     m.qs[i] = d->q_stride[i]; m.ks[i] = d->k_stride[i]; m.vs[i] = d->v_stride[i]; m.os[i] = d->o_stride[i];
-    for (int64_t s : {m.qs[i], m.ks[i], m.vs[i], m.os[i]}) {
-      PG_CHECK(s >= 0 && s % 8 == 0, "mha: strides must be >= 0 and multiples of 8");
-      PG_CHECK(s < (1LL << 60) / big, "mha: a stride is too large");
+    const int64_t n[4][3] = {{m.B, m.Sq, m.Hq}, {m.B, m.Sk, m.Hk}, {m.B, m.Sk, m.Hk}, {m.B, m.Sq, m.Hq}};
+    const int64_t st[4] = {m.qs[i], m.ks[i], m.vs[i], m.os[i]};
+    for (int t = 0; t < 4; ++t) {
+      PG_CHECK(st[t] >= 0 && st[t] % 8 == 0, "mha: strides must be >= 0 and multiples of 8");
+      PG_CHECK((__int128)st[t] * (n[t][i] - 1) < ((__int128)1 << 60), "mha: a stride is too large");
     }
   }
   for (int64_t t : {m.qs[1], m.ks[1], m.vs[1], m.os[1]})   // a tile of 64 tokens is addressed in 32 bits

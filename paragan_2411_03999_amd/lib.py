@@ -220,6 +220,23 @@ def _ptr(t):
     return C.c_void_p(t.data_ptr())
 
 
+def _typed(t, dtype, what):
+    """As _ptr, of a contiguous tensor of one type (whose elements the library reads as such)."""
+    if t is None:
+        return None
+    if str(t.dtype) != "torch." + dtype or not t.is_contiguous():
+        raise ParaganError(EINVAL, "%s must be a contiguous %s tensor" % (what, dtype))
+    return C.c_void_p(t.data_ptr())
+
+
+def _f32(t, what):
+    return _typed(t, "float32", what)
+
+
+def _i32(t, what):
+    return _typed(t, "int32", what)
+
+
 class Context:
     """A libparagan context bound to a torch CUDA (HIP) stream."""
 
@@ -392,14 +409,16 @@ def paragan_qknorm_ws_size(desc):
 
 
 def paragan_qknorm_fwd(ctx, desc, q, k, gain_q, gain_k, table, pos, qo, ko):
-    return ctx.check(load().paragan_qknorm_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(gain_q), _ptr(gain_k),
-                                               _ptr(table), _ptr(pos), _ptr(qo), _ptr(ko)))
+    return ctx.check(load().paragan_qknorm_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _f32(gain_q, "gain_q"),
+                                               _f32(gain_k, "gain_k"), _f32(table, "table"), _i32(pos, "pos"), _ptr(qo),
+                                               _ptr(ko)))
 
 
 def paragan_qknorm_bwd(ctx, desc, q, k, gain_q, gain_k, table, pos, dqo, dko, dq, dk, dgain_q, dgain_k, ws):
-    return ctx.check(load().paragan_qknorm_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(gain_q), _ptr(gain_k),
-                                               _ptr(table), _ptr(pos), _ptr(dqo), _ptr(dko), _ptr(dq), _ptr(dk),
-                                               _ptr(dgain_q), _ptr(dgain_k), _ptr(ws)))
+    return ctx.check(load().paragan_qknorm_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _f32(gain_q, "gain_q"),
+                                               _f32(gain_k, "gain_k"), _f32(table, "table"), _i32(pos, "pos"), _ptr(dqo),
+                                               _ptr(dko), _ptr(dq), _ptr(dk), _f32(dgain_q, "dgain_q"),
+                                               _f32(dgain_k, "dgain_k"), _ptr(ws)))
 
 
 def mha_desc(q, k, v, o, *, scale, causal=False, window=0, n_sink=0, n_buckets=0, max_distance=0):
@@ -429,14 +448,14 @@ def paragan_mha_sizes(desc):
 
 def paragan_mha_fwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, ws):
     """saved: None when no backward follows."""
-    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(table),
-                                            _ptr(len_q), _ptr(len_k), _ptr(o), _ptr(saved), _ptr(ws)))
+    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _f32(table, "table"),
+                                            _i32(len_q, "len_q"), _i32(len_k, "len_k"), _ptr(o), _ptr(saved), _ptr(ws)))
 
 
 def paragan_mha_bwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, dout, dq, dk, dv, dtable, ws):
-    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(table),
-                                            _ptr(len_q), _ptr(len_k), _ptr(o), _ptr(saved), _ptr(dout), _ptr(dq),
-                                            _ptr(dk), _ptr(dv), _ptr(dtable), _ptr(ws)))
+    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _f32(table, "table"),
+                                            _i32(len_q, "len_q"), _i32(len_k, "len_k"), _ptr(o), _ptr(saved), _ptr(dout),
+                                            _ptr(dq), _ptr(dk), _ptr(dv), _f32(dtable, "dtable"), _ptr(ws)))
 
 
 def paragan_gout_layout(desc):

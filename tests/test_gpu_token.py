@@ -196,7 +196,8 @@ TRAIN = [
     (1, 1100, 1100, 1, 1, 24, 0, 0, 0, 64, 512), (1, 70, 200, 2, 2, 64, 1), (1, 200, 70, 2, 1, 64, 1),
     (1, 65, 130, 2, 1, 32, 0, 30, 3, 12, 40), (3, 96, 96, 8, 1, 64, 1, 1, 0), (1, 96, 96, 2, 2, 16, 1, 1, 1, 2, 2),
     (1, 513, 513, 2, 2, 128, 0, 0, 0, 32, 128), (1, 600, 600, 1, 1, 128, 1, 100, 200, 16, 50),
-    (1, 2100, 2100, 4, 1, 64, 1, 64, 5), (1, 1500, 1500, 2, 2, 32, 0, 90, 130)]
+    (1, 2100, 2100, 4, 1, 64, 1, 64, 5), (1, 1500, 1500, 2, 2, 32, 0, 90, 130),
+    (1, 100, 100, 1, 1, 32, 1, 10, 1000), (1, 100, 100, 1, 1, 32, 0, 1 << 29, 1 << 29), (1, 200, 200, 2, 1, 32, 1, 1 << 29)]
 
 
 @pytest.mark.parametrize("case", TRAIN, ids=[("-".join(map(str, c))) for c in TRAIN])
@@ -232,6 +233,12 @@ def test_mha_step(case):
     lk = [max(1, Sk - 17 * b - Sk // 3) for b in range(B)]
     lq = [Sq if b % 2 == 0 else max(0, Sq - 1) for b in range(B)]
     mha_case(*case, lq=lq, lk=lk, train=False, seed=6, layout="heads")
+
+
+def test_mha_forward_alone_of_many_rows():
+    """Without a backward to follow, and too many rows for the form of few."""
+    mha_case(20, 40, 40, 8, 8, 32, 1, 0, 0, 8, 20, train=False, seed=13)
+    mha_case(20, 40, 55, 8, 8, 72, 0, 9, 2, lq=[2 * b for b in range(20)], lk=[55 - b for b in range(20)], train=False, seed=14)
 
 
 def test_mha_step_reads_only_what_is_seen():

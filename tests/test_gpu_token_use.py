@@ -1,0 +1,321 @@
+"""The token attention operators as a program uses them: norm, rotation and
+attention together through forward and backward, steps of new tokens over a
+cache, repeated calls, captured graphs, two streams, caches past 32-bit
+offsets, and calls that are refused."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import token as T
+from paragan_2411_03999_amd import lib
+
+from .parity import need_gpu
+from .test_gpu_token import held
+
+pytestmark = pytest.mark.gpu
+
+EPS = 1e-6
+
+
+class Block:
+    """Norm and rotation of q and k out of one projection buffer, then attention; forward and backward."""
+
+    def __init__(self, torch, ctx, B, S, Hq, Hk, d, gen, causal=1, window=40, sink=3, nb=16, maxd=64, ragged=True):
+        self.t, self.ctx, self.dims = torch, ctx, (B, S, Hq, Hk, d)
+        rn = lambda *s: torch.randn(s, generator=gen)  # noqa: E731
+        self.qkv = rn(B, S, Hq + 2 * Hk, d).bfloat16().cuda()
+        self.dout = rn(B, S, Hq, d).bfloat16().cuda()
+        self.gain = (1 + 0.1 * rn(2, d)).cuda()
+        self.table = (0.5 * rn(Hq, nb)).cuda()
+        ang = torch.arange(S, dtype=torch.float64)[:, None] / 10000 ** (torch.arange(d // 2) / (d // 2))
+        self.turn = torch.stack([ang.cos(), ang.sin()], -1).float().cuda()
+        self.lens = [S - 7 * b for b in range(B)] if ragged else [S] * B
+        self.len = torch.tensor(self.lens, dtype=torch.int32, device="cuda")
+        self.attn = dict(scale=1 / math.sqrt(d), causal=causal, window=window, n_sink=sink, n_buckets=nb, max_distance=maxd)
+        e = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+        self.nq, self.nk, self.o = e(B, S, Hq, d), e(B, S, Hk, d), e(B, S, Hq, d)
+        self.dnq, self.dnk, self.dqkv = e(B, S, Hq, d), e(B, S, Hk, d), e(B, S, Hq + 2 * Hk, d)
+        self.dgain, self.dtable = e(2, d, dt=torch.float32), e(Hq, nb, dt=torch.float32)
+        tok = lambda t: t.flatten(0, 1)  # noqa: E731
+        f = self.qkv.view(B * S, Hq + 2 * Hk, d)
+        self.q, self.k, self.v = f[:, :Hq], f[:, Hq:Hq + Hk], self.qkv[:, :, Hq + Hk:]
+        g = self.dqkv.view(B * S, Hq + 2 * Hk, d)
+        self.dq, self.dk, self.dv = g[:, :Hq], g[:, Hq:Hq + Hk], self.dqkv[:, :, Hq + Hk:]
+        self.qd = lib.qknorm_desc(self.q, self.k, tok(self.nq), tok(self.nk), rot=d, interleaved=0, n_pos=S, eps=EPS)
+        self.md = lib.mha_desc(self.nq, self.nk, self.v, self.o, **self.attn)
+        # dk of the attention goes to a buffer of nk's layout, dv straight into the projection's gradient
+        sb, wb = lib.paragan_mha_sizes(self.md)
+        self.saved, self.ws = lib.workspace(sb), lib.workspace(max(wb, lib.paragan_qknorm_ws_size(self.qd)))
+
+    def run(self):
+        lib.paragan_qknorm_fwd(self.ctx, self.qd, self.q, self.k, self.gain[0], self.gain[1], self.turn, None, self.nq, self.nk)
+        lib.paragan_mha_fwd(self.ctx, self.md, self.nq, self.nk, self.v, self.table, self.len, self.len, self.o, self.saved, self.ws)
+        lib.paragan_mha_bwd(self.ctx, self.md, self.nq, self.nk, self.v, self.table, self.len, self.len, self.o, self.saved,
+                            self.dout, self.dnq, self.dnk, self.dv, self.dtable, self.ws)
+        lib.paragan_qknorm_bwd(self.ctx, self.qd, self.q, self.k, self.gain[0], self.gain[1], self.turn, None, self.dnq,
+                               self.dnk, self.dq, self.dk, self.dgain[0], self.dgain[1], self.ws)
+
+    def outs(self):
+        return [t.clone() for t in (self.o, self.dqkv, self.dgain, self.dtable)]
+
+
+def test_block_against_the_definitions():
+    """norm -> attention -> backward of both, each step held to the float64 definition of the same bf16 inputs, and the
+    whole to the chain of definitions within the sum of the steps' errors (relative 2-norm)."""
+    torch = need_gpu()
+    B, S, Hq, Hk, d = 2, 150, 4, 2, 64
+    blk = Block(torch, lib.Context(), B, S, Hq, Hk, d, torch.Generator().manual_seed(1))
+    blk.run()
+    torch.cuda.synchronize()
+    n = lambda t: t.detach().double().cpu().numpy()  # noqa: E731
+    a = blk.attn
+    kw = dict(causal=True, window=a["window"], n_sink=a["n_sink"], table=n(blk.table), max_distance=a["max_distance"],
+              len_q=blk.lens, len_k=blk.lens)
+    r = T.mha(n(blk.nq), n(blk.nk), n(blk.v), float(np.float32(a["scale"])), dout=n(blk.dout), **kw)
+    for name, got in (("o", blk.o), ("dq", blk.dnq), ("dk", blk.dnk), ("dv", blk.dv), ("dtable", blk.dtable)):
+        held(name, got, r[name], r["tol." + name] + 1e-30)
+    # the chain from the projections on, nothing rounded in between
+    pos = np.tile(np.arange(S), B)
+    qkv, turn, gain = n(blk.qkv).reshape(B * S, Hq + 2 * Hk, d), n(blk.turn), n(blk.gain)
+    q, k = qkv[:, :Hq], qkv[:, Hq:Hq + Hk]
+    nq, nk = (T.qknorm_fwd(x, gain[i], turn, pos, d, False, EPS) for i, x in enumerate((q, k)))
+    r = T.mha(nq.reshape(B, S, Hq, d), nk.reshape(B, S, Hk, d), n(blk.v), a["scale"], dout=n(blk.dout), **kw)
+    dq, gq = T.qknorm_bwd(q, gain[0], turn, pos, d, False, EPS, r["dq"].reshape(B * S, Hq, d))
+    dk, gk = T.qknorm_bwd(k, gain[1], turn, pos, d, False, EPS, r["dk"].reshape(B * S, Hk, d))
+    rel = lambda g, w: np.linalg.norm(n(g).reshape(w.shape) - w) / np.linalg.norm(w)  # noqa: E731
+    # half steps of bf16 in a row: q, k, o, P, dS, the attention's gradients, the outputs, and what a rounded q or k
+    # moves a score by (|s| stays below 8 here, so e^s moves by at most 8 half steps twice): 22 of 2^-8
+    errs = dict(o=rel(blk.o, r["o"]), dq=rel(blk.dq, dq), dk=rel(blk.dk, dk), dv=rel(blk.dv, r["dv"]), gq=rel(blk.dgain[0], gq),
+                gk=rel(blk.dgain[1], gk), dtable=rel(blk.dtable, r["dtable"]))
+    print("  chain", {k2: "%.2e" % v for k2, v in errs.items()}, flush=True)
+    assert max(errs.values()) < 22 * 2.0 ** -8
+
+
+def test_steps_over_a_cache_follow_the_whole_sequence():
+    """Prefill, then one token at a time: norm straight into the cache, attention over it; each new output is the row
+    that one call over the whole sequence gives."""
+    torch = need_gpu()
+    B, S, Hq, Hk, d, first = 3, 70, 8, 2, 64, 61
+    gen = torch.Generator().manual_seed(2)
+    qkv = torch.randn(B, S, Hq + 2 * Hk, d, generator=gen).bfloat16().cuda()
+    gain = torch.ones(d, device="cuda")
+    ang = torch.rand(S, d // 2, generator=gen, dtype=torch.float64)
+    turn = torch.stack([ang.cos(), ang.sin()], -1).float().cuda()
+    table = torch.randn(Hq, 8, generator=gen).cuda()
+    ctx = lib.Context()
+    kw = dict(scale=0.125, causal=1, window=30, n_sink=2, n_buckets=8, max_distance=20)
+
+    def norm(t0, t1, qo, ko):
+        x = qkv[:, t0:t1].reshape(B * (t1 - t0), Hq + 2 * Hk, d)
+        ds = lib.qknorm_desc(x[:, :Hq], x[:, Hq:Hq + Hk], qo.flatten(0, 1) if qo.shape[1] > 1 else qo[:, 0],
+                             ko.flatten(0, 1) if ko.shape[1] > 1 else ko[:, 0], rot=d, interleaved=1, n_pos=S, eps=EPS)
+        pos = torch.arange(t0, t1, dtype=torch.int32, device="cuda").repeat(B)
+        lib.paragan_qknorm_fwd(ctx, ds, x[:, :Hq], x[:, Hq:Hq + Hk], gain, gain, turn, pos, qo, ko)
+
+    def attend(q, k, v, lens=None):
+        o = torch.empty_like(q)
+        ds = lib.mha_desc(q, k, v, o, **kw)
+        lib.paragan_mha_fwd(ctx, ds, q, k, v, table, None, lens, o, None, lib.workspace(lib.paragan_mha_sizes(ds)[1]))
+        return o
+    nq, nk = torch.empty(B, S, Hq, d, dtype=torch.bfloat16, device="cuda"), torch.empty(B, S, Hk, d, dtype=torch.bfloat16, device="cuda")
+    norm(0, S, nq, nk)
+    whole = attend(nq, nk, qkv[:, :, Hq + Hk:])
+    cache = torch.full((2, B, S + 5, Hk, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    cache[0, :, :first], cache[1, :, :first] = nk[:, :first], qkv[:, :first, Hq + Hk:]
+    for t in range(first, S):
+        q1 = torch.empty(B, 1, Hq, d, dtype=torch.bfloat16, device="cuda")
+        norm(t, t + 1, q1, cache[0, :, t:t + 1])
+        cache[1, :, t] = qkv[:, t, Hq + Hk:]
+        assert torch.equal(cache[0, :, t], nk[:, t]) and torch.equal(q1[:, 0], nq[:, t])
+        lens = torch.full((B,), t + 1, dtype=torch.int32, device="cuda")
+        o = attend(q1, cache[0], cache[1], lens)
+        want = T.mha(nq[:, :t + 1].double().cpu().numpy(), nk[:, :t + 1].double().cpu().numpy(),
+                     qkv[:, :t + 1, Hq + Hk:].double().cpu().numpy(), 0.125, True, 30, 2, table.double().cpu().numpy(), 20)
+        held("token %d" % t, o[:, 0], want["o"][:, t], want["tol.o"][:, t])
+        held("whole %d" % t, whole[:, t], want["o"][:, t], want["tol.o"][:, t])
+
+
+def test_the_same_call_gives_the_same_bits():
+    torch = need_gpu()
+    blk = Block(torch, lib.Context(), 2, 700, 4, 1, 128, torch.Generator().manual_seed(3), window=64, sink=5)
+    blk.run()
+    first = blk.outs()
+    for _ in range(3):
+        blk.ws.fill_(255)
+        blk.run()
+        assert all(torch.equal(a, b) for a, b in zip(first, blk.outs()))
+
+
+def test_captured_and_replayed():
+    """Two captured passes that share a workspace, replayed in turn with eager work between and new inputs."""
+    torch = need_gpu()
+    side = torch.cuda.Stream()
+    ctx = lib.Context(side)
+    gen = torch.Generator().manual_seed(4)
+    blks = [Block(torch, ctx, 2, 130, 4, 2, 64, gen), Block(torch, ctx, 1, 300, 4, 4, 32, gen, window=0, sink=0, causal=0)]
+    ws = max((b.ws for b in blks), key=lambda t: t.numel())
+    graphs = []
+    for b in blks:
+        b.ws = ws
+        with torch.cuda.stream(side):
+            b.run()                       # once before, as any program does
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            b.run()
+        graphs.append(g)
+    for rep in range(3):
+        for b, g in zip(blks, graphs):
+            b.qkv.copy_(torch.randn(b.qkv.shape, generator=gen).bfloat16())
+            b.dout.copy_(torch.randn(b.dout.shape, generator=gen).bfloat16())
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                b.run()
+            torch.cuda.synchronize()
+            want = b.outs()
+            for t in (b.o, b.dqkv, b.dgain, b.dtable):
+                t.fill_(9.0)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for x, y in zip(want, b.outs())), rep
+
+
+def test_step_captured_with_growing_lengths():
+    torch = need_gpu()
+    side = torch.cuda.Stream()
+    ctx = lib.Context(side)
+    q, k, v = (torch.randn(2, s, h, 64, device="cuda").bfloat16() for s, h in ((1, 8), (3000, 2), (3000, 2)))
+    o, lens = torch.empty_like(q), torch.tensor([5, 900], dtype=torch.int32, device="cuda")
+    d = lib.mha_desc(q, k, v, o, scale=0.125, causal=1)
+    ws = lib.workspace(lib.paragan_mha_sizes(d)[1])
+    call = lambda: lib.paragan_mha_fwd(ctx, d, q, k, v, None, None, lens, o, None, ws)  # noqa: E731
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        call()
+    for step in range(4):
+        lens.copy_(torch.tensor([5 + 700 * step, 900 + step]))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.synchronize()
+        want = o.clone()
+        o.fill_(9.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
+
+
+def test_two_streams_at_once():
+    torch = need_gpu()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    blks = [Block(torch, lib.Context(s), 2, 400, 4, 2, 64, torch.Generator().manual_seed(5 + i)) for i, s in enumerate(streams)]
+    torch.cuda.synchronize()
+    want = []
+    for b, s in zip(blks, streams):
+        with torch.cuda.stream(s):
+            b.run()
+        torch.cuda.synchronize()
+        want.append(b.outs())
+    for b in blks:
+        b.ws.fill_(255)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b in blks:
+            b.run()
+    torch.cuda.synchronize()
+    for b, w in zip(blks, want):
+        assert all(torch.equal(x, y) for x, y in zip(w, b.outs()))
+
+
+def test_offsets_past_32_bits():
+    """Tokens 32 MB apart and sequences over 4 GB apart, forward, step and backward."""
+    torch = need_gpu()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB")
+    S, ts = 150, (1 << 24) - 8
+    gen = torch.Generator().manual_seed(6)
+    k, v = (torch.randn(2, S, 1, 64, generator=gen).bfloat16() for _ in range(2))
+    big = torch.zeros(2 * S * ts, dtype=torch.bfloat16, device="cuda")      # 10 GB: k and v side by side
+    grad = torch.zeros_like(big)
+    view = lambda b, off: b.as_strided((2, S, 1, 64), (S * ts, ts, 64, 1), off)  # noqa: E731
+    K, V = view(big, 0), view(big, 64)
+    K.copy_(k), V.copy_(v)
+    n = lambda t: t.double().cpu().numpy()  # noqa: E731
+    for Sq in (1, S):
+        print("far offsets, Sq", Sq, flush=True)
+        q, do = (torch.randn(2, Sq, 2, 64, generator=gen).bfloat16() for _ in range(2))
+        Q, DO, O = q.cuda(), do.cuda(), torch.empty(2, Sq, 2, 64, dtype=torch.bfloat16, device="cuda")
+        want = T.mha(n(q), n(k), n(v), 0.125, True, dout=n(do))
+        d = lib.mha_desc(Q, K, V, O, scale=0.125, causal=1)
+        sb, wb = lib.paragan_mha_sizes(d)
+        ws, saved = lib.workspace(wb), lib.workspace(sb)
+        for sv in (None, saved):
+            O.zero_()
+            lib.paragan_mha_fwd(lib.Context(), d, Q, K, V, None, None, None, O, sv, ws)
+            held("o", O, want["o"], want["tol.o"])
+        DQ, DK, DV = torch.empty_like(Q), view(grad, 0), view(grad, 64)
+        lib.paragan_mha_bwd(lib.Context(), d, Q, K, V, None, None, None, O, saved, DO, DQ, DK, DV, None, ws)
+        for name, t in (("dq", DQ), ("dk", DK), ("dv", DV)):
+            held(name, t.contiguous(), want[name], want["tol." + name] + 1e-30)
+
+
+def test_broadcast_keys_forward_only():
+    """One cache for all sequences (batch stride zero): read by the forward, refused by the backward."""
+    torch = need_gpu()
+    gen = torch.Generator().manual_seed(7)
+    q, k, v = (torch.randn(b, s, h, 32, generator=gen).bfloat16() for b, s, h in ((3, 40, 4), (1, 90, 1), (1, 90, 1)))
+    K, V = (t.cuda().expand(3, 90, 4, 32)[:, :, :1] for t in (k, v))
+    Q = q.cuda()
+    O = torch.empty_like(Q)
+    d = lib.mha_desc(Q, K, V, O, scale=0.2, causal=1)
+    assert d.k_stride[0] == 0
+    ctx = lib.Context()
+    sb, wb = lib.paragan_mha_sizes(d)
+    saved, ws = lib.workspace(sb), lib.workspace(wb)
+    n = lambda t: t.double().numpy()  # noqa: E731
+    want = T.mha(n(q), n(k.expand(3, 90, 1, 32)), n(v.expand(3, 90, 1, 32)), float(np.float32(0.2)), True)
+    lib.paragan_mha_fwd(ctx, d, Q, K, V, None, None, None, O, saved, ws)
+    held("o", O, want["o"], want["tol.o"])
+    with pytest.raises(lib.ParaganError, match="overlaps itself"):
+        lib.paragan_mha_bwd(ctx, d, Q, K, V, None, None, None, O, saved, O, Q, K, V, None, ws)
+
+
+def test_refused_calls_touch_nothing():
+    torch = need_gpu()
+    ctx = lib.Context()
+    z = lambda *s, dt=torch.bfloat16: torch.full(s, 3.0, dtype=dt, device="cuda")  # noqa: E731
+    q, k, v, o = z(1, 8, 2, 32), z(1, 8, 2, 32), z(1, 8, 2, 32), z(1, 8, 2, 32)
+    d = lib.mha_desc(q, k, v, o, scale=0.1, n_buckets=4, max_distance=8)
+    sb, wb = lib.paragan_mha_sizes(d)
+    ws, saved, tab, i32 = lib.workspace(wb), lib.workspace(sb), z(2, 4, dt=torch.float32), torch.zeros(1, dtype=torch.int32, device="cuda")
+    odd = z(1 * 8 * 2 * 32 + 8).view(-1)[1:]
+    fwd = [q, k, v, tab, None, None, o, saved, ws]
+    for i, bad in ((0, None), (1, None), (2, odd), (3, None), (6, odd), (8, None), (8, ws[1:]), (7, saved[16:]),
+                   (3, tab.double()), (4, i32.long()), (5, i32.float()), (3, z(2, 8, dt=torch.float32)[:, :4])):
+        args = list(fwd)
+        args[i] = bad
+        with pytest.raises(lib.ParaganError):
+            lib.paragan_mha_fwd(ctx, d, *args)
+    bwd = [q, k, v, tab, None, None, o, saved, o, z(1, 8, 2, 32), z(1, 8, 2, 32), z(1, 8, 2, 32), z(2, 4, dt=torch.float32), ws]
+    for i, bad in ((7, None), (8, None), (9, odd), (10, None), (11, None), (12, None), (13, None), (13, ws[8:])):
+        args = list(bwd)
+        args[i] = bad
+        with pytest.raises(lib.ParaganError):
+            lib.paragan_mha_bwd(ctx, d, *args)
+    x, g = z(5, 2, 32), z(32, dt=torch.float32)
+    t, pos = z(4, 16, 2, dt=torch.float32), torch.zeros(5, dtype=torch.int32, device="cuda")
+    nd = lib.qknorm_desc(x, x, rot=32, interleaved=0, n_pos=4, eps=1e-6)
+    nf = [x, x, g, g, t, pos, z(5, 2, 32), z(5, 2, 32)]
+    for i, bad in ((0, None), (2, None), (4, None), (6, odd), (5, pos.long()), (3, g.half())):
+        args = list(nf)
+        args[i] = bad
+        with pytest.raises(lib.ParaganError):
+            lib.paragan_qknorm_fwd(ctx, nd, *args)
+    torch.cuda.synchronize()
+    assert bool((o == 3.0).all()) and all(bool((y == 3.0).all()) for y in bwd[9:13] + nf[6:])

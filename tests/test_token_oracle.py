@@ -141,9 +141,9 @@ def s3(*v):
 def test_mha_refusals(L):
     assert lib.paragan_mha_check(mh()) == lib.OK
     ok = [dict(window=0), dict(n_buckets=0, max_distance=0), dict(causal=0), dict(d=8), dict(n_buckets=256, max_distance=512),
-          dict(k_stride=s3(0, 128, 64)), dict(q_stride=s3(0, 0, 0)),            # broadcast inputs of a forward
+          dict(k_stride=s3(0, 128, 64)), dict(k_stride=s3(1 << 32, (1 << 24) - 8, 64)), dict(window=1 << 29, n_sink=1 << 29), dict(q_stride=s3(0, 0, 0)),            # broadcast inputs of a forward
           dict(o_stride=s3(64 * 100 * 8, 64, 6400)), dict(n_buckets=2, max_distance=2),
-          dict(B=1, Hq=2, Hk=1, Sk=1 << 30, Sq=1, k_stride=s3(0, 64, 64), o_stride=s3(0, 0, 64))]
+          dict(B=1, Hq=2, Hk=1, Sk=1 << 29, Sq=1, k_stride=s3(0, 64, 64), o_stride=s3(0, 0, 64))]
     for g in ok:
         assert lib.paragan_mha_check(mh(**g)) == lib.OK, (g, L.paragan_last_error(None))
     bad = [dict(B=0), dict(Sq=0), dict(Sk=0), dict(Hq=0), dict(Hk=0), dict(Hk=3), dict(d=0), dict(d=4), dict(d=136),
@@ -151,8 +151,8 @@ def test_mha_refusals(L):
            dict(causal=0, n_buckets=2), dict(causal=0, n_buckets=33), dict(max_distance=513), dict(max_distance=16),
            dict(max_distance=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
            dict(q_stride=s3(51200, 512, 60)), dict(k_stride=s3(-128, 128, 64)), dict(v_stride=s3(1 << 62, 128, 64)),
-           dict(o_stride=s3(0, 512, 64)), dict(o_stride=s3(51200, 512, 56)), dict(Sq=(1 << 30) + 8), dict(B=1 << 30),
-           dict(Sq=1 << 30, Sk=1 << 30)]
+           dict(o_stride=s3(0, 512, 64)), dict(o_stride=s3(51200, 512, 56)), dict(Sq=(1 << 29) + 8), dict(window=(1 << 29) + 1), dict(n_sink=(1 << 29) + 1), dict(k_stride=s3(1 << 32, 1 << 24, 64)), dict(B=1 << 30),
+           dict(Sq=1 << 29, Sk=1 << 29)]
     for b in bad:
         assert lib.paragan_mha_check(mh(**b)) == lib.EINVAL, b
         assert b"mha" in L.paragan_last_error(None)
