@@ -81,6 +81,7 @@ struct Span {
   PG_DEV int key0(int n) const { return TK * (n < st ? n : n - st + ws); }
   PG_DEV bool row(int j) const { return (j >= lo && j < hi) || j < ns; }
   PG_DEV bool tile(int k0) const { return (k0 + TK > lo && k0 < hi) || k0 < ns; }
+  PG_DEV bool whole(int k0) const { return (k0 >= lo && k0 + TK <= hi) || k0 + TK <= ns; }
 };
 template <int TK>
 PG_DEV Span<TK> span_of(const MhaArgs& a, int lk, int p0, int p1) {
@@ -170,14 +171,20 @@ struct Ring {
       off[j] = c * 8 < d ? (uint32_t)(r * (int)ld * 2 + c * 16) : kOOB;
     }
   }
-  // base: row 0 of the tile (uniform); rows r0 + r
+  // base: row 0 of the tile (uniform); rows r0 + r, `all` of which are wanted or those that `ok` says
   template <class F>
-  PG_DEV void issue(bf16_t* tile, const bf16_t* base, int64_t ld, int r0, int wave, F ok) const {
+  PG_DEV void issue(bf16_t* tile, const bf16_t* base, int64_t ld, int r0, int wave, bool all, F ok) const {
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, ((ROWS - 1) * ld + NC * 8) * 2);
     const uint32_t dst = lds_addr(tile) + wave * 1024;
+    if (all) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (4 * j + 3 < L || 4 * j + wave < L) lds_load16(dst + j * 4096, ok(r0 + row[j]) ? off[j] : kOOB, 0, rs);
+      for (int j = 0; j < N; ++j)
+        if (4 * j + 3 < L || 4 * j + wave < L) lds_load16(dst + j * 4096, off[j], 0, rs);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (4 * j + 3 < L || 4 * j + wave < L) lds_load16(dst + j * 4096, ok(r0 + row[j]) ? off[j] : kOOB, 0, rs);
+    }
   }
 };
 
@@ -229,15 +236,17 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
   auto load = [&](int n, int bf) {
     const int k0 = sp.key0(n);
     auto ok = [&](int j) { return sp.row(j); };
-    rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, ok);
-    rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, ok);
+    const bool all = sp.whole(k0);
+    rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, all, ok);
+    rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, all, ok);
   };
-  if (sp.nt > 0) load(0, 0);
-  for (int n = 0; n < sp.nt; ++n) {
+  // the buffer is known at compile time, so that LDS addresses need no arithmetic
+  auto visit = [&](auto buf_c, int n) {
+    constexpr int buf = decltype(buf_c)::value;
     wait_barrier<0>();   // tile n is in LDS, and every wave has left tile n - 1
-    const int buf = n & 1, k0 = sp.key0(n);
+    const int k0 = sp.key0(n);
     if (n + 1 < sp.nt) load(n + 1, buf ^ 1);
-    if (!mine || !sw.tile(k0)) continue;
+    if (!mine || !sw.tile(k0)) return;
     const bf16_t* ks = Ks[buf];
     const bf16_t* vs = Vs[buf];
     f32x16 s[2];
@@ -301,6 +310,11 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
       for (int j = 0; j < NT; ++j)
         acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(vs + 32 * DT * (t >> 1), t & 1, 32 * j, lane), pb, acc[j], 0, 0, 0);
     }
+  };
+  if (sp.nt > 0) load(0, 0);
+  for (int n = 0; n < sp.nt; n += 2) {
+    visit(std::integral_constant<int, 0>(), n);
+    if (n + 1 < sp.nt) visit(std::integral_constant<int, 1>(), n + 1);
   }
   const float lt = l + __shfl_xor(l, 32, 64);
   const bool any = q < sq.lq && lt > 0.f;
@@ -596,7 +610,7 @@ PG_DEV void diag_add(float* arr, const f32x16& v, int lane) {
 }
 
 template <int DT, bool BIAS>
-__global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
+__global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][TK * DT];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][TK * DT];
@@ -659,8 +673,9 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
   auto load = [&](int n, int bf) {
     const int k0 = sp.key0(n);
     auto ok = [&](int j) { return sp.row(j); };
-    rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, ok);
-    rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, ok);
+    const bool all = sp.whole(k0);
+    rk.issue(Ks[bf], K + k0 * a.ks[1], a.ks[1], k0, wv, all, ok);
+    rv.issue(Vs[bf], V + k0 * a.vs[1], a.vs[1], k0, wv, all, ok);
   };
   // One pass over the keys.  NEAR (after the other, with a bias): see below.
   auto pass = [&](auto near_c) {
@@ -671,13 +686,13 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
         while (n < sp.nt && !(sp.key0(n) + TK - 1 - pb0 > -a.maxd && sp.key0(n) - pb1 < a.maxd)) ++n;
       return n;
     };
-    int n = next(0), buf = 0;
-    if (n < sp.nt) load(n, 0);
-    while (n < sp.nt) {
+    // visits tile n, returns the one after it (the buffer known at compile time, as in the forward)
+    auto visit = [&](auto buf_c, int n) {
+      constexpr int buf = decltype(buf_c)::value;
       wait_barrier<0>();   // tile n is in LDS, and every wave has left the tile before
       const int n1 = next(n + 1);
       if (n1 < sp.nt) load(n1, buf ^ 1);
-#pragma unroll 1
+#pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int k0 = sp.key0(n) + 32 * x;
         const bool near = BIAS && k0 + 31 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd;
@@ -743,8 +758,13 @@ __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_dq(MhaArgs a) {
             acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(ks, t2, 32 * j, lane), sb, acc[j], 0, 0, 0);
         }
       }
-      n = n1;
-      buf ^= 1;
+      return n1;
+    };
+    int n = next(0);
+    if (n < sp.nt) load(n, 0);
+    while (n < sp.nt) {
+      n = visit(std::integral_constant<int, 0>(), n);
+      if (n < sp.nt) n = visit(std::integral_constant<int, 1>(), n);
     }
     __syncthreads();   // the tiles are free and the sums whole
   };
@@ -908,29 +928,41 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
 #pragma unroll
     for (int x = 0; x < 2; ++x)
       rv.issue(Vt + 64 * DT * x, a.v + b * a.vs[0] + (kblk + 64 * x) * a.vs[1] + hk * a.vs[2], a.vs[1], kblk + 64 * x, wv,
-               [&](int j) { return j < sq.lk; });
+               false, [&](int j) { return j < sq.lk; });
   }
-  auto load = [&](int n, int bf) {
-    const int h = hk * a.G + n / nt, q0 = TQ * (t0 + n % nt);
+  // step (h, ti): query head of the group, query tile
+  auto load = [&](int hg, int ti, int bf) {
+    const int h = hk * a.G + hg, q0 = TQ * (t0 + ti);
     auto ok = [&](int i) { return i >= i0 && i < i1; };
-    rq.issue(Qs[bf], a.q + b * a.qs[0] + h * a.qs[2] + q0 * a.qs[1], a.qs[1], q0, wv, ok);
-    rd.issue(Ds[bf], a.dO + b * a.os[0] + h * a.os[2] + q0 * a.os[1], a.os[1], q0, wv, ok);
+    const bool all = q0 >= i0 && q0 + TQ <= i1;
+    rq.issue(Qs[bf], a.q + b * a.qs[0] + h * a.qs[2] + q0 * a.qs[1], a.qs[1], q0, wv, all, ok);
+    rd.issue(Ds[bf], a.dO + b * a.os[0] + h * a.os[2] + q0 * a.os[1], a.os[1], q0, wv, all, ok);
     // TQ rows of both: the buffers are padded to 64, rows past len_q hold +inf and 0
     const int64_t x = ((int64_t)b * a.Hq + h) * a.Sqp + q0;
     if (wv == 0) lds_load4(lds_addr(ex + bf * 128), lane * 4, make_rsrc(a.lse + x, TQ * 4));
     if (wv == 1) lds_load4(lds_addr(ex + bf * 128 + 64), lane * 4, make_rsrc(a.D + x, TQ * 4));
   };
-  if (n0 < n1) load(n0, 0);
-  for (int n = n0; n < n1; ++n) {
+  int hg = 0, ti = 0;
+  if (n0 < n1) {
+    hg = n0 / nt;
+    ti = n0 - hg * nt;
+    load(hg, ti, 0);
+  }
+  auto visit = [&](auto buf_c, int n) {
+    const int buf = buf_c;
     wait_barrier<0>();   // tile n is in LDS, and every wave has left tile n - 1
-    const int buf = (n - n0) & 1;
-    if (n + 1 < n1) load(n + 1, buf ^ 1);
-    if (BIAS && (n == n0 || n % nt == 0)) {   // the next head's bias
-      for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, hk * a.G + n / nt, bl - 1 - e);
+    const int h = hg, qt = TQ * (t0 + ti), pt = qt + sq.off;
+    const bool fresh = n == n0 || ti == 0;
+    if (++ti == nt) {
+      ti = 0;
+      ++hg;
+    }
+    if (n + 1 < n1) load(hg, ti, buf ^ 1);
+    if (BIAS && fresh) {   // the next head's bias
+      for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, hk * a.G + h, bl - 1 - e);
       __syncthreads();
     }
-    const int qt = TQ * (t0 + n % nt), pt = qt + sq.off;
-#pragma unroll 1
+#pragma unroll
     for (int x = 0; x < TQ / 32; ++x) {
       const int q0 = qt + 32 * x, p0 = pt + 32 * x;
       if (q0 + 32 <= w0 || q0 >= w1) continue;
@@ -985,6 +1017,14 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
           adk[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_tr<NC>(qs, t, 32 * j, lane), sb, adk[j], 0, 0, 0);
         }
       }
+    }
+  };
+  if constexpr (VL) {   // no registers to spare for two copies of the loop
+    for (int n = n0; n < n1; ++n) visit((n - n0) & 1, n);
+  } else {
+    for (int n = n0; n < n1; n += 2) {
+      visit(std::integral_constant<int, 0>(), n);
+      if (n + 1 < n1) visit(std::integral_constant<int, 1>(), n + 1);
     }
   }
   if (nt * a.G > a.chunk) {   // one of several splits: partials, key rows of dk then of dv
