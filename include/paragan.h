@@ -327,7 +327,7 @@ typedef struct {
   int32_t window, n_sink;          /* 0: no window; n_sink counts with a window only; <= 2^29 */
   int32_t n_buckets, max_distance; /* 0: no bias; up to 256 (causal >= 2, otherwise even and >= 4);
                                       max_distance above half of a side's buckets, up to 512 */
-  float scale;                     /* > 0, finite */
+  float scale;                     /* 1e-30 .. 1e30 */
   int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
 } paragan_mha_desc;
 

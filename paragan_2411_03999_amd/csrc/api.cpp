@@ -553,7 +553,7 @@ static Mha make_mha(const paragan_mha_desc* d) {
     PG_CHECK(d->max_distance > side / 2 && d->max_distance <= kMhaMaxDist,
              "mha: max_distance must be above half of a side's buckets and at most 512");
   }
-  PG_CHECK(d->scale > 0.f && std::isfinite(d->scale), "mha: scale must be > 0 and finite");
+  PG_CHECK(d->scale >= 1e-30f && d->scale <= 1e30f, "mha: scale must be 1e-30 .. 1e30");
   // a launch has fewer than 2^32 threads: blocks of 256 threads, at least 128 rows of one head in each
   PG_CHECK((int64_t)d->B * d->Hq < (1 << 24) && (int64_t)d->B * d->Hq * cdiv(d->Sq, 128) < (1 << 24) &&
                (int64_t)d->B * d->Hk * cdiv(d->Sk, 128) < (1 << 24),

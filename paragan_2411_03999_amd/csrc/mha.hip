@@ -44,7 +44,7 @@ struct MhaArgs {
   bf16_t *o, *dq, *dk, *dv;
   const float* table;
   const int32_t *len_q, *len_k;
-  float *lse, *D, *part;
+  float *lse, *D, *L, *part;     // D: minus do . o of a row; L: minus its log2 sum over c
   uint2* olo;                   // what rounding took off the output, bf16, in register layout: [32-query tile][DT / 8][64 lanes][4]
   uint16_t start[257];          // smallest distance of each bucket of one side
   uint8_t lut[kMhaMaxDist + 8]; // bucket (of one side) of each distance
@@ -581,7 +581,8 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 }
 
 // ------------------------------------------------------------- dq (query-owned)
-// Also D = do . o, kept for the key-owned pass, and the bias gradient: dS of
+// Also the row terms D = do . o and the log sums, kept for the key-owned pass
+// as it starts its products from them, and the bias gradient: dS of
 // the tiles near the diagonal, in a second visit, is summed per distance into
 // an array of each wave (an order that is fixed; fp32 atomics in LDS took
 // 134 cycles a wave instruction here), tiles past max_distance add into one
@@ -652,8 +653,11 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
     for (int e = 0; e < 8; ++e) dd = fmaf(x[e], o[e] + e8[e], dd);
   }
   dd += __shfl_xor(dd, 32, 64);
-  if (g == 0 && q < a.Sqp) a.D[(int64_t)bh * a.Sqp + q] = valid ? dd : 0.f;
   const float ls2 = valid ? a.lse[(int64_t)bh * a.Sqp + q] : INFINITY;
+  if (g == 0 && q < a.Sqp) {
+    a.D[(int64_t)bh * a.Sqp + q] = valid ? -dd : 0.f;
+    a.L[(int64_t)bh * a.Sqp + q] = -ls2 / a.c;
+  }
   const Row rw = row_of(a, sq.lk, q + sq.off);
   f32x16 acc[NT];
 #pragma unroll
@@ -886,7 +890,7 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t Ds[2][TQ * DT];
   constexpr bool VL = DT > 64;
   __shared__ __attribute__((aligned(16))) bf16_t Vt[VL ? 128 * DT : 8];
-  extern __shared__ float ex[];   // rows' log sums and D of the two tiles, then the current head's bias by query minus key
+  extern __shared__ float ex[];   // rows' L and D of the two tiles, then the current head's bias by query minus key
   float* const bs = ex + 4 * 64;
   const KItem it = item_of(a, block_no(a, a.nks * a.ns_sink + (a.nblk - a.nks) * a.ns_reg));
   const int hk = it.bh % a.Hk, b = it.bh / a.Hk;
@@ -937,9 +941,9 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
     const bool all = q0 >= i0 && q0 + TQ <= i1;
     rq.issue(Qs[bf], a.q + b * a.qs[0] + h * a.qs[2] + q0 * a.qs[1], a.qs[1], q0, wv, all, ok);
     rd.issue(Ds[bf], a.dO + b * a.os[0] + h * a.os[2] + q0 * a.os[1], a.os[1], q0, wv, all, ok);
-    // TQ rows of both: the buffers are padded to 64, rows past len_q hold +inf and 0
+    // TQ rows of both: the buffers are padded to 64, rows past len_q hold -inf and 0
     const int64_t x = ((int64_t)b * a.Hq + h) * a.Sqp + q0;
-    if (wv == 0) lds_load4(lds_addr(ex + bf * 128), lane * 4, make_rsrc(a.lse + x, TQ * 4));
+    if (wv == 0) lds_load4(lds_addr(ex + bf * 128), lane * 4, make_rsrc(a.L + x, TQ * 4));
     if (wv == 1) lds_load4(lds_addr(ex + bf * 128 + 64), lane * 4, make_rsrc(a.D + x, TQ * 4));
   };
   int hg = 0, ti = 0;
@@ -970,8 +974,14 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
       const bf16_t* ds = Ds[buf] + 32 * DT * x;
       const float* Ls = ex + buf * 128 + 32 * x;
       f32x16 s, dp;
+      // the products start from the row terms: s comes out as the score less the log sum (over c), dp less D
 #pragma unroll
-      for (int r = 0; r < 16; ++r) { s[r] = 0.f; dp[r] = 0.f; }
+      for (int i = 0; i < 4; ++i) {
+        const float4 l4 = *reinterpret_cast<const float4*>(Ls + 8 * i + 4 * g);
+        const float4 d4 = *reinterpret_cast<const float4*>(Ls + 64 + 8 * i + 4 * g);
+        s[4 * i] = l4.x; s[4 * i + 1] = l4.y; s[4 * i + 2] = l4.z; s[4 * i + 3] = l4.w;
+        dp[4 * i] = d4.x; dp[4 * i + 1] = d4.y; dp[4 * i + 2] = d4.z; dp[4 * i + 3] = d4.w;
+      }
 #pragma unroll
       for (int t = 0; t < KF; ++t) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(qs, lk, 16 * t + 8 * g), kf[t], s, 0, 0, 0);
@@ -997,16 +1007,9 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
       }
       f32x16 p;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 lv = *reinterpret_cast<const float4*>(Ls + 8 * i + 4 * g);
-        const float4 dv4 = *reinterpret_cast<const float4*>(Ls + 64 + 8 * i + 4 * g);
-        const float lsv[4] = {lv.x, lv.y, lv.z, lv.w}, ddv[4] = {dv4.x, dv4.y, dv4.z, dv4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * i + e;
-          p[r] = exp2_(BIAS ? fmaf(s[r], cm, off - lsv[e]) : fmaf(s[r], a.c, -lsv[e]));
-          s[r] = p[r] * (dp[r] - ddv[e]);
-        }
+      for (int r = 0; r < 16; ++r) {
+        p[r] = exp2_(BIAS ? fmaf(s[r], cm, off) : s[r] * a.c);
+        s[r] = p[r] * dp[r];
       }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -1201,10 +1204,10 @@ size_t mha_saved_bytes(const Mha& m) {
 
 size_t mha_ws_bytes(const Mha& m) {
   const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 64) * 64;
-  // the rows' D, then the bias partials or (after these are joined) those of dk and dv
+  // the rows' D and L, then the bias partials or (after these are joined) those of dk and dv
   const size_t bias = (size_t)m.B * m.Hq * cdiv(m.Sq, 128) * m.n_buckets * 4;
   const size_t keys = (size_t)plan_keys(m).slots * 128 * 2 * pad_d(m.d) * 4;
-  const size_t bwd = align256(rows * 4) + align256(std::max(bias, keys));
+  const size_t bwd = 2 * align256(rows * 4) + align256(std::max(bias, keys));
   size_t step = 0;
   if (few_rows(m)) step = (size_t)m.B * m.Hk * row_tiles(m) * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
   return std::max<size_t>(std::max(bwd, align256(step)), 256);
@@ -1258,7 +1261,8 @@ void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   const size_t rows = (size_t)m.B * m.Hq * a.Sqp;
   a.olo = (uint2*)((char*)const_cast<void*>(saved) + align256(rows * 4));
   a.D = (float*)ws;
-  a.part = (float*)((char*)ws + align256(rows * 4));
+  a.L = (float*)((char*)ws + align256(rows * 4));
+  a.part = (float*)((char*)ws + 2 * align256(rows * 4));
   ProfScope prof(st);
   PG_DT(m.d, {
     a.nblk = (int)cdiv(m.Sq, 128);

@@ -149,7 +149,7 @@ def test_mha_refusals(L):
     bad = [dict(B=0), dict(Sq=0), dict(Sk=0), dict(Hq=0), dict(Hk=0), dict(Hk=3), dict(d=0), dict(d=4), dict(d=136),
            dict(causal=2), dict(window=-1), dict(n_sink=-1), dict(n_buckets=-2), dict(n_buckets=1), dict(n_buckets=257),
            dict(causal=0, n_buckets=2), dict(causal=0, n_buckets=33), dict(max_distance=513), dict(max_distance=16),
-           dict(max_distance=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
+           dict(max_distance=0), dict(scale=0.0), dict(scale=1e-38), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")),
            dict(q_stride=s3(51200, 512, 60)), dict(k_stride=s3(-128, 128, 64)), dict(v_stride=s3(1 << 62, 128, 64)),
            dict(o_stride=s3(0, 512, 64)), dict(o_stride=s3(51200, 512, 56)), dict(Sq=(1 << 29) + 8), dict(window=(1 << 29) + 1), dict(n_sink=(1 << 29) + 1), dict(k_stride=s3(1 << 32, 1 << 24, 64)), dict(B=1 << 30),
            dict(Sq=1 << 29, Sk=1 << 29)]
