@@ -198,6 +198,13 @@ PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
 // ------------------------------------------------------------- forward
 // A wave owns 32 queries of one head, a block of 4 waves 128.  Keys and
 // values come in tiles of 64, the next one loading while this one is used.
+// Bound by the issue of exponentials and their neighbours beside the matrix
+// products: at 128 channels the vector unit is busy 46 % of the time and the
+// matrix cores 44 %, and they overlap little.  Causal 2 x 8192 x 16/4 heads x
+// 128: 553 us, 994 TFLOP/s (a large library product reaches 1225 here).
+// Tried and slower: two query tiles a wave at 128 channels (2421 us, one wave a
+// SIMD), the next tile's scores formed beside this one's exponentials (602),
+// raised wave priority over the products (571 and, through a window, 73 for 66).
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
@@ -581,6 +588,8 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 }
 
 // ------------------------------------------------------------- dq (query-owned)
+// Issue-bound, as the forward: its three products fill the matrix cores a third
+// of the time (4 x 4096 x 8 heads x 64 with bias: 400 us of the pass's 787).
 // Also the row terms D = do . o and the log sums, kept for the key-owned pass
 // as it starts its products from them, and the bias gradient: dS of
 // the tiles near the diagonal, in a second visit, is summed per distance into
@@ -845,6 +854,10 @@ __global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int
 // shared head are summed in registers.  A key block that many queries see
 // (first tokens beside a window; few, long sequences) is split over blocks of
 // `chunk` steps, whose fp32 partials k_mha_dkv_join adds in split order.
+// Issue-bound too: 82 % of the issue slots taken, matrix cores busy 33 % (4 x
+// 4096 x 8 heads x 64: 330 us).  Both halves of a query tile in one stretch
+// without branches needed registers that cost more (355 -> 362 us a pass, 448
+// -> 519 at 128 channels); operands read ahead changed nothing.
 
 // At head widths past 64 the values of the block's keys stay in LDS and the
 // query tiles have 32 rows: two waves fit a SIMD then (with everything in

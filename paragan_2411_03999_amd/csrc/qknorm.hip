@@ -16,10 +16,10 @@
 // group (lane moves in the vector unit up to 16 lanes); in the half-split
 // order the pair's other element sits rot / 16 lanes away and comes by a lane
 // exchange.  Blocks of the grid's second dimension take q or k.
-// Measured: forward of 32768 tokens x 16 heads x 64 in bf16 24 us (5.6 TB/s,
-// part of it from cache), backward of 15005 x 40 x 128 100 us (4.6 TB/s, as a
-// plain copy); fewer registers for more waves, or two heads in flight, were
-// slower (backward 104 to 396 us).
+// Measured: forward of 32768 tokens x 16 heads x 64 in bf16 31 us (4.4 TB/s;
+// 24 us from cache), backward of 15005 x 40 x 128 106 us (4.4 TB/s; a copy
+// reaches 4.8).  Fewer registers for more waves, or two heads in flight, were
+// slower (backward 104 to 396 us where this took 100).
 #include "token.hpp"
 
 namespace pg {
