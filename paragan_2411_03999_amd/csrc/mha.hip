@@ -1173,6 +1173,7 @@ int step_splits(const Mha& m) {
 // `chunk` steps: the number of pieces with the least modelled time, the steps
 // over the places on the card plus half the last piece, a piece's partials
 // costing about as much as 256 queries to write and add.
+constexpr int64_t kMaxSlots = 8192;   // partials of at most 1 GB (128 keys x 2 x 128 channels each)
 struct KPlan { int nkb, nks, ns_sink, ns_reg, chunk; int64_t items, slots; };
 KPlan plan_keys(const Mha& m) {
   const int64_t tq = dkv_tile(pad_d(m.d)), G = m.Hq / m.Hk, all = G * cdiv(m.Sq, tq), bh = (int64_t)m.B * m.Hk, nkb = cdiv(m.Sk, 128);
@@ -1180,8 +1181,8 @@ KPlan plan_keys(const Mha& m) {
   const int64_t nks = m.window && reg < all ? std::min<int64_t>(nkb, cdiv(m.n_sink, 128)) : 0;
   const double places = 512, used = m.causal && !m.window ? 0.5 : 1.0;   // half of a triangle
   const double total = (double)bh * (nks * all + (nkb - nks) * reg * used);
-  KPlan best{};
-  double least = 0;
+  KPlan best{(int)nkb, (int)nks, 1, 1, (int)std::min<int64_t>(all, 1 << 30), bh * nkb, 0};   // nothing split
+  double least = total / places + 0.5 * best.chunk;
   for (int64_t ns = 1; ns <= 16; ++ns) {
     KPlan p{};
     p.nkb = (int)nkb; p.nks = (int)nks;
@@ -1191,7 +1192,7 @@ KPlan plan_keys(const Mha& m) {
     p.items = bh * (nks * p.ns_sink + (nkb - nks) * p.ns_reg);
     p.slots = bh * ((p.ns_sink > 1 ? nks * p.ns_sink : 0) + (p.ns_reg > 1 ? (nkb - nks) * p.ns_reg : 0));
     const double t = (total + 256.0 / tq * used * p.slots) / places + 0.5 * p.chunk;
-    if (p.items < (1 << 24) && (ns == 1 || t < least)) { best = p; least = t; }
+    if (p.slots <= kMaxSlots && p.items < (1 << 24) && t < least) { best = p; least = t; }
   }
   return best;
 }
@@ -1222,7 +1223,7 @@ size_t mha_ws_bytes(const Mha& m) {
   const size_t keys = (size_t)plan_keys(m).slots * 128 * 2 * pad_d(m.d) * 4;
   const size_t bwd = 2 * align256(rows * 4) + align256(std::max(bias, keys));
   size_t step = 0;
-  if (few_rows(m)) step = (size_t)m.B * m.Hk * row_tiles(m) * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
+  if (few_rows(m) && step_splits(m) > 1) step = (size_t)m.B * m.Hk * row_tiles(m) * step_splits(m) * 32 * (pad_d(m.d) + 2) * 4;
   return std::max<size_t>(std::max(bwd, align256(step)), 256);
 }
 

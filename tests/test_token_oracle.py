@@ -163,6 +163,20 @@ def test_mha_refusals(L):
     assert L.paragan_mha_bwd(None, C.byref(mh()), *[None] * 14) == lib.EINVAL
 
 
+def test_mha_workspaces_stay_in_proportion(L):
+    """Half a long sequence as first tokens of a short window would give millions of pieces of key blocks; many
+    sequences of one new token need no partials."""
+    one = dict(B=1, Hq=1, Hk=1, n_buckets=0, max_distance=0)
+    for n in (1 << 20, 1 << 22):
+        st = s3(64 * n, 64, 64)
+        d = mh(Sq=n, Sk=n, window=16, n_sink=n // 2, q_stride=st, k_stride=st, v_stride=st, o_stride=st, **one)
+        assert lib.paragan_mha_check(d) == lib.OK
+        assert lib.paragan_mha_sizes(d)[1] < 2 * 4 * n + (3 << 29)
+    d = mh(B=4096, Sq=1, Sk=4096, n_buckets=0, max_distance=0, q_stride=s3(512, 512, 64), o_stride=s3(512, 512, 64),
+           k_stride=s3(4096 * 128, 128, 64), v_stride=s3(4096 * 128, 128, 64))
+    assert lib.paragan_mha_sizes(d)[1] < 64 << 20
+
+
 def test_descriptors_refuse_tensors_that_do_not_belong_together():
     torch = pytest.importorskip("torch")
     z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
