@@ -205,8 +205,12 @@ PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
 // Tried and slower: two query tiles a wave at 128 channels (2421 us, one wave a
 // SIMD), the next tile's scores formed beside this one's exponentials (602),
 // raised wave priority over the products (571 and, through a window, 73 for 66).
+// At 64 channels four waves a SIMD hide more than the third of the registers
+// is worth, though the bias then spills 20 bytes a lane: with it 64 x 256 x 8
+// heads 22.0 us against 24.5 with three; without it, 4 x 4099 x 16 heads
+// through a window of 512, 56.8 against 57.6.
 template <int DT, bool BIAS>
-__global__ __launch_bounds__(256, DT == 64 ? 3 : 2) void k_mha_fwd(MhaArgs a) {
+__global__ __launch_bounds__(256, DT == 64 ? 4 : 2) void k_mha_fwd(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
   __shared__ __attribute__((aligned(16))) bf16_t Ks[2][TK * DT];
   __shared__ __attribute__((aligned(16))) bf16_t Vs[2][TK * DT];
@@ -589,7 +593,7 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 
 // ------------------------------------------------------------- dq (query-owned)
 // Issue-bound, as the forward: its three products fill the matrix cores a third
-// of the time (4 x 4096 x 8 heads x 64 with bias: 400 us of the pass's 787).
+// of the time (4 x 4096 x 8 heads x 64 with bias: 400 us of the pass's 772).
 // Also the row terms D = do . o and the log sums, kept for the key-owned pass
 // as it starts its products from them, and the bias gradient: dS of
 // the tiles near the diagonal, in a second visit, is summed per distance into
