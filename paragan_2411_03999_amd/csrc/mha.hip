@@ -623,6 +623,8 @@ PG_DEV void diag_add(float* arr, const f32x16& v, int lane) {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
+// Three waves a SIMD where the registers suffice; with bias they spill 112 bytes
+// a lane then (training 4 x 4096 x 8 heads x 64: 1053 us against 803).
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
@@ -900,6 +902,9 @@ PG_DEV KItem item_of(const MhaArgs& a, int x) {
   return it;
 }
 
+// Two waves a SIMD: a third at 64 channels spills 20 to 44 bytes a lane (the
+// training of 4 x 4096 x 8 heads with bias 878 us against 803, without bias 4 x 2048 x 16 heads 363
+// against 359).
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
   constexpr int TQ = dkv_tile(DT), NC = DT / 8, NT = DT / 32, KF = DT / 16;
