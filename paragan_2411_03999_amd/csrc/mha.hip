@@ -871,7 +871,7 @@ __global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int
 // 128, window 1024).
 constexpr int dkv_tile(int dt) { return dt > 64 ? 32 : 64; }
 
-// the queries [i0, i1) that see some key of [j0, j1]
+// the queries [i0, i1) that see some key of [j0, j1]: none, and no step, where all of these lie behind the last key
 PG_DEV void seen_by(const MhaArgs& a, const Seq& sq, int j0, int j1, int& i0, int& i1) {
   j1 = min(j1, sq.lk - 1);
   const bool sink = a.window && j0 < a.n_sink;
@@ -879,7 +879,7 @@ PG_DEV void seen_by(const MhaArgs& a, const Seq& sq, int j0, int j1, int& i0, in
   const int hi = a.window && !sink ? j1 + a.window - 1 : 0x40000000;
   i0 = max(lo - sq.off, 0);
   i1 = min(hi - sq.off + 1, sq.lq);
-  if (j1 < j0) i1 = i0;
+  if (j1 < j0) i0 = i1 = 0;
 }
 
 // item of a launch: key block, split, and the slot of its partials

@@ -218,6 +218,14 @@ def test_mha_more_queries_than_keys_leaves_empty_rows():
     mha_case(2, 90, 90, 2, 1, 32, 1, 10, 4, 0, 0, [90, 12], [30, 12], seed=4)
 
 
+@pytest.mark.parametrize("causal,window,sink", [(1, 0, 0), (1, 20, 3), (0, 20, 0)])
+def test_mha_key_blocks_behind_the_last_key(causal, window, sink):
+    """Caches far longer than their sequences, with few queries: the key blocks behind the last key have no query tile to
+    walk (the first of their queries would lie past the rows of a head), and their gradients are zeros."""
+    mha_case(3, 40, 700, 4, 2, 64, causal, window, sink, 0, 0, [33, 0, 7], [5, 3, 300], seed=21)
+    mha_case(3, 40, 700, 2, 1, 128, causal, window, sink, 8, 30, [33, 0, 7], [5, 3, 300], seed=22)
+
+
 STEP = [
     (1, 1, 1, 1, 1, 8, 1), (3, 1, 40, 4, 4, 64, 1), (2, 1, 1000, 32, 8, 128, 1), (2, 4, 777, 8, 1, 96, 1),
     (1, 1, 5000, 16, 2, 64, 1, 300, 4, 32, 128), (2, 3, 900, 10, 1, 32, 1, 64, 40), (1, 1, 4000, 8, 8, 128, 0, 0, 0, 16, 512),
