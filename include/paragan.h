@@ -299,7 +299,8 @@ int paragan_qknorm_bwd(paragan_ctx* ctx, const paragan_qknorm_desc* d,
  * p = i + len_k - len_q, so a few new queries are the last tokens of a cache.
  * Key j is visible to it when j < len_k and
  *   causal: j <= p;   window > 0: |p - j| < window or j < n_sink.
- * A query that sees nothing gets zeros.  Rows at and past len_q of o (and
+ * A query that sees nothing gets zeros, one with a NaN among its scores gets
+ * NaN.  Rows at and past len_q of o (and
  * of dq), rows at and past len_k of dk and dv, are written as zeros.  Keys
  * and values at and past len_k, and keys that no query of the call sees, may
  * hold anything; a NaN or infinity in a key or value that some query sees

@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256, DT == 64 ? 4 : 2) void k_mha_fwd(MhaArgs a) {
     if (n + 1 < sp.nt) visit(std::integral_constant<int, 1>(), n + 1);
   }
   const float lt = l + __shfl_xor(l, 32, 64);
-  const bool any = q < sq.lq && lt > 0.f;
+  const bool any = q < sq.lq && lt != 0.f;   // a NaN goes on: only a row that sees nothing is zeros
   const float inv = any ? 1.f / lt : 0.f;
   bf16_t* orow = a.o + b * a.os[0] + q * a.os[1] + h * a.os[2];
   uint2* const lo = a.olo && qw < a.Sqp ? a.olo + ((int64_t)bh * (a.Sqp / 32) + qw / 32) * (DT / 8) * 64 + lane : nullptr;
@@ -546,7 +546,7 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
     return;
   }
   if (rho >= R) return;
-  const bool any = live && L > 0.f;
+  const bool any = live && L != 0.f;   // as in the forward
   const float inv = any ? 1.f / L : 0.f;
   bf16_t* orow = a.o + b * a.os[0] + i * a.os[1] + h * a.os[2];
 #pragma unroll
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
   }
   const int i = rho % a.Sq, h = hk * a.G + rho / a.Sq;
   const Seq sq = seq_of(a, b);
-  const bool any = i < sq.lq && L > 0.f;
+  const bool any = i < sq.lq && L != 0.f;
   const float inv = any ? 1.f / L : 0.f;
   if (!any) s = make_float4(0.f, 0.f, 0.f, 0.f);
   st4(a.o + b * a.os[0] + i * a.os[1] + h * a.os[2], c, a.d, s.x * inv, s.y * inv, s.z * inv, s.w * inv);

@@ -299,6 +299,56 @@ def test_mha_large_scores():
     mha_case(1, 2, 600, 8, 1, 64, 1, scale=8.0, seed=12, train=False)
 
 
+@pytest.mark.parametrize("Sq,Sk,Hq,Hk,train,nb", [(150, 150, 2, 1, True, 0), (150, 150, 2, 2, True, 8), (300, 300, 64, 64, False, 0),
+                                                  (2, 200, 4, 1, False, 8), (1, 3000, 4, 2, False, 0)])
+def test_mha_nan_comes_out(Sq, Sk, Hq, Hk, train, nb):
+    """A NaN or infinity in a query, and a NaN in a key, make the outputs of the rows that meet it NaN (forward, backward,
+    few rows, few rows with split keys); other rows keep their bits."""
+    torch = need_gpu()
+    print("nan", Sq, Sk, Hq, Hk, train, nb, flush=True)
+    gen = torch.Generator().manual_seed(31)
+    q, k, v, do = (torch.randn(1, s, h, 64, generator=gen).bfloat16().cuda() for s, h in ((Sq, Hq), (Sk, Hk), (Sk, Hk), (Sq, Hq)))
+    table = torch.randn(Hq, nb, generator=gen).cuda() if nb else None
+
+    def run(q, k):
+        o, dq, dk, dv = torch.empty_like(q), torch.empty_like(q), torch.empty_like(k), torch.empty_like(k)
+        dt = torch.empty_like(table) if nb else None
+        d = lib.mha_desc(q, k, v, o, scale=0.125, causal=1, n_buckets=nb, max_distance=30 if nb else 0)
+        sb, wb = lib.paragan_mha_sizes(d)
+        ctx, ws, saved = lib.Context(), lib.workspace(wb), lib.workspace(sb) if train else None
+        lib.paragan_mha_fwd(ctx, d, q, k, v, table, None, None, o, saved, ws)
+        if train:
+            lib.paragan_mha_bwd(ctx, d, q, k, v, table, None, None, o, saved, do, dq, dk, dv, dt, ws)
+        torch.cuda.synchronize()
+        return o, dq, dk, dv, dt
+    ref = run(q, k)
+    row, h = Sq // 2, Hq - 1
+    hk = h // (Hq // Hk)
+    for bad in (float("nan"), float("inf")):
+        q2 = q.clone()
+        q2[0, row, h, 5] = bad
+        got = run(q2, k)
+        for i in ((0, 1) if train else (0,)):
+            assert bool(torch.isnan(got[i][0, row, h]).all()), i
+            same = got[i].clone()
+            same[0, row, h] = ref[i][0, row, h]
+            assert torch.equal(same, ref[i]), i
+        if train:        # every key up to the row's own position
+            assert not bool(torch.isfinite(got[2][0, :row + 1, hk].float()).all(-1).any())
+            assert bool(torch.isnan(got[3][0, :row + 1, hk]).all())
+            assert bool(torch.isnan(got[4][h]).any()) if nb else True
+    k2, key = k.clone(), Sk - Sq // 2 - 1
+    k2[0, key, hk, 3] = float("nan")
+    got = run(q, k2)
+    first = key - (Sk - Sq)                                       # the first query that sees it
+    for hh in range(Hq):
+        if hh // (Hq // Hk) == hk:
+            assert bool(torch.isnan(got[0][0, max(first, 0):, hh]).all())
+            assert torch.equal(got[0][0, :max(first, 0), hh], ref[0][0, :max(first, 0), hh])
+        else:
+            assert torch.equal(got[0][:, :, hh], ref[0][:, :, hh])
+
+
 @pytest.mark.parametrize("nb,maxd,causal", [(32, 128, 1), (32, 128, 0), (2, 2, 1), (4, 500, 0), (64, 100, 1), (256, 512, 0)])
 def test_every_bucket(nb, maxd, causal):
     """One query over keys at every distance, equal scores: o is the softmax of the bias alone."""
