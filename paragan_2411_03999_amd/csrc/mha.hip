@@ -31,6 +31,10 @@ namespace pg {
 namespace {
 
 constexpr int kStepTable = 64;  // buckets up to which a step keeps its rows' bias in LDS (8 KB)
+// A bias this large (in log2 units) leaves nothing of a score's fraction in their fp32 sum.  The sum is formed all the same
+// then, away from the diagonal too, where a smaller bias goes into the exponent beside the running maximum: taken apart,
+// a row of such biases alone would weigh its keys by scores that the sums near the diagonal have lost, up to infinity.
+constexpr float kDeep = 0x1p24f;
 constexpr int kMargin = 96;   // distances past max_distance that a 64 x 32 tile can reach, rounded up
 
 struct MhaArgs {
@@ -152,6 +156,11 @@ PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
   return log2_bias(a.table[(int64_t)h * a.nb + b]);
 }
 PG_DEV int bias_len(const MhaArgs& a) { return 2 * (a.maxd + kMargin) + 1; }
+// where key k0's bias for the query at p0 stands in that array, if the tile is near the diagonal; else the 31st of an
+// end's kMargin + 1 equal elements, of which a tile of 64 keys takes those from 31 before to 63 behind
+PG_DEV int bias_row(const MhaArgs& a, bool near, int k0, int p0) {
+  return near ? k0 - p0 + a.maxd + kMargin : 31 + (k0 < p0 ? 0 : 2 * a.maxd + kMargin);
+}
 
 // ROWS rows x NC chunks from memory straight into a swizzled LDS tile by 4
 // waves: 16-byte slot i of the tile (lane order) holds chunk (i % NC) ^ swizzle
@@ -271,15 +280,17 @@ __global__ __launch_bounds__(256, DT == 64 ? 4 : 2) void k_mha_fwd(MhaArgs a) {
     // a score in log2 units is s cm + off: near the diagonal the bias is added to each, elsewhere it is one number
     float cm = a.c, off = 0.f;
     if (BIAS) {
-      if (k0 + TK - 1 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd) {
-        const float* bl = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
+      const bool near = k0 + TK - 1 - p0 > -a.maxd && k0 - p0 - 31 < a.maxd;
+      const float far = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
+      if (near || fabsf(far) >= kDeep) {
+        const float* bl = bs + bias_row(a, near, k0, p0) - lq + 4 * g;
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[x][r] = fmaf(s[x][r], a.c, bl[32 * x + 8 * (r >> 2) + (r & 3)]);
         cm = 1.f;
       } else {
-        off = k0 < p0 ? bs[0] : bs[bias_len(a) - 1];
+        off = far;
       }
     }
     if (!all_seen<TK>(a, sq.lk, k0, p0, p0 + 31)) {
@@ -465,7 +476,8 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
     for (int t = 0; t < KF; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ks, lq, 16 * t + 8 * g), qf[t], s, 0, 0, 0);
     float cm = cs, off = 0.f;
     if (BIAS) {
-      if (k0 + 31 - sq.off > -a.maxd && k0 - (sq.off + sq.lq - 1) < a.maxd) {
+      const float far = k0 < sq.off ? flo : fhi;
+      if ((k0 + 31 - sq.off > -a.maxd && k0 - (sq.off + sq.lq - 1) < a.maxd) || fabsf(far) >= kDeep) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int rel = min(max(k0 + acc_row(r, g) - i - sq.off, -a.maxd), a.maxd);
@@ -473,7 +485,7 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
         }
         cm = 1.f;
       } else {
-        off = k0 < sq.off ? flo : fhi;
+        off = far;
       }
     }
     if (!all_seen<32>(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) hide(s, rw, k0, g);

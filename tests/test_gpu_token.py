@@ -292,6 +292,18 @@ def test_mha_lowest_and_infinite_bias():
         held("o", o, mean, (3 * U16) * np.abs(v.double().cpu().numpy()).mean() + np.zeros_like(mean))
 
 
+@pytest.mark.parametrize("Sq,Sk,Hq,Hk,causal,window", [(300, 300, 2, 1, 0, 0), (300, 300, 2, 1, 1, 0), (300, 300, 40, 40, 1, 90),
+                                                       (1, 300, 4, 2, 1, 0), (3, 3000, 2, 1, 1, 0), (5, 700, 1, 1, 0, 200)])
+def test_mha_lowest_bias_alone(Sq, Sk, Hq, Hk, causal, window):
+    """The lowest finite value in every bucket: scores vanish in it, near the diagonal and far from it, so that each row is
+    the mean of the values that it sees, also where scores pass what an exponential holds."""
+    def low(t):
+        return torch.full_like(t, torch.finfo(torch.float32).min)
+    torch = need_gpu()
+    for scale in (None, 8.0):
+        mha_case(1, Sq, Sk, Hq, Hk, 64, causal, window, 0, 8, 9, tab=low, train=False, seed=41, scale=scale)
+
+
 def test_mha_large_scores():
     """Scores of a few hundred: the running maximum moves, nothing overflows."""
     for train in (True, False):
