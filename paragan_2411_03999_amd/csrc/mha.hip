@@ -35,6 +35,10 @@ constexpr int kStepTable = 64;  // buckets up to which a step keeps its rows' bi
 // then, away from the diagonal too, where a smaller bias goes into the exponent beside the running maximum: taken apart,
 // a row of such biases alone would weigh its keys by scores that the sums near the diagonal have lost, up to infinity.
 constexpr float kDeep = 0x1p24f;
+// From a bias this large on (log2 units; of a head's any finite one) the backward keeps a row's maximum and the logarithm of
+// its sum apart: as one number, as exact as 2^-14 up to here, it would lose the sum beside a bias that scores vanish in too.
+// (Training 4 x 4096 x 8 heads x 64 pays 1 % for it, 790 us against 780.)
+constexpr float kSteep = 0x1p10f;
 constexpr int kMargin = 96;   // distances past max_distance that a 64 x 32 tile can reach, rounded up
 
 struct MhaArgs {
@@ -48,7 +52,8 @@ struct MhaArgs {
   bf16_t *o, *dq, *dk, *dv;
   const float* table;
   const int32_t *len_q, *len_k;
-  float *lse, *D, *L, *part;     // D: minus do . o of a row; L: minus its log2 sum over c
+  float *top, *lg;              // of a row, in log2 units: its maximum and the log of its sum (no bias: top is both); infinity if it sees nothing
+  float *D, *L, *part;          // D: minus do . o of a row; L: what its products start from in the key-owned pass
   uint2* olo;                   // what rounding took off the output, bf16, in register layout: [32-query tile][DT / 8][64 lanes][4]
   uint16_t start[257];          // smallest distance of each bucket of one side
   uint8_t lut[kMhaMaxDist + 8]; // bucket (of one side) of each distance
@@ -154,6 +159,16 @@ PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {
   const int rel = min(max(e - a.maxd - kMargin, -a.maxd), a.causal ? 0 : a.maxd);
   const int b = (int)a.lut[rel < 0 ? -rel : rel] + (rel > 0 ? a.half : 0);
   return log2_bias(a.table[(int64_t)h * a.nb + b]);
+}
+PG_DEV float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+// Is one of head h's biases that large?  (Every wave looks for itself.)
+PG_DEV bool steep_bias(const MhaArgs& a, int h, int lane) {
+  bool big = false;
+  for (int k = lane; k < a.nb; k += 64) {
+    const float b = fabsf(log2_bias(a.table[(int64_t)h * a.nb + k]));
+    big |= b >= kSteep && b <= FLT_MAX;
+  }
+  return __any(big);
 }
 PG_DEV int bias_len(const MhaArgs& a) { return 2 * (a.maxd + kMargin) + 1; }
 // where key k0's bias for the query at p0 stands in that array, if the tile is near the diagonal; else the 31st of an
@@ -357,7 +372,11 @@ __global__ __launch_bounds__(256, DT == 64 ? 4 : 2) void k_mha_fwd(MhaArgs a) {
         lo[(4 * j + i) * 64] = make_uint2(f2bf2(f[0], f[1]), f2bf2(f[2], f[3]));
       }
     }
-  if (a.lse && g == 0 && q < a.Sqp) a.lse[(int64_t)bh * a.Sqp + q] = any ? m2 + __log2f(lt) : INFINITY;
+  if (a.top && g == 0 && q < a.Sqp) {
+    const float lg = any ? __log2f(lt) : 0.f;
+    a.top[(int64_t)bh * a.Sqp + q] = any ? (BIAS ? m2 : m2 + lg) : INFINITY;
+    if (BIAS) a.lg[(int64_t)bh * a.Sqp + q] = lg;
+  }
 }
 
 // ------------------------------------------------------------- a few new tokens
@@ -656,6 +675,8 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
     for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, h, e);
     for (int e = tid; e < 4 * bl; e += 256) bs[bl + e] = 0.f;
   }
+  const bool steep = BIAS && steep_bias(a, h, lane);
+  const float far_lo = BIAS ? uniform(bias2_at(a, h, 0)) : 0.f, far_hi = BIAS ? uniform(bias2_at(a, h, bl - 1)) : 0.f;
   const bool valid = q < sq.lq;
   const bf16_t* Q = a.q + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
   const bf16_t* DO = a.dO + b * a.os[0] + q * a.os[1] + h * a.os[2];
@@ -680,10 +701,13 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
     for (int e = 0; e < 8; ++e) dd = fmaf(x[e], o[e] + e8[e], dd);
   }
   dd += __shfl_xor(dd, 32, 64);
-  const float ls2 = valid ? a.lse[(int64_t)bh * a.Sqp + q] : INFINITY;
+  // p = 2^(score - top), P = p inv.  Without a bias the log sum is part of top; with one (see kSteep) inv is multiplied
+  // into the sums over a row at their end, so that it costs nothing in the loop.
+  const float top = valid ? a.top[(int64_t)bh * a.Sqp + q] : INFINITY, lg = BIAS && valid ? a.lg[(int64_t)bh * a.Sqp + q] : 0.f;
+  const float inv = BIAS ? exp2_(-lg) : 1.f;
   if (g == 0 && q < a.Sqp) {
     a.D[(int64_t)bh * a.Sqp + q] = valid ? -dd : 0.f;
-    a.L[(int64_t)bh * a.Sqp + q] = -ls2 / a.c;
+    a.L[(int64_t)bh * a.Sqp + q] = steep && top != INFINITY ? 0.f : -(top + lg) / a.c;
   }
   const Row rw = row_of(a, sq.lk, q + sq.off);
   f32x16 acc[NT];
@@ -691,7 +715,8 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
-  // BIAS, per row: dS of the far tiles on either side, sum of dS, P of the far tiles of earlier keys, P of the near tiles
+  // BIAS, per row (over inv, but for the last): dS of the far tiles on either side, sum of dS, P of the far tiles of earlier
+  // keys, P of the near tiles
   float flo = 0.f, fhi = 0.f, rho = 0.f, wlo = 0.f, wn = 0.f;
   bool lo_far = false, hi_far = false;
   Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128, sq.lq) - 1 + sq.off);
@@ -738,20 +763,22 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
           s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ks, lq, 16 * t + 8 * g), qf[t], s, 0, 0, 0);
           dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(vs, lq, 16 * t + 8 * g), df[t], dp, 0, 0, 0);
         }
-        if (BIAS && near) {
-          const float* bl4 = bs + (k0 - p0 - lq + a.maxd + kMargin) + 4 * g;
+        // scores as the forward forms them
+        const float far = k0 < p0 ? far_lo : far_hi;
+        if (BIAS && (near || fabsf(far) >= kDeep)) {
+          const float* bl4 = bs + bias_row(a, near, k0, p0) - lq + 4 * g;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, bl4[8 * (r >> 2) + (r & 3)] - ls2);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, bl4[8 * (r >> 2) + (r & 3)]) - top;
         } else {
-          const float far = (BIAS ? (k0 < p0 ? bs[0] : bs[bl - 1]) : 0.f) - ls2;
+          const float ft = far - top;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, far);
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, ft);
         }
         if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) hide(s, rw, k0, g);
         if constexpr (NEAR) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const float p = exp2_(s[r]);
+            const float p = exp2_(s[r]) * inv;
             wn += p;
             s[r] = p * (dp[r] - (dd + rho));
           }
@@ -775,10 +802,10 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
           rho += t;
           if (!near && k0 < p0) {
             flo += t;
-            lo_far = bs[0] != -INFINITY;   // a hidden bucket holds nothing, and gets nothing
+            lo_far = far_lo != -INFINITY;   // a hidden bucket holds nothing, and gets nothing
           } else if (!near) {
             fhi += t;
-            hi_far = bs[bl - 1] != -INFINITY;
+            hi_far = far_hi != -INFINITY;
           }
         }
 #pragma unroll
@@ -805,7 +832,10 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
     // rho = (true D) - D, and the bias gradient, many sums of dS with little
     // left over, would show it.  The true dS is dS - rho P: the near tiles are
     // visited again for theirs, the far ones together hold what is left of 1.
-    rho += __shfl_xor(rho, 32, 64);
+    rho = (rho + __shfl_xor(rho, 32, 64)) * inv;
+    flo *= inv;
+    fhi *= inv;
+    wlo *= inv;
     pass(std::integral_constant<bool, true>());
     const float rest = (g == 0 ? 1.f : 0.f) - wn;   // the two lanes of a row together: P of its far tiles
     if (a.causal) wlo = rest;
@@ -814,7 +844,7 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
   }
   if (q < a.Sq) {
     bf16_t* row = a.dq + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];
-    const float f = valid ? a.scale : 0.f;
+    const float f = valid ? a.scale * inv : 0.f;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -926,6 +956,8 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t Vt[VL ? 128 * DT : 8];
   extern __shared__ float ex[];   // rows' L and D of the two tiles, then the current head's bias by query minus key
   float* const bs = ex + 4 * 64;
+  bool steep = false;                       // of the current head: has it a bias that large, and
+  float far_lo = 0.f, far_hi = 0.f;         // its biases past max_distance, of earlier and later keys
   const KItem it = item_of(a, block_no(a, a.nks * a.ns_sink + (a.nblk - a.nks) * a.ns_reg));
   const int hk = it.bh % a.Hk, b = it.bh / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, lk = lane & 31;
@@ -998,6 +1030,9 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
     if (n + 1 < n1) load(hg, ti, buf ^ 1);
     if (BIAS && fresh) {   // the next head's bias
       for (int e = tid; e < bl; e += 256) bs[e] = bias2_at(a, hk * a.G + h, bl - 1 - e);
+      steep = steep_bias(a, hk * a.G + h, lane);
+      far_lo = uniform(bias2_at(a, hk * a.G + h, 0));
+      far_hi = uniform(bias2_at(a, hk * a.G + h, bl - 1));
       __syncthreads();
     }
 #pragma unroll
@@ -1008,7 +1043,8 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
       const bf16_t* ds = Ds[buf] + 32 * DT * x;
       const float* Ls = ex + buf * 128 + 32 * x;
       f32x16 s, dp;
-      // the products start from the row terms: s comes out as the score less the log sum (over c), dp less D
+      // the products start from the row terms: s comes out as the score less the log sum (over c; with a steep bias as the
+      // score alone), dp less D
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 l4 = *reinterpret_cast<const float4*>(Ls + 8 * i + 4 * g);
@@ -1024,13 +1060,31 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
       }
       float cm = a.c, off = 0.f;   // as in the forward
       if (BIAS) {
-        if (kw + 31 - p0 > -a.maxd && kw - p0 - 31 < a.maxd) {
-          const float* bn = bs + (p0 - kw - lk + a.maxd + kMargin) + 4 * g;
+        const bool near = kw + 31 - p0 > -a.maxd && kw - p0 - 31 < a.maxd;
+        const float far = kw < p0 ? far_lo : far_hi;
+        if (near || (steep && fabsf(far) >= kDeep)) {
+          // queries are to keys here as keys to queries there
+          const float* bn = bs + bias_row(a, near, p0, kw) - lk + 4 * g;
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], a.c, bn[8 * (r >> 2) + (r & 3)]);
           cm = 1.f;
         } else {
-          off = kw < p0 ? bs[bl - 1] : bs[0];
+          off = far;
+        }
+        if (steep) {   // rare: the rows' terms from memory
+          const int64_t row = ((int64_t)b * a.Hq + hk * a.G + h) * a.Sqp + q0 + 4 * g;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 m4 = *reinterpret_cast<const float4*>(a.top + row + 8 * i);
+            const float4 g4 = *reinterpret_cast<const float4*>(a.lg + row + 8 * i);
+            s[4 * i] = fmaf(s[4 * i], cm, off - m4.x) - g4.x;
+            s[4 * i + 1] = fmaf(s[4 * i + 1], cm, off - m4.y) - g4.y;
+            s[4 * i + 2] = fmaf(s[4 * i + 2], cm, off - m4.z) - g4.z;
+            s[4 * i + 3] = fmaf(s[4 * i + 3], cm, off - m4.w) - g4.w;
+            asm volatile("" ::: "memory");   // few of them in registers at once
+          }
+          cm = 1.f;
+          off = 0.f;
         }
       }
       if (!all_seen<32>(a, sq.lk, kw, p0, p0 + 31)) {
@@ -1170,6 +1224,13 @@ MhaArgs make_args(const Mha& m) {
   return a;
 }
 
+void set_saved(MhaArgs& a, void* saved) {
+  const size_t rows = align256((size_t)a.B * a.Hq * a.Sqp * 4);
+  a.top = (float*)saved;
+  a.lg = (float*)((char*)saved + rows);
+  a.olo = (uint2*)((char*)saved + 2 * rows);
+}
+
 int64_t row_tiles(const Mha& m) { return cdiv((int64_t)m.Sq * (m.Hq / m.Hk), 32); }
 // Which calls without a backward take the form for a few new tokens: those of
 // few queries (the other form leaves three of its four waves idle: 64 x 16
@@ -1234,7 +1295,7 @@ size_t bias_bytes(const Mha& m, int arrays) {
 
 size_t mha_saved_bytes(const Mha& m) {
   const size_t rows = (size_t)m.B * m.Hq * (size_t)cdiv(m.Sq, 64) * 64;
-  return align256(rows * 4) + align256(rows * pad_d(m.d) * 2);   // the rows' log2 sums, the output's remainder
+  return 2 * align256(rows * 4) + align256(rows * pad_d(m.d) * 2);   // the rows' maxima and log2 sums, the output's remainder
 }
 
 size_t mha_ws_bytes(const Mha& m) {
@@ -1271,8 +1332,7 @@ void mha_fwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
     prof.done("k_mha_step<" + std::to_string(pad_d(m.d)) + ">", flops);
     return;
   }
-  a.lse = (float*)saved;
-  if (saved) a.olo = (uint2*)((char*)saved + align256((size_t)m.B * m.Hq * a.Sqp * 4));
+  if (saved) set_saved(a, saved);
   a.nblk = (int)cdiv(m.Sq, 128);
   a.hset = head_set((int64_t)m.B * m.Hq, a.G, len_k || len_q);
   const dim3 grid((unsigned)((int64_t)m.B * m.Hq * a.nblk));
@@ -1292,9 +1352,8 @@ void mha_bwd(hipStream_t st, const Mha& m, const void* q, const void* k, const v
   a.q = (const bf16_t*)q; a.k = (const bf16_t*)k; a.v = (const bf16_t*)v; a.o = (bf16_t*)const_cast<void*>(o);
   a.table = table; a.len_q = len_q; a.len_k = len_k;
   a.dO = (const bf16_t*)dO; a.dq = (bf16_t*)dq; a.dk = (bf16_t*)dk; a.dv = (bf16_t*)dv;
-  a.lse = (float*)const_cast<void*>(saved);
+  set_saved(a, const_cast<void*>(saved));
   const size_t rows = (size_t)m.B * m.Hq * a.Sqp;
-  a.olo = (uint2*)((char*)const_cast<void*>(saved) + align256(rows * 4));
   a.D = (float*)ws;
   a.L = (float*)((char*)ws + align256(rows * 4));
   a.part = (float*)((char*)ws + 2 * align256(rows * 4));

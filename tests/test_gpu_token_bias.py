@@ -1,0 +1,95 @@
+"""Attention with relative position biases that are large against the scores: the lowest finite value and the usual
+masks of -1e4 and below, in rows that see other keys too and in rows that see nothing else, forward and backward.
+
+A bias that a row's keys share shifts its scores and leaves the softmax as it is.  With equal keys the scores of a
+row are equal too, so their fp32 sums with the bias round alike and the probabilities are exact; with a bias that
+scores vanish in they are equal whatever the keys.  The bounds are therefore those of the definition without that
+bias (oracle/token.py)."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import token as T
+from paragan_2411_03999_amd import lib
+
+from .parity import need_gpu
+from .test_gpu_token import held
+
+pytestmark = pytest.mark.gpu
+
+LOWEST = float(np.finfo(np.float32).min)
+
+
+def trained(q, k, v, do, table, scale=0.125, **kw):
+    """o, dq, dk, dv, dtable of one forward and backward."""
+    torch = need_gpu()
+    Q, K, V, DO, TB = (t.cuda() for t in (q, k, v, do, table))
+    out = {"o": torch.empty_like(Q), "dq": torch.empty_like(Q), "dk": torch.empty_like(K), "dv": torch.empty_like(V),
+           "dtable": torch.empty_like(TB)}
+    d = lib.mha_desc(Q, K, V, out["o"], scale=scale, n_buckets=table.shape[1], **kw)
+    sb, wb = lib.paragan_mha_sizes(d)
+    ctx, ws, saved = lib.Context(), lib.workspace(wb), lib.workspace(sb)
+    ws.fill_(255)
+    lib.paragan_mha_fwd(ctx, d, Q, K, V, TB, None, None, out["o"], saved, ws)
+    ws.fill_(255)
+    lib.paragan_mha_bwd(ctx, d, Q, K, V, TB, None, None, out["o"], saved, DO, out["dq"], out["dk"], out["dv"], out["dtable"], ws)
+    torch.cuda.synchronize()
+    return out
+
+
+def against(out, q, k, v, do, table, scale=0.125, **kw):
+    n = lambda t: t.double().numpy()  # noqa: E731
+    want = T.mha(n(q), n(k), n(v), scale, table=n(table), dout=n(do), **kw)
+    for name, t in out.items():
+        held(name, t, want[name], want["tol." + name] + 1e-30)
+
+
+def inputs(torch, seed, B, Sq, Sk, Hq, Hk, d):
+    gen = torch.Generator().manual_seed(seed)
+    return [torch.randn(B, s, h, d, generator=gen).bfloat16() for s, h in ((Sq, Hq), (Sk, Hk), (Sk, Hk), (Sq, Hq))], gen
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("value", [LOWEST, -1e9, -1e5, -2e3])
+def test_own_position_masked(value, d):
+    """Causal, bucket 0 very low: the first query sees its own key alone and takes all of it, the others take nothing of
+    theirs (2^-2885 is zero in float64 too, so the definition gives the same for all four)."""
+    torch = need_gpu()
+    print("own position masked", value, d, flush=True)
+    (q, k, v, do), gen = inputs(torch, 1, 2, 170, 170, 4, 2, d)
+    table = torch.randn(4, 8, generator=gen)
+    given = table.clone()
+    table[:, 0], given[:, 0] = LOWEST, value
+    kw = dict(causal=1, max_distance=30)
+    against(trained(q, k, v, do, given, **kw), q, k, v, do, table, **kw)
+
+
+@pytest.mark.parametrize("causal,window", [(0, 0), (1, 0), (1, 90), (0, 90)])
+@pytest.mark.parametrize("value", [LOWEST, -1e9, 1e9, -1e8])
+def test_rows_of_nothing_else(value, causal, window):
+    """Every bucket of one head holds a value that scores vanish in, near the diagonal and past max_distance: its rows are
+    means.  The other query head of the same key head has an ordinary bias."""
+    torch = need_gpu()
+    print("nothing else", value, causal, window, flush=True)
+    (q, k, v, do), gen = inputs(torch, 2, 1, 300, 300, 2, 1, 64)
+    table = torch.randn(2, 8, generator=gen)
+    given = table.clone()
+    table[0], given[0] = LOWEST, value
+    kw = dict(causal=causal, window=window, max_distance=9)
+    against(trained(q, k, v, do, given, **kw), q, k, v, do, table, **kw)
+
+
+@pytest.mark.parametrize("Sq,Sk", [(150, 150), (40, 150)])
+@pytest.mark.parametrize("value", [-1e9, -1e6, -1e5, -1e4, 3e4, 900.0, 500.0])
+def test_equal_keys_under_one_bias(value, Sq, Sk):
+    """One value in every bucket of a head, equal keys: the probabilities are those of no bias at all."""
+    torch = need_gpu()
+    print("equal keys", value, Sq, Sk, flush=True)
+    (q, k, v, do), gen = inputs(torch, 3, 1, Sq, Sk, 2, 1, 64)
+    k[:] = k[:, :1]
+    table = torch.randn(2, 16, generator=gen)
+    given = table.clone()
+    table[1], given[1] = 0.0, value
+    kw = dict(causal=1, max_distance=200)                          # no tile lies past it
+    against(trained(q, k, v, do, given, **kw), q, k, v, do, table, **kw)
