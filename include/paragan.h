@@ -311,8 +311,9 @@ int paragan_qknorm_bwd(paragan_ctx* ctx, const paragan_qknorm_desc* d,
  * m buckets of a side, n < m/2 (rounded down) has bucket n, and above
  *   m/2 + floor(log(n / (m/2)) / log(max_distance / (m/2)) * (m - m/2)),
  * the last one from max_distance on.  Entries may be -infinity (such keys
- * are not visible); the lowest finite value is a number like any other: the
- * sum of a score and its bias is formed in fp32, forward and backward.
+ * are not visible); the lowest finite value is a number like any other (past
+ * 2.3e38 in size all are one): the sum of a score and its bias is formed in
+ * fp32, forward and backward.
  * Element (b, s, h, c) of a tensor is at b * stride[0] + s * stride[1]
  * + h * stride[2] + c.  q, k, v may repeat through zero strides in the
  * forward; o, and in the backward q, k and v (whose strides dq, dk and dv

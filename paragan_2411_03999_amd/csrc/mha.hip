@@ -151,8 +151,11 @@ PG_DEV float max3(float a, float b, float c) {
   return r;
 }
 
-// a bias in log2 units; the lowest finite value stays finite (a row of nothing else is uniform)
-PG_DEV float log2_bias(float t) { return t < 0.f && t >= -FLT_MAX ? fmaxf(t * kL2E, -FLT_MAX) : t * kL2E; }
+// a bias in log2 units; the lowest and the largest finite values stay finite (a row of nothing else is uniform)
+PG_DEV float log2_bias(float t) {
+  const float x = t * kL2E;
+  return fabsf(t) <= FLT_MAX && fabsf(x) > FLT_MAX ? copysignf(FLT_MAX, t) : x;
+}
 
 // bias in log2 units at distance index e = rel + maxd + kMargin; distances past max_distance are its own
 PG_DEV float bias2_at(const MhaArgs& a, int h, int e) {

@@ -93,3 +93,22 @@ def test_equal_keys_under_one_bias(value, Sq, Sk):
     table[1], given[1] = 0.0, value
     kw = dict(causal=1, max_distance=200)                          # no tile lies past it
     against(trained(q, k, v, do, given, **kw), q, k, v, do, table, **kw)
+
+
+@pytest.mark.parametrize("value", [float(np.finfo(np.float32).max), 2.5e38])
+def test_largest_values_stay_finite(value):
+    """A value whose multiple by log2(e) passes float32: in one bucket it takes the whole row, in all of them the row is a
+    mean; forward, backward and the form for few rows."""
+    torch = need_gpu()
+    print("largest", value, flush=True)
+    (q, k, v, do), gen = inputs(torch, 4, 1, 150, 150, 2, 1, 64)
+    table = torch.randn(2, 8, generator=gen)
+    table[0], table[1, 0] = value, value
+    for causal in (0, 1):
+        kw = dict(causal=causal, max_distance=9)
+        against(trained(q, k, v, do, table, **kw), q, k, v, do, table, **kw)
+        o = torch.empty_like(q).cuda()
+        d = lib.mha_desc(q.cuda(), k.cuda(), v.cuda(), o, scale=0.125, n_buckets=8, **kw)
+        lib.paragan_mha_fwd(lib.Context(), d, q.cuda(), k.cuda(), v.cuda(), table.cuda(), None, None, o, None,
+                            lib.workspace(lib.paragan_mha_sizes(d)[1]))
+        against({"o": o}, q, k, v, do, table, **kw)
