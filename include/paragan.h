@@ -300,11 +300,12 @@ int paragan_qknorm_bwd(paragan_ctx* ctx, const paragan_qknorm_desc* d,
  * Key j is visible to it when j < len_k and
  *   causal: j <= p;   window > 0: |p - j| < window or j < n_sink.
  * A query that sees nothing gets zeros, one with a NaN among its scores gets
- * NaN.  Rows at and past len_q of o (and
- * of dq), rows at and past len_k of dk and dv, are written as zeros.  Keys
- * and values at and past len_k, and keys that no query of the call sees, may
- * hold anything; a NaN or infinity in a key or value that some query sees
- * can reach other queries.
+ * NaN.  Rows at and past len_q of o (and of dq), rows at and past len_k of dk
+ * and dv, are written as zeros.  Keys and values at and past len_k, and those
+ * that length, order and window let no query see, may hold anything and get
+ * zero gradients; a NaN or infinity in a key or value that some query sees
+ * can reach other queries, and one in a query or its dout other keys'
+ * gradients (also where a bias of -infinity hides the key).
  * bias (n_buckets > 0): table fp32 [Hq][n_buckets] at the bucket of j - p.
  * With causal all buckets are for distances n = p - j >= 0; otherwise the
  * first half is for n = p - j >= 0 and the second for n = j - p > 0.  Of the

@@ -926,6 +926,12 @@ PG_DEV void seen_by(const MhaArgs& a, const Seq& sq, int j0, int j1, int& i0, in
   i1 = min(hi - sq.off + 1, sq.lq);
   if (j1 < j0) i0 = i1 = 0;
 }
+// does some query see key j?  (Others may hold anything: as zeros they give nothing to a product with P = 0.)
+PG_DEV bool key_seen(const MhaArgs& a, const Seq& sq, int j) {
+  int i0, i1;
+  seen_by(a, sq, j, j, i0, i1);
+  return i0 < i1;
+}
 
 // item of a launch: key block, split, and the slot of its partials
 struct KItem { int bh, kb, z; int64_t slot; };
@@ -973,7 +979,7 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
   const int n0 = it.z * a.chunk, n1 = min(n0 + a.chunk, nt * a.G);
   if (it.z > 0 && n0 >= n1) return;
   const int kw = kblk + wv * 32, key = kw + lk;
-  const bool kv = key < sq.lk;
+  const bool kv = key_seen(a, sq, key);
   const int bl = BIAS ? bias_len(a) : 0;
   bf16x8 kf[KF], vf[VL ? 1 : KF];
 #pragma unroll
@@ -1001,7 +1007,7 @@ __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
 #pragma unroll
     for (int x = 0; x < 2; ++x)
       rv.issue(Vt + 64 * DT * x, a.v + b * a.vs[0] + (kblk + 64 * x) * a.vs[1] + hk * a.vs[2], a.vs[1], kblk + 64 * x, wv,
-               false, [&](int j) { return j < sq.lk; });
+               false, [&](int j) { return key_seen(a, sq, j); });
   }
   // step (h, ti): query head of the group, query tile
   auto load = [&](int hg, int ti, int bf) {

@@ -268,6 +268,35 @@ def test_mha_step_reads_only_what_is_seen():
         held("o", O, want["o"], want["tol.o"])
 
 
+@pytest.mark.parametrize("d", [32, 64, 96, 128])
+@pytest.mark.parametrize("Sq,Sk,causal,window,sink,lq,lk", [(65, 130, 0, 30, 3, None, None), (65, 330, 1, 30, 3, None, None),
+                                                            (20, 200, 1, 9, 0, [20, 3], [200, 77])])
+def test_mha_training_reads_only_what_is_seen(Sq, Sk, causal, window, sink, lq, lk, d):
+    """Keys and values that no query sees hold NaN and infinities, beside seen ones: their gradients are zeros."""
+    torch = need_gpu()
+    print("training, unseen keys", Sq, Sk, causal, window, sink, d, flush=True)
+    B, gen = 2, torch.Generator().manual_seed(51)
+    q, k, v, do = (torch.randn(B, s, h, d, generator=gen).bfloat16() for s, h in ((Sq, 2), (Sk, 1), (Sk, 1), (Sq, 2)))
+    n = lambda t: t.double().numpy()  # noqa: E731
+    want = T.mha(n(q), n(k), n(v), 0.125, causal, window, sink, len_q=lq, len_k=lk, dout=n(do))
+    for b in range(B):
+        nq, nk = (Sq, Sk) if lq is None else (lq[b], lk[b])
+        unseen = ~T.visible(np.arange(nq) + nk - nq, np.arange(Sk), nk, causal, window, sink).any(0)
+        assert 0 < unseen.sum() < Sk and not want["dk"][b, unseen].any()
+        k[b, unseen], v[b, unseen] = float("nan"), float("inf")
+    Q, K, V, DO = (t.cuda() for t in (q, k, v, do))
+    out = {"o": torch.empty_like(Q), "dq": torch.empty_like(Q), "dk": torch.empty_like(K), "dv": torch.empty_like(V)}
+    LQ, LK = (None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda") for x in (lq, lk))
+    ds = lib.mha_desc(Q, K, V, out["o"], scale=0.125, causal=causal, window=window, n_sink=sink)
+    sb, wb = lib.paragan_mha_sizes(ds)
+    ctx, ws, saved = lib.Context(), lib.workspace(wb), lib.workspace(sb)
+    lib.paragan_mha_fwd(ctx, ds, Q, K, V, None, LQ, LK, out["o"], saved, ws)
+    lib.paragan_mha_bwd(ctx, ds, Q, K, V, None, LQ, LK, out["o"], saved, DO, out["dq"], out["dk"], out["dv"], None, ws)
+    torch.cuda.synchronize()
+    for name, t in out.items():
+        held(name, t, want[name], want["tol." + name] + 1e-30)
+
+
 def test_mha_lowest_and_infinite_bias():
     """-infinity hides keys (all of them: zeros); the lowest finite value everywhere leaves the softmax of equal scores."""
     torch = need_gpu()
