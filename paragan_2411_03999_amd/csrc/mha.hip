@@ -383,7 +383,8 @@ __global__ __launch_bounds__(256, DT == 64 ? 4 : 2) void k_mha_fwd(MhaArgs a) {
 }
 
 // ------------------------------------------------------------- a few new tokens
-// The rows (query head of the group, query) of one key head form tiles of 32;
+// The rows (query, query head of the group) of one key head form tiles of 32,
+// of neighbouring queries, so that a tile visits no more keys than these see;
 // a block's 4 waves take tiles of 32 keys in turn, each with its own running
 // softmax, joined at the end; nsplit blocks share a long cache and leave
 // partials.  Bound by reading keys and values once: a wave has its next tile
@@ -430,10 +431,12 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Seq sq = seq_of(a, b);
   const int rho = rt * 32 + lq, R = a.G * a.Sq;
-  const int i = rho % a.Sq, h = hk * a.G + min(rho / a.Sq, a.G - 1);
+  const int i = rho / a.G, h = hk * a.G + rho - i * a.G;
   const bool live = rho < R && i < sq.lq;
-  Span<32> sp = span_of<32>(a, sq.lk, sq.off, sq.off + sq.lq - 1);
-  if (sq.lq == 0) sp.nt = 0;
+  // positions of the tile's queries
+  const int i0 = rt * 32 / a.G, p0 = sq.off + i0, p1 = sq.off + min((rt * 32 + 31) / a.G, sq.lq - 1);
+  Span<32> sp = span_of<32>(a, sq.lk, p0, p1);
+  if (i0 >= sq.lq) sp.nt = 0;
   const int per = (sp.nt + a.nsplit - 1) / a.nsplit, n1 = min(sp.nt, (z + 1) * per);
   const bf16_t* K = a.k + b * a.ks[0] + hk * a.ks[2];
   const bf16_t* V = a.v + b * a.vs[0] + hk * a.vs[2];
@@ -466,7 +469,7 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
     if (a.nb <= kStepTable) {
       float* tw = dyn + (bias_len(a) + 3) / 4;
       for (int e = tid; e < 32 * a.nb; e += 256)
-        tw[e] = a.table[(int64_t)(hk * a.G + min((rt * 32 + e / a.nb) / a.Sq, a.G - 1)) * a.nb + e % a.nb];
+        tw[e] = a.table[(int64_t)(hk * a.G + (rt * 32 + e / a.nb) % a.G) * a.nb + e % a.nb];
       tab = tw + lq * a.nb;
     }
     __syncthreads();
@@ -498,8 +501,8 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
     for (int t = 0; t < KF; ++t) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ld_row<NC>(ks, lq, 16 * t + 8 * g), qf[t], s, 0, 0, 0);
     float cm = cs, off = 0.f;
     if (BIAS) {
-      const float far = k0 < sq.off ? flo : fhi;
-      if ((k0 + 31 - sq.off > -a.maxd && k0 - (sq.off + sq.lq - 1) < a.maxd) || fabsf(far) >= kDeep) {
+      const float far = k0 < p0 ? flo : fhi;
+      if ((k0 + 31 - p0 > -a.maxd && k0 - p1 < a.maxd) || fabsf(far) >= kDeep) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int rel = min(max(k0 + acc_row(r, g) - i - sq.off, -a.maxd), a.maxd);
@@ -510,7 +513,7 @@ __global__ __launch_bounds__(256, DT <= 64 ? 2 : 1) void k_mha_step(MhaArgs a) {
         off = far;
       }
     }
-    if (!all_seen<32>(a, sq.lk, k0, sq.off, sq.off + sq.lq - 1)) hide(s, rw, k0, g);
+    if (!all_seen<32>(a, sq.lk, k0, p0, p1)) hide(s, rw, k0, g);
     float mb = s[0];
 #pragma unroll
     for (int r = 1; r < 15; r += 2) mb = max3(mb, s[r], s[r + 1]);
@@ -617,7 +620,7 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
     L += p[32 + lr] * f;
     s.x += v.x * f; s.y += v.y * f; s.z += v.z * f; s.w += v.w * f;
   }
-  const int i = rho % a.Sq, h = hk * a.G + rho / a.Sq;
+  const int i = rho / a.G, h = hk * a.G + rho - i * a.G;
   const Seq sq = seq_of(a, b);
   const bool any = i < sq.lq && L != 0.f;
   const float inv = any ? 1.f / L : 0.f;
@@ -1245,15 +1248,17 @@ int64_t row_tiles(const Mha& m) { return cdiv((int64_t)m.Sq * (m.Hq / m.Hk), 32)
 // few queries (the other form leaves three of its four waves idle: 64 x 16
 // queries of 32 / 8 heads x 128 over 1024 keys 93 us against 140; at 32
 // queries 46 against 44) and those whose row tiles leave CUs without work (128
-// queries of 8 heads over 32768 keys 58 us against 846; 512 tiles over 1024
-// keys 35 against 28).
+// queries of 8 heads x 64 over 32768 keys 39 us against 605, 8192 causal queries of
+// one head 53 against 128 and through a window of 16 5 against 8; 512 tiles
+// over 1024 keys 35 against 28).
 bool few_rows(const Mha& m) { return m.Sq <= 16 || (int64_t)m.B * m.Hk * row_tiles(m) <= 256; }
 
 // Splits of the keys: a block for each CU, at least 8 tiles in each (two a
 // wave): the caches are read at 5.1 TB/s then, and three blocks a CU lose 15 %
 // to the partials they leave.
 int step_splits(const Mha& m) {
-  const int64_t tiles = m.window ? std::min<int64_t>(cdiv(m.Sk, 32), cdiv((m.causal ? 1 : 2) * (int64_t)m.window + m.Sq, 32) + 1 + cdiv(m.n_sink, 32))
+  const int64_t queries = std::min<int64_t>(m.Sq, cdiv(32, m.Hq / m.Hk) + 1);   // of a row tile
+  const int64_t tiles = m.window ? std::min<int64_t>(cdiv(m.Sk, 32), cdiv((m.causal ? 1 : 2) * (int64_t)m.window + queries, 32) + 1 + cdiv(m.n_sink, 32))
                                  : cdiv(m.Sk, 32);
   return (int)std::max<int64_t>(1, std::min(256 / (m.B * m.Hk * row_tiles(m)), cdiv(tiles, 8)));
 }

@@ -268,6 +268,28 @@ def test_mha_step_reads_only_what_is_seen():
         held("o", O, want["o"], want["tol.o"])
 
 
+@pytest.mark.parametrize("S,Hq,Hk,causal", [(1024, 2, 2, 1), (1000, 4, 1, 1), (1003, 6, 2, 0)])
+def test_mha_few_heads_visit_only_their_window(S, Hq, Hk, causal):
+    """Long sequences of few heads take the form of few rows, whose tiles are of 32 rows: each walks the keys that its own
+    queries see, so that a NaN among the values reaches no query further off than a tile of rows and one of keys."""
+    torch = need_gpu()
+    print("few heads, window", S, Hq, Hk, causal, flush=True)
+    gen, w, at = torch.Generator().manual_seed(61), 16, 500
+    q, k, v = (torch.randn(1, S, h, 64, generator=gen).bfloat16().cuda() for h in (Hq, Hk, Hk))
+    o = [torch.empty_like(q) for _ in range(2)]
+    d = lib.mha_desc(q, k, v, o[0], scale=0.125, causal=causal, window=w)
+    ws = lib.workspace(lib.paragan_mha_sizes(d)[1])
+    for out in o:
+        lib.paragan_mha_fwd(lib.Context(), d, q, k, v, None, None, None, out, None, ws)
+        torch.cuda.synchronize()
+        v[0, at, 0] = float("nan")
+    i = torch.arange(S)
+    meets = (i - at >= 0 if causal else i - at > -w) & (i - at < w)
+    assert bool(torch.isnan(o[1][0, meets, 0]).all())
+    far = (i - at).abs() >= w + 64
+    assert torch.equal(o[0][0, far], o[1][0, far])
+
+
 @pytest.mark.parametrize("d", [32, 64, 96, 128])
 @pytest.mark.parametrize("Sq,Sk,causal,window,sink,lq,lk", [(65, 130, 0, 30, 3, None, None), (65, 330, 1, 30, 3, None, None),
                                                             (20, 200, 1, 9, 0, [20, 3], [200, 77])])
