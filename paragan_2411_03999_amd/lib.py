@@ -1,10 +1,12 @@
 """ctypes binding of libparagan (include/paragan.h).
 
 Argument marshalling only: every function here forwards to the C ABI of the
-same name; torch tensors supply device memory and the stream.  There is no
+same name; torch tensors supply device memory and the stream, and where a
+descriptor says how they lie they are held to it.  There is no
 fallback: if the in-tree libparagan.so is missing, loading raises.
 """
 import ctypes as C
+import math
 import os
 
 import numpy as np
@@ -226,7 +228,7 @@ def _typed(t, dtype, what):
         return None
     if str(t.dtype) != "torch." + dtype or not t.is_contiguous():
         raise ParaganError(EINVAL, "%s must be a contiguous %s tensor" % (what, dtype))
-    return C.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _f32(t, what):
@@ -235,6 +237,57 @@ def _f32(t, what):
 
 def _i32(t, what):
     return _typed(t, "int32", what)
+
+
+def _sized(t, dtype, what, *shape):
+    """As _typed, of a tensor on the GPU that holds (at least) an array of that shape, its rows as long."""
+    if t is None:
+        return None
+    p = _typed(t, dtype, what)
+    if t.numel() < math.prod(shape) or (len(shape) > 1 and t.dim() > 1 and t.shape[-1] != shape[-1]):
+        raise ParaganError(EINVAL, "%s must hold %s elements, not %s" % (what, list(shape), list(t.shape)))
+    if not t.is_cuda:
+        raise ParaganError(EINVAL, "%s must be on the GPU" % what)
+    return p
+
+
+def _merged(dims):
+    """(size, stride) pairs of a layout with neighbours that are walked as one joined: equal for layouts that reach the
+    same offsets in the same order."""
+    out = []
+    for n, st in dims:
+        if n == 1:
+            continue
+        if out and out[-1][1] == n * st:
+            out[-1] = (out[-1][0] * n, st)
+        else:
+            out.append((n, st))
+    return out
+
+
+def _placed(desc, dims, names, *tensors):
+    """Device pointers of tensors that lie where the descriptor says: dims(desc, name) gives the type and layout of each.
+    Types and layouts that were found right are noted with the descriptor's contents, so that a call in a loop only compares
+    them."""
+    key = [bytes(desc)]
+    for t in tensors:
+        key += (None,) if t is None else (t.dtype, t.shape, t.stride(), t.is_cuda)
+    try:
+        known = desc._known
+    except AttributeError:
+        known = desc._known = []
+    if key not in known:
+        for t, name in zip(tensors, names):
+            if t is None:
+                continue
+            dtype, layout = dims(desc, name)
+            if str(t.dtype) != "torch." + dtype or _merged(zip(t.shape, t.stride())) != _merged(layout):
+                raise ParaganError(EINVAL, "%s is not where the descriptor says: %s %s with strides %s, not %s of (size, stride) %s" %
+                                   (name, t.dtype, list(t.shape), list(t.stride()), dtype, layout))
+            if not t.is_cuda:
+                raise ParaganError(EINVAL, "%s must be on the GPU" % name)
+        known[:] = known[-7:] + [key]
+    return [None if t is None else t.data_ptr() for t in tensors]
 
 
 class Context:
@@ -446,16 +499,34 @@ def paragan_mha_sizes(desc):
     return _sizes(load().paragan_mha_sizes, desc)
 
 
+def _mha_dims(desc, name):
+    what = name.lstrip("d")
+    if what in ("q", "o", "out"):
+        S, H, st = desc.Sq, desc.Hq, desc.q_stride if what == "q" else desc.o_stride
+    else:
+        S, H, st = desc.Sk, desc.Hk, desc.k_stride if what == "k" else desc.v_stride
+    return "bfloat16", [(desc.B, st[0]), (S, st[1]), (H, st[2]), (desc.d, 1)]
+
+
+def _bias_table(desc, t, what):
+    return _sized(t, "float32", what, desc.Hq, desc.n_buckets) if desc.n_buckets else _f32(t, what)
+
+
 def paragan_mha_fwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, ws):
     """saved: None when no backward follows."""
-    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _f32(table, "table"),
-                                            _i32(len_q, "len_q"), _i32(len_k, "len_k"), _ptr(o), _ptr(saved), _ptr(ws)))
+    q, k, v, o = _placed(desc, _mha_dims, ("q", "k", "v", "o"), q, k, v, o)
+    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), q, k, v, _bias_table(desc, table, "table"),
+                                            _sized(len_q, "int32", "len_q", desc.B), _sized(len_k, "int32", "len_k", desc.B),
+                                            o, _ptr(saved), _ptr(ws)))
 
 
 def paragan_mha_bwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, dout, dq, dk, dv, dtable, ws):
-    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _ptr(v), _f32(table, "table"),
-                                            _i32(len_q, "len_q"), _i32(len_k, "len_k"), _ptr(o), _ptr(saved), _ptr(dout),
-                                            _ptr(dq), _ptr(dk), _ptr(dv), _f32(dtable, "dtable"), _ptr(ws)))
+    """dout lies as o, dq, dk and dv as q, k and v."""
+    q, k, v, o, dout, dq, dk, dv = _placed(desc, _mha_dims, ("q", "k", "v", "o", "dout", "dq", "dk", "dv"), q, k, v, o, dout,
+                                           dq, dk, dv)
+    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), q, k, v, _bias_table(desc, table, "table"),
+                                            _sized(len_q, "int32", "len_q", desc.B), _sized(len_k, "int32", "len_k", desc.B),
+                                            o, _ptr(saved), dout, dq, dk, dv, _bias_table(desc, dtable, "dtable"), _ptr(ws)))
 
 
 def paragan_gout_layout(desc):

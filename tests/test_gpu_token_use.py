@@ -319,3 +319,36 @@ def test_refused_calls_touch_nothing():
             lib.paragan_qknorm_fwd(ctx, nd, *args)
     torch.cuda.synchronize()
     assert bool((o == 3.0).all()) and all(bool((y == 3.0).all()) for y in bwd[9:13] + nf[6:])
+
+
+def test_tensors_elsewhere_than_the_descriptor_says_are_refused():
+    """Gradients of fused views in buffers of their own, lengths and tables of other sizes: refused, nothing written; other
+    views of the right memory are taken."""
+    torch = need_gpu()
+    ctx = lib.Context()
+    z = lambda *s, dt=torch.bfloat16: torch.full(s, 3.0, dtype=dt, device="cuda")  # noqa: E731
+    qkv, o = z(2, 9, 8, 32), z(2, 9, 4, 32)
+    q, k, v = qkv[:, :, :4], qkv[:, :, 4:6], qkv[:, :, 6:]
+    d = lib.mha_desc(q, k, v, o, scale=0.1, n_buckets=4, max_distance=8)
+    sb, wb = lib.paragan_mha_sizes(d)
+    ws, saved, tab = lib.workspace(wb), lib.workspace(sb), z(4, 4, dt=torch.float32)
+    lens = torch.full((2,), 9, dtype=torch.int32, device="cuda")
+    g, out = z(2, 9, 8, 32), [z(2, 9, 4, 32), z(2, 9, 2, 32), z(2, 9, 2, 32)]
+    bwd = [q, k, v, tab, lens, lens, o, saved, z(2, 9, 4, 32), g[:, :, :4], g[:, :, 4:6], g[:, :, 6:], z(4, 4, dt=torch.float32), ws]
+    for i, bad in ((9, out[0]), (10, out[1]), (11, out[2]), (8, g[:, :, :4]), (9, g[:, :, :4].float()), (0, out[0]), (6, g[:, :, :4]),
+                   (12, z(3, 4, dt=torch.float32)), (3, z(4, 3, dt=torch.float32)), (4, lens[:1]), (5, lens[:1]), (5, lens.cpu()),
+                   (9, g[:, :, :4].cpu())):
+        args = list(bwd)
+        args[i] = bad
+        with pytest.raises(lib.ParaganError):
+            lib.paragan_mha_bwd(ctx, d, *args)
+        if i < 7 and i != 6:
+            with pytest.raises(lib.ParaganError):
+                lib.paragan_mha_fwd(ctx, d, *args[:6], o, saved, ws)
+    torch.cuda.synchronize()
+    assert all(bool((t == 3.0).all()) for t in out + [g, o, bwd[12]])
+    lib.paragan_mha_fwd(ctx, d, *bwd[:6], o.view(18, 128), saved, ws)
+    lib.paragan_mha_bwd(ctx, d, *bwd[:6], o.view(18, 128), *bwd[7:])
+    torch.cuda.synchronize()
+    # equal values: o is their mean, 3; dq and dk vanish, and a key's dv is 3 a query head, each of 9 queries giving a ninth
+    assert bool((o == 3.0).all()) and bool((g[:, :, :6].abs() < 1.0).all()) and bool(((g[:, :, 6:] - 6.0).abs() < 0.1).all())

@@ -196,3 +196,40 @@ def test_descriptors_refuse_tensors_that_do_not_belong_together():
                  (z(4, 9, 16).transpose(0, 1), z(9, 2, 16))):
         with pytest.raises(lib.ParaganError):
             lib.qknorm_desc(q, k, rot=0, interleaved=0, n_pos=1, eps=1e-6)
+
+
+def test_mha_tensors_are_held_to_the_descriptor():
+    """Tensors that lie elsewhere than the descriptor says, or are too short, are refused before any pointer is passed on;
+    other views of the same memory are as good (these stop at not being on the GPU)."""
+    torch = pytest.importorskip("torch")
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
+    qkv = z(2, 7, 8, 32)                                          # one projection buffer, and its gradient's views
+    q, k, v, o = qkv[:, :, :4], qkv[:, :, 4:6], qkv[:, :, 6:], z(2, 7, 4, 32)
+    d = lib.mha_desc(q, k, v, o, scale=0.1, n_buckets=8, max_distance=20)
+    g = torch.empty_like(qkv)
+    put = lambda t, name: lib._placed(d, lib._mha_dims, (name,), t)[0]  # noqa: E731
+    for t, kind in ((g[:, :, :4], "dq"), (g[:, :, 4:6], "dk"), (g[:, :, 6:], "dv"), (torch.empty_like(o), "dout"), (q, "q"),
+                    (k, "k"), (v, "v"), (o, "o"), (z(14, 128), "o"), (z(2, 7, 2, 64), "o"), (z(2, 7, 1, 4, 32), "o")):
+        with pytest.raises(lib.ParaganError, match="on the GPU"):
+            put(t, kind)
+    for t, kind in ((torch.empty_like(k), "dk"), (z(2, 7, 2, 32), "dv"), (z(2, 7, 4, 32), "dq"), (g[:, :, :2], "q"),
+                    (g[:, :, :4], "o"), (z(2, 7, 4, 32, dt=torch.float32), "o"), (z(2, 7, 4, 32, dt=torch.float16), "o"),
+                    (z(2, 6, 4, 32), "o"), (z(2, 4, 7, 32).transpose(1, 2), "o"), (g[:1, :, :4], "q"), (z(2 * 7 * 4 * 32), "q")):
+        with pytest.raises(lib.ParaganError, match="not where the descriptor says"):
+            put(t, kind)
+    d.Sq, d.Sk = 6, 6                                             # a descriptor changed afterwards
+    with pytest.raises(lib.ParaganError, match="not where"):
+        put(torch.empty_like(o), "o")
+    one = lib.mha_desc(z(1, 1, 1, 8), z(1, 9, 1, 8), z(1, 9, 1, 8), z(1, 1, 1, 8), scale=1.0)
+    with pytest.raises(lib.ParaganError, match="on the GPU"):
+        lib._placed(one, lib._mha_dims, ("o",), z(8))
+    with pytest.raises(lib.ParaganError, match="on the GPU"):     # strides of single elements mean nothing
+        lib._placed(one, lib._mha_dims, ("o",), z(3, 5, 2, 8)[:1, :1, :1])
+    f = torch.float32
+    for t, shape in ((z(4, 8, dt=f), (4, 8)), (z(32, dt=f), (4, 8)), (z(6, 8, dt=f), (4, 8)), (z(9, dt=f), (9,)), (z(0, dt=f), (0,))):
+        with pytest.raises(lib.ParaganError, match="on the GPU"):
+            lib._sized(t, "float32", "table", *shape)
+    for t, shape in ((z(3, 8, dt=f), (4, 8)), (z(8, 4, dt=f), (4, 8)), (z(4, 9, dt=f), (4, 8)), (z(31, dt=f), (4, 8)), (z(8, dt=f), (9,))):
+        with pytest.raises(lib.ParaganError, match="must hold"):
+            lib._sized(t, "float32", "table", *shape)
+    assert lib._sized(None, "float32", "table", 4) is None and put(None, "q") is None
