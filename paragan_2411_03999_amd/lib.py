@@ -6,7 +6,6 @@ descriptor says how they lie they are held to it.  There is no
 fallback: if the in-tree libparagan.so is missing, loading raises.
 """
 import ctypes as C
-import math
 import os
 
 import numpy as np
@@ -222,35 +221,6 @@ def _ptr(t):
     return C.c_void_p(t.data_ptr())
 
 
-def _typed(t, dtype, what):
-    """As _ptr, of a contiguous tensor of one type (whose elements the library reads as such)."""
-    if t is None:
-        return None
-    if str(t.dtype) != "torch." + dtype or not t.is_contiguous():
-        raise ParaganError(EINVAL, "%s must be a contiguous %s tensor" % (what, dtype))
-    return t.data_ptr()
-
-
-def _f32(t, what):
-    return _typed(t, "float32", what)
-
-
-def _i32(t, what):
-    return _typed(t, "int32", what)
-
-
-def _sized(t, dtype, what, *shape):
-    """As _typed, of a tensor on the GPU that holds (at least) an array of that shape, its rows as long."""
-    if t is None:
-        return None
-    p = _typed(t, dtype, what)
-    if t.numel() < math.prod(shape) or (len(shape) > 1 and t.dim() > 1 and t.shape[-1] != shape[-1]):
-        raise ParaganError(EINVAL, "%s must hold %s elements, not %s" % (what, list(shape), list(t.shape)))
-    if not t.is_cuda:
-        raise ParaganError(EINVAL, "%s must be on the GPU" % what)
-    return p
-
-
 def _merged(dims):
     """(size, stride) pairs of a layout with neighbours that are walked as one joined: equal for layouts that reach the
     same offsets in the same order."""
@@ -265,11 +235,26 @@ def _merged(dims):
     return out
 
 
+def _hold(name, t, dtype, layout, row=0):
+    """Refuses a tensor that is not of that type, not on the GPU or does not lie so: a list of (size, stride), or a contiguous
+    array of that many elements at least, in rows of `row` if it has rows."""
+    if isinstance(layout, int):
+        if str(t.dtype) != "torch." + dtype or not t.is_contiguous():
+            raise ParaganError(EINVAL, "%s must be a contiguous %s tensor" % (name, dtype))
+        if t.numel() < layout or (row and t.dim() > 1 and t.shape[-1] != row):
+            raise ParaganError(EINVAL, "%s must hold %d elements%s, not %s" %
+                               (name, layout, " in rows of %d" % row if row else "", list(t.shape)))
+    elif str(t.dtype) != "torch." + dtype or _merged(zip(t.shape, t.stride())) != _merged(layout):
+        raise ParaganError(EINVAL, "%s is not where the descriptor says: %s %s with strides %s, not %s of (size, stride) %s" %
+                           (name, t.dtype, list(t.shape), list(t.stride()), dtype, layout))
+    if not t.is_cuda:
+        raise ParaganError(EINVAL, "%s must be on the GPU" % name)
+
+
 def _placed(desc, dims, names, *tensors):
-    """Device pointers of tensors that lie where the descriptor says: dims(desc, name) gives the type and layout of each.
-    Types and layouts that were found right are noted with the descriptor's contents, so that a call in a loop only compares
-    them."""
-    key = [bytes(desc)]
+    """Device pointers of tensors that are what the descriptor says (dims(desc, name): what _hold asks of each).  Types and
+    layouts that were found right are noted with the descriptor's contents, so that a call in a loop only compares them."""
+    key = [bytes(desc), names]
     for t in tensors:
         key += (None,) if t is None else (t.dtype, t.shape, t.stride(), t.is_cuda)
     try:
@@ -278,14 +263,8 @@ def _placed(desc, dims, names, *tensors):
         known = desc._known = []
     if key not in known:
         for t, name in zip(tensors, names):
-            if t is None:
-                continue
-            dtype, layout = dims(desc, name)
-            if str(t.dtype) != "torch." + dtype or _merged(zip(t.shape, t.stride())) != _merged(layout):
-                raise ParaganError(EINVAL, "%s is not where the descriptor says: %s %s with strides %s, not %s of (size, stride) %s" %
-                                   (name, t.dtype, list(t.shape), list(t.stride()), dtype, layout))
-            if not t.is_cuda:
-                raise ParaganError(EINVAL, "%s must be on the GPU" % name)
+            if t is not None:
+                _hold(name, t, *dims(desc, name))
         known[:] = known[-7:] + [key]
     return [None if t is None else t.data_ptr() for t in tensors]
 
@@ -441,6 +420,9 @@ def qknorm_desc(q, k, qo=None, ko=None, *, rot, interleaved, n_pos, eps):
         raise ParaganError(EINVAL, "qknorm: q and k differ in tokens, head width or type")
     if q.dtype not in (torch.bfloat16, torch.float32):
         raise ParaganError(EINVAL, "qknorm: q must be bfloat16 or float32")
+    for t, like in ((qo, q), (ko, k)):
+        if t is not None and (t.shape != like.shape or t.dtype != like.dtype):
+            raise ParaganError(EINVAL, "qknorm: an output differs from its input in shape or type")
     for t in (q, k, qo, ko):
         if t is not None and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
             raise ParaganError(EINVAL, "qknorm: the heads of a token must lie side by side")
@@ -461,17 +443,29 @@ def paragan_qknorm_ws_size(desc):
     return n.value
 
 
+def _qknorm_dims(desc, name):
+    if name in ("table", "pos"):
+        return ("float32", desc.n_pos * desc.rot) if name == "table" else ("int32", desc.T)
+    if "gain" in name:
+        return "float32", desc.d
+    H, ld = {"q": (desc.Hq, desc.ldq), "dq": (desc.Hq, desc.ldq), "k": (desc.Hk, desc.ldk), "dk": (desc.Hk, desc.ldk),
+             "qo": (desc.Hq, desc.ldqo), "dqo": (desc.Hq, desc.ldqo), "ko": (desc.Hk, desc.ldko), "dko": (desc.Hk, desc.ldko)}[name]
+    return "bfloat16" if desc.dtype == BF16 else "float32", [(desc.T, ld), (H, desc.d), (desc.d, 1)]
+
+
+_QKNORM_FWD = ("q", "k", "gain_q", "gain_k", "table", "pos", "qo", "ko")
+_QKNORM_BWD = _QKNORM_FWD[:6] + ("dqo", "dko", "dq", "dk", "dgain_q", "dgain_k")
+
+
 def paragan_qknorm_fwd(ctx, desc, q, k, gain_q, gain_k, table, pos, qo, ko):
-    return ctx.check(load().paragan_qknorm_fwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _f32(gain_q, "gain_q"),
-                                               _f32(gain_k, "gain_k"), _f32(table, "table"), _i32(pos, "pos"), _ptr(qo),
-                                               _ptr(ko)))
+    return ctx.check(load().paragan_qknorm_fwd(ctx.h, C.byref(desc), *_placed(
+        desc, _qknorm_dims, _QKNORM_FWD, q, k, gain_q, gain_k, table, pos, qo, ko)))
 
 
 def paragan_qknorm_bwd(ctx, desc, q, k, gain_q, gain_k, table, pos, dqo, dko, dq, dk, dgain_q, dgain_k, ws):
-    return ctx.check(load().paragan_qknorm_bwd(ctx.h, C.byref(desc), _ptr(q), _ptr(k), _f32(gain_q, "gain_q"),
-                                               _f32(gain_k, "gain_k"), _f32(table, "table"), _i32(pos, "pos"), _ptr(dqo),
-                                               _ptr(dko), _ptr(dq), _ptr(dk), _f32(dgain_q, "dgain_q"),
-                                               _f32(dgain_k, "dgain_k"), _ptr(ws)))
+    """dqo and dko lie as the outputs, dq and dk as q and k."""
+    return ctx.check(load().paragan_qknorm_bwd(ctx.h, C.byref(desc), *_placed(
+        desc, _qknorm_dims, _QKNORM_BWD, q, k, gain_q, gain_k, table, pos, dqo, dko, dq, dk, dgain_q, dgain_k), _ptr(ws)))
 
 
 def mha_desc(q, k, v, o, *, scale, causal=False, window=0, n_sink=0, n_buckets=0, max_distance=0):
@@ -500,6 +494,10 @@ def paragan_mha_sizes(desc):
 
 
 def _mha_dims(desc, name):
+    if name in ("len_q", "len_k"):
+        return "int32", desc.B
+    if name in ("table", "dtable"):
+        return "float32", desc.Hq * desc.n_buckets, desc.n_buckets
     what = name.lstrip("d")
     if what in ("q", "o", "out"):
         S, H, st = desc.Sq, desc.Hq, desc.q_stride if what == "q" else desc.o_stride
@@ -508,25 +506,20 @@ def _mha_dims(desc, name):
     return "bfloat16", [(desc.B, st[0]), (S, st[1]), (H, st[2]), (desc.d, 1)]
 
 
-def _bias_table(desc, t, what):
-    return _sized(t, "float32", what, desc.Hq, desc.n_buckets) if desc.n_buckets else _f32(t, what)
+_MHA_FWD = ("q", "k", "v", "table", "len_q", "len_k", "o")
+_MHA_BWD = _MHA_FWD + ("dout", "dq", "dk", "dv", "dtable")
 
 
 def paragan_mha_fwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, ws):
     """saved: None when no backward follows."""
-    q, k, v, o = _placed(desc, _mha_dims, ("q", "k", "v", "o"), q, k, v, o)
-    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), q, k, v, _bias_table(desc, table, "table"),
-                                            _sized(len_q, "int32", "len_q", desc.B), _sized(len_k, "int32", "len_k", desc.B),
-                                            o, _ptr(saved), _ptr(ws)))
+    return ctx.check(load().paragan_mha_fwd(ctx.h, C.byref(desc), *_placed(
+        desc, _mha_dims, _MHA_FWD, q, k, v, table, len_q, len_k, o), _ptr(saved), _ptr(ws)))
 
 
 def paragan_mha_bwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, dout, dq, dk, dv, dtable, ws):
     """dout lies as o, dq, dk and dv as q, k and v."""
-    q, k, v, o, dout, dq, dk, dv = _placed(desc, _mha_dims, ("q", "k", "v", "o", "dout", "dq", "dk", "dv"), q, k, v, o, dout,
-                                           dq, dk, dv)
-    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), q, k, v, _bias_table(desc, table, "table"),
-                                            _sized(len_q, "int32", "len_q", desc.B), _sized(len_k, "int32", "len_k", desc.B),
-                                            o, _ptr(saved), dout, dq, dk, dv, _bias_table(desc, dtable, "dtable"), _ptr(ws)))
+    p = _placed(desc, _mha_dims, _MHA_BWD, q, k, v, table, len_q, len_k, o, dout, dq, dk, dv, dtable)
+    return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), *p[:7], _ptr(saved), *p[7:], _ptr(ws)))
 
 
 def paragan_gout_layout(desc):

@@ -352,3 +352,36 @@ def test_tensors_elsewhere_than_the_descriptor_says_are_refused():
     torch.cuda.synchronize()
     # equal values: o is their mean, 3; dq and dk vanish, and a key's dv is 3 a query head, each of 9 queries giving a ninth
     assert bool((o == 3.0).all()) and bool((g[:, :, :6].abs() < 1.0).all()) and bool(((g[:, :, 6:] - 6.0).abs() < 0.1).all())
+
+
+def test_norm_tensors_elsewhere_than_the_descriptor_says_are_refused():
+    torch = need_gpu()
+    ctx = lib.Context()
+    z = lambda *s, dt=torch.bfloat16: torch.full(s, 3.0, dtype=dt, device="cuda")  # noqa: E731
+    f = torch.float32
+    x, g = z(6, 9, 16), z(6, 9, 16)
+    d = lib.qknorm_desc(x[:, :4], x[:, 4:6], rot=16, interleaved=0, n_pos=5, eps=1e-6)
+    pos = torch.arange(6, dtype=torch.int32, device="cuda") % 5
+    turn = torch.zeros(5, 8, 2, device="cuda")
+    turn[:, :, 0] = 1.0
+    fwd = [x[:, :4], x[:, 4:6], z(16, dt=f), z(16, dt=f), turn, pos, z(6, 4, 16), z(6, 2, 16)]
+    for i, bad in ((0, z(6, 4, 16)), (1, z(6, 2, 16)), (2, z(8, dt=f)), (3, z(15, dt=f)), (4, turn[:4]), (5, pos[:5]), (5, pos.cpu()),
+                   (6, g[:, :4]), (7, z(5, 2, 16)), (6, z(6, 4, 16, dt=f)), (7, z(6, 2, 16).cpu())):
+        args = list(fwd)
+        args[i] = bad
+        with pytest.raises(lib.ParaganError):
+            lib.paragan_qknorm_fwd(ctx, d, *args)
+    bwd = fwd[:6] + [z(6, 4, 16), z(6, 2, 16), g[:, :4], g[:, 4:6], z(16, dt=f), z(16, dt=f), lib.workspace(lib.paragan_qknorm_ws_size(d))]
+    for i, bad in ((6, g[:, :4]), (7, z(6, 2, 16, dt=f)), (8, z(6, 4, 16)), (9, z(6, 2, 16)), (10, z(8, dt=f)), (11, z(15, dt=f)),
+                   (8, x[:5, :4])):
+        args = list(bwd)
+        args[i] = bad
+        with pytest.raises(lib.ParaganError):
+            lib.paragan_qknorm_bwd(ctx, d, *args)
+    torch.cuda.synchronize()
+    assert all(bool((t == 3.0).all()) for t in fwd[6:] + [g, bwd[10], bwd[11]])
+    # equal elements of 3 under a gain of 3 come out as 3 times their sign, and their gradient vanishes
+    lib.paragan_qknorm_fwd(ctx, d, *fwd[:6], fwd[6].view(2, 3, 4, 16), fwd[7].view(6, 32))
+    lib.paragan_qknorm_bwd(ctx, d, *bwd)
+    torch.cuda.synchronize()
+    assert all(bool(((t - 3.0).abs() < 0.02).all()) for t in fwd[6:]) and bool((g[:, :6].abs() < 1e-3).all()) and bool((g[:, 6:] == 3.0).all())

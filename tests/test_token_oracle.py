@@ -226,10 +226,43 @@ def test_mha_tensors_are_held_to_the_descriptor():
     with pytest.raises(lib.ParaganError, match="on the GPU"):     # strides of single elements mean nothing
         lib._placed(one, lib._mha_dims, ("o",), z(3, 5, 2, 8)[:1, :1, :1])
     f = torch.float32
-    for t, shape in ((z(4, 8, dt=f), (4, 8)), (z(32, dt=f), (4, 8)), (z(6, 8, dt=f), (4, 8)), (z(9, dt=f), (9,)), (z(0, dt=f), (0,))):
+    for t, n in ((z(4, 8, dt=f), (32, 8)), (z(32, dt=f), (32, 8)), (z(6, 8, dt=f), (32, 8)), (z(9, dt=f), (9,)), (z(0, dt=f), (0,))):
         with pytest.raises(lib.ParaganError, match="on the GPU"):
-            lib._sized(t, "float32", "table", *shape)
-    for t, shape in ((z(3, 8, dt=f), (4, 8)), (z(8, 4, dt=f), (4, 8)), (z(4, 9, dt=f), (4, 8)), (z(31, dt=f), (4, 8)), (z(8, dt=f), (9,))):
+            lib._hold("table", t, "float32", *n)
+    for t, n in ((z(3, 8, dt=f), (32, 8)), (z(8, 4, dt=f), (32, 8)), (z(4, 9, dt=f), (32, 8)), (z(31, dt=f), (32, 8)), (z(8, dt=f), (9,))):
         with pytest.raises(lib.ParaganError, match="must hold"):
-            lib._sized(t, "float32", "table", *shape)
-    assert lib._sized(None, "float32", "table", 4) is None and put(None, "q") is None
+            lib._hold("table", t, "float32", *n)
+    assert put(None, "q") is None
+
+
+def test_qknorm_tensors_are_held_to_the_descriptor():
+    torch = pytest.importorskip("torch")
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
+    x = z(6, 9, 16)                                               # q of 4 heads, k of 2, others'
+    q, k = x[:, :4], x[:, 4:6]
+    kw = dict(rot=16, interleaved=0, n_pos=5, eps=1e-6)
+    for bad in ((z(6, 4, 16, dt=torch.float32), None), (z(5, 4, 16), None), (z(6, 2, 16), None), (None, z(6, 4, 16)),
+                (None, z(6, 2, 8)), (None, z(6, 2, 16, dt=torch.float16))):
+        with pytest.raises(lib.ParaganError, match="an output differs"):
+            lib.qknorm_desc(q, k, *bad, **kw)
+    d = lib.qknorm_desc(q, k, **kw)
+    put = lambda t, name: lib._placed(d, lib._qknorm_dims, (name,), t)  # noqa: E731
+    for t, name in ((q, "q"), (k, "k"), (torch.empty_like(x)[:, :4], "dq"), (torch.empty_like(x)[:, 4:6], "dk"), (z(6, 4, 16), "qo"),
+                    (z(2, 3, 4, 16), "dqo"), (z(6, 32), "ko"), (z(6, 1, 2, 16), "dko"), (z(2, 3, 9, 16)[:, :, :4], "dq")):
+        with pytest.raises(lib.ParaganError, match="on the GPU"):
+            put(t, name)
+    for t, name in ((z(6, 4, 16), "dq"), (z(6, 2, 16), "dk"), (x[:, :4], "qo"), (z(6, 4, 16), "ko"), (z(5, 4, 16), "qo"),
+                    (z(6, 4, 16, dt=torch.float32), "dqo"), (z(2, 4, 9, 16)[:, :3, :4], "dq"), (z(4, 6, 16).transpose(0, 1), "qo")):
+        with pytest.raises(lib.ParaganError, match="not where the descriptor says"):
+            put(t, name)
+    f = torch.float32
+    for name, t in (("gain_q", z(8, dt=f)), ("gain_k", z(15, dt=f)), ("dgain_q", z(2, dt=f)), ("table", z(4, 8, 2, dt=f)),
+                    ("pos", z(5, dt=torch.int32))):
+        with pytest.raises(lib.ParaganError, match="must hold"):
+            put(t, name)
+    for name, t in (("gain_q", z(16, dt=f)), ("dgain_k", z(16, dt=f)), ("table", z(5, 8, 2, dt=f)), ("pos", z(9, dt=torch.int32))):
+        with pytest.raises(lib.ParaganError, match="on the GPU"):
+            put(t, name)
+    one = lib.qknorm_desc(z(1, 3, 8), z(1, 1, 8), rot=0, interleaved=0, n_pos=1, eps=1e-6)
+    with pytest.raises(lib.ParaganError, match="on the GPU"):      # a single token has no stride to speak of
+        lib._placed(one, lib._qknorm_dims, ("q",), z(4, 9, 8)[:1, :3])
