@@ -272,7 +272,7 @@ typedef struct {
   int32_t interleaved;             /* pair order, 0 or 1 */
   int32_t n_pos;                   /* rows of the table, >= 1 */
   int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: q, k, outputs, gradients */
-  float eps;                       /* > 0 */
+  float eps;                       /* > 0, no smaller than the least normal float (1.2e-38) */
   int64_t ldq, ldk, ldqo, ldko;    /* >= heads * d */
 } paragan_qknorm_desc;
 

@@ -7,6 +7,7 @@
 #include "blocks.hpp"
 #include "net.hpp"
 #include "token.hpp"
+#include <cfloat>
 #include <cmath>
 
 using namespace pg;
@@ -468,7 +469,8 @@ static QkNorm make_qk(const paragan_qknorm_desc* d) {
   PG_CHECK(d->interleaved == 0 || d->interleaved == 1, "qknorm: interleaved must be 0 or 1");
   PG_CHECK(d->n_pos >= 1, "qknorm: n_pos must be >= 1");
   PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "qknorm: dtype must be PARAGAN_BF16 or PARAGAN_F32");
-  PG_CHECK(d->eps > 0.f && std::isfinite(d->eps), "qknorm: eps must be > 0");
+  // a smaller one is zero to the reciprocal root: infinity, and NaN where a row is zero or padding
+  PG_CHECK(d->eps >= FLT_MIN && std::isfinite(d->eps), "qknorm: eps must be > 0 and no smaller than the least normal float");
   const int64_t wq = (int64_t)d->Hq * d->d, wk = (int64_t)d->Hk * d->d;
   PG_CHECK(d->ldq >= wq && d->ldqo >= wq && d->ldk >= wk && d->ldko >= wk, "qknorm: a token stride is below heads * d");
   PG_CHECK(d->ldq % 8 == 0 && d->ldqo % 8 == 0 && d->ldk % 8 == 0 && d->ldko % 8 == 0,

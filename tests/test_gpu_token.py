@@ -132,6 +132,28 @@ def test_qknorm_padding_is_not_read():
     assert bool(torch.isfinite(dg).all())
 
 
+def test_qknorm_least_eps():
+    """Zero rows and padding under the least eps taken: zeros, and gradients of zero rows that are r t."""
+    torch = need_gpu()
+    x = torch.zeros(4, 2, 16, device="cuda")
+    x[1] = 1.0
+    pos = torch.tensor([0, 0, 0, -1], dtype=torch.int32, device="cuda")
+    one, out, dx, dg = torch.ones(16, device="cuda"), torch.empty(2, 4, 2, 16, device="cuda"), torch.empty(2, 4, 2, 16, device="cuda"), torch.empty(2, 16, device="cuda")
+    eps = float(np.finfo(np.float32).tiny)
+    d = lib.qknorm_desc(x, x, rot=0, interleaved=0, n_pos=1, eps=eps)
+    ctx = lib.Context()
+    lib.paragan_qknorm_fwd(ctx, d, x, x, one, one, None, pos, out[0], out[1])
+    dy = torch.full_like(x, 2.0 ** -20)
+    lib.paragan_qknorm_bwd(ctx, d, x, x, one, one, None, pos, dy, dy, dx[0], dx[1], dg[0], dg[1],
+                           lib.workspace(lib.paragan_qknorm_ws_size(d)))
+    torch.cuda.synchronize()
+    for t in range(2):
+        assert not out[t][[0, 2, 3]].any() and bool((out[t][1] == 1.0).all())
+        # 2^-20 / sqrt(2^-126) = 2^43, a reciprocal root being off by a step at most
+        assert bool(((dx[t][[0, 2]] / 2.0 ** 43 - 1).abs() <= 2 * 2.0 ** -23).all()) and not dx[t][3].any()
+    assert bool(torch.isfinite(dg).all())
+
+
 # ------------------------------------------------------------- attention
 def mha_case(B, Sq, Sk, Hq, Hk, d, causal=0, window=0, sink=0, nb=0, maxd=0, lq=None, lk=None, train=True, seed=0,
              layout="fused", scale=None, tab=None, poison=True):

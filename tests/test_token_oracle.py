@@ -266,3 +266,10 @@ def test_qknorm_tensors_are_held_to_the_descriptor():
     one = lib.qknorm_desc(z(1, 3, 8), z(1, 1, 8), rot=0, interleaved=0, n_pos=1, eps=1e-6)
     with pytest.raises(lib.ParaganError, match="on the GPU"):      # a single token has no stride to speak of
         lib._placed(one, lib._qknorm_dims, ("q",), z(4, 9, 8)[:1, :3])
+
+
+def test_qknorm_refuses_an_eps_that_the_hardware_takes_for_zero(L):
+    least = float(np.finfo(np.float32).tiny)
+    assert lib.paragan_qknorm_check(qk(eps=least)) == lib.OK
+    for eps in (np.nextafter(np.float32(least), np.float32(0)), 1e-39, 1e-45, -least):
+        assert lib.paragan_qknorm_check(qk(eps=float(eps))) == lib.EINVAL, eps
