@@ -217,26 +217,28 @@ __global__ __launch_bounds__(256, BWD ? 2 : 4) void k_qknorm(QkArgs a) {
       }
     }
   }
-  if (BWD) {   // gain partials of the block: the groups' sums in group order
+  if (BWD) {   // gain partials of the block: the groups' sums in group order, in 64 bits
     __shared__ float sh[256 * 8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) sh[tid * 8 + e] = dg[e];
     __syncthreads();
     if (tid < a.d) {
-      float s = 0.f;
+      double s = 0.0;
       for (int j = 0; j < GPB; ++j) s += sh[j * LPH * 8 + tid];
-      a.part[((int64_t)(blockIdx.y ? a.side[0].grid : 0) + blockIdx.x) * a.d + tid] = s;
+      a.part[((int64_t)(blockIdx.y ? a.side[0].grid : 0) + blockIdx.x) * a.d + tid] = (float)s;
     }
   }
 }
 
 // dg[c] = sum over the blocks of q (blockIdx.y = 0) or k of part[block][c]:
-// 16 columns x 64 row lanes a block, the rows of a lane and the lanes in order
+// 16 columns x 64 row lanes a block, the rows of a lane and the lanes in
+// order, in 64 bits (the sums of a gradient over all tokens and heads mostly
+// cancel, and the joins would lose more of them than the sums in the registers do)
 __global__ __launch_bounds__(1024) void k_qknorm_gain(const float* part, int nq, int nk, int d, float* dgq, float* dgk) {
-  __shared__ float sh[64][17];
+  __shared__ double sh[64][17];
   const int c = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4, nb = blockIdx.y ? nk : nq;
   const float* p = part + (blockIdx.y ? (int64_t)nq * d : 0);
-  float s = 0.f;
+  double s = 0.0;
   if (c < d) {
 #pragma unroll 8
     for (int b = r; b < nb; b += 64) s += p[(int64_t)b * d + c];
@@ -244,10 +246,10 @@ __global__ __launch_bounds__(1024) void k_qknorm_gain(const float* part, int nq,
   sh[r][threadIdx.x & 15] = s;
   __syncthreads();
   if (threadIdx.x >= 16 || c >= d) return;
-  float v = 0.f;
+  double v = 0.0;
 #pragma unroll
   for (int j = 0; j < 64; ++j) v += sh[j][threadIdx.x];
-  (blockIdx.y ? dgk : dgq)[c] = v;
+  (blockIdx.y ? dgk : dgq)[c] = (float)v;
 }
 
 int lanes_per_head(int d) {

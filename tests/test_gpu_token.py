@@ -132,6 +132,26 @@ def test_qknorm_padding_is_not_read():
     assert bool(torch.isfinite(dg).all())
 
 
+def test_qknorm_gain_sums_beside_a_large_term():
+    """Gain gradients that are a sum over tokens, one of them 2^26: every block's partial but one is 256 x 3/256 = 3, below
+    half a step of the large one, so joining in 32 bits loses those that meet it.  The blocks' partials are rounded once
+    (the large one by 4 at most) and so is the result (by 4)."""
+    torch = need_gpu()
+    T_, d = 131072, 8
+    print("gain sums", T_, flush=True)
+    x = torch.ones(T_, 1, d, device="cuda")
+    dy = torch.full((T_, 1, d), 3.0 / 256, device="cuda")
+    dy[0] = 2.0 ** 26
+    one, dg = torch.ones(d, device="cuda"), torch.empty(2, d, device="cuda")
+    ds = lib.qknorm_desc(x, x, rot=0, interleaved=0, n_pos=1, eps=1e-12)          # 1 / sqrt(1 + 1e-12) is 1 in float32
+    lib.paragan_qknorm_bwd(lib.Context(), ds, x, x, one, one, None, None, dy, dy, torch.empty_like(x), torch.empty_like(x), dg[0],
+                           dg[1], lib.workspace(lib.paragan_qknorm_ws_size(ds)))
+    torch.cuda.synchronize()
+    want = 2.0 ** 26 + (T_ - 1) * 3.0 / 256
+    print("  off by", (dg.double() - want).abs().max().item(), flush=True)
+    assert bool(((dg.double() - want).abs() <= 8.0).all())
+
+
 def test_qknorm_least_eps():
     """Zero rows and padding under the least eps taken: zeros, and gradients of zero rows that are r t."""
     torch = need_gpu()
