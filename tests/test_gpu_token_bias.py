@@ -112,3 +112,61 @@ def test_largest_values_stay_finite(value):
         lib.paragan_mha_fwd(lib.Context(), d, q.cuda(), k.cuda(), v.cuda(), table.cuda(), None, None, o, None,
                             lib.workspace(lib.paragan_mha_sizes(d)[1]))
         against({"o": o}, q, k, v, do, table, **kw)
+
+
+@pytest.mark.parametrize("case", [
+    # Sq, Hq, Hk, d, causal, window, sink, nb, maxd, masked bucket
+    (2100, 4, 1, 64, 1, 64, 5, 16, 40, 0), (700, 6, 2, 96, 1, 0, 0, 256, 512, 200), (600, 2, 2, 128, 0, 100, 130, 130, 300, 129),
+    (130, 8, 1, 40, 1, 1, 0, 8, 20, 0)])
+def test_masked_bucket_in_split_blocks_and_wide_tables(case):
+    """A lowest-value bucket of one head of a group: key blocks that are split, tables wider than a wave, a far bucket, and
+    rows (window of one) that see it alone."""
+    torch = need_gpu()
+    Sq, Hq, Hk, d, causal, window, sink, nb, maxd, bucket = case
+    print("masked bucket", case, flush=True)
+    (q, k, v, do), gen = inputs(torch, 6, 1, Sq, Sq, Hq, Hk, d)
+    table = torch.randn(Hq, nb, generator=gen)
+    table[Hq - 1, bucket] = LOWEST
+    kw = dict(causal=causal, window=window, n_sink=sink, max_distance=maxd)
+    against(trained(q, k, v, do, table, **kw), q, k, v, do, table, **kw)
+
+
+def test_masked_bias_captured_and_replayed():
+    """A captured pass whose table changes between replays, from ordinary values to masks and back."""
+    torch = need_gpu()
+    (q, k, v, do), gen = inputs(torch, 7, 1, 170, 170, 2, 1, 64)
+    side = torch.cuda.Stream()
+    ctx = lib.Context(side)
+    q, k, v, do, table = (t.cuda() for t in (q, k, v, do, torch.randn(2, 8, generator=gen)))
+    out = [torch.empty_like(t) for t in (q, q, k, v, table)]
+    d = lib.mha_desc(q, k, v, out[0], scale=0.125, causal=1, n_buckets=8, max_distance=30)
+    sb, wb = lib.paragan_mha_sizes(d)
+    saved, ws = lib.workspace(sb), lib.workspace(wb)
+
+    def run():
+        lib.paragan_mha_fwd(ctx, d, q, k, v, table, None, None, out[0], saved, ws)
+        lib.paragan_mha_bwd(ctx, d, q, k, v, table, None, None, out[0], saved, do, out[1], out[2], out[3], out[4], ws)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        run()
+    base = table.clone()
+    for rep, value in enumerate((LOWEST, None, -1e9, None)):
+        table.copy_(base)
+        if value is not None:
+            table[:, 0] = value
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            run()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in out]
+        for t in out:
+            t.fill_(9.0)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(out, want)), rep
