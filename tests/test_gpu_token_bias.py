@@ -14,7 +14,7 @@ from oracle import token as T
 from paragan_2411_03999_amd import lib
 
 from .parity import need_gpu
-from .test_gpu_token import held
+from .test_gpu_token import held, mha_case
 
 pytestmark = pytest.mark.gpu
 
@@ -170,3 +170,15 @@ def test_masked_bias_captured_and_replayed():
             g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(out, want)), rep
+
+
+@pytest.mark.parametrize("lq,lk", [([140, 77, 1, 0], [140, 77, 1, 0]), ([140, 90, 7, 3], [30, 0, 50, 129])])
+def test_masked_bucket_in_ragged_batches(lq, lk):
+    """Padded batches, rows that see nothing among them, with the nearest bucket of two heads at the lowest value."""
+    def low(t):
+        t = t.clone()
+        t[:2, 0] = LOWEST
+        return t
+    for causal, window in ((1, 0), (1, 20), (0, 20)):
+        mha_case(4, 140, 140, 4, 2, 64, causal, window, 3 if window else 0, 16, 60, lq, lk, seed=71, tab=low)
+        mha_case(4, 140, 140, 4, 2, 128, causal, window, 3 if window else 0, 16, 60, lq, lk, seed=72, tab=low, train=False)
