@@ -336,7 +336,8 @@ typedef struct {
 } paragan_mha_desc;
 
 int paragan_mha_check(const paragan_mha_desc* d);
-/* saved: kept from a forward to its backward; ws: scratch of either call. */
+/* saved: kept from a forward to its backward; ws: scratch of either call (the
+ * larger of both, mostly the backward's). */
 int paragan_mha_sizes(const paragan_mha_desc* d, size_t* saved_bytes,
                       size_t* ws_bytes);
 /* saved may be NULL when no backward follows (sampling, new tokens over a

@@ -226,16 +226,18 @@ PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
 // A wave owns 32 queries of one head, a block of 4 waves 128.  Keys and
 // values come in tiles of 64, the next one loading while this one is used.
 // Bound by the issue of exponentials and their neighbours beside the matrix
-// products: at 128 channels the vector unit is busy 46 % of the time and the
-// matrix cores 44 %, and they overlap little.  Causal 2 x 8192 x 16/4 heads x
-// 128: 553 us, 994 TFLOP/s (a large library product reaches 1225 here).
-// Tried and slower: two query tiles a wave at 128 channels (2421 us, one wave a
-// SIMD), the next tile's scores formed beside this one's exponentials (602),
-// raised wave priority over the products (571 and, through a window, 73 for 66).
+// products: at 128 channels the matrix cores are busy 44 % of the time and
+// vector instructions are issued in 39 %, and they overlap little.  Causal
+// 2 x 8192 x 16/4 heads x 128: 589 us, 933 TFLOP/s, on new inputs every time,
+// 553 on the same (a large library product reaches 1225 TFLOP/s here).
+// Tried and slower, where it took 575 then: two query tiles a wave at 128
+// channels (2421 us, one wave a SIMD), the next tile's scores formed beside this
+// one's exponentials (602), raised wave priority over the products (571 and,
+// through a window, 73 for 66).
 // At 64 channels four waves a SIMD hide more than the third of the registers
-// is worth, though the bias then spills 20 bytes a lane: with it 64 x 256 x 8
-// heads 22.0 us against 24.5 with three; without it, 4 x 4099 x 16 heads
-// through a window of 512, 56.8 against 57.6.
+// is worth, though the bias then spills 16 bytes a lane: with it 64 x 256 x 8
+// heads 23.5 us against 24.9 with three; without it, 4 x 4099 x 16 heads
+// through a window of 512, 56.7 against 57.5 (ragged) and 61.2 against 61.9.
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(256, DT == 64 ? 4 : 2) void k_mha_fwd(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
@@ -629,8 +631,10 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 }
 
 // ------------------------------------------------------------- dq (query-owned)
-// Issue-bound, as the forward: its three products fill the matrix cores a third
-// of the time (4 x 4096 x 8 heads x 64 with bias: 400 us of the pass's 772).
+// Issue-bound, as the forward: its three products fill the matrix cores 28 %
+// of the time and vector instructions are issued in half of it (4 x 4096 x 8 heads
+// x 64 with bias: 365 us of the pass's 804).  With a bias tiles near the diagonal
+// are formed twice (below): all of them where none lies past max_distance.
 // Also the row terms D = do . o and the log sums, kept for the key-owned pass
 // as it starts its products from them, and the bias gradient: dS of
 // the tiles near the diagonal, in a second visit, is summed per distance into
@@ -660,8 +664,10 @@ PG_DEV void diag_add(float* arr, const f32x16& v, int lane) {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// Three waves a SIMD where the registers suffice; with bias they spill 112 bytes
-// a lane then (training 4 x 4096 x 8 heads x 64: 1053 us against 803).
+// Three waves a SIMD where the registers suffice; with bias they spill 44 bytes
+// a lane then, which gains where most tiles are formed once and loses elsewhere
+// (training 4 x 4096 x 8 heads x 64 777 us against 783, 16 x 300 with a
+// max_distance of 256 85.0 against 83.2, 4 x 1024 with 512 149.7 against 147.0).
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaArgs a) {
   constexpr int TK = 64, NC = DT / 8, NT = DT / 32, KF = DT / 16;
@@ -908,10 +914,12 @@ __global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int
 // shared head are summed in registers.  A key block that many queries see
 // (first tokens beside a window; few, long sequences) is split over blocks of
 // `chunk` steps, whose fp32 partials k_mha_dkv_join adds in split order.
-// Issue-bound too: 82 % of the issue slots taken, matrix cores busy 33 % (4 x
-// 4096 x 8 heads x 64: 330 us).  Both halves of a query tile in one stretch
-// without branches needed registers that cost more (355 -> 362 us a pass, 448
-// -> 519 at 128 channels); operands read ahead changed nothing.
+// Held by dependences between its products and the exponentials at two waves a
+// SIMD: matrix cores busy 35 % of the time, vector instructions issued in 32 %,
+// waves waiting 46 % of theirs (4 x 4096 x 8 heads x 64 with bias: 374 us).  Both
+// halves of a query tile in one stretch without branches needed registers that
+// cost more (355 -> 362 us a pass, 448 -> 519 at 128 channels); operands read
+// ahead changed nothing.
 
 // At head widths past 64 the values of the block's keys stay in LDS and the
 // query tiles have 32 rows: two waves fit a SIMD then (with everything in
@@ -956,9 +964,9 @@ PG_DEV KItem item_of(const MhaArgs& a, int x) {
   return it;
 }
 
-// Two waves a SIMD: a third at 64 channels spills 20 to 44 bytes a lane (the
-// training of 4 x 4096 x 8 heads with bias 878 us against 803, without bias 4 x 2048 x 16 heads 363
-// against 359).
+// Two waves a SIMD: a third at 64 channels spills (the training of 4 x 4096 x 8
+// heads with bias 869 us against 783, without bias 4 x 2048 x 16 heads 349
+// against 345).
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(256, 2) void k_mha_dkv(MhaArgs a) {
   constexpr int TQ = dkv_tile(DT), NC = DT / 8, NT = DT / 32, KF = DT / 16;
@@ -1246,16 +1254,19 @@ void set_saved(MhaArgs& a, void* saved) {
 int64_t row_tiles(const Mha& m) { return cdiv((int64_t)m.Sq * (m.Hq / m.Hk), 32); }
 // Which calls without a backward take the form for a few new tokens: those of
 // few queries (the other form leaves three of its four waves idle: 64 x 16
-// queries of 32 / 8 heads x 128 over 1024 keys 93 us against 140; at 32
-// queries 46 against 44) and those whose row tiles leave CUs without work (128
-// queries of 8 heads x 64 over 32768 keys 39 us against 605, 8192 causal queries of
-// one head 53 against 128 and through a window of 16 5 against 8; 512 tiles
-// over 1024 keys 35 against 28).
+// queries of 32 / 8 heads x 128 over 1024 keys 94 us against 137; 32 queries
+// 183 against 142) and those whose row tiles leave CUs without work (128
+// queries of 8 heads x 64 over 32768 keys 39 us against 605; 8192 causal queries
+// of one head 53 against 128, through a window of 16 5 against 8; 256 tiles, causal
+// 2 x 512 x 8 heads x 128, 12.5 against 16.3; 512 of them, 4 x 512, 25 against 17,
+// though 16 against 20 at 64 channels over 1024 keys).
 bool few_rows(const Mha& m) { return m.Sq <= 16 || (int64_t)m.B * m.Hk * row_tiles(m) <= 256; }
 
 // Splits of the keys: a block for each CU, at least 8 tiles in each (two a
 // wave): the caches are read at 5.1 TB/s then, and three blocks a CU lose 15 %
-// to the partials they leave.
+// to the partials they leave.  In whole numbers, so that row tiles past half of
+// the CUs or just past all of them leave CUs idle: caches of 8192 x 8 heads x 128
+// are read at 5.7 TB/s for 32 sequences, 4.5 for 17 and 3.8 for 33 (same inputs every time).
 int step_splits(const Mha& m) {
   const int64_t queries = std::min<int64_t>(m.Sq, cdiv(32, m.Hq / m.Hk) + 1);   // of a row tile
   const int64_t tiles = m.window ? std::min<int64_t>(cdiv(m.Sk, 32), cdiv((m.causal ? 1 : 2) * (int64_t)m.window + queries, 32) + 1 + cdiv(m.n_sink, 32))
@@ -1268,7 +1279,10 @@ int step_splits(const Mha& m) {
 // query sees, and all blocks where they are few, are split into pieces of
 // `chunk` steps: the number of pieces with the least modelled time, the steps
 // over the places on the card plus half the last piece, a piece's partials
-// costing about as much as 256 queries to write and add.
+// costing about as much as 256 queries to write and add.  The model is not
+// exact: swept by hand it was 5 to 7 % off the best number of pieces (2 x 4096 x 16
+// / 4 heads x 128 in 1, 2, 3, 6 and 10 pieces: window 1024 491, 389, 435, 452, 513 us
+// and its 4 pieces 417; causal 1219, 916, 807, 827, 833 and its own 847).
 constexpr int64_t kMaxSlots = 8192;   // partials of at most 1 GB (128 keys x 2 x 128 channels each)
 struct KPlan { int nkb, nks, ns_sink, ns_reg, chunk; int64_t items, slots; };
 KPlan plan_keys(const Mha& m) {
