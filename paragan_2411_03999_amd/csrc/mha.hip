@@ -727,10 +727,8 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
   for (int j = 0; j < NT; ++j)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[j][r] = 0.f;
-  // BIAS, per row (over inv, but for the last): dS of the far tiles on either side, sum of dS, P of the far tiles of earlier
-  // keys, P of the near tiles
-  float flo = 0.f, fhi = 0.f, rho = 0.f, wlo = 0.f, wn = 0.f;
-  bool lo_far = false, hi_far = false;
+  // BIAS, per row (over inv): dS of the far tiles on either side, sum of dS, P of the far tiles on either side
+  float flo = 0.f, fhi = 0.f, rho = 0.f, wlo = 0.f, whi = 0.f;
   Span<TK> sp = span_of<TK>(a, sq.lk, qblk + sq.off, min(qblk + 128, sq.lq) - 1 + sq.off);
   if (qblk >= sq.lq) sp.nt = 0;
   const Span<32> sw = span_of<32>(a, sq.lk, p0, min(qw + 32, sq.lq) - 1 + sq.off);
@@ -789,20 +787,15 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
         if (!all_seen<32>(a, sq.lk, k0, p0, p0 + 31)) hide(s, rw, k0, g);
         if constexpr (NEAR) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float p = exp2_(s[r]) * inv;
-            wn += p;
-            s[r] = p * (dp[r] - (dd + rho));
-          }
+          for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]) * inv * (dp[r] - (dd + rho));
           diag_add(gs + k0 - p0 + a.maxd + kMargin, s, lane);
           continue;
         }
-        if (BIAS && !near && !a.causal && k0 < p0) {
+        float w = 0.f;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) wlo += s[r] = exp2_(s[r]);
-        } else {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r]);
+        for (int r = 0; r < 16; ++r) {
+          s[r] = exp2_(s[r]);
+          if (BIAS) w += s[r];
         }
         float t = 0.f;
 #pragma unroll
@@ -814,10 +807,10 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
           rho += t;
           if (!near && k0 < p0) {
             flo += t;
-            lo_far = far_lo != -INFINITY;   // a hidden bucket holds nothing, and gets nothing
+            wlo += w;
           } else if (!near) {
             fhi += t;
-            hi_far = far_hi != -INFINITY;
+            whi += w;
           }
         }
 #pragma unroll
@@ -843,16 +836,11 @@ __global__ __launch_bounds__(256, DT == 64 && !BIAS ? 3 : 2) void k_mha_dq(MhaAr
     // dS sums to zero over a row, but with D from an output of rounded P it sums to
     // rho = (true D) - D, and the bias gradient, many sums of dS with little
     // left over, would show it.  The true dS is dS - rho P: the near tiles are
-    // visited again for theirs, the far ones together hold what is left of 1.
+    // visited again for theirs, the far ones have their P summed a side.
     rho = (rho + __shfl_xor(rho, 32, 64)) * inv;
-    flo *= inv;
-    fhi *= inv;
-    wlo *= inv;
     pass(std::integral_constant<bool, true>());
-    const float rest = (g == 0 ? 1.f : 0.f) - wn;   // the two lanes of a row together: P of its far tiles
-    if (a.causal) wlo = rest;
-    if (lo_far) flo -= rho * wlo;
-    if (hi_far) fhi -= rho * (rest - wlo);
+    flo = (flo - rho * wlo) * inv;
+    fhi = (fhi - rho * whi) * inv;
   }
   if (q < a.Sq) {
     bf16_t* row = a.dq + b * a.qs[0] + q * a.qs[1] + h * a.qs[2];

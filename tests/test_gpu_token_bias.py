@@ -182,3 +182,22 @@ def test_masked_bucket_in_ragged_batches(lq, lk):
     for causal, window in ((1, 0), (1, 20), (0, 20)):
         mha_case(4, 140, 140, 4, 2, 64, causal, window, 3 if window else 0, 16, 60, lq, lk, seed=71, tab=low)
         mha_case(4, 140, 140, 4, 2, 128, causal, window, 3 if window else 0, 16, 60, lq, lk, seed=72, tab=low, train=False)
+
+
+@pytest.mark.parametrize("value", [LOWEST, -math.inf, -1e4, -40.0])
+@pytest.mark.parametrize("causal,window", [(0, 0), (1, 0), (0, 120)])
+def test_gradient_of_far_buckets_that_hold_nothing(value, causal, window):
+    """The buckets past max_distance take a share of their rows that is zero (or e^-40): so is their gradient, with nothing in
+    it of what rounding leaves of the rest."""
+    torch = need_gpu()
+    print("far buckets", value, causal, window, flush=True)
+    (q, k, v, do), gen = inputs(torch, 8, 1, 300, 300, 2, 1, 64)
+    table = torch.randn(2, 8, generator=gen)
+    table[0, 7], table[1, 7] = value, value
+    if not causal:
+        table[1, 3] = value
+    kw = dict(causal=causal, window=window, max_distance=40)
+    out = trained(q, k, v, do, table, **kw)
+    against(out, q, k, v, do, table, **kw)
+    if value < -100:
+        assert not out["dtable"][:, 7].any()
