@@ -228,7 +228,7 @@ PG_DEV void st4(bf16_t* row, int e, int d, float a, float b, float c, float f) {
 // Bound by the issue of exponentials and their neighbours beside the matrix
 // products: at 128 channels the matrix cores are busy 44 % of the time and
 // vector instructions are issued in 39 %, and they overlap little.  Causal
-// 2 x 8192 x 16/4 heads x 128: 589 us, 933 TFLOP/s, on new inputs every time,
+// 2 x 8192 x 16/4 heads x 128: 581 us, 946 TFLOP/s, on new inputs every time,
 // 553 on the same (a large library product reaches 1225 TFLOP/s here).
 // Tried and slower, where it took 575 then: two query tiles a wave at 128
 // channels (2421 us, one wave a SIMD), the next tile's scores formed beside this
@@ -631,9 +631,9 @@ __global__ __launch_bounds__(256) void k_mha_join(MhaArgs a) {
 }
 
 // ------------------------------------------------------------- dq (query-owned)
-// Issue-bound, as the forward: its three products fill the matrix cores 28 %
+// Issue-bound, as the forward: its three products fill the matrix cores 29 %
 // of the time and vector instructions are issued in half of it (4 x 4096 x 8 heads
-// x 64 with bias: 365 us of the pass's 804).  With a bias tiles near the diagonal
+// x 64 with bias: two fifths of the pass's 795 us).  With a bias tiles near the diagonal
 // are formed twice (below): all of them where none lies past max_distance.
 // Also the row terms D = do . o and the log sums, kept for the key-owned pass
 // as it starts its products from them, and the bias gradient: dS of
@@ -904,7 +904,8 @@ __global__ __launch_bounds__(256) void k_mha_dbias(const float* part, int B, int
 // `chunk` steps, whose fp32 partials k_mha_dkv_join adds in split order.
 // Held by dependences between its products and the exponentials at two waves a
 // SIMD: matrix cores busy 35 % of the time, vector instructions issued in 32 %,
-// waves waiting 46 % of theirs (4 x 4096 x 8 heads x 64 with bias: 374 us).  Both
+// waves waiting 46 % of theirs (4 x 4096 x 8 heads x 64 with bias: two fifths of
+// the pass's 795 us).  Both
 // halves of a query tile in one stretch without branches needed registers that
 // cost more (355 -> 362 us a pass, 448 -> 519 at 128 channels); operands read
 // ahead changed nothing.
