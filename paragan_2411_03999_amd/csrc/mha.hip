@@ -37,7 +37,7 @@ constexpr int kStepTable = 64;  // buckets up to which a step keeps its rows' bi
 constexpr float kDeep = 0x1p24f;
 // From a bias this large on (log2 units; of a head's any finite one) the backward keeps a row's maximum and the logarithm of
 // its sum apart: as one number, as exact as 2^-14 up to here, it would lose the sum beside a bias that scores vanish in too.
-// (Training 4 x 4096 x 8 heads x 64 pays 1 % for it, 790 us against 780.)
+// (Training 4 x 4096 x 8 heads x 64: 790 us against 780 as one number; 914 where every head has such a bias.)
 constexpr float kSteep = 0x1p10f;
 constexpr int kMargin = 96;   // distances past max_distance that a 64 x 32 tile can reach, rounded up
 

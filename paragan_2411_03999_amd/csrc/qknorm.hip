@@ -17,8 +17,8 @@
 // order the pair's other element sits rot / 16 lanes away and comes by a lane
 // exchange.  Blocks of the grid's second dimension take q or k.
 // Measured: forward of 32768 tokens x 16 heads x 64 in bf16 31 us (4.4 TB/s;
-// 24 us from cache), backward of 15005 x 40 x 128 106 us (4.4 TB/s; a copy
-// reaches 4.8).  Fewer registers for more waves, or two heads in flight, were
+// 24 us from cache), in fp32 53 us (5.1 TB/s, partly from cache), backward of
+// 15005 x 40 x 128 105 us (4.4 TB/s; a copy reaches 4.8).  Fewer registers for more waves, or two heads in flight, were
 // slower (backward 104 to 396 us where this took 100).
 #include "token.hpp"
 
