@@ -356,6 +356,151 @@ int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d,
                     float* dtable, void* ws);
 
 /* ---------------------------------------------------------------------
+ * The rest of a conditioned token block, and its training: the norms before
+ * and after a block with modulation, gate and residual scale in one pass, a
+ * gated linear recurrence that mixes tokens at linear cost, and the norm of
+ * all gradients with clipping.  Pointers of token tensors are 16-byte
+ * aligned, strides are in elements and multiples of 8, and sequence b has
+ * len[b] tokens (device array [B], or NULL for S; values are clamped to
+ * [0, S]): rows at and past it are not used, add to no gradient, and are
+ * written as zeros.  The current device must be the context's.
+ *
+ * Block norm, for token (b, s) of the stream x and a block's output h (D
+ * elements each):
+ *   v = h   or, with post,  norm(h) * gain_post
+ *   z = x + res_scale * gate[b] * v            (branch 0: z = x, no h)
+ *   y = norm(z) * gain_pre * (1 + scale[b]) + shift[b]   (pre 0: no y)
+ *   norm(t) = (t - mean t) * (mean (t - mean t)^2 + eps)^(-1/2)   (PARAGAN_NORM_LAYER)
+ *           = t * (mean t^2 + eps)^(-1/2)                         (PARAGAN_NORM_RMS)
+ * so one call ends a block and norms the next one's input; y is formed from
+ * the unrounded z.  gain_post, gain_pre: fp32 [D]; gate, scale, shift: fp32
+ * rows of D, mod_stride elements from one sequence's to the next one's (views
+ * of one projection of the condition, for instance), or 0 for one row that
+ * all sequences share (a norm's bias, a learned gate).  Each may be NULL: a
+ * gain or gate of ones, a scale or shift of zeros.  Statistics and sums are
+ * fp32 (sums over tokens are joined in 64 bits).
+ * Element (b, s, c) of a tensor is at b * stride[0] + s * stride[1] + c.
+ * z may be x and y may be h (same pointer and strides) where no backward
+ * follows, which reads x and h; outputs must not overlap inputs otherwise.
+ * ------------------------------------------------------------------- */
+enum { PARAGAN_NORM_RMS = 0, PARAGAN_NORM_LAYER = 1 };
+
+typedef struct {
+  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S < 2^31 */
+  int32_t D;                       /* width, a multiple of 8 up to 8192 */
+  int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: h, y and their gradients */
+  int32_t stream_dtype;            /* x, z and their gradients: dtype, or PARAGAN_F32 */
+  int32_t kind;                    /* PARAGAN_NORM_RMS or PARAGAN_NORM_LAYER */
+  int32_t branch, post, pre;       /* 0 or 1; branch or pre at least, post only with branch */
+  float eps;                       /* > 0, no smaller than the least normal float (1.2e-38) */
+  float res_scale;                 /* finite */
+  int64_t mod_stride;              /* 0, or >= D and a multiple of 8 */
+  int64_t x_stride[2], h_stride[2], z_stride[2], y_stride[2];
+} paragan_blocknorm_desc;
+
+int paragan_blocknorm_check(const paragan_blocknorm_desc* d);
+/* saved: kept from a forward to its backward; ws: scratch of the backward. */
+int paragan_blocknorm_sizes(const paragan_blocknorm_desc* d, size_t* saved_bytes,
+                            size_t* ws_bytes);
+/* saved may be NULL when no backward follows. */
+int paragan_blocknorm_fwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
+                          const void* x, const void* h, const float* gain_post,
+                          const float* gate, const float* gain_pre,
+                          const float* scale, const float* shift,
+                          const int32_t* len, void* z, void* y, void* saved);
+/* From the forward's inputs and saved, dz (NULL: zero; z's strides, or x's
+ * without a branch) and dy (y's strides; with pre): dx (x's strides), dh
+ * (h's strides; with branch) and the gradients of the rows, fp32,
+ * overwritten: dgain_post, dgain_pre [D]; dgate, dscale, dshift as gate, scale and shift lie (with mod_stride 0
+ * one row, the sum over all sequences).  Each of these five may be NULL: not
+ * wanted. */
+int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
+                          const void* x, const void* h, const float* gain_post,
+                          const float* gate, const float* gain_pre,
+                          const float* scale, const float* shift,
+                          const int32_t* len, const void* saved,
+                          const void* dz, const void* dy, void* dx, void* dh,
+                          float* dgain_post, float* dgate, float* dgain_pre,
+                          float* dscale, float* dshift, void* ws);
+
+/* Gated linear recurrence, for every channel c of D by itself:
+ *   a_t = exp(-sharp * softplus(decay[c]) * sigmoid(r_t)),
+ *   h_t = a_t h_{t-1} + (1 - a_t^2)^(1/2) * sigmoid(g_t) * x_t,   y_t = h_t,
+ * over the tokens of a sequence from the first to the last, or with reverse
+ * from the last to the first.  x, r, g are the program's projections; decay:
+ * fp32 [D], finite.  h0: the states before the first token taken, fp32
+ * [B][D], or NULL for zeros; ht: those after the last, or NULL.  A sequence
+ * of no tokens has ht = h0.  ht may be h0: with S = 1 that is the step of one
+ * new token.  States and sums are fp32, the root no smaller than 1.1e-19.  A
+ * NaN or infinity in a token reaches the tokens after it (in the backward
+ * those before it) of its sequence and channel, and the channel's ddecay. */
+typedef struct {
+  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S < 2^31 */
+  int32_t D;                       /* channels, a multiple of 8, up to 2^20; B * D < 2^31 */
+  int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: x, r, g, y and their gradients */
+  int32_t reverse;                 /* 0 or 1 */
+  float sharp;                     /* > 0, finite */
+  int64_t x_stride[2], r_stride[2], g_stride[2], y_stride[2];   /* as above */
+} paragan_scan_desc;
+
+int paragan_scan_check(const paragan_scan_desc* d);
+/* saved: kept from a forward to its backward; ws: scratch of either call. */
+int paragan_scan_sizes(const paragan_scan_desc* d, size_t* saved_bytes, size_t* ws_bytes);
+/* saved may be NULL when no backward follows.  x, r, g may repeat through
+ * zero strides in the forward; y, and in the backward x, r and g (whose
+ * strides dx, dr and dg share), must not overlap themselves. */
+int paragan_scan_fwd(paragan_ctx* ctx, const paragan_scan_desc* d, const void* x,
+                     const void* r, const void* g, const float* decay,
+                     const int32_t* len, const float* h0, void* y, float* ht,
+                     void* saved, void* ws);
+/* From the forward's inputs and saved, dy (y's strides) and dht (fp32
+ * [B][D], or NULL: zero): dx, dr, dg, ddecay (fp32 [D], overwritten) and dh0
+ * (fp32 [B][D], or NULL: not wanted; it may be dht). */
+int paragan_scan_bwd(paragan_ctx* ctx, const paragan_scan_desc* d, const void* x,
+                     const void* r, const void* g, const float* decay,
+                     const int32_t* len, const void* saved, const void* dy,
+                     const float* dht, void* dx, void* dr, void* dg,
+                     float* ddecay, float* dh0, void* ws);
+
+/* The norm of all gradients together, and clipping:
+ *   norm = grad_scale * (sum over all tensors of g^2)^(1/2),
+ *   factor = grad_scale * (norm <= max_norm ? 1 : max_norm / norm),
+ *   out = factor * g,
+ * the sum in 64 bits and in a fixed order.  A NaN among the gradients makes
+ * norm, factor and all outputs NaN; an infinity makes the norm infinite and
+ * (with a finite max_norm) the factor zero, as these formulas say.  max_norm may be
+ * infinite: nothing is clipped.  Outputs in place whose factor is one are
+ * left alone.
+ * The tensors are named once, in a plan: paragan_clip_plan writes it to host
+ * memory of the size that paragan_clip_sizes gives, the caller copies it to
+ * the device (8-byte aligned) and keeps the tensors where they are.  A tensor is n
+ * contiguous elements at any place its type is aligned to; out may be grad
+ * (in place); otherwise no two of them may overlap (refused).  n may be 0. */
+typedef struct {
+  const void* grad;
+  void* out;                       /* grad's type and size; may be grad */
+  int64_t n;                       /* 0 .. 2^40 */
+  int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32 */
+  int32_t reserved;                /* 0 */
+} paragan_clip_tensor;
+
+/* Filled by paragan_clip_plan, passed unchanged to paragan_clip. */
+typedef struct {
+  int64_t n_elements, n_pieces, bytes;
+  int32_t n_tensors;
+  int32_t in_place;                /* every out is its grad */
+} paragan_clip_desc;
+
+int paragan_clip_sizes(const paragan_clip_tensor* t, int32_t n_tensors,
+                       size_t* plan_bytes, size_t* ws_bytes);
+int paragan_clip_plan(const paragan_clip_tensor* t, int32_t n_tensors,
+                      paragan_clip_desc* desc, void* plan_host);
+/* plan: device copy; max_norm > 0; grad_scale > 0, finite; norm: device fp32
+ * [2], written with norm and factor. */
+int paragan_clip(paragan_ctx* ctx, const paragan_clip_desc* d, const void* plan,
+                 float max_norm, float grad_scale, float* norm, void* ws);
+
+/* ---------------------------------------------------------------------
  * Generator output layer (the last generator layer of the model,
  * Evaluation "Experiment Setup"; kept in fp32 arithmetic by the paper's
  * mixed-precision placement, Design "System Optimizations"):

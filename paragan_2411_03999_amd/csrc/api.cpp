@@ -625,6 +625,259 @@ extern "C" int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d, cons
   })
 }
 
+// ------------------------------------------------------------ token block: norms with modulation, recurrence, clipping
+// (b, s) strides of a tensor of B x S rows of D elements
+static void token_strides(const int64_t* st, int64_t* out, int64_t B, int64_t S, const char* what) {
+  for (int i = 0; i < 2; ++i) {
+    if (st[i] < 0 || st[i] % 8 != 0)
+      throw Error{PARAGAN_EINVAL, std::string(what) + ": strides must be >= 0 and multiples of 8"};
+    if ((__int128)st[i] * (i ? S : B) >= ((__int128)1 << 60))
+      throw Error{PARAGAN_EINVAL, std::string(what) + ": a stride is too large"};
+    out[i] = st[i];
+  }
+}
+static bool rows_distinct(const int64_t* st, int64_t B, int64_t S, int64_t D) {
+  const int64_t s[3] = {st[0], st[1], 0};
+  return distinct(s, B, S, 1, D);
+}
+
+static BlockNorm make_bn(const paragan_blocknorm_desc* d) {
+  if (!d) throw Error{PARAGAN_EINVAL, "blocknorm: desc is NULL"};
+  PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S < (1LL << 31), "blocknorm: B, S must be >= 1 and B * S below 2^31");
+  PG_CHECK(d->D >= 8 && d->D <= 8192 && d->D % 8 == 0, "blocknorm: D must be a multiple of 8 up to 8192");
+  PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "blocknorm: dtype must be PARAGAN_BF16 or PARAGAN_F32");
+  PG_CHECK(d->stream_dtype == PARAGAN_F32 || d->stream_dtype == d->dtype,
+           "blocknorm: stream_dtype must be dtype or PARAGAN_F32");
+  PG_CHECK(d->kind == PARAGAN_NORM_RMS || d->kind == PARAGAN_NORM_LAYER,
+           "blocknorm: kind must be PARAGAN_NORM_RMS or PARAGAN_NORM_LAYER");
+  for (int32_t f : {d->branch, d->post, d->pre}) PG_CHECK(f == 0 || f == 1, "blocknorm: branch, post, pre must be 0 or 1");
+  PG_CHECK(d->branch || d->pre, "blocknorm: neither branch nor pre leaves nothing to do");
+  PG_CHECK(d->branch || !d->post, "blocknorm: post needs a branch");
+  PG_CHECK(d->eps >= FLT_MIN && std::isfinite(d->eps), "blocknorm: eps must be > 0 and no smaller than the least normal float");
+  PG_CHECK(std::isfinite(d->res_scale), "blocknorm: res_scale must be finite");
+  PG_CHECK(d->mod_stride == 0 || (d->mod_stride >= d->D && d->mod_stride % 8 == 0 && d->mod_stride < (1LL << 60) / d->B),
+           "blocknorm: mod_stride must be 0, or >= D and a multiple of 8");
+  BlockNorm a;
+  a.B = d->B; a.S = d->S; a.D = d->D; a.f32 = d->dtype == PARAGAN_F32; a.res32 = d->stream_dtype == PARAGAN_F32;
+  a.layer = d->kind == PARAGAN_NORM_LAYER; a.branch = d->branch; a.post = d->post; a.pre = d->pre;
+  a.eps = d->eps; a.res_scale = d->res_scale; a.mod = d->mod_stride;
+  token_strides(d->x_stride, a.xs, a.B, a.S, "blocknorm: x");
+  token_strides(d->h_stride, a.hs, a.B, a.S, "blocknorm: h");
+  token_strides(a.branch ? d->z_stride : d->x_stride, a.zs, a.B, a.S, "blocknorm: z");
+  token_strides(d->y_stride, a.ys, a.B, a.S, "blocknorm: y");
+  PG_CHECK(!a.branch || rows_distinct(a.zs, a.B, a.S, a.D), "blocknorm: z overlaps itself");
+  PG_CHECK(!a.pre || rows_distinct(a.ys, a.B, a.S, a.D), "blocknorm: y overlaps itself");
+  return a;
+}
+static BlockNormRows bn_rows(const float* gain_post, const float* gate, const float* gain_pre, const float* scale,
+                             const float* shift) {
+  const float* p[5] = {gain_post, gate, gain_pre, scale, shift};
+  const char* n[5] = {"gain_post", "gate", "gain_pre", "scale", "shift"};
+  for (int i = 0; i < 5; ++i)
+    if (p[i]) need16(p[i], n[i]);
+  return BlockNormRows{gain_post, gate, gain_pre, scale, shift};
+}
+
+extern "C" int paragan_blocknorm_check(const paragan_blocknorm_desc* d) { PG_TRY(nullptr, make_bn(d)) }
+
+extern "C" int paragan_blocknorm_sizes(const paragan_blocknorm_desc* d, size_t* saved, size_t* ws) {
+  PG_TRY(nullptr, {
+    const BlockNorm a = make_bn(d);
+    if (saved) *saved = blocknorm_saved_bytes(a);
+    if (ws) *ws = blocknorm_ws_bytes(a);
+  })
+}
+
+extern "C" int paragan_blocknorm_fwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d, const void* x, const void* h,
+                                     const float* gain_post, const float* gate, const float* gain_pre,
+                                     const float* scale, const float* shift, const int32_t* len, void* z, void* y,
+                                     void* saved) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const BlockNorm a = make_bn(d);
+    const BlockNormRows w = bn_rows(gain_post, gate, gain_pre, scale, shift);
+    need16(x, "x");
+    if (a.branch) { need16(h, "h"); need16(z, "z"); }
+    if (a.pre) need16(y, "y");
+    if (saved) aligned(saved, "saved");
+    on_device(ctx, "blocknorm_fwd");
+    blocknorm_fwd(ctx->stream, a, w, x, h, len, z, y, saved);
+  })
+}
+
+extern "C" int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d, const void* x, const void* h,
+                                     const float* gain_post, const float* gate, const float* gain_pre,
+                                     const float* scale, const float* shift, const int32_t* len, const void* saved,
+                                     const void* dz, const void* dy, void* dx, void* dh, float* dgain_post,
+                                     float* dgate, float* dgain_pre, float* dscale, float* dshift, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const BlockNorm a = make_bn(d);
+    const BlockNormRows w = bn_rows(gain_post, gate, gain_pre, scale, shift);
+    PG_CHECK(rows_distinct(a.xs, a.B, a.S, a.D) && (!a.branch || rows_distinct(a.hs, a.B, a.S, a.D)),
+             "blocknorm_bwd: x or h overlaps itself (dx and dh share their strides)");
+    need16(x, "x"); need16(dx, "dx");
+    if (a.branch) { need16(h, "h"); need16(dh, "dh"); }
+    if (a.pre) need16(dy, "dy");
+    PG_CHECK(a.pre || dz, "blocknorm_bwd: dz is NULL and there is no y");
+    if (dz) need16(dz, "dz");
+    PG_CHECK(a.branch || (!dgate && !dgain_post), "blocknorm_bwd: dgate, dgain_post need a branch");
+    PG_CHECK(a.post || !dgain_post, "blocknorm_bwd: dgain_post needs post");
+    PG_CHECK(a.pre || (!dgain_pre && !dscale && !dshift), "blocknorm_bwd: dgain_pre, dscale, dshift need pre");
+    need(saved, "saved"); need(ws, "ws");
+    aligned(saved, "saved"); aligned(ws, "ws");
+    on_device(ctx, "blocknorm_bwd");
+    blocknorm_bwd(ctx->stream, a, w, x, h, len, saved, dz, dy, dx, dh,
+                  BlockNormGrads{dgain_post, dgate, dgain_pre, dscale, dshift}, ws);
+  })
+}
+
+static Scan make_scan(const paragan_scan_desc* d) {
+  if (!d) throw Error{PARAGAN_EINVAL, "scan: desc is NULL"};
+  PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S < (1LL << 31), "scan: B, S must be >= 1 and B * S below 2^31");
+  PG_CHECK(d->D >= 8 && d->D <= (1 << 20) && d->D % 8 == 0 && (int64_t)d->B * d->D < (1LL << 31),
+           "scan: D must be a multiple of 8 up to 2^20 and B * D below 2^31");
+  PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "scan: dtype must be PARAGAN_BF16 or PARAGAN_F32");
+  PG_CHECK(d->reverse == 0 || d->reverse == 1, "scan: reverse must be 0 or 1");
+  PG_CHECK(d->sharp > 0.f && std::isfinite(d->sharp), "scan: sharp must be > 0 and finite");
+  Scan a;
+  a.B = d->B; a.S = d->S; a.D = d->D; a.f32 = d->dtype == PARAGAN_F32; a.reverse = d->reverse == 1; a.sharp = d->sharp;
+  token_strides(d->x_stride, a.xs, a.B, a.S, "scan: x");
+  token_strides(d->r_stride, a.rs, a.B, a.S, "scan: r");
+  token_strides(d->g_stride, a.gs, a.B, a.S, "scan: g");
+  token_strides(d->y_stride, a.ys, a.B, a.S, "scan: y");
+  PG_CHECK(rows_distinct(a.ys, a.B, a.S, a.D), "scan: y overlaps itself");
+  return a;
+}
+
+extern "C" int paragan_scan_check(const paragan_scan_desc* d) { PG_TRY(nullptr, make_scan(d)) }
+
+extern "C" int paragan_scan_sizes(const paragan_scan_desc* d, size_t* saved, size_t* ws) {
+  PG_TRY(nullptr, {
+    const Scan a = make_scan(d);
+    if (saved) *saved = scan_saved_bytes(a);
+    if (ws) *ws = scan_ws_bytes(a);
+  })
+}
+
+extern "C" int paragan_scan_fwd(paragan_ctx* ctx, const paragan_scan_desc* d, const void* x, const void* r,
+                                const void* g, const float* decay, const int32_t* len, const float* h0, void* y,
+                                float* ht, void* saved, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const Scan a = make_scan(d);
+    need16(x, "x"); need16(r, "r"); need16(g, "g"); need16(decay, "decay"); need16(y, "y"); need(ws, "ws");
+    if (h0) need16(h0, "h0");
+    if (ht) need16(ht, "ht");
+    aligned(ws, "ws");
+    if (saved) aligned(saved, "saved");
+    on_device(ctx, "scan_fwd");
+    scan_fwd(ctx->stream, a, x, r, g, decay, len, h0, y, ht, saved, ws);
+  })
+}
+
+extern "C" int paragan_scan_bwd(paragan_ctx* ctx, const paragan_scan_desc* d, const void* x, const void* r,
+                                const void* g, const float* decay, const int32_t* len, const void* saved,
+                                const void* dy, const float* dht, void* dx, void* dr, void* dg, float* ddecay,
+                                float* dh0, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    const Scan a = make_scan(d);
+    PG_CHECK(rows_distinct(a.xs, a.B, a.S, a.D) && rows_distinct(a.rs, a.B, a.S, a.D) && rows_distinct(a.gs, a.B, a.S, a.D),
+             "scan_bwd: x, r or g overlaps itself (dx, dr, dg share their strides)");
+    need16(x, "x"); need16(r, "r"); need16(g, "g"); need16(decay, "decay"); need16(dy, "dy");
+    need16(dx, "dx"); need16(dr, "dr"); need16(dg, "dg"); need(ddecay, "ddecay");
+    if (dht) need16(dht, "dht");
+    if (dh0) need16(dh0, "dh0");
+    need(saved, "saved"); need(ws, "ws");
+    aligned(saved, "saved"); aligned(ws, "ws");
+    on_device(ctx, "scan_bwd");
+    scan_bwd(ctx->stream, a, x, r, g, decay, len, saved, dy, dht, dx, dr, dg, ddecay, dh0, ws);
+  })
+}
+
+// The pieces of all tensors, and what is wrong with the list
+static paragan_clip_desc clip_desc(const paragan_clip_tensor* t, int32_t n) {
+  if (!t) throw Error{PARAGAN_EINVAL, "clip: the tensors are NULL"};
+  PG_CHECK(n >= 1, "clip: n_tensors must be >= 1");
+  paragan_clip_desc d{};
+  d.n_tensors = n;
+  d.in_place = 1;
+  struct Span { uint64_t at, end; };
+  std::vector<Span> spans;
+  for (int32_t i = 0; i < n; ++i) {
+    PG_CHECK(t[i].dtype == PARAGAN_BF16 || t[i].dtype == PARAGAN_F32, "clip: dtype must be PARAGAN_BF16 or PARAGAN_F32");
+    PG_CHECK(t[i].reserved == 0, "clip: reserved must be 0");
+    PG_CHECK(t[i].n >= 0 && t[i].n <= (1LL << 40), "clip: n must be 0 .. 2^40");
+    if (t[i].n == 0) continue;
+    const uint64_t el = t[i].dtype == PARAGAN_BF16 ? 2 : 4, g = (uint64_t)(uintptr_t)t[i].grad, o = (uint64_t)(uintptr_t)t[i].out;
+    PG_CHECK(g && o, "clip: a gradient or output is NULL");
+    PG_CHECK(g % el == 0 && o % el == 0, "clip: a gradient or output is not aligned to its type");
+    spans.push_back({g, g + el * (uint64_t)t[i].n});
+    if (o != g) {
+      spans.push_back({o, o + el * (uint64_t)t[i].n});
+      d.in_place = 0;
+    }
+    d.n_elements += t[i].n;
+    d.bytes += (int64_t)el * t[i].n;
+    d.n_pieces += cdiv(t[i].n, kClipPiece);
+    PG_CHECK(d.n_pieces < (1LL << 31), "clip: too many elements");
+  }
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+  for (size_t i = 1; i < spans.size(); ++i)
+    PG_CHECK(spans[i].at >= spans[i - 1].end, "clip: two tensors overlap (a gradient named twice, or an output on another)");
+  return d;
+}
+
+extern "C" int paragan_clip_sizes(const paragan_clip_tensor* t, int32_t n, size_t* plan_bytes, size_t* ws_bytes) {
+  PG_TRY(nullptr, {
+    const paragan_clip_desc d = clip_desc(t, n);
+    if (plan_bytes) *plan_bytes = (size_t)d.n_pieces * sizeof(ClipPiece);
+    if (ws_bytes) *ws_bytes = clip_ws_bytes();
+  })
+}
+
+extern "C" int paragan_clip_plan(const paragan_clip_tensor* t, int32_t n, paragan_clip_desc* desc, void* plan_host) {
+  PG_TRY(nullptr, {
+    need(desc, "desc");
+    const paragan_clip_desc d = clip_desc(t, n);
+    if (d.n_pieces) need(plan_host, "plan_host");
+    ClipPiece* out = (ClipPiece*)plan_host;
+    for (int32_t i = 0; i < n; ++i) {
+      const uint64_t el = t[i].dtype == PARAGAN_BF16 ? 2 : 4;
+      for (int64_t at = 0; at < t[i].n; at += kClipPiece) {
+        const ClipPiece p{(uint64_t)(uintptr_t)t[i].grad + el * at, (uint64_t)(uintptr_t)t[i].out + el * at,
+                          (int32_t)std::min<int64_t>(kClipPiece, t[i].n - at), (int32_t)(t[i].dtype == PARAGAN_BF16)};
+        std::memcpy(out++, &p, sizeof(p));
+      }
+    }
+    *desc = d;
+  })
+}
+
+extern "C" int paragan_clip(paragan_ctx* ctx, const paragan_clip_desc* d, const void* plan, float max_norm,
+                            float grad_scale, float* norm, void* ws) {
+  if (!ctx) return PARAGAN_EINVAL;
+  ProfBind pb(ctx);
+  PG_TRY(ctx, {
+    if (!d) throw Error{PARAGAN_EINVAL, "clip: desc is NULL"};
+    PG_CHECK(d->n_tensors >= 1 && d->n_pieces >= 0 && d->n_pieces < (1LL << 31) && (d->in_place == 0 || d->in_place == 1),
+             "clip: desc is not one of paragan_clip_plan");
+    if (d->n_pieces) need(plan, "plan");
+    PG_CHECK(((uintptr_t)plan & 7) == 0, "clip: plan is not 8-byte aligned");
+    PG_CHECK(max_norm > 0.f, "clip: max_norm must be > 0");
+    PG_CHECK(grad_scale > 0.f && std::isfinite(grad_scale), "clip: grad_scale must be > 0 and finite");
+    need(norm, "norm"); need(ws, "ws");
+    aligned(ws, "ws");
+    on_device(ctx, "clip");
+    clip(ctx->stream, d->n_pieces, (double)d->bytes, d->in_place == 1, plan, max_norm, grad_scale, norm, ws);
+  })
+}
+
 // ------------------------------------------------------------ generator output layer
 static void ocheck(const paragan_gout_desc* d) {
   if (!d) throw Error{PARAGAN_EINVAL, "gout: desc is NULL"};

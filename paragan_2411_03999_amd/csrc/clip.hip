@@ -1,0 +1,135 @@
+// The norm of many gradients together, and clipping by it.
+//
+//   norm = grad_scale (sum g^2)^1/2,  factor = grad_scale (norm <= max ? 1 : max / norm),  out = factor g.
+//
+// Bound by memory: the tensors are read for the sum, and read and written
+// for the result.  The tensors come as pieces of up to kClipPiece elements
+// from a table in device memory, so one launch takes all of them; a block
+// takes pieces in a fixed order.  Squares are summed in 64 bits, where those
+// of the largest and smallest floats are finite and not zero, in a thread,
+// over a block's threads and over the blocks in order: the same call gives
+// the same bits.
+#include "token.hpp"
+
+namespace pg {
+
+namespace {
+
+constexpr int kBlocks = 2048;      // at most: blocks of either launch
+
+PG_DEV void square8(uint4 v, double& s) {
+  float f[8];
+  unpack8(v, f);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fma((double)f[e], (double)f[e], s);
+}
+PG_DEV void square4(float4 v, double& s) {
+  s = fma((double)v.x, (double)v.x, s);
+  s = fma((double)v.y, (double)v.y, s);
+  s = fma((double)v.z, (double)v.z, s);
+  s = fma((double)v.w, (double)v.w, s);
+}
+
+// elements of p ahead of the next 16-byte place, at most n
+template <typename T>
+PG_DEV int ahead(const T* p, int n) {
+  return min(n, (int)(((16 - ((uintptr_t)p & 15)) & 15) / sizeof(T)));
+}
+
+template <typename T>
+PG_DEV double piece_sum(const T* p, int n) {
+  const int tid = threadIdx.x, h = ahead(p, n), V = 16 / sizeof(T), nv = (n - h) / V;
+  double s = 0.0;
+  for (int i = tid; i < h; i += 256) {
+    const double v = ld<T>(p, i);
+    s = fma(v, v, s);
+  }
+#pragma unroll 4
+  for (int i = tid; i < nv; i += 256) {
+    if constexpr (sizeof(T) == 2) square8(reinterpret_cast<const uint4*>(p + h)[i], s);
+    else square4(reinterpret_cast<const float4*>(p + h)[i], s);
+  }
+  for (int i = h + nv * V + tid; i < n; i += 256) {
+    const double v = ld<T>(p, i);
+    s = fma(v, v, s);
+  }
+  return s;
+}
+
+__global__ __launch_bounds__(256) void k_clip_sum(const ClipPiece* plan, int64_t n_pieces, double* part) {
+  __shared__ double sh[4];
+  double s = 0.0;
+  for (int64_t i = blockIdx.x; i < n_pieces; i += gridDim.x) {
+    const ClipPiece p = plan[i];
+    s += p.bf16 ? piece_sum((const bf16_t*)p.src, p.n) : piece_sum((const float*)p.src, p.n);
+  }
+  s = wave_sum_d(s);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.x] = ((sh[0] + sh[1]) + sh[2]) + sh[3];
+}
+
+template <typename T>
+PG_DEV void piece_scale(const T* p, T* o, int n, float k) {
+  const int tid = threadIdx.x, V = 16 / sizeof(T);
+  // vectors where both lie alike
+  const int h = (((uintptr_t)p ^ (uintptr_t)o) & 15) ? n : ahead(p, n), nv = (n - h) / V;
+  for (int i = tid; i < h; i += 256) st<T>(o, i, ld<T>(p, i) * k);
+#pragma unroll 4
+  for (int i = tid; i < nv; i += 256) {
+    if constexpr (sizeof(T) == 2) {
+      float f[8];
+      unpack8(reinterpret_cast<const uint4*>(p + h)[i], f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] *= k;
+      reinterpret_cast<uint4*>(o + h)[i] = pack8(f);
+    } else {
+      float4 v = reinterpret_cast<const float4*>(p + h)[i];
+      v.x *= k; v.y *= k; v.z *= k; v.w *= k;
+      reinterpret_cast<float4*>(o + h)[i] = v;
+    }
+  }
+  for (int i = h + nv * V + tid; i < n; i += 256) st<T>(o, i, ld<T>(p, i) * k);
+}
+
+__global__ __launch_bounds__(256) void k_clip_scale(const ClipPiece* plan, int64_t n_pieces, const double* part, int n_part,
+                                                    float max_norm, float grad_scale, int in_place, float* norm) {
+  __shared__ double sh[4];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n_part; i += 256) s += part[i];
+  s = wave_sum_d(s);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = (double)grad_scale * sqrt(((sh[0] + sh[1]) + sh[2]) + sh[3]);
+  const float k = (float)((double)grad_scale * (s <= (double)max_norm ? 1.0 : (double)max_norm / s));
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    norm[0] = (float)s;
+    norm[1] = k;
+  }
+  if (in_place && k == 1.f) return;
+  for (int64_t i = blockIdx.x; i < n_pieces; i += gridDim.x) {
+    const ClipPiece p = plan[n_pieces - 1 - i];   // the last ones read are the nearest
+    if (k == 1.f && p.src == p.dst) continue;
+    if (p.bf16) piece_scale((const bf16_t*)p.src, (bf16_t*)p.dst, p.n, k);
+    else piece_scale((const float*)p.src, (float*)p.dst, p.n, k);
+  }
+}
+
+}  // namespace
+
+size_t clip_ws_bytes() { return kBlocks * sizeof(double); }
+
+void clip(hipStream_t st, int64_t n_pieces, double bytes, bool in_place, const void* plan, float max_norm,
+          float grad_scale, float* norm, void* ws) {
+  const int grid = (int)std::min<int64_t>(std::max<int64_t>(n_pieces, 1), kBlocks);
+  const ClipPiece* p = (const ClipPiece*)plan;
+  ProfScope prof(st);
+  hipLaunchKernelGGL(k_clip_sum, dim3(grid), dim3(256), 0, st, p, n_pieces, (double*)ws);
+  PG_LAUNCH_CHECK();
+  hipLaunchKernelGGL(k_clip_scale, dim3(grid), dim3(256), 0, st, p, n_pieces, (const double*)ws, grid, max_norm,
+                     grad_scale, (int)in_place, norm);
+  PG_LAUNCH_CHECK();
+  prof.done_bytes("k_clip", 3.0 * bytes);
+}
+
+}  // namespace pg

@@ -16,6 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libparagan.so")
 OK, EINVAL, EUNSUPPORTED, EWORKSPACE, EHIP, ENONFINITE, ETIMEOUT = 0, -1, -2, -3, -4, -5, -6
 F32, BF16 = 0, 1
 ADAM, ADABELIEF = 0, 1
+NORM_RMS, NORM_LAYER = 0, 1
 
 
 class ParaganError(RuntimeError):
@@ -64,6 +65,29 @@ class MhaDesc(C.Structure):
                 ("n_buckets", C.c_int32), ("max_distance", C.c_int32), ("scale", C.c_float),
                 ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
                 ("o_stride", C.c_int64 * 3)]
+
+
+class BlockNormDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("S", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32), ("stream_dtype", C.c_int32),
+                ("kind", C.c_int32), ("branch", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32), ("eps", C.c_float),
+                ("res_scale", C.c_float), ("mod_stride", C.c_int64), ("x_stride", C.c_int64 * 2),
+                ("h_stride", C.c_int64 * 2), ("z_stride", C.c_int64 * 2), ("y_stride", C.c_int64 * 2)]
+
+
+class ScanDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("S", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32), ("reverse", C.c_int32),
+                ("sharp", C.c_float), ("x_stride", C.c_int64 * 2), ("r_stride", C.c_int64 * 2),
+                ("g_stride", C.c_int64 * 2), ("y_stride", C.c_int64 * 2)]
+
+
+class ClipTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class ClipDesc(C.Structure):
+    _fields_ = [("n_elements", C.c_int64), ("n_pieces", C.c_int64), ("bytes", C.c_int64), ("n_tensors", C.c_int32),
+                ("in_place", C.c_int32)]
 
 
 class Optim(C.Structure):
@@ -160,6 +184,17 @@ _SIGS = {
     "paragan_mha_sizes": (C.c_int, [_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "paragan_mha_fwd": (C.c_int, [_P] * 11),
     "paragan_mha_bwd": (C.c_int, [_P] * 16),
+    "paragan_blocknorm_check": (C.c_int, [_P]),
+    "paragan_blocknorm_sizes": (C.c_int, [_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "paragan_blocknorm_fwd": (C.c_int, [_P] * 13),
+    "paragan_blocknorm_bwd": (C.c_int, [_P] * 21),
+    "paragan_scan_check": (C.c_int, [_P]),
+    "paragan_scan_sizes": (C.c_int, [_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "paragan_scan_fwd": (C.c_int, [_P] * 12),
+    "paragan_scan_bwd": (C.c_int, [_P] * 16),
+    "paragan_clip_sizes": (C.c_int, [_P, C.c_int32, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "paragan_clip_plan": (C.c_int, [_P, C.c_int32, _P, _P]),
+    "paragan_clip": (C.c_int, [_P, _P, _P, C.c_float, C.c_float, _P, _P]),
     "paragan_gout_layout": (C.c_int, [_P, _P, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_int64),
                                       C.POINTER(C.c_int64)]),
     "paragan_gout_sizes": (C.c_int, [_P, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
@@ -520,6 +555,158 @@ def paragan_mha_bwd(ctx, desc, q, k, v, table, len_q, len_k, o, saved, dout, dq,
     """dout lies as o, dq, dk and dv as q, k and v."""
     p = _placed(desc, _mha_dims, _MHA_BWD, q, k, v, table, len_q, len_k, o, dout, dq, dk, dv, dtable)
     return ctx.check(load().paragan_mha_bwd(ctx.h, C.byref(desc), *p[:7], _ptr(saved), *p[7:], _ptr(ws)))
+
+
+def _token_stride(t):   # the stride of a dimension of one element means nothing
+    return (C.c_int64 * 2)(*(0 if t is None or t.shape[i] == 1 else t.stride(i) for i in range(2)))
+
+
+def _token_dtype(what, t):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ParaganError(EINVAL, what + ": tensors must be bfloat16 or float32")
+    return BF16 if t.dtype == torch.bfloat16 else F32
+
+
+def blocknorm_desc(x, h, z, y, mod=None, *, kind, post=0, eps, res_scale=1.0):
+    """BlockNormDesc of x, z (the stream) and h, y (a block's output, the next one's input), [B][S][D] tensors or views of any
+    strides (the last dimension contiguous); h and z None: no branch; y None: no norm after it.  mod: any of gate, scale and
+    shift, which lie alike: [B][D], rows of any stride, or [1][D] or [D] for one row that all sequences share (also None)."""
+    B, S, D = x.shape
+    if (h is None) != (z is None):
+        raise ParaganError(EINVAL, "blocknorm: h and z belong together")
+    like = h if h is not None else y
+    if like is None:
+        raise ParaganError(EINVAL, "blocknorm: neither h and z nor y")
+    for t, dt in ((x, x.dtype), (z, x.dtype), (h, like.dtype), (y, like.dtype)):
+        if t is not None and (tuple(t.shape) != (B, S, D) or t.dtype != dt or (D > 1 and t.stride(2) != 1)):
+            raise ParaganError(EINVAL, "blocknorm: x, h, z and y differ in shape, or x and z, h and y in type, or the last "
+                                       "dimension is not contiguous")
+    ms = 0
+    if mod is not None and mod.dim() == 2 and mod.shape[0] > 1:
+        ms = mod.stride(0)
+    if mod is not None and (mod.shape[-1] != D or mod.dim() > 2 or (mod.dim() == 2 and mod.shape[0] not in (1, B))):
+        raise ParaganError(EINVAL, "blocknorm: a modulation must be [B][D], [1][D] or [D]")
+    return BlockNormDesc(B, S, D, _token_dtype("blocknorm", like), _token_dtype("blocknorm", x), int(kind), int(h is not None),
+                         int(post), int(y is not None), eps, res_scale, ms, _token_stride(x), _token_stride(h),
+                         _token_stride(z), _token_stride(y))
+
+
+def paragan_blocknorm_check(desc):
+    return load().paragan_blocknorm_check(C.byref(desc))
+
+
+def paragan_blocknorm_sizes(desc):
+    return _sizes(load().paragan_blocknorm_sizes, desc)
+
+
+def _blocknorm_dims(desc, name):
+    what = name[1:] if name.startswith("d") else name
+    if name == "len":
+        return "int32", desc.B
+    if what.startswith("gain"):
+        return "float32", [(desc.D, 1)]
+    if what in ("gate", "scale", "shift"):
+        return "float32", [(desc.B if desc.mod_stride else 1, desc.mod_stride), (desc.D, 1)]
+    st = {"x": desc.x_stride, "h": desc.h_stride, "z": desc.z_stride if desc.branch else desc.x_stride,
+          "y": desc.y_stride}[what]
+    dt = desc.stream_dtype if what in "xz" else desc.dtype
+    return "bfloat16" if dt == BF16 else "float32", [(desc.B, st[0]), (desc.S, st[1]), (desc.D, 1)]
+
+
+_BLOCKNORM_FWD = ("x", "h", "gain_post", "gate", "gain_pre", "scale", "shift", "len", "z", "y")
+_BLOCKNORM_BWD = _BLOCKNORM_FWD[:8] + ("dz", "dy", "dx", "dh", "dgain_post", "dgate", "dgain_pre", "dscale", "dshift")
+
+
+def paragan_blocknorm_fwd(ctx, desc, x, h, gain_post, gate, gain_pre, scale, shift, len_, z, y, saved):
+    """saved: None when no backward follows."""
+    return ctx.check(load().paragan_blocknorm_fwd(ctx.h, C.byref(desc), *_placed(
+        desc, _blocknorm_dims, _BLOCKNORM_FWD, x, h, gain_post, gate, gain_pre, scale, shift, len_, z, y), _ptr(saved)))
+
+
+def paragan_blocknorm_bwd(ctx, desc, x, h, gain_post, gate, gain_pre, scale, shift, len_, saved, dz, dy, dx, dh, dgain_post,
+                          dgate, dgain_pre, dscale, dshift, ws):
+    """dz and dy lie as z (x without a branch) and y, dx and dh as x and h, the rows' gradients (None: not wanted) as the rows."""
+    p = _placed(desc, _blocknorm_dims, _BLOCKNORM_BWD, x, h, gain_post, gate, gain_pre, scale, shift, len_, dz, dy, dx, dh,
+                dgain_post, dgate, dgain_pre, dscale, dshift)
+    return ctx.check(load().paragan_blocknorm_bwd(ctx.h, C.byref(desc), *p[:8], _ptr(saved), *p[8:], _ptr(ws)))
+
+
+def scan_desc(x, r, g, y, *, sharp, reverse=0):
+    """ScanDesc of x, r, g, y [B][S][D], tensors or views of any strides (the last dimension contiguous)."""
+    for t in (x, r, g, y):
+        if tuple(t.shape) != tuple(x.shape) or t.dtype != x.dtype or t.dim() != 3 or t.stride(2) != 1:
+            raise ParaganError(EINVAL, "scan: x, r, g and y differ in shape or type, or the last dimension is not contiguous")
+    return ScanDesc(*x.shape, _token_dtype("scan", x), int(reverse), sharp, *(_token_stride(t) for t in (x, r, g, y)))
+
+
+def paragan_scan_check(desc):
+    return load().paragan_scan_check(C.byref(desc))
+
+
+def paragan_scan_sizes(desc):
+    return _sizes(load().paragan_scan_sizes, desc)
+
+
+def _scan_dims(desc, name):
+    if name == "len":
+        return "int32", desc.B
+    if name in ("decay", "ddecay"):
+        return "float32", desc.D
+    if name in ("h0", "ht", "dht", "dh0"):
+        return "float32", desc.B * desc.D, desc.D
+    st = {"x": desc.x_stride, "r": desc.r_stride, "g": desc.g_stride, "y": desc.y_stride}[name.lstrip("d")]
+    return "bfloat16" if desc.dtype == BF16 else "float32", [(desc.B, st[0]), (desc.S, st[1]), (desc.D, 1)]
+
+
+_SCAN_FWD = ("x", "r", "g", "decay", "len", "h0", "y", "ht")
+_SCAN_BWD = _SCAN_FWD[:5] + ("dy", "dht", "dx", "dr", "dg", "ddecay", "dh0")
+
+
+def paragan_scan_fwd(ctx, desc, x, r, g, decay, len_, h0, y, ht, saved, ws):
+    """saved: None when no backward follows."""
+    return ctx.check(load().paragan_scan_fwd(ctx.h, C.byref(desc), *_placed(
+        desc, _scan_dims, _SCAN_FWD, x, r, g, decay, len_, h0, y, ht), _ptr(saved), _ptr(ws)))
+
+
+def paragan_scan_bwd(ctx, desc, x, r, g, decay, len_, saved, dy, dht, dx, dr, dg, ddecay, dh0, ws):
+    """dy lies as y, dx, dr and dg as x, r and g."""
+    p = _placed(desc, _scan_dims, _SCAN_BWD, x, r, g, decay, len_, dy, dht, dx, dr, dg, ddecay, dh0)
+    return ctx.check(load().paragan_scan_bwd(ctx.h, C.byref(desc), *p[:5], _ptr(saved), *p[5:], _ptr(ws)))
+
+
+class ClipPlan:
+    """The tensors of paragan_clip, kept alive here, and their plan on the GPU.  grads, outs: contiguous bfloat16 or float32
+    tensors, an output of its gradient's type and size; outs None: in place."""
+
+    def __init__(self, grads, outs=None):
+        import torch
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if len(outs) != len(grads) or not grads:
+            raise ParaganError(EINVAL, "clip: needs gradients and as many outputs")
+        arr = (ClipTensor * len(grads))()
+        for i, (g, o) in enumerate(zip(grads, outs)):
+            for t in (g, o):
+                if t.dtype != g.dtype or t.numel() != g.numel() or not t.is_contiguous():
+                    raise ParaganError(EINVAL, "clip: tensor %d: gradient and output must be contiguous, of one type and size" % i)
+                if not t.is_cuda or t.device != grads[0].device:
+                    raise ParaganError(EINVAL, "clip: tensor %d must be on the GPU, all on the same one" % i)
+            arr[i] = ClipTensor(g.data_ptr(), o.data_ptr(), g.numel(), _token_dtype("clip", g), 0)
+        n, w = C.c_size_t(), C.c_size_t()
+        _check_static(load().paragan_clip_sizes(arr, len(grads), C.byref(n), C.byref(w)))
+        host = np.zeros(max(n.value, 8), dtype=np.uint8)
+        self.desc = ClipDesc()
+        _check_static(load().paragan_clip_plan(arr, len(grads), C.byref(self.desc), C.c_void_p(host.ctypes.data)))
+        self.tensors, self.ws_bytes = (grads, outs), w.value
+        self.table = torch.from_numpy(host).to(grads[0].device)
+
+
+def paragan_clip(ctx, plan, max_norm, grad_scale, norm, ws):
+    """plan: ClipPlan; norm: float32 [2], norm and factor."""
+    _hold("norm", norm, "float32", 2)
+    return ctx.check(load().paragan_clip(ctx.h, C.byref(plan.desc), _ptr(plan.table), max_norm, grad_scale, _ptr(norm),
+                                         _ptr(ws)))
 
 
 def paragan_gout_layout(desc):
