@@ -13,7 +13,7 @@ namespace pg {
 
 namespace {
 
-constexpr int kStep = 16;          // tokens between two states that a forward keeps
+constexpr int kStep = 16, kKeep = 64;   // tokens between two states that a forward keeps: a thread a sequence, tiles
 
 struct ScArgs {
   const void *x, *r, *g, *dy;
@@ -22,10 +22,12 @@ struct ScArgs {
   const float* h0;                 // backward: dht
   float* ht;                       // backward: dh0
   void *y, *dr, *dg;               // y; backward: dx in y
-  float* saved;                    // [B][ceil(S / kStep)][D]: the state ahead of every kStep tokens
-  double* part;                    // [B][D]: sums of dla s
+  float* saved;                    // [B][ceil(S / kStep or kKeep)][D]: the state ahead of that many tokens
+  float* maps;                     // [B][chunks][D][2]: A, H of every chunk
+  double* part;                    // [B][chunks][D]: sums of dla s
   int64_t xs[2], rs[2], gs[2], ys[2];
-  int S, D, reverse;
+  int B, S, D, reverse;
+  int slabs, nc, chunk;            // slabs of channels; chunks of a sequence, tokens of one
   float sharp;
 };
 
@@ -196,55 +198,624 @@ __global__ __launch_bounds__(64) void k_scan_seq_bwd(ScArgs a) {
   a.part[o + 1] = sum[1];
 }
 
-// ddecay = -sharp sigmoid(decay) times the sum over the sequences, in order
-__global__ __launch_bounds__(256) void k_scan_decay(const double* part, const float* decay, int B, int D, float sharp,
-                                                    float* ddecay) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= D) return;
-  double s = 0.0;
+// ------------------------------------------------------------- tiles of tokens
+// A block takes a slab of 2 CL channels through tiles of TT tokens that lie
+// one behind the other in memory: lane (cl, tl) of wave w holds TOK tokens of
+// segment w TL + tl in order, two channels of each.  A segment is a linear map
+// of the state ahead of it, h -> A h + H: the lanes of a wave join theirs by
+// exchanges, the waves through LDS (two halves used in turn: one barrier a
+// tile), and every thread then runs its own tokens from the state at its
+// segment's start.  The next tile's loads are under way meanwhile.  Loads and
+// stores go through buffer descriptors that begin at the tile and end at the
+// sequence's length: a lane's offset is fixed, a token's is uniform, and what
+// is past the length or the last channel reads as zero and is not written.
+template <typename T> PG_DEV Two<T> never();   // sigmoid 0: a token that keeps the state and adds nothing
+template <> PG_DEV Two<bf16_t> never<bf16_t>() { return Two<bf16_t>{0xff80ff80u}; }
+template <> PG_DEV Two<float> never<float>() { return Two<float>{make_float2(-INFINITY, -INFINITY)}; }
+
+template <typename T_, int CL_, int NW_>
+struct Form {
+  typedef T_ T;
+  static constexpr int CL = CL_, NW = NW_, TOK = sizeof(T) == 2 ? 8 : 4, TL = 64 / CL, NSEG = NW * TL, TT = NSEG * TOK;
+};
+
+template <typename F>
+struct Place {
+  int cl, tl, wave, seg, mseg, c, cc;   // mseg: the segment's place in memory; c: first channel, cc: one that exists
+  bool ok;
+  int b, chunk, len, lo, hi, n;         // tokens [lo, hi) in memory of the chunk, tiles of it that hold tokens
+  PG_DEV Place(const ScArgs& a) {
+    const int lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    cl = lane % F::CL; tl = lane / F::CL;
+    seg = wave * F::TL + tl;
+    mseg = a.reverse ? F::NSEG - 1 - seg : seg;
+    // neighbouring slabs on one XCD: they share cache lines and pages
+    const uint32_t id = blockIdx.x, per = gridDim.x / 8;
+    uint32_t l = (id % 8) * per + id / 8;
+    chunk = l % a.nc;
+    l /= a.nc;
+    const int slab = l % a.slabs;
+    b = l / a.slabs;
+    c = (slab * F::CL + cl) * 2;
+    ok = c < a.D;
+    cc = ok ? c : 0;
+    if (b < a.B) {
+      len = __builtin_amdgcn_readfirstlane(a.len ? min(max(a.len[b], 0), a.S) : a.S);
+      lo = (a.reverse ? a.nc - 1 - chunk : chunk) * a.chunk;
+      hi = min(a.S, lo + a.chunk);
+      n = len > lo ? (min(hi, len) - lo + F::TT - 1) / F::TT : 0;
+    }
+  }
+  // where tile k, in order, begins in memory
+  PG_DEV int tile(int k, int reverse) const { return lo + (reverse ? n - 1 - k : k) * F::TT; }
+};
+
+PG_DEV void buf_load(Two<bf16_t>& v, __amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t so) {
+  v.v = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, (int)so, 0);
+}
+PG_DEV void buf_load(Two<float>& v, __amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t so) {
+  v.v = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, (int)so, 0));
+}
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+template <typename T>
+PG_DEV void buf_store(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t so, float2 v) {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b32(f2bf2(v.x, v.y), r, (int)off, (int)so, 0);
+  else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, (int)off, (int)so, 0);
+}
+
+// A tensor's tokens as a lane takes them: `run` tokens in memory from mseg * run on.
+template <typename F>
+struct Tokens {
+  typedef typename F::T T;
+  const char* base;                // the sequence
+  int64_t st;                      // bytes between tokens
+  uint32_t lane;
+  PG_DEV Tokens(const void* p, const int64_t* s, const Place<F>& q, int run = F::TOK) {
+    base = (const char*)p + q.b * s[0] * (int64_t)sizeof(T);
+    st = s[1] * (int64_t)sizeof(T);
+    lane = q.ok ? (uint32_t)q.mseg * (uint32_t)run * (uint32_t)st + (uint32_t)q.c * (uint32_t)sizeof(T) : kOOB;
+  }
+  // descriptor from token m on; all of one row where tokens repeat
+  PG_DEV __amdgpu_buffer_rsrc_t at(int m, int len) const {
+    const int64_t n = (int64_t)(len - m) * st;
+    return make_rsrc(base + m * st, st == 0 || n > kBufMax ? kBufMax : n < 0 ? 0 : n);
+  }
+  PG_DEV uint32_t place(int j, int reverse) const { return (uint32_t)(reverse ? F::TOK - 1 - j : j) * (uint32_t)st; }
+  PG_DEV void load(Two<T>* v, int m, int len, int reverse, uint32_t so = 0) const {
+    const __amdgpu_buffer_rsrc_t r = at(m, len);
+#pragma unroll
+    for (int j = 0; j < F::TOK; ++j) buf_load(v[j], r, lane, so + place(j, reverse));
+  }
+  template <typename G> PG_DEV void store(int m, int len, int reverse, G&& get) const {
+    const __amdgpu_buffer_rsrc_t r = at(m, len);
+#pragma unroll
+    for (int j = 0; j < F::TOK; ++j) buf_store<T>(r, lane, place(j, reverse), get(j));
+  }
+  // rows [max(lo, len), hi) become zeros
+  PG_DEV void zero(const Place<F>& p) const {
+    for (int t = max(p.lo, p.len) + p.seg; t < p.hi; t += F::NSEG)
+      if (p.ok) st2f((T*)(const_cast<char*>(base) + t * st) + p.c, 0.f, 0.f);
+  }
+};
+// tokens from m on (of this lane) past the length never come in
+template <typename F>
+PG_DEV void past(Two<typename F::T>* r, int m, int len, int reverse) {
+#pragma unroll
+  for (int j = 0; j < F::TOK; ++j)
+    if (m + (reverse ? F::TOK - 1 - j : j) >= len) r[j] = never<typename F::T>();
+}
+
+// (A, H) of what lies ahead of this lane's segment in its wave (ahead), and of
+// the wave's segments up to it (A, H)
+template <int CL>
+PG_DEV void join_up(float2& A, float2& H, float2& Ae, float2& He) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = CL; d < 64; d *= 2) {
+    const float a0 = __shfl_up(A.x, d, 64), a1 = __shfl_up(A.y, d, 64), h0 = __shfl_up(H.x, d, 64), h1 = __shfl_up(H.y, d, 64);
+    if (lane >= d) {
+      H = make_float2(fmaf(A.x, h0, H.x), fmaf(A.y, h1, H.y));
+      A = make_float2(A.x * a0, A.y * a1);
+    }
+  }
+  const float a0 = __shfl_up(A.x, CL, 64), a1 = __shfl_up(A.y, CL, 64), h0 = __shfl_up(H.x, CL, 64), h1 = __shfl_up(H.y, CL, 64);
+  const bool first = lane < CL;
+  Ae = first ? make_float2(1.f, 1.f) : make_float2(a0, a1);
+  He = first ? make_float2(0.f, 0.f) : make_float2(h0, h1);
+}
+template <int CL>
+PG_DEV void join_down(float2& A, float2& H, float2& Ae, float2& He) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = CL; d < 64; d *= 2) {
+    const float a0 = __shfl_down(A.x, d, 64), a1 = __shfl_down(A.y, d, 64), h0 = __shfl_down(H.x, d, 64), h1 = __shfl_down(H.y, d, 64);
+    if (lane + d < 64) {
+      H = make_float2(fmaf(A.x, h0, H.x), fmaf(A.y, h1, H.y));
+      A = make_float2(A.x * a0, A.y * a1);
+    }
+  }
+  const float a0 = __shfl_down(A.x, CL, 64), a1 = __shfl_down(A.y, CL, 64), h0 = __shfl_down(H.x, CL, 64), h1 = __shfl_down(H.y, CL, 64);
+  const bool last = lane >= 64 - CL;
+  Ae = last ? make_float2(1.f, 1.f) : make_float2(a0, a1);
+  He = last ? make_float2(0.f, 0.f) : make_float2(h0, h1);
+}
+PG_DEV float2 fold(float2 A, float2 H, float2 h) { return make_float2(fmaf(A.x, h.x, H.x), fmaf(A.y, h.y, H.y)); }
+
+PG_DEV float sigmoid1(float v) {   // alone: 1 / (1 + e^-v), which may be infinite
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e));
+}
+// a and u of one element
+PG_DEV void gate(float x, float r, float g, float k, float& a, float& u) {
+  float p;
+  decay_of(k * sigmoid1(r), a, p);
+  u = __builtin_amdgcn_sqrtf(p) * sigmoid1(g) * x;
+}
+
+// SPLIT: the chunks of a sequence start from the folded maps of those ahead
+template <typename F, bool SPLIT>
+__global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
+  constexpr int CL = F::CL, NW = F::NW, TOK = F::TOK;
+  typedef typename F::T T;
+  __shared__ float4 sh[2][NW][CL];
+  const Place<F> p(a);
+  if (p.b >= a.B) return;
+  const Tokens<F> x(a.x, a.xs, p), r(a.r, a.rs, p), g(a.g, a.gs, p), y(a.y, a.ys, p);
+  const int64_t o = (int64_t)p.b * a.D + p.cc;
+  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
+  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  float2 h = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
+  Two<T> X[TOK], R[TOK], G[TOK];
+  auto load = [&](int m) {
+    r.load(R, m, p.len, a.reverse);
+    g.load(G, m, p.len, a.reverse);
+    x.load(X, m, p.len, a.reverse);
+  };
+  if (p.n) load(p.tile(0, a.reverse));
+  if constexpr (SPLIT) {
+    const float* m = a.maps + ((int64_t)p.b * a.nc * a.D + p.cc) * 2;
 #pragma unroll 8
-  for (int b = 0; b < B; ++b) s += part[(int64_t)b * D + c];
+    for (int j = 0; j < p.chunk; ++j) {
+      const float4 q = *reinterpret_cast<const float4*>(m + (int64_t)j * a.D * 2);
+      h = fold(make_float2(q.x, q.z), make_float2(q.y, q.w), h);
+    }
+  }
+  int turn = 0;
+  for (int t = 0; t < p.n; ++t, turn ^= 1) {
+    const int m0 = p.tile(t, a.reverse), mine = m0 + p.mseg * TOK;
+    if (m0 + F::TT > p.len) past<F>(R, mine, p.len, a.reverse);
+    float2 av[TOK], uv[TOK], A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < TOK; ++j) {
+      const float2 xx = X[j].get(), rr = R[j].get(), gg = G[j].get();
+      gate(xx.x, rr.x, gg.x, k.x, av[j].x, uv[j].x);
+      gate(xx.y, rr.y, gg.y, k.y, av[j].y, uv[j].y);
+      H = fold(av[j], uv[j], H);
+      A.x *= av[j].x;
+      A.y *= av[j].y;
+    }
+    if (t + 1 < p.n) load(p.tile(t + 1, a.reverse));
+    float2 Ae, He;
+    join_up<CL>(A, H, Ae, He);
+    if (p.tl == F::TL - 1) sh[turn][p.wave][p.cl] = make_float4(A.x, A.y, H.x, H.y);
+    __syncthreads();
+    float2 hw = h;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float4 q = sh[turn][w][p.cl];
+      if (w == p.wave) hw = h;
+      h = fold(make_float2(q.x, q.y), make_float2(q.z, q.w), h);
+    }
+    hw = fold(Ae, He, hw);
+    // the first segment of kKeep tokens keeps the state ahead of them
+    const int keep = mine / kKeep;
+    if (a.saved && p.ok && (mine + (a.reverse ? TOK : 0)) % kKeep == 0 && keep * kKeep < p.len)
+      *reinterpret_cast<float2*>(a.saved + ((int64_t)p.b * cdiv(a.S, kKeep) + keep) * a.D + p.c) = hw;
+    y.store(m0, p.len, a.reverse, [&](int j) { return hw = fold(av[j], uv[j], hw); });
+  }
+  y.zero(p);
+  if (a.ht && p.chunk == a.nc - 1 && p.seg == 0 && p.ok) *reinterpret_cast<float2*>(a.ht + o) = h;
+}
+
+// The map (A, H) of every chunk: its segments run through it side by side,
+// TOK tokens at a time, and are joined once at the end.
+template <typename F>
+__global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
+  constexpr int CL = F::CL, NW = F::NW, TOK = F::TOK;
+  typedef typename F::T T;
+  __shared__ float4 sh[NW][CL];
+  const Place<F> p(a);
+  if (p.b >= a.B || p.chunk == a.nc - 1) return;   // nobody comes after the last one
+  const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;   // a chunk is whole tiles
+  const Tokens<F> x(a.x, a.xs, p, run), r(a.r, a.rs, p, run), g(a.g, a.gs, p, run);
+  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
+  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
+  Two<T> X[TOK], R[TOK], G[TOK];
+  auto load = [&](int i) {         // i: order index in the run
+    const int at = a.reverse ? run - TOK - i : i;
+    r.load(R, p.lo, p.len, a.reverse, (uint32_t)at * (uint32_t)r.st);
+    g.load(G, p.lo, p.len, a.reverse, (uint32_t)at * (uint32_t)g.st);
+    x.load(X, p.lo, p.len, a.reverse, (uint32_t)at * (uint32_t)x.st);
+  };
+  if (p.n) {
+    load(0);
+    for (int i = 0; i < run; i += TOK) {
+      float2 av[TOK], uv[TOK];
+      if (p.lo + a.chunk > p.len) past<F>(R, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) {
+        const float2 xx = X[j].get(), rr = R[j].get(), gg = G[j].get();
+        gate(xx.x, rr.x, gg.x, k.x, av[j].x, uv[j].x);
+        gate(xx.y, rr.y, gg.y, k.y, av[j].y, uv[j].y);
+      }
+      if (i + TOK < run) load(i + TOK);
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) {
+        H = fold(av[j], uv[j], H);
+        A.x *= av[j].x;
+        A.y *= av[j].y;
+      }
+    }
+  }
+  float2 Ae, He;
+  join_up<CL>(A, H, Ae, He);
+  if (p.tl == F::TL - 1) sh[p.wave][p.cl] = make_float4(A.x, A.y, H.x, H.y);
+  __syncthreads();
+  if (p.seg == 0 && p.ok) {
+    A = make_float2(1.f, 1.f);
+    H = make_float2(0.f, 0.f);
+    for (int w = 0; w < NW; ++w) {
+      const float4 q = sh[w][p.cl];
+      H = fold(make_float2(q.x, q.y), make_float2(q.z, q.w), H);
+      A.x *= q.x;
+      A.y *= q.y;
+    }
+    *reinterpret_cast<float4*>(a.maps + (((int64_t)p.b * a.nc + p.chunk) * a.D + p.c) * 2) = make_float4(A.x, H.x, A.y, H.y);
+  }
+}
+
+// What one element needs after its gates are known: dx = E fx, dg = E fg,
+// dr = E M fr, ddecay += E M s, with M = a h_{t-1} - v.
+struct Grad {
+  float a, u, v, fx, fg, fr, s;
+};
+PG_DEV void grad_gate(float x, float r, float g, float k, Grad& e) {
+  float cs, sg, cg, p;
+  sigmoid(r, e.s, cs);
+  sigmoid(g, sg, cg);
+  const float l2 = k * e.s;
+  decay_of(l2, e.a, p);
+  const float q = __builtin_amdgcn_rsqf(p), aq = e.a * q;
+  e.fx = p * q * sg;
+  e.u = e.fx * x;
+  e.v = e.u * aq * aq;
+  e.fg = e.u * cg;
+  e.fr = l2 * kLn2 * cs;
+}
+
+// Backward of a tile: the states ahead of its segments from the forward's
+// kept state, what flows back into them from the tile behind it, both joined
+// at the same barrier.
+template <typename F, bool SPLIT>
+__global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
+  constexpr int CL = F::CL, NW = F::NW, TOK = F::TOK;
+  typedef typename F::T T;
+  __shared__ float4 sh[2][NW][CL];
+  __shared__ float2 sc[2][NW][CL];
+  __shared__ double sd[NW][64][2];
+  const Place<F> p(a);
+  if (p.b >= a.B) return;
+  const Tokens<F> x(a.x, a.xs, p), r(a.r, a.rs, p), g(a.g, a.gs, p), dy(a.dy, a.ys, p);
+  const Tokens<F> dx(a.y, a.xs, p), dr(a.dr, a.rs, p), dg(a.dg, a.gs, p);
+  const int64_t o = (int64_t)p.b * a.D + p.cc;
+  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
+  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  float2 c = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);   // flows back into the tile
+  const float* keep = a.saved + (int64_t)p.b * cdiv(a.S, kKeep) * a.D + p.cc;
+  Two<T> X[TOK], R[TOK], G[TOK], Y[TOK], Yn[TOK];
+  float2 hn = make_float2(0.f, 0.f);
+  auto load = [&](int m) {
+    r.load(R, m, p.len, a.reverse);
+    g.load(G, m, p.len, a.reverse);
+    x.load(X, m, p.len, a.reverse);
+    dy.load(Yn, m, p.len, a.reverse);
+    // ahead of the tile's first tokens (past the length nothing comes in)
+    const int i = a.reverse ? min((m + F::TT) / kKeep - 1, (p.len - 1) / kKeep) : m / kKeep;
+    hn = *reinterpret_cast<const float2*>(keep + (int64_t)i * a.D);
+  };
+  if (p.n) load(p.tile(p.n - 1, a.reverse));
+  if constexpr (SPLIT) {
+    const float* m = a.maps + ((int64_t)p.b * a.nc * a.D + p.cc) * 2;
+#pragma unroll 8
+    for (int j = a.nc - 1; j > p.chunk; --j) {
+      const float4 q = *reinterpret_cast<const float4*>(m + (int64_t)j * a.D * 2);
+      c = fold(make_float2(q.x, q.z), make_float2(q.y, q.w), c);
+    }
+  }
+  int turn = 0;
+  double sum0 = 0.0, sum1 = 0.0;
+  for (int t = p.n - 1; t >= 0; --t, turn ^= 1) {
+    const int m0 = p.tile(t, a.reverse);
+    if (m0 + F::TT > p.len) past<F>(R, m0 + p.mseg * TOK, p.len, a.reverse);
+    Grad e0[TOK], e1[TOK];
+    float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f), C = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < TOK; ++j) {
+      Y[j] = Yn[j];
+      const float2 xx = X[j].get(), rr = R[j].get(), gg = G[j].get();
+      grad_gate(xx.x, rr.x, gg.x, k.x, e0[j]);
+      grad_gate(xx.y, rr.y, gg.y, k.y, e1[j]);
+      H = make_float2(fmaf(e0[j].a, H.x, e0[j].u), fmaf(e1[j].a, H.y, e1[j].u));
+      A.x *= e0[j].a;
+      A.y *= e1[j].a;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    float2 h = hn;
+    if (t > 0) load(p.tile(t - 1, a.reverse));
+#pragma unroll
+    for (int j = TOK - 1; j >= 0; --j) {
+      const float2 d = Y[j].get();
+      C = make_float2(e0[j].a * (d.x + C.x), e1[j].a * (d.y + C.y));
+    }
+    float2 Ad = A, Ae, He, Ce, Ade;
+    join_up<CL>(A, H, Ae, He);
+    join_down<CL>(Ad, C, Ade, Ce);
+    if (p.tl == F::TL - 1) sh[turn][p.wave][p.cl] = make_float4(A.x, A.y, H.x, H.y);
+    if (p.tl == 0) sc[turn][p.wave][p.cl] = C;
+    __syncthreads();
+    float2 cw = c;
+#pragma unroll 2
+    for (int w = 0; w < NW; ++w) {
+      const float4 q = sh[turn][w][p.cl];
+      if (w < p.wave) h = fold(make_float2(q.x, q.y), make_float2(q.z, q.w), h);
+    }
+#pragma unroll 2
+    for (int w = NW - 1; w >= 0; --w) {
+      const float4 q = sh[turn][w][p.cl];
+      if (w == p.wave) cw = c;
+      c = fold(make_float2(q.x, q.y), sc[turn][w][p.cl], c);
+    }
+    h = fold(Ae, He, h);
+    cw = fold(Ade, Ce, cw);
+#pragma unroll
+    for (int j = 0; j < TOK; ++j) {   // v becomes M
+      e0[j].v = fmaf(e0[j].a, h.x, -e0[j].v);
+      e1[j].v = fmaf(e1[j].a, h.y, -e1[j].v);
+      h = make_float2(fmaf(e0[j].a, h.x, e0[j].u), fmaf(e1[j].a, h.y, e1[j].u));
+    }
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int j = TOK - 1; j >= 0; --j) {   // u becomes E
+      const float2 d = Y[j].get();
+      const float E0 = d.x + cw.x, E1 = d.y + cw.y;
+      cw = make_float2(e0[j].a * E0, e1[j].a * E1);
+      e0[j].u = E0;
+      e1[j].u = E1;
+      e0[j].v *= E0;
+      e1[j].v *= E1;
+      s0 = fmaf(e0[j].v, e0[j].s, s0);
+      s1 = fmaf(e1[j].v, e1[j].s, s1);
+    }
+    sum0 += s0;
+    sum1 += s1;
+    dx.store(m0, p.len, a.reverse, [&](int j) { return make_float2(e0[j].u * e0[j].fx, e1[j].u * e1[j].fx); });
+    dr.store(m0, p.len, a.reverse, [&](int j) { return make_float2(e0[j].v * e0[j].fr, e1[j].v * e1[j].fr); });
+    dg.store(m0, p.len, a.reverse, [&](int j) { return make_float2(e0[j].u * e0[j].fg, e1[j].u * e1[j].fg); });
+  }
+  dx.zero(p);
+  dr.zero(p);
+  dg.zero(p);
+  if (a.ht && p.chunk == 0 && p.seg == 0 && p.ok) *reinterpret_cast<float2*>(a.ht + o) = c;
+  const int lane = threadIdx.x & 63;
+  sd[p.wave][lane][0] = sum0;
+  sd[p.wave][lane][1] = sum1;
+  __syncthreads();
+  if (p.seg == 0 && p.ok) {          // the block's segments in order
+    sum0 = sum1 = 0.0;
+    for (int i = 0; i < F::NSEG; ++i) {
+      sum0 += sd[i / F::TL][i % F::TL * CL + p.cl][0];
+      sum1 += sd[i / F::TL][i % F::TL * CL + p.cl][1];
+    }
+    double* q = a.part + ((int64_t)p.b * a.nc + p.chunk) * a.D + p.c;
+    q[0] = sum0;
+    q[1] = sum1;
+  }
+}
+
+// The map c -> A c + C by which what flows into a chunk from behind leaves it
+// ahead: from the decays and dy alone.
+template <typename F>
+__global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
+  constexpr int CL = F::CL, NW = F::NW, TOK = F::TOK;
+  typedef typename F::T T;
+  __shared__ float4 sh[NW][CL];
+  const Place<F> p(a);
+  if (p.b >= a.B || p.chunk == 0) return;
+  const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;
+  const Tokens<F> r(a.r, a.rs, p, run), dy(a.dy, a.ys, p, run);
+  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
+  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
+  Two<T> R[TOK], Y[TOK];
+  auto load = [&](int i) {
+    const int at = a.reverse ? run - TOK - i : i;
+    r.load(R, p.lo, p.len, a.reverse, (uint32_t)at * (uint32_t)r.st);
+    dy.load(Y, p.lo, p.len, a.reverse, (uint32_t)at * (uint32_t)dy.st);
+  };
+  if (p.n) {
+    load(run - TOK);
+    for (int i = run - TOK; i >= 0; i -= TOK) {
+      float2 av[TOK], d[TOK];
+      if (p.lo + a.chunk > p.len) past<F>(R, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) {
+        const float2 rr = R[j].get();
+        float s, cs;
+        sigmoid(rr.x, s, cs);
+        av[j].x = __builtin_amdgcn_exp2f(k.x * s);
+        sigmoid(rr.y, s, cs);
+        av[j].y = __builtin_amdgcn_exp2f(k.y * s);
+        d[j] = Y[j].get();
+      }
+      if (i > 0) load(i - TOK);
+#pragma unroll
+      for (int j = TOK - 1; j >= 0; --j) {
+        H = make_float2(av[j].x * (d[j].x + H.x), av[j].y * (d[j].y + H.y));
+        A.x *= av[j].x;
+        A.y *= av[j].y;
+      }
+    }
+  }
+  float2 Ae, He;
+  join_down<CL>(A, H, Ae, He);
+  if (p.tl == 0) sh[p.wave][p.cl] = make_float4(A.x, A.y, H.x, H.y);
+  __syncthreads();
+  if (p.seg == 0 && p.ok) {
+    A = make_float2(1.f, 1.f);
+    H = make_float2(0.f, 0.f);
+    for (int w = NW - 1; w >= 0; --w) {
+      const float4 q = sh[w][p.cl];
+      H = fold(make_float2(q.x, q.y), make_float2(q.z, q.w), H);
+      A.x *= q.x;
+      A.y *= q.y;
+    }
+    *reinterpret_cast<float4*>(a.maps + (((int64_t)p.b * a.nc + p.chunk) * a.D + p.c) * 2) = make_float4(A.x, H.x, A.y, H.y);
+  }
+}
+
+// ddecay = -sharp sigmoid(decay) times the sum over the chunks of all
+// sequences: 32 channels x 8 lanes a block, in order
+__global__ __launch_bounds__(256) void k_scan_decay(const double* part, const float* decay, int64_t n, int D, float sharp,
+                                                    float* ddecay) {
+  __shared__ double sh[8][33];
+  const int j = threadIdx.x & 31, l = threadIdx.x >> 5, c = blockIdx.x * 32 + j;
+  double s = 0.0;
+  if (c < D) {
+#pragma unroll 8
+    for (int64_t i = l; i < n; i += 8) s += part[i * D + c];
+  }
+  sh[l][j] = s;
+  __syncthreads();
+  if (l > 0 || c >= D) return;
+  s = 0.0;
+  for (int i = 0; i < 8; ++i) s += sh[i][j];
   ddecay[c] = (float)(-(double)sharp / (1.0 + exp(-(double)decay[c])) * s);
 }
 
-ScArgs make_args(const Scan& a, const void* x, const void* r, const void* g, const float* decay, const int32_t* len) {
+// Which form a call takes, from its sizes alone.
+struct Plan {
+  int cl, nw;                      // 0: a thread a sequence and two channels
+  int slabs, nc, chunk;
+};
+Plan plan_of(const Scan& a, bool bwd) {
+  Plan p{0, 0, 0, 1, a.S};
+  if (a.S <= 32) return p;
+  p.cl = 32;
+  p.nw = 8;
+  p.slabs = (int)cdiv(a.D, 2 * p.cl);
+  const int tt = p.nw * (64 / p.cl) * (a.f32 ? 4 : 8);
+  // few slabs: chunks of sequences side by side, at the price of a pass over the inputs ahead
+  const int64_t rows = (int64_t)a.B * p.slabs, want = bwd ? 384 : 768, enough = bwd ? 192 : 128;
+  const int64_t nc = rows >= enough ? 1 : std::max<int64_t>(1, std::min<int64_t>(want / rows, a.S / (2 * tt)));
+  // a chunk is addressed in 32 bits
+  const int64_t st = std::max(std::max(a.xs[1], a.rs[1]), std::max(a.gs[1], a.ys[1])) * (a.f32 ? 4 : 2);
+  const int64_t most = std::max<int64_t>(1, kBufMax / std::max<int64_t>(st, 1) / tt) * tt;
+  p.chunk = (int)std::min(cdiv(cdiv(a.S, nc), tt) * tt, most);
+  p.nc = (int)cdiv(a.S, p.chunk);
+  return p;
+}
+
+ScArgs make_args(const Scan& a, const Plan& p, const void* x, const void* r, const void* g, const float* decay,
+                 const int32_t* len) {
   ScArgs k{};
   k.x = x; k.r = r; k.g = g; k.decay = decay; k.len = len;
   for (int i = 0; i < 2; ++i) { k.xs[i] = a.xs[i]; k.rs[i] = a.rs[i]; k.gs[i] = a.gs[i]; k.ys[i] = a.ys[i]; }
-  k.S = a.S; k.D = a.D; k.reverse = a.reverse; k.sharp = a.sharp;
+  k.B = a.B; k.S = a.S; k.D = a.D; k.reverse = a.reverse; k.sharp = a.sharp;
+  k.slabs = p.slabs; k.nc = p.nc; k.chunk = p.chunk;
   return k;
+}
+size_t maps_bytes(const Scan& a, const Plan& p) { return align256((size_t)a.B * p.nc * a.D * 2 * sizeof(float)); }
+
+enum { kFwd, kFwdSplit, kMaps, kBwd, kBwdSplit, kBackMaps };
+template <typename F>
+void launch1(int what, hipStream_t st, const ScArgs& k, unsigned blocks) {
+  const dim3 g(blocks), b(F::NW * 64);
+  switch (what) {
+    case kFwd: hipLaunchKernelGGL((k_scan_fwd<F, false>), g, b, 0, st, k); break;
+    case kFwdSplit: hipLaunchKernelGGL((k_scan_fwd<F, true>), g, b, 0, st, k); break;
+    case kMaps: hipLaunchKernelGGL((k_scan_maps<F>), g, b, 0, st, k); break;
+    case kBwd: hipLaunchKernelGGL((k_scan_bwd<F, false>), g, b, 0, st, k); break;
+    case kBwdSplit: hipLaunchKernelGGL((k_scan_bwd<F, true>), g, b, 0, st, k); break;
+    case kBackMaps: hipLaunchKernelGGL((k_scan_back_maps<F>), g, b, 0, st, k); break;
+  }
+  PG_LAUNCH_CHECK();
+}
+void launch(int what, hipStream_t st, const Scan& a, const Plan& p, const ScArgs& k) {
+  const unsigned blocks = (unsigned)(cdiv((int64_t)a.B * p.slabs * p.nc, 8) * 8);
+#define PG_SC(CL, NW)                                                  \
+  if (p.cl == CL && p.nw == NW) {                                      \
+    if (a.f32) launch1<Form<float, CL, NW>>(what, st, k, blocks);   \
+    else launch1<Form<bf16_t, CL, NW>>(what, st, k, blocks);        \
+    return;                                                            \
+  }
+  PG_SC(32, 8)
+#undef PG_SC
+  throw Error{-2, "scan: no such form"};
 }
 
 }  // namespace
 
-size_t scan_saved_bytes(const Scan& a) { return align256((size_t)a.B * cdiv(a.S, kStep) * a.D * sizeof(float)); }
-size_t scan_ws_bytes(const Scan& a) { return align256((size_t)a.B * a.D * sizeof(double)); }
+size_t scan_saved_bytes(const Scan& a) {
+  return align256((size_t)a.B * cdiv(a.S, plan_of(a, false).cl ? kKeep : kStep) * a.D * sizeof(float));
+}
+size_t scan_ws_bytes(const Scan& a) {
+  const Plan f = plan_of(a, false), b = plan_of(a, true);
+  return std::max(maps_bytes(a, f), maps_bytes(a, b) + align256((size_t)a.B * b.nc * a.D * sizeof(double)));
+}
 
 void scan_fwd(hipStream_t st, const Scan& a, const void* x, const void* r, const void* g, const float* decay,
               const int32_t* len, const float* h0, void* y, float* ht, void* saved, void* ws) {
-  ScArgs k = make_args(a, x, r, g, decay, len);
-  k.h0 = h0; k.y = y; k.ht = ht; k.saved = (float*)saved;
-  const dim3 grid((unsigned)a.B, (unsigned)cdiv(a.D, 128));
+  const Plan p = plan_of(a, false);
+  ScArgs k = make_args(a, p, x, r, g, decay, len);
+  k.h0 = h0; k.y = y; k.ht = ht; k.saved = (float*)saved; k.maps = (float*)ws;
   ProfScope prof(st);
-  if (a.f32) hipLaunchKernelGGL(k_scan_seq_fwd<float>, grid, dim3(64), 0, st, k);
-  else hipLaunchKernelGGL(k_scan_seq_fwd<bf16_t>, grid, dim3(64), 0, st, k);
-  PG_LAUNCH_CHECK();
+  if (!p.cl) {
+    const dim3 grid((unsigned)a.B, (unsigned)cdiv(a.D, 128));
+    if (a.f32) hipLaunchKernelGGL(k_scan_seq_fwd<float>, grid, dim3(64), 0, st, k);
+    else hipLaunchKernelGGL(k_scan_seq_fwd<bf16_t>, grid, dim3(64), 0, st, k);
+    PG_LAUNCH_CHECK();
+  } else if (p.nc == 1) {
+    launch(kFwd, st, a, p, k);
+  } else {
+    launch(kMaps, st, a, p, k);
+    launch(kFwdSplit, st, a, p, k);
+  }
   prof.done_bytes("k_scan_fwd", (a.f32 ? 16.0 : 8.0) * a.B * a.S * a.D);
 }
 
 void scan_bwd(hipStream_t st, const Scan& a, const void* x, const void* r, const void* g, const float* decay,
               const int32_t* len, const void* saved, const void* dy, const float* dht, void* dx, void* dr, void* dg,
               float* ddecay, float* dh0, void* ws) {
-  ScArgs k = make_args(a, x, r, g, decay, len);
+  const Plan p = plan_of(a, true);
+  ScArgs k = make_args(a, p, x, r, g, decay, len);
   k.dy = dy; k.h0 = dht; k.ht = dh0; k.y = dx; k.dr = dr; k.dg = dg; k.saved = (float*)const_cast<void*>(saved);
-  k.part = (double*)ws;
-  const dim3 grid((unsigned)a.B, (unsigned)cdiv(a.D, 128));
+  k.maps = (float*)ws;
+  k.part = (double*)((char*)ws + maps_bytes(a, p));
   ProfScope prof(st);
-  if (a.f32) hipLaunchKernelGGL(k_scan_seq_bwd<float>, grid, dim3(64), 0, st, k);
-  else hipLaunchKernelGGL(k_scan_seq_bwd<bf16_t>, grid, dim3(64), 0, st, k);
-  PG_LAUNCH_CHECK();
-  hipLaunchKernelGGL(k_scan_decay, dim3((unsigned)cdiv(a.D, 256)), dim3(256), 0, st, k.part, decay, a.B, a.D, a.sharp,
-                     ddecay);
+  if (!p.cl) {
+    const dim3 grid((unsigned)a.B, (unsigned)cdiv(a.D, 128));
+    if (a.f32) hipLaunchKernelGGL(k_scan_seq_bwd<float>, grid, dim3(64), 0, st, k);
+    else hipLaunchKernelGGL(k_scan_seq_bwd<bf16_t>, grid, dim3(64), 0, st, k);
+    PG_LAUNCH_CHECK();
+  } else if (p.nc == 1) {
+    launch(kBwd, st, a, p, k);
+  } else {
+    launch(kBackMaps, st, a, p, k);
+    launch(kBwdSplit, st, a, p, k);
+  }
+  hipLaunchKernelGGL(k_scan_decay, dim3((unsigned)cdiv(a.D, 32)), dim3(256), 0, st, k.part, decay, (int64_t)a.B * p.nc, a.D,
+                     a.sharp, ddecay);
   PG_LAUNCH_CHECK();
   prof.done_bytes("k_scan_bwd", (a.f32 ? 28.0 : 14.0) * a.B * a.S * a.D);
 }

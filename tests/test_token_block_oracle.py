@@ -140,7 +140,7 @@ def test_scan_refusals(L):
     nan = float("nan")
     for kw in (dict(B=0), dict(S=0), dict(B=1 << 16, S=1 << 15), dict(D=0), dict(D=12), dict(D=(1 << 20) + 8), dict(dtype=3), dict(reverse=2),
                dict(sharp=0.0), dict(sharp=-1.0), dict(sharp=nan), dict(sharp=float("inf")), dict(y_stride=(0, 64)), dict(y_stride=(640, 56)),
-               dict(x_stride=(1920, 100)), dict(g_stride=(-1920, 192)), dict(r_stride=(1 << 58, 192)), dict(B=1 << 14, D=1 << 17)):
+               dict(x_stride=(1920, 100)), dict(g_stride=(-1920, 192)), dict(r_stride=(1 << 58, 192)), dict(B=1 << 14, D=1 << 17), dict(x_stride=(1 << 28, 1 << 20))):
         assert lib.paragan_scan_check(sc(**kw)) == lib.EINVAL, kw
         assert L.paragan_last_error(None).decode().startswith("scan")
     assert L.paragan_scan_check(None) == lib.EINVAL
