@@ -16,9 +16,13 @@
 // between stays in registers in fp32.  A lane holds 8 elements of a row (a
 // 16-byte access in bf16), a row lies over 8 to 64 lanes of a wave or over
 // the waves of a block, whose columns' rows (k, m, shift) stay in registers
-// over the tokens of one sequence that the block takes.
+// over the tokens of one sequence that the block takes.  The backward's
+// blocks fill a CU with rows side by side (1024 threads, 128 registers a
+// lane), so that few blocks have column sums to be joined, and a row's loads
+// are under way while the one before it is summed.
 #include "rows.hpp"
 #include "token.hpp"
+#include <type_traits>
 
 namespace pg {
 
@@ -45,6 +49,14 @@ PG_DEV void ld8(const float* p, float* f) {
   f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
 
+// Element c of the row at p + row: a uniform address and a lane's 32-bit
+// offset where a row lies over a block.
+template <typename T>
+PG_DEV T* place(T* p, int64_t row, int c) {
+  typedef typename std::conditional<std::is_const<T>::value, const char, char>::type B;
+  return reinterpret_cast<T*>(reinterpret_cast<B*>(p + row) + (uint32_t)(c * (int)sizeof(T)));
+}
+
 // Sums of two values over the lanes of a row.  P = 0: over the waves of the
 // block, through sh[2][16] float2, whose halves are used in turn so that one
 // barrier a sum is enough: who writes a half again has passed the barrier
@@ -52,7 +64,7 @@ PG_DEV void ld8(const float* p, float* f) {
 template <int P>
 struct RowSum {
   float2 (*sh)[16];
-  int turn, wave, waves;
+  int turn, wave, first, waves;    // this wave; the row's first and how many
   PG_DEV float2 operator()(float a, float b) {
     if constexpr (P > 0) {
       return make_float2(group_sum<P>(a), group_sum<P>(b));
@@ -62,12 +74,10 @@ struct RowSum {
       turn ^= 1;
       if ((threadIdx.x & 63) == 0) sh[turn][wave] = make_float2(a, b);
       __syncthreads();
-      float2 s = sh[turn][0];
-      for (int i = 1; i < waves; ++i) {
-        s.x += sh[turn][i].x;
-        s.y += sh[turn][i].y;
-      }
-      return s;
+      // every 16 lanes sum the waves' once more: one read, and lane moves
+      const int i = threadIdx.x & 15;
+      const float2 s = i < waves ? sh[turn][first + i] : make_float2(0.f, 0.f);
+      return make_float2(group_sum<16>(s.x), group_sum<16>(s.y));
     }
   }
 };
@@ -97,12 +107,13 @@ template <typename TX, typename TH, int P, bool POST>
 __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
   __shared__ float2 sh[2][16];
   constexpr int NG = P ? 256 / P : 1;
-  const int tid = threadIdx.x, grp = P ? tid / P : 0, ch = P ? tid % P : tid;
+  const int tid = threadIdx.x, ch = P ? tid % P : tid;
+  const int grp = P == 0 ? 0 : P == 64 ? __builtin_amdgcn_readfirstlane(tid / 64) : tid / P;
   const bool act = ch * 8 < a.D;
   const int c8 = act ? ch * 8 : 0;
   const int b = blockIdx.x / a.nc, r0 = (blockIdx.x - b * a.nc) * a.R, r1 = min(a.S, r0 + a.R);
-  const int len = a.len ? min(max(a.len[b], 0), a.S) : a.S;
-  RowSum<P> sum{sh, 0, tid >> 6, (int)blockDim.x >> 6};
+  const int len = __builtin_amdgcn_readfirstlane(a.len ? min(max(a.len[b], 0), a.S) : a.S);
+  RowSum<P> sum{sh, 0, tid >> 6, 0, (int)blockDim.x >> 6};
   float k[8], m[8], f[8], g1[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) { k[e] = a.res_scale; m[e] = 1.f; f[e] = 0.f; g1[e] = 1.f; }
@@ -120,21 +131,21 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
     for (int e = 0; e < 8; ++e) m[e] *= 1.f + s[e];
   }
   if (a.w.shift) ld8(a.w.shift + b * a.mod + c8, f);
-  const TX* x = (const TX*)a.x + b * a.xs[0] + c8;
-  const TH* h = (const TH*)a.h + b * a.hs[0] + c8;
-  TX* z = (TX*)a.z + b * a.zs[0] + c8;
-  TH* y = (TH*)a.y + b * a.ys[0] + c8;
+  const TX* x = (const TX*)a.x + b * a.xs[0];
+  const TH* h = (const TH*)a.h + b * a.hs[0];
+  TX* z = (TX*)a.z + b * a.zs[0];
+  TH* y = (TH*)a.y + b * a.ys[0];
   for (int rr = r0; rr < r1; rr += NG) {       // as often for every group
     const int r = min(rr + grp, r1 - 1);
     const bool ok = act && rr + grp < r1, real = act && r < len;
     float xv[8] = {}, hv[8] = {};
     if (real) {
       Raw<TX> q;
-      q.load(x + r * a.xs[1]);
+      q.load(place(x, r * a.xs[1], c8));
       q.get(xv);
       if (a.branch) {
         Raw<TH> p;
-        p.load(h + r * a.hs[1]);
+        p.load(place(h, r * a.hs[1], c8));
         p.get(hv);
       }
     }
@@ -143,13 +154,13 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
     if (a.branch) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) xv[e] = real ? fmaf(k[e], POST ? hv[e] * g1[e] : hv[e], xv[e]) : 0.f;
-      if (ok) st8f<TX>(z + r * a.zs[1], xv);
+      if (ok) st8f<TX>(place(z, r * a.zs[1], c8), xv);
     }
     if (a.pre) {
       const float2 stz = normalise<P>(sum, a.layer, act, a.inv_d, a.eps, xv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) xv[e] = real ? fmaf(xv[e], m[e], f[e]) : 0.f;
-      if (ok) st8f<TH>(y + r * a.ys[1], xv);
+      if (ok) st8f<TH>(place(y, r * a.ys[1], c8), xv);
       if (a.stats && ok && ch == 0)
         reinterpret_cast<float4*>(a.stats)[(int64_t)b * a.S + r] = make_float4(sth.x, sth.y, stz.x, stz.y);
     } else if (a.stats && ok && ch == 0) {
@@ -159,15 +170,16 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
 }
 
 template <typename TX, typename TH, int P, bool POST>
-__global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_bwd(BnArgs a) {
+__global__ __launch_bounds__(1024) void k_blocknorm_bwd(BnArgs a) {
   __shared__ float2 sh[2][16];
-  constexpr int NG = P ? 256 / P : 1;
-  const int tid = threadIdx.x, grp = P ? tid / P : 0, ch = P ? tid % P : tid;
+  // lanes of a row, rows a block takes side by side
+  const int tid = threadIdx.x, W = P ? P : (a.D + 511) / 512 * 64, NG = (int)blockDim.x / W;
+  const int grp = P == 0 || P == 64 ? __builtin_amdgcn_readfirstlane(tid / W) : tid / W, ch = tid - grp * W;
   const bool act = ch * 8 < a.D;
   const int c8 = act ? ch * 8 : 0;
   const int b = blockIdx.x / a.nc, r0 = (blockIdx.x - b * a.nc) * a.R, r1 = min(a.S, r0 + a.R);
-  const int len = a.len ? min(max(a.len[b], 0), a.S) : a.S;
-  RowSum<P> sum{sh, 0, tid >> 6, (int)blockDim.x >> 6};
+  const int len = __builtin_amdgcn_readfirstlane(a.len ? min(max(a.len[b], 0), a.S) : a.S);
+  RowSum<P> sum{sh, 0, tid >> 6, grp * (W >> 6), W >> 6};
   float k[8], m[8], se[8] = {}, sq[8] = {}, sp[8] = {};
 #pragma unroll
   for (int e = 0; e < 8; ++e) { k[e] = a.res_scale; m[e] = 1.f; }
@@ -189,40 +201,45 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_bwd(BnArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) m[e] *= 1.f + s[e];
   }
-  const TX* x = (const TX*)a.x + b * a.xs[0] + c8;
-  const TH* h = (const TH*)a.h + b * a.hs[0] + c8;
-  const TX* dz = (const TX*)a.dz + b * a.zs[0] + c8;
-  const TH* dy = (const TH*)a.dy + b * a.ys[0] + c8;
-  TX* dx = (TX*)a.z + b * a.xs[0] + c8;
-  TH* dh = (TH*)a.y + b * a.hs[0] + c8;
+  const TX* x = (const TX*)a.x + b * a.xs[0];
+  const TH* h = (const TH*)a.h + b * a.hs[0];
+  const TX* dz = (const TX*)a.dz + b * a.zs[0];
+  const TH* dy = (const TH*)a.dy + b * a.ys[0];
+  TX* dx = (TX*)a.z + b * a.xs[0];
+  TH* dh = (TH*)a.y + b * a.hs[0];
+  // the next row's loads are under way while this one is summed; rows that are none read one that is
+  Raw<TX> xr{}, zr{};
+  Raw<TH> hr{}, yr{};
+  float4 sr;
+  auto fetch = [&](int r) {
+    const int64_t q = min(r, max(len - 1, 0));
+    sr = reinterpret_cast<const float4*>(a.stats)[(int64_t)b * a.S + q];
+    if (a.branch) hr.load(place(h, q * a.hs[1], c8));
+    if (a.dz) zr.load(place(dz, q * a.zs[1], c8));
+    if (a.pre) {
+      xr.load(place(x, q * a.xs[1], c8));
+      yr.load(place(dy, q * a.ys[1], c8));
+    }
+  };
+  fetch(r0 + grp);
   for (int rr = r0; rr < r1; rr += NG) {
-    const int r = min(rr + grp, r1 - 1);
-    const bool ok = act && rr + grp < r1, real = ok && r < len;
-    float n[8] = {}, hn[8] = {}, dZ[8] = {}, dv[8] = {};
-    const float4 st = reinterpret_cast<const float4*>(a.stats)[(int64_t)b * a.S + r];
-    if (real) {
-      Raw<TX> q;
-      Raw<TH> p;
-      if (a.branch) {
-        p.load(h + r * a.hs[1]);
-        p.get(hn);
-      }
-      if (a.dz) {
-        q.load(dz + r * a.zs[1]);
-        q.get(dZ);
-      }
-      if (a.pre) {
-        q.load(x + r * a.xs[1]);
-        q.get(n);
-        p.load(dy + r * a.ys[1]);
-        p.get(dv);
-      }
+    const int r = rr + grp;
+    const bool ok = act && r < r1, real = ok && r < len;
+    float n[8], hn[8], dZ[8], dv[8];
+    const float4 st = sr;
+    xr.get(n);
+    hr.get(hn);
+    zr.get(dZ);
+    yr.get(dv);
+    if (rr + NG < r1) fetch(rr + NG + grp);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (POST) hn[e] = (hn[e] - st.x) * st.y;
-        if (a.branch) n[e] = fmaf(k[e], hn[e], n[e]);
-        n[e] = (n[e] - st.z) * st.w;
-      }
+    for (int e = 0; e < 8; ++e) {
+      if (POST) hn[e] = (hn[e] - st.x) * st.y;
+      if (a.branch) n[e] = fmaf(k[e], hn[e], n[e]);
+      n[e] = real ? (n[e] - st.z) * st.w : 0.f;
+      hn[e] = real ? hn[e] : 0.f;
+      dZ[e] = real ? dZ[e] : 0.f;
+      dv[e] = real ? dv[e] : 0.f;
     }
     if (a.pre) {
       float s1 = 0.f, s2 = 0.f;
@@ -239,7 +256,7 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_bwd(BnArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) dZ[e] = real ? fmaf(st.w, dv[e] - c1 - n[e] * c2, dZ[e]) : 0.f;
     }
-    if (ok) st8f<TX>(dx + r * a.xs[1], dZ);
+    if (ok) st8f<TX>(place(dx, r * a.xs[1], c8), dZ);
     if (a.branch) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -258,105 +275,110 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_bwd(BnArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) dv[e] = real ? st.y * (dv[e] - c1 - hn[e] * c2) : 0.f;
       }
-      if (ok) st8f<TH>(dh + r * a.hs[1], dv);
+      if (ok) st8f<TH>(place(dh, r * a.hs[1], c8), dv);
     }
   }
   // the item's column sums: the groups' in group order
   float* part = a.part + (int64_t)blockIdx.x * 3 * a.D;
-  if constexpr (P == 0) {
+  if (NG == 1) {
     if (act) {
-#pragma unroll
-      for (int w = 0; w < 3; ++w) st8f<float>(part + (int64_t)w * a.D + c8, w == 0 ? se : w == 1 ? sq : sp);
+      st8f<float>(part + c8, se);
+      st8f<float>(part + a.D + c8, sq);
+      st8f<float>(part + 2 * (int64_t)a.D + c8, sp);
     }
-  } else {
-    __shared__ float cols[256 * 8];
-#pragma unroll
-    for (int w = 0; w < 3; ++w) {
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) cols[tid * 8 + e] = w == 0 ? se[e] : w == 1 ? sq[e] : sp[e];
-      __syncthreads();
-      for (int c = tid; c < a.D; c += 256) {
-        double s = 0.0;
-        for (int j = 0; j < NG; ++j) s += cols[j * P * 8 + c];
-        part[(int64_t)w * a.D + c] = (float)s;
-      }
-    }
+    return;
+  }
+  __shared__ float cols[3][1024 * 8];
+  st8f<float>(cols[0] + tid * 8, se);
+  st8f<float>(cols[1] + tid * 8, sq);
+  st8f<float>(cols[2] + tid * 8, sp);
+  __syncthreads();
+  const int n = W * 8;             // floats of a group
+  for (int i = tid; i < 3 * a.D; i += blockDim.x) {
+    const int w = i / a.D, c = i - w * a.D;
+    double s = 0.0;
+    for (int j = 0; j < NG; ++j) s += cols[w][j * n + c];
+    part[i] = (float)s;
   }
 }
+
+constexpr int kAhead = 16;         // items of a lane whose loads are under way together
 
 struct BnJoin {
   BlockNormRows w;
   BlockNormGrads g;
   const float* part;
-  double* seq;                     // [B][3][D], sums of every sequence
   int64_t mod;
-  int B, D, nc;
+  int B, D, nc, gs;                // gs: lanes that share a sequence's items, a power of two
   float res_scale;
 };
 
-// Sums over the items of one sequence (blockIdx.x): 32 columns x 8 item lanes
-// a block, in order, in 64 bits; the sequence's own gradients from them.
-__global__ __launch_bounds__(256) void k_blocknorm_seq(BnJoin a) {
-  __shared__ double sh[3][8][33];
-  const int j = threadIdx.x & 31, l = threadIdx.x >> 5, c = blockIdx.y * 32 + j, b = blockIdx.x;
-  double s[3] = {0.0, 0.0, 0.0};
-  if (c < a.D) {
-    const float* p = a.part + (int64_t)b * a.nc * 3 * a.D + c;
-#pragma unroll 4
-    for (int i = l; i < a.nc; i += 8)
-#pragma unroll
-      for (int w = 0; w < 3; ++w) s[w] += p[((int64_t)i * 3 + w) * a.D];
-  }
-#pragma unroll
-  for (int w = 0; w < 3; ++w) sh[w][l][j] = s[w];
-  __syncthreads();
-  if (l > 0 || c >= a.D) return;
-#pragma unroll
-  for (int w = 0; w < 3; ++w) {
-    s[w] = 0.0;
-    for (int i = 0; i < 8; ++i) s[w] += sh[w][i][j];
-    if (a.seq) a.seq[((int64_t)b * 3 + w) * a.D + c] = s[w];
-  }
-  if (a.mod) {
-    const int64_t o = b * a.mod + c;
-    if (a.g.shift) a.g.shift[o] = (float)s[0];
-    if (a.g.scale) a.g.scale[o] = (float)((a.w.gain_pre ? a.w.gain_pre[c] : 1.0) * s[1]);
-    if (a.g.gate) a.g.gate[o] = (float)((double)a.res_scale * (a.w.gain_post ? a.w.gain_post[c] : 1.0) * s[2]);
-  }
-}
-
-// Sums over the sequences: the gains' gradients, and those of shared rows
-__global__ __launch_bounds__(256) void k_blocknorm_join(BnJoin a) {
-  __shared__ double sh[5][8][33];
-  const int j = threadIdx.x & 31, l = threadIdx.x >> 5, c = blockIdx.x * 32 + j;
-  double s[5] = {0.0, 0.0, 0.0, 0.0, 0.0};   // e, q, p, (1 + scale) q, gate p
-  if (c < a.D) {
-#pragma unroll 2
-    for (int b = l; b < a.B; b += 8) {
-      const double* p = a.seq + (int64_t)b * 3 * a.D + c;
-      const double e = p[0], q = p[a.D], pp = p[2 * (int64_t)a.D];
-      s[0] += e; s[1] += q; s[2] += pp;
-      s[3] += (1.0 + (a.w.scale ? a.w.scale[b * a.mod + c] : 0.0)) * q;
-      s[4] += (a.w.gate ? a.w.gate[b * a.mod + c] : 1.0) * pp;
+// The rows' gradients from the items' sums, in 64 bits and in order: 16
+// columns x 64 lanes a block.  Lanes take sequences; where these are fewer, gs
+// lanes share the items of one.  What all sequences share is summed over the
+// lanes at the end.
+__global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
+  __shared__ double sh[5][64][17];
+  const int j = threadIdx.x & 15, l = threadIdx.x >> 4, c = blockIdx.x * 16 + j, cc = min(c, a.D - 1);
+  const int grp = l / a.gs, li = l % a.gs, ng = 64 / a.gs;
+  const double g1 = a.w.gain_post ? a.w.gain_post[cc] : 1.0, g2 = a.w.gain_pre ? a.w.gain_pre[cc] : 1.0;
+  const double rs = a.res_scale;
+  double t[5] = {0.0, 0.0, 0.0, 0.0, 0.0};   // over the sequences: e, q, p, (1 + scale) q, gate p
+  auto done = [&](int b, double e, double q, double p) {
+    const int64_t o = b * a.mod + cc;
+    t[0] += e; t[1] += q; t[2] += p;
+    t[3] += (1.0 + (a.w.scale ? a.w.scale[o] : 0.0)) * q;
+    t[4] += (a.w.gate ? a.w.gate[o] : 1.0) * p;
+    if (a.mod && c < a.D) {
+      if (a.g.shift) a.g.shift[o] = (float)e;
+      if (a.g.scale) a.g.scale[o] = (float)(g2 * q);
+      if (a.g.gate) a.g.gate[o] = (float)(rs * g1 * p);
     }
+  };
+  double s[3] = {0.0, 0.0, 0.0};
+  for (int b = grp; b < a.B; b += ng) {
+    const float* p = a.part + (int64_t)b * a.nc * 3 * a.D + cc;
+    s[0] = s[1] = s[2] = 0.0;
+    for (int i0 = li; i0 < a.nc; i0 += kAhead * a.gs) {
+      float v[kAhead][3];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int w = 0; w < 3; ++w) v[u][w] = p[((int64_t)min(i0 + u * a.gs, a.nc - 1) * 3 + w) * a.D];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int w = 0; w < 3; ++w) s[w] += i0 + u * a.gs < a.nc ? v[u][w] : 0.f;
+    }
+    if (a.gs == 1) done(b, s[0], s[1], s[2]);
+  }
+  if (a.gs > 1) {                  // then a group of lanes has one sequence or none
+#pragma unroll
+    for (int w = 0; w < 3; ++w) sh[w][l][j] = s[w];
+    __syncthreads();
+    if (li == 0 && grp < a.B) {
+#pragma unroll
+      for (int w = 0; w < 3; ++w) {
+        s[w] = 0.0;
+        for (int i = 0; i < a.gs; ++i) s[w] += sh[w][l + i][j];
+      }
+      done(grp, s[0], s[1], s[2]);
+    }
+    __syncthreads();
   }
 #pragma unroll
-  for (int w = 0; w < 5; ++w) sh[w][l][j] = s[w];
+  for (int w = 0; w < 5; ++w) sh[w][l][j] = t[w];
   __syncthreads();
-  if (l > 0 || c >= a.D) return;
-#pragma unroll
-  for (int w = 0; w < 5; ++w) {
-    s[w] = 0.0;
-    for (int i = 0; i < 8; ++i) s[w] += sh[w][i][j];
-  }
-  if (a.g.gain_pre) a.g.gain_pre[c] = (float)s[3];
-  if (a.g.gain_post) a.g.gain_post[c] = (float)((double)a.res_scale * s[4]);
-  if (!a.mod) {
-    if (a.g.shift) a.g.shift[c] = (float)s[0];
-    if (a.g.scale) a.g.scale[c] = (float)((a.w.gain_pre ? a.w.gain_pre[c] : 1.0) * s[1]);
-    if (a.g.gate) a.g.gate[c] = (float)((double)a.res_scale * (a.w.gain_post ? a.w.gain_post[c] : 1.0) * s[2]);
-  }
+  if (l >= 5 || c >= a.D) return;
+  double v = 0.0;
+#pragma unroll 8
+  for (int i = 0; i < 64; ++i) v += sh[l][i][j];
+  if (l == 3 && a.g.gain_pre) a.g.gain_pre[c] = (float)v;
+  if (l == 4 && a.g.gain_post) a.g.gain_post[c] = (float)(rs * v);
+  if (a.mod) return;
+  if (l == 0 && a.g.shift) a.g.shift[c] = (float)v;
+  if (l == 1 && a.g.scale) a.g.scale[c] = (float)(g2 * v);
+  if (l == 2 && a.g.gate) a.g.gate[c] = (float)(rs * g1 * v);
 }
 
 // lanes of a row inside a wave, or 0 where it lies over a block's waves
@@ -366,10 +388,14 @@ int row_lanes(int D) {
   return 0;
 }
 
+// Threads of a block, and rows it takes side by side
+int row_threads(int D) { return row_lanes(D) ? row_lanes(D) : (int)cdiv(D, 512) * 64; }
+int bwd_threads(int D) { return 1024 / row_threads(D) * row_threads(D); }
+
 // Items: tokens of one sequence a block takes; enough of them to fill the
 // card (`want` blocks) and at most kMaxRows a thread, whole rounds of groups.
-void split(const BlockNorm& a, int64_t want, int& R, int& nc) {
-  const int p = row_lanes(a.D), ng = p ? 256 / p : 1;
+void split(const BlockNorm& a, int threads, int64_t want, int& R, int& nc) {
+  const int ng = threads / row_threads(a.D);
   int64_t r = cdiv((int64_t)a.B * a.S, want);
   r = std::min<int64_t>(cdiv(std::max<int64_t>(r, 1), ng) * ng, (int64_t)kMaxRows * ng);
   R = (int)r;
@@ -388,7 +414,7 @@ BnArgs make_args(const BlockNorm& a, const BlockNormRows& w, const int32_t* len,
 template <bool BWD, typename TX, typename TH, bool POST>
 void launch2(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
   const int p = row_lanes(a.D);
-  const dim3 grid((unsigned)((int64_t)a.B * g.nc)), blk(p ? 256 : (unsigned)cdiv(a.D, 512) * 64);
+  const dim3 grid((unsigned)((int64_t)a.B * g.nc)), blk(BWD ? bwd_threads(a.D) : p ? 256 : row_threads(a.D));
 #define PG_BN(P)                                                                              \
   case P:                                                                                     \
     if (BWD) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, P, POST>), grid, blk, 0, st, g);     \
@@ -408,7 +434,7 @@ void launch(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
 #undef PG_BN
 }
 
-constexpr int64_t kFwdItems = 4096, kBwdItems = 1024;
+constexpr int64_t kFwdItems = 4096, kBwdItems = 256;
 
 }  // namespace
 
@@ -416,15 +442,15 @@ size_t blocknorm_saved_bytes(const BlockNorm& a) { return align256((size_t)a.B *
 
 size_t blocknorm_ws_bytes(const BlockNorm& a) {
   int R, nc;
-  split(a, kBwdItems, R, nc);
-  return align256((size_t)a.B * nc * 3 * a.D * sizeof(float)) + align256((size_t)a.B * 3 * a.D * sizeof(double));
+  split(a, bwd_threads(a.D), kBwdItems, R, nc);
+  return align256((size_t)a.B * nc * 3 * a.D * sizeof(float));
 }
 
 void blocknorm_fwd(hipStream_t st, const BlockNorm& a, const BlockNormRows& w, const void* x, const void* h,
                    const int32_t* len, void* z, void* y, void* saved) {
   BnArgs g = make_args(a, w, len, x, h);
   g.z = z; g.y = y; g.stats = (float*)saved;
-  split(a, kFwdItems, g.R, g.nc);
+  split(a, row_lanes(a.D) ? 256 : row_threads(a.D), kFwdItems, g.R, g.nc);
   ProfScope prof(st);
   launch<false>(st, a, g);
   const double one = (a.res32 ? 4.0 : 2.0) * (1 + a.branch) + (a.f32 ? 4.0 : 2.0) * (a.branch + a.pre);
@@ -436,18 +462,14 @@ void blocknorm_bwd(hipStream_t st, const BlockNorm& a, const BlockNormRows& w, c
                    const BlockNormGrads& gr, void* ws) {
   BnArgs g = make_args(a, w, len, x, h);
   g.dz = dz; g.dy = dy; g.z = dx; g.y = dh; g.stats = (float*)const_cast<void*>(saved); g.part = (float*)ws;
-  split(a, kBwdItems, g.R, g.nc);
+  split(a, bwd_threads(a.D), kBwdItems, g.R, g.nc);
   ProfScope prof(st);
   launch<true>(st, a, g);
-  BnJoin j{w, gr, g.part, nullptr, a.mod, a.B, a.D, g.nc, a.res_scale};
-  const bool shared = gr.gain_pre || gr.gain_post || (!a.mod && (gr.gate || gr.scale || gr.shift));
-  if (shared) j.seq = (double*)((char*)ws + align256((size_t)a.B * g.nc * 3 * a.D * sizeof(float)));
-  if (shared || gr.gate || gr.scale || gr.shift) {
-    hipLaunchKernelGGL(k_blocknorm_seq, dim3((unsigned)a.B, (unsigned)cdiv(a.D, 32)), dim3(256), 0, st, j);
-    PG_LAUNCH_CHECK();
-  }
-  if (shared) {
-    hipLaunchKernelGGL(k_blocknorm_join, dim3((unsigned)cdiv(a.D, 32)), dim3(256), 0, st, j);
+  if (gr.gain_pre || gr.gain_post || gr.gate || gr.scale || gr.shift) {
+    int gs = 64;
+    while (gs > 1 && 64 / gs < a.B) gs /= 2;
+    hipLaunchKernelGGL(k_blocknorm_join, dim3((unsigned)cdiv(a.D, 16)), dim3(1024), 0, st,
+                       BnJoin{w, gr, g.part, a.mod, a.B, a.D, g.nc, gs, a.res_scale});
     PG_LAUNCH_CHECK();
   }
   const double one = (a.res32 ? 4.0 : 2.0) * (1 + (dz ? 1 : 0) + a.pre) + (a.f32 ? 4.0 : 2.0) * (2 * a.branch + a.pre);

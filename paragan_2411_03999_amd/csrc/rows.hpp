@@ -34,6 +34,19 @@ template <int CTRL>
 PG_DEV float lane_move(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
 }
+// v of this lane and of the lane N away (16 or 32, the bit of the lane's number flipped): the swap leaves one of them in
+// either of its results
+template <int N>
+PG_DEV float half_sum(float v) {
+  const uint32_t u = __float_as_uint(v);
+  if constexpr (N == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+}
 // sum over the LPH lanes of a group, in every lane
 template <int LPH>
 PG_DEV float group_sum(float v) {
@@ -41,8 +54,8 @@ PG_DEV float group_sum(float v) {
   if (LPH > 2) v += lane_move<0x4E>(v);    // quad lanes 2 3 0 1
   if (LPH > 4) v += lane_move<0x141>(v);   // the other quad of 8 (mirrored; a quad is uniform by now)
   if (LPH > 8) v += lane_move<0x140>(v);   // the other half of 16 (mirrored)
-  if (LPH > 16) v += __shfl_xor(v, 16, 64);
-  if (LPH > 32) v += __shfl_xor(v, 32, 64);
+  if (LPH > 16) v = half_sum<16>(v);
+  if (LPH > 32) v = half_sum<32>(v);
   return v;
 }
 
