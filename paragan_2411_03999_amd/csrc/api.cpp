@@ -826,7 +826,7 @@ static paragan_clip_desc clip_desc(const paragan_clip_tensor* t, int32_t n) {
     }
     d.n_elements += t[i].n;
     d.bytes += (int64_t)el * t[i].n;
-    d.n_pieces += cdiv(t[i].n, kClipPiece);
+    d.n_pieces += cdiv(t[i].n, kClipPiece / (int64_t)el);
     PG_CHECK(d.n_pieces < (1LL << 31), "clip: too many elements");
   }
   std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
@@ -851,9 +851,10 @@ extern "C" int paragan_clip_plan(const paragan_clip_tensor* t, int32_t n, paraga
     ClipPiece* out = (ClipPiece*)plan_host;
     for (int32_t i = 0; i < n; ++i) {
       const uint64_t el = t[i].dtype == PARAGAN_BF16 ? 2 : 4;
-      for (int64_t at = 0; at < t[i].n; at += kClipPiece) {
+      const int64_t per = kClipPiece / (int64_t)el;
+      for (int64_t at = 0; at < t[i].n; at += per) {
         const ClipPiece p{(uint64_t)(uintptr_t)t[i].grad + el * at, (uint64_t)(uintptr_t)t[i].out + el * at,
-                          (int32_t)std::min<int64_t>(kClipPiece, t[i].n - at), (int32_t)(t[i].dtype == PARAGAN_BF16)};
+                          (int32_t)std::min<int64_t>(per, t[i].n - at), (int32_t)(t[i].dtype == PARAGAN_BF16)};
         std::memcpy(out++, &p, sizeof(p));
       }
     }

@@ -69,7 +69,7 @@ void scan_bwd(hipStream_t st, const Scan& a, const void* x, const void* r, const
               const int32_t* len, const void* saved, const void* dy, const float* dht, void* dx, void* dr, void* dg,
               float* ddecay, float* dh0, void* ws);
 
-constexpr int kClipPiece = 16384;              // elements of a piece of a tensor
+constexpr int kClipPiece = 16384;              // bytes of a piece of a tensor
 struct ClipPiece {                             // one entry of a plan
   uint64_t src, dst;
   int32_t n, bf16;
