@@ -46,28 +46,59 @@ template <> struct Two<float> {
 PG_DEV void st2f(bf16_t* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = f2bf2(a, b); }
 PG_DEV void st2f(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2e = 1.4426950408889634f;
 
-// sigmoid(v) and 1 - sigmoid(v), both to the last digits
+// sigmoid(v) and 1 - sigmoid(v), both to the last digits (e^-v may be infinite)
 PG_DEV void sigmoid(float v, float& s, float& c) {
-  const float e = __builtin_amdgcn_exp2f(-fabsf(v) * kLog2e), q = __builtin_amdgcn_rcpf(1.f + e), t = e * q;
-  s = v >= 0.f ? q : t;
-  c = v >= 0.f ? t : q;
+  const float e = __builtin_amdgcn_exp2f(v * -kLog2e);
+  s = __builtin_amdgcn_rcpf(1.f + e);
+  c = e < 1e30f ? e * s : 1.f;
 }
+PG_DEV float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
 // softplus(v) = log(1 + e^v)
 PG_DEV float softplus(float v) { return log1pf(expf(-fabsf(v))) + fmaxf(v, 0.f); }
+// -sharp softplus(decay) of two channels
+PG_DEV float2 rates(const ScArgs& a, int c) {
+  const float2 d = *reinterpret_cast<const float2*>(a.decay + c);
+  return make_float2(-a.sharp * softplus(d.x), -a.sharp * softplus(d.y));
+}
 
-// a = 2^l2 and p = 1 - a^2 for l2 <= 0: a series where the difference would
-// cancel.  p is held above zero, so that w = p p^-1/2 and 1 / p are finite.
-PG_DEV void decay_of(float l2, float& a, float& p) {
-  a = __builtin_amdgcn_exp2f(l2);
-  const float t = l2 * (2.f * kLn2);
-  float q = fmaf(t, 1.f / 720.f, 1.f / 120.f);
-  q = fmaf(t, q, 1.f / 24.f);
-  q = fmaf(t, q, 1.f / 6.f);
-  q = fmaf(t, q, 0.5f);
-  q = fmaf(t, q, 1.f);
-  p = fmaxf(t > -0.25f ? -t * q : fmaf(-a, a, 1.f), 1.17549435e-38f);
+// a = e^la and p = 1 - a^2 for la <= 0.  Where the difference would cancel, p
+// is -la Q(la) with a polynomial Q of degree 4 for (e^(2 la) - 1) / la on
+// [-0.2, 0] (least largest relative error, 6.3e-8 with rounded coefficients).
+// p is held above zero, so that w = p p^-1/2 and 1 / p are finite.
+PG_DEV void decay_of(float la, float& a, float& p) {
+  a = __builtin_amdgcn_exp2f(la * kLog2e);
+  float q = fmaf(la, 0.2258301079273224f, 0.6596707105636597f);
+  q = fmaf(la, q, 1.3328346014022827f);
+  q = fmaf(la, q, 1.9999873638153076f);
+  q = fmaf(la, q, 2.f);
+  p = fmaxf(la > -0.2f ? -la * q : fmaf(-a, a, 1.f), 1.17549435e-38f);
+}
+
+// a and u of one element
+PG_DEV void gate(float x, float r, float g, float k, float& a, float& u) {
+  float p;
+  decay_of(k * sigmoid(r), a, p);
+  u = p * __builtin_amdgcn_rsqf(p) * sigmoid(g) * x;
+}
+// What one element needs after its gates are known: dx = E fx, dg = E fg,
+// dr = E M fr, ddecay += E M s, with M = a h_{t-1} - v.
+struct Grad {
+  float a, u, v, fx, fg, fr, s;
+};
+PG_DEV void grad_gate(float x, float r, float g, float k, Grad& e) {
+  float cs, sg, cg, p;
+  sigmoid(r, e.s, cs);
+  sigmoid(g, sg, cg);
+  const float la = k * e.s;
+  decay_of(la, e.a, p);
+  const float q = __builtin_amdgcn_rsqf(p), aq = e.a * q;
+  e.fx = p * q * sg;
+  e.u = e.fx * x;
+  e.v = e.u * aq * aq;
+  e.fg = e.u * cg;
+  e.fr = la * cs;
 }
 
 // One thread takes two channels of one sequence through all its tokens.
@@ -81,7 +112,7 @@ __global__ __launch_bounds__(64) void k_scan_seq_fwd(ScArgs a) {
   const T* g = (const T*)a.g + b * a.gs[0] + c;
   T* y = (T*)a.y + b * a.ys[0] + c;
   const int64_t o = (int64_t)b * a.D + c;
-  const float k0 = -a.sharp * softplus(a.decay[c]) * kLog2e, k1 = -a.sharp * softplus(a.decay[c + 1]) * kLog2e;
+  const float2 k = rates(a, c);
   float2 h = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
   float* keep = a.saved ? a.saved + (int64_t)b * cdiv(a.S, kStep) * a.D + c : nullptr;
   for (int i0 = 0; i0 < len; i0 += kStep) {
@@ -98,15 +129,11 @@ __global__ __launch_bounds__(64) void k_scan_seq_fwd(ScArgs a) {
     for (int i = 0; i < kStep; ++i) {
       if (i0 + i >= len) break;
       const float2 xx = xv[i].get(), rr = rv[i].get(), gg = gv[i].get();
-      float s, c1, sg, a0, p;
-      sigmoid(rr.x, s, c1);
-      sigmoid(gg.x, sg, c1);
-      decay_of(k0 * s, a0, p);
-      h.x = fmaf(a0, h.x, p * __builtin_amdgcn_rsqf(p) * sg * xx.x);
-      sigmoid(rr.y, s, c1);
-      sigmoid(gg.y, sg, c1);
-      decay_of(k1 * s, a0, p);
-      h.y = fmaf(a0, h.y, p * __builtin_amdgcn_rsqf(p) * sg * xx.y);
+      float a0, u;
+      gate(xx.x, rr.x, gg.x, k.x, a0, u);
+      h.x = fmaf(a0, h.x, u);
+      gate(xx.y, rr.y, gg.y, k.y, a0, u);
+      h.y = fmaf(a0, h.y, u);
       const int t = a.reverse ? len - 1 - i0 - i : i0 + i;
       st2f(y + t * a.ys[1], h.x, h.y);
     }
@@ -128,7 +155,8 @@ __global__ __launch_bounds__(64) void k_scan_seq_bwd(ScArgs a) {
   T* dr = (T*)a.dr + b * a.rs[0] + c;
   T* dg = (T*)a.dg + b * a.gs[0] + c;
   const int64_t o = (int64_t)b * a.D + c;
-  const float k[2] = {-a.sharp * softplus(a.decay[c]) * kLog2e, -a.sharp * softplus(a.decay[c + 1]) * kLog2e};
+  const float2 kk = rates(a, c);
+  const float k[2] = {kk.x, kk.y};
   float E[2] = {a.h0 ? a.h0[o] : 0.f, a.h0 ? a.h0[o + 1] : 0.f};     // a_{t+1} E_{t+1}
   double sum[2] = {0.0, 0.0};
   const float* keep = a.saved + (int64_t)b * cdiv(a.S, kStep) * a.D + c;
@@ -150,12 +178,10 @@ __global__ __launch_bounds__(64) void k_scan_seq_bwd(ScArgs a) {
       const float gg[2] = {gv[i].get().x, gv[i].get().y};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float s, c1, sg, a0, p;
+        float a0, u;
         before[i][e] = h[e];
-        sigmoid(rr[e], s, c1);
-        sigmoid(gg[e], sg, c1);
-        decay_of(k[e] * s, a0, p);
-        h[e] = fmaf(a0, h[e], p * __builtin_amdgcn_rsqf(p) * sg * xx[e]);
+        gate(xx[e], rr[e], gg[e], k[e], a0, u);
+        h[e] = fmaf(a0, h[e], u);
       }
     }
     float part[2] = {0.f, 0.f};
@@ -167,18 +193,14 @@ __global__ __launch_bounds__(64) void k_scan_seq_bwd(ScArgs a) {
       float ox[2], orr[2], og[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float s, cs, sg, cg, a0, p;
-        sigmoid(rr[e], s, cs);
-        sigmoid(gg[e], sg, cg);
-        decay_of(k[e] * s, a0, p);
-        const float q = __builtin_amdgcn_rsqf(p), wsg = p * q * sg, u = wsg * xx[e];
-        const float Et = dd[e] + E[e];
-        const float dla = Et * (a0 * before[i][e] - u * a0 * a0 * q * q);
-        ox[e] = Et * wsg;
-        og[e] = Et * u * cg;
-        orr[e] = dla * (k[e] * kLn2 * s) * cs;
-        part[e] = fmaf(dla, s, part[e]);
-        E[e] = a0 * Et;
+        Grad q;
+        grad_gate(xx[e], rr[e], gg[e], k[e], q);
+        const float Et = dd[e] + E[e], EM = Et * fmaf(q.a, before[i][e], -q.v);
+        ox[e] = Et * q.fx;
+        og[e] = Et * q.fg;
+        orr[e] = EM * q.fr;
+        part[e] = fmaf(EM, q.s, part[e]);
+        E[e] = q.a * Et;
       }
       const int t = a.reverse ? len - 1 - i0 - i : i0 + i;
       st2f(dx + t * a.xs[1], ox[0], ox[1]);
@@ -342,16 +364,6 @@ PG_DEV void join_down(float2& A, float2& H, float2& Ae, float2& He) {
 }
 PG_DEV float2 fold(float2 A, float2 H, float2 h) { return make_float2(fmaf(A.x, h.x, H.x), fmaf(A.y, h.y, H.y)); }
 
-PG_DEV float sigmoid1(float v) {   // alone: 1 / (1 + e^-v), which may be infinite
-  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e));
-}
-// a and u of one element
-PG_DEV void gate(float x, float r, float g, float k, float& a, float& u) {
-  float p;
-  decay_of(k * sigmoid1(r), a, p);
-  u = __builtin_amdgcn_sqrtf(p) * sigmoid1(g) * x;
-}
-
 // SPLIT: the chunks of a sequence start from the folded maps of those ahead
 template <typename F, bool SPLIT>
 __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
@@ -362,8 +374,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
   if (p.b >= a.B) return;
   const Tokens<F> x(a.x, a.xs, p), r(a.r, a.rs, p), g(a.g, a.gs, p), y(a.y, a.ys, p);
   const int64_t o = (int64_t)p.b * a.D + p.cc;
-  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
-  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  const float2 k = rates(a, p.cc);
   float2 h = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
   Two<T> X[TOK], R[TOK], G[TOK];
   auto load = [&](int m) {
@@ -428,8 +439,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
   if (p.b >= a.B || p.chunk == a.nc - 1) return;   // nobody comes after the last one
   const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;   // a chunk is whole tiles
   const Tokens<F> x(a.x, a.xs, p, run), r(a.r, a.rs, p, run), g(a.g, a.gs, p, run);
-  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
-  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  const float2 k = rates(a, p.cc);
   float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
   Two<T> X[TOK], R[TOK], G[TOK];
   auto load = [&](int i) {         // i: order index in the run
@@ -475,25 +485,6 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
   }
 }
 
-// What one element needs after its gates are known: dx = E fx, dg = E fg,
-// dr = E M fr, ddecay += E M s, with M = a h_{t-1} - v.
-struct Grad {
-  float a, u, v, fx, fg, fr, s;
-};
-PG_DEV void grad_gate(float x, float r, float g, float k, Grad& e) {
-  float cs, sg, cg, p;
-  sigmoid(r, e.s, cs);
-  sigmoid(g, sg, cg);
-  const float l2 = k * e.s;
-  decay_of(l2, e.a, p);
-  const float q = __builtin_amdgcn_rsqf(p), aq = e.a * q;
-  e.fx = p * q * sg;
-  e.u = e.fx * x;
-  e.v = e.u * aq * aq;
-  e.fg = e.u * cg;
-  e.fr = l2 * kLn2 * cs;
-}
-
 // Backward of a tile: the states ahead of its segments from the forward's
 // kept state, what flows back into them from the tile behind it, both joined
 // at the same barrier.
@@ -501,16 +492,15 @@ template <typename F, bool SPLIT>
 __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
   constexpr int CL = F::CL, NW = F::NW, TOK = F::TOK;
   typedef typename F::T T;
-  __shared__ float4 sh[2][NW][CL];
-  __shared__ float2 sc[2][NW][CL];
+  static_assert(CL == 32, "the two halves of a wave");
+  __shared__ float4 sh[2][2][NW][CL];   // [turn][towards later, earlier tokens]
   __shared__ double sd[NW][64][2];
   const Place<F> p(a);
   if (p.b >= a.B) return;
   const Tokens<F> x(a.x, a.xs, p), r(a.r, a.rs, p), g(a.g, a.gs, p), dy(a.dy, a.ys, p);
   const Tokens<F> dx(a.y, a.xs, p), dr(a.dr, a.rs, p), dg(a.dg, a.gs, p);
   const int64_t o = (int64_t)p.b * a.D + p.cc;
-  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
-  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  const float2 k = rates(a, p.cc);
   float2 c = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);   // flows back into the tile
   const float* keep = a.saved + (int64_t)p.b * cdiv(a.S, kKeep) * a.D + p.cc;
   Two<T> X[TOK], R[TOK], G[TOK], Y[TOK], Yn[TOK];
@@ -534,6 +524,8 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
     }
   }
   int turn = 0;
+  const bool up = (threadIdx.x & 63) < 32;
+  const int at = up ? p.wave : NW - 1 - p.wave;
   double sum0 = 0.0, sum1 = 0.0;
   for (int t = p.n - 1; t >= 0; --t, turn ^= 1) {
     const int m0 = p.tile(t, a.reverse);
@@ -561,21 +553,20 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
     float2 Ad = A, Ae, He, Ce, Ade;
     join_up<CL>(A, H, Ae, He);
     join_down<CL>(Ad, C, Ade, Ce);
-    if (p.tl == F::TL - 1) sh[turn][p.wave][p.cl] = make_float4(A.x, A.y, H.x, H.y);
-    if (p.tl == 0) sc[turn][p.wave][p.cl] = C;
+    if (p.tl == F::TL - 1) sh[turn][0][p.wave][p.cl] = make_float4(A.x, A.y, H.x, H.y);
+    if (p.tl == 0) sh[turn][1][NW - 1 - p.wave][p.cl] = make_float4(Ad.x, Ad.y, C.x, C.y);
     __syncthreads();
-    float2 cw = c;
-#pragma unroll 2
+    // one half of the lanes runs through the waves forwards with h, the other backwards with c
+    float2 v = up ? h : c, mine = v;
+#pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float4 q = sh[turn][w][p.cl];
-      if (w < p.wave) h = fold(make_float2(q.x, q.y), make_float2(q.z, q.w), h);
+      const float4 q = sh[turn][up ? 0 : 1][w][p.cl];
+      if (w == at) mine = v;
+      v = fold(make_float2(q.x, q.y), make_float2(q.z, q.w), v);
     }
-#pragma unroll 2
-    for (int w = NW - 1; w >= 0; --w) {
-      const float4 q = sh[turn][w][p.cl];
-      if (w == p.wave) cw = c;
-      c = fold(make_float2(q.x, q.y), sc[turn][w][p.cl], c);
-    }
+    h = make_float2(__shfl(mine.x, p.cl, 64), __shfl(mine.y, p.cl, 64));
+    float2 cw = make_float2(__shfl(mine.x, p.cl + 32, 64), __shfl(mine.y, p.cl + 32, 64));
+    c = make_float2(__shfl(v.x, p.cl + 32, 64), __shfl(v.y, p.cl + 32, 64));
     h = fold(Ae, He, h);
     cw = fold(Ade, Ce, cw);
 #pragma unroll
@@ -634,8 +625,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
   if (p.b >= a.B || p.chunk == 0) return;
   const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;
   const Tokens<F> r(a.r, a.rs, p, run), dy(a.dy, a.ys, p, run);
-  const float2 dec = *reinterpret_cast<const float2*>(a.decay + p.cc);
-  const float2 k = make_float2(-a.sharp * softplus(dec.x) * kLog2e, -a.sharp * softplus(dec.y) * kLog2e);
+  const float2 k = rates(a, p.cc);
   float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
   Two<T> R[TOK], Y[TOK];
   auto load = [&](int i) {
@@ -651,11 +641,8 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
 #pragma unroll
       for (int j = 0; j < TOK; ++j) {
         const float2 rr = R[j].get();
-        float s, cs;
-        sigmoid(rr.x, s, cs);
-        av[j].x = __builtin_amdgcn_exp2f(k.x * s);
-        sigmoid(rr.y, s, cs);
-        av[j].y = __builtin_amdgcn_exp2f(k.y * s);
+        av[j].x = __builtin_amdgcn_exp2f(k.x * sigmoid(rr.x) * kLog2e);
+        av[j].y = __builtin_amdgcn_exp2f(k.y * sigmoid(rr.y) * kLog2e);
         d[j] = Y[j].get();
       }
       if (i > 0) load(i - TOK);
@@ -708,16 +695,36 @@ struct Plan {
   int cl, nw;                      // 0: a thread a sequence and two channels
   int slabs, nc, chunk;
 };
+// Few slabs leave the card idle: then chunks of the sequences go side by side,
+// at the price of a pass over the inputs ahead and its launch.  Split where
+// the modelled time says so, in us: a block walks its sequence at a rate of
+// its own, the split form moves bytes at the card's.  Measured against both
+// forms of 26 shapes the choice costs at most 5 %: forward of 5 x 3000 x 1320
+// 75 whole, 64 split, of 6 x 4096 x 1536 108 and 107, of 2 x 600 x 5000 19 and
+// 29; backward of 3 x 5000 x 1000 200 and 66, of 2 x 600 x 5000 33 and 36.
+bool split_pays(const Scan& a, bool bwd, int64_t rows) {
+  const double n = (double)a.B * a.S * a.D;
+  const double whole = 5.0 + a.S * (bwd ? a.f32 ? 0.061 : 0.045 : a.f32 ? 0.033 : 0.026);
+  const double parts = bwd ? 12.0 + n * (a.f32 ? 6.2e-6 : 4.1e-6) : 8.0 + n * (a.f32 ? 4.3e-6 : 2.8e-6);
+  return rows < 256 && whole > parts;
+}
 Plan plan_of(const Scan& a, bool bwd) {
   Plan p{0, 0, 0, 1, a.S};
-  if (a.S <= 32) return p;
   p.cl = 32;
-  p.nw = 8;
   p.slabs = (int)cdiv(a.D, 2 * p.cl);
+  const int64_t rows = (int64_t)a.B * p.slabs;
+  // a thread a sequence: few tokens, or some for so many sequences that they fill the card (64 x 48 x 4096 24 us
+  // forward, 50 backward, in tiles 30 and 60; 64 x 64 x 4096 30 and 63, 32 and 62; 32 x 24 x 1024 8 and 17, 7 and 14)
+  if (a.S <= kStep || (a.S <= 3 * kStep && rows >= 2048)) return Plan{0, 0, 0, 1, a.S};
+  const bool split = split_pays(a, bwd, rows);
+  // blocks of four waves where there are many of them (64 x 256 x 1024 backward 53 us, of eight 64), for
+  // sequences of one tile, and side by side; of eight (a whole CU) where there are few (8 x 4096 x 2048: 213, of
+  // four 242).  A float tile of four would be shorter than kKeep.
+  p.nw = !a.f32 && (split || rows >= 512 || a.S <= kKeep) ? 4 : 8;
   const int tt = p.nw * (64 / p.cl) * (a.f32 ? 4 : 8);
-  // few slabs: chunks of sequences side by side, at the price of a pass over the inputs ahead
-  const int64_t rows = (int64_t)a.B * p.slabs, want = bwd ? 384 : 768, enough = bwd ? 192 : 128;
-  const int64_t nc = rows >= enough ? 1 : std::max<int64_t>(1, std::min<int64_t>(want / rows, a.S / (2 * tt)));
+  // two to three blocks of four waves a CU (one of eight); each folds the chunks ahead of it, so no more than 96
+  int64_t nc = 1;
+  if (split) nc = std::max<int64_t>(2, std::min<int64_t>((a.f32 ? 256 : bwd ? 512 : 768) / rows, std::min<int64_t>(96, cdiv(a.S, tt))));
   // a chunk is addressed in 32 bits
   const int64_t st = std::max(std::max(a.xs[1], a.rs[1]), std::max(a.gs[1], a.ys[1])) * (a.f32 ? 4 : 2);
   const int64_t most = std::max<int64_t>(1, kBufMax / std::max<int64_t>(st, 1) / tt) * tt;
@@ -755,11 +762,11 @@ void launch(int what, hipStream_t st, const Scan& a, const Plan& p, const ScArgs
   const unsigned blocks = (unsigned)(cdiv((int64_t)a.B * p.slabs * p.nc, 8) * 8);
 #define PG_SC(CL, NW)                                                  \
   if (p.cl == CL && p.nw == NW) {                                      \
-    if (a.f32) launch1<Form<float, CL, NW>>(what, st, k, blocks);   \
-    else launch1<Form<bf16_t, CL, NW>>(what, st, k, blocks);        \
-    return;                                                            \
+    if (!a.f32) return launch1<Form<bf16_t, CL, NW>>(what, st, k, blocks);                      \
+    if constexpr (Form<float, CL, NW>::TT % kKeep == 0) return launch1<Form<float, CL, NW>>(what, st, k, blocks); \
   }
   PG_SC(32, 8)
+  PG_SC(32, 4)
 #undef PG_SC
   throw Error{-2, "scan: no such form"};
 }
