@@ -95,6 +95,19 @@ int paragan_sync(paragan_ctx* ctx);
  * other values. */
 int paragan_set_overlap_wgrad(paragan_ctx* ctx, int on);
 
+/* Clipping inside the step calls (paragan_d_step, paragan_g_step,
+ * paragan_train_step, paragan_async_step).  With max_norm_g (max_norm_d) > 0
+ * the generator's (discriminator's) optimiser steps take their gradient times
+ * min(1, max_norm / norm), norm being the 2-norm of all of it; the gradients
+ * the call leaves in `grads` are not clipped.  0 (the default): off, with the
+ * results of before; infinity: only the norms are taken.  buf: device buffer
+ * of paragan_grad_clip_size() bytes, 256-byte aligned, kept by the caller
+ * while clipping is on (NULL when both are off): its first four floats are the
+ * generator's last norm and factor, then the discriminator's. */
+int paragan_grad_clip_size(size_t* bytes);
+int paragan_set_grad_clip(paragan_ctx* ctx, float max_norm_g, float max_norm_d,
+                          void* buf);
+
 /* Channel stride of an activation tensor with c channels. */
 int64_t paragan_cpad(int64_t c);
 

@@ -104,6 +104,23 @@ int paragan_set_overlap_wgrad(paragan_ctx* ctx, int on) {
   return PARAGAN_OK;
 }
 
+int paragan_grad_clip_size(size_t* bytes) {
+  if (!bytes) return fail(nullptr, PARAGAN_EINVAL, "paragan_grad_clip_size: bytes is NULL");
+  *bytes = 256 + 2 * kClipFlatBlocks * sizeof(double);
+  return PARAGAN_OK;
+}
+int paragan_set_grad_clip(paragan_ctx* ctx, float max_norm_g, float max_norm_d, void* buf) {
+  if (!ctx) return PARAGAN_EINVAL;
+  if (!(max_norm_g >= 0.f) || !(max_norm_d >= 0.f))
+    return fail(ctx, PARAGAN_EINVAL, "paragan_set_grad_clip: the norms must be >= 0");
+  if ((max_norm_g > 0.f || max_norm_d > 0.f) && (!buf || ((uintptr_t)buf & 255)))
+    return fail(ctx, PARAGAN_EINVAL, "paragan_set_grad_clip: buf must be a 256-byte aligned device buffer");
+  ctx->clip_g = max_norm_g;
+  ctx->clip_d = max_norm_d;
+  ctx->clip_buf = buf;
+  return PARAGAN_OK;
+}
+
 int64_t paragan_cpad(int64_t c) { return cpad(c); }
 
 }  // extern "C"

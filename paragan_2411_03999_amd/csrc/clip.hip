@@ -133,7 +133,40 @@ __global__ __launch_bounds__(256) void k_clip_scale(const ClipPiece* plan, int64
   }
 }
 
+__global__ __launch_bounds__(256) void k_clip_flat(const float* g, int64_t n, double* part) {
+  __shared__ double sh[4];
+  double s = 0.0;
+  constexpr int64_t per = kClipPiece / 4;
+  for (int64_t i = blockIdx.x * per; i < n; i += gridDim.x * per) s += piece_sum(g + i, (int)min(per, n - i));
+  s = wave_sum_d(s);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) part[blockIdx.x] = ((sh[0] + sh[1]) + sh[2]) + sh[3];
+}
+__global__ __launch_bounds__(256) void k_clip_factor(const double* part, int n, float max_norm, float* norm) {
+  __shared__ double sh[4];
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += 256) s += part[i];
+  s = wave_sum_d(s);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
+  s = sqrt(((sh[0] + sh[1]) + sh[2]) + sh[3]);
+  norm[0] = (float)s;
+  norm[1] = s <= (double)max_norm ? 1.f : (float)((double)max_norm / s);
+}
+
 }  // namespace
+
+void clip_flat(hipStream_t st, const float* g, int64_t n, float max_norm, float* norm, double* part) {
+  const int grid = (int)std::min<int64_t>(cdiv(n, kClipPiece / 4), kClipFlatBlocks);
+  ProfScope prof(st);
+  hipLaunchKernelGGL(k_clip_flat, dim3(grid), dim3(256), 0, st, g, n, part);
+  PG_LAUNCH_CHECK();
+  hipLaunchKernelGGL(k_clip_factor, dim3(1), dim3(256), 0, st, part, grid, max_norm, norm);
+  PG_LAUNCH_CHECK();
+  prof.done_bytes("k_clip_flat", 4.0 * n);
+}
 
 size_t clip_ws_bytes() { return kBlocks * sizeof(double); }
 

@@ -168,6 +168,9 @@ struct paragan_ctx {
   hipStream_t wside = nullptr;
   hipEvent_t wev[2] = {nullptr, nullptr};
   bool overlap_wgrad = false;   // use wside (paragan_set_overlap_wgrad)
+  // clipping inside the step calls (paragan_set_grad_clip): 0 is off; the caller's device buffer
+  float clip_g = 0.f, clip_d = 0.f;
+  void* clip_buf = nullptr;
   int device = 0;
   int n_cu = 0;
   void* sn_scratch = nullptr;   // the device's address of the library's SN scratch array

@@ -1086,13 +1086,17 @@ PG_DEV void optim1(float& p, float g, float& m, float& v, float b1, float b2, fl
 }
 template <int KIND>
 __global__ void k_optim(float* p, const float* g, float* m, float* v, int64_t n, float b1, float b2, float lr_t,
-                        float c2, float eps) {
+                        float c2, float eps, const float* factor) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t n4 = n >> 2;
   if (i < n4) {
     float4 pp = reinterpret_cast<float4*>(p)[i], mm = reinterpret_cast<float4*>(m)[i];
     float4 vv = reinterpret_cast<float4*>(v)[i];
-    const float4 gg = reinterpret_cast<const float4*>(g)[i];
+    float4 gg = reinterpret_cast<const float4*>(g)[i];
+    if (factor) {
+      const float k = *factor;
+      gg.x *= k; gg.y *= k; gg.z *= k; gg.w *= k;
+    }
     optim1<KIND>(pp.x, gg.x, mm.x, vv.x, b1, b2, lr_t, c2, eps);
     optim1<KIND>(pp.y, gg.y, mm.y, vv.y, b1, b2, lr_t, c2, eps);
     optim1<KIND>(pp.z, gg.z, mm.z, vv.z, b1, b2, lr_t, c2, eps);
@@ -1102,12 +1106,12 @@ __global__ void k_optim(float* p, const float* g, float* m, float* v, int64_t n,
     reinterpret_cast<float4*>(v)[i] = vv;
   } else if (i < n4 + (n & 3)) {
     const int64_t j = 4 * n4 + (i - n4);
-    optim1<KIND>(p[j], g[j], m[j], v[j], b1, b2, lr_t, c2, eps);
+    optim1<KIND>(p[j], factor ? g[j] * *factor : g[j], m[j], v[j], b1, b2, lr_t, c2, eps);
   }
 }
 
 void optim_step(hipStream_t st, int kind, float* p, const float* g, float* m, float* v, int64_t n, float b1,
-                float b2, float lr, float eps, int64_t t) {
+                float b2, float lr, float eps, int64_t t, const float* factor) {
   if (n <= 0) return;
   PG_CHECK((((uintptr_t)p | (uintptr_t)g | (uintptr_t)m | (uintptr_t)v) & 15) == 0,
            "optimiser: 16-byte aligned buffers");
@@ -1118,9 +1122,9 @@ void optim_step(hipStream_t st, int kind, float* p, const float* g, float* m, fl
   const dim3 grid((unsigned)cdiv(threads, 256));
   ProfScope ps(st);
   if (kind == 0)
-    hipLaunchKernelGGL(k_optim<0>, grid, dim3(256), 0, st, p, g, m, v, n, b1, b2, (float)lr_t, (float)c2, eps);
+    hipLaunchKernelGGL(k_optim<0>, grid, dim3(256), 0, st, p, g, m, v, n, b1, b2, (float)lr_t, (float)c2, eps, factor);
   else
-    hipLaunchKernelGGL(k_optim<1>, grid, dim3(256), 0, st, p, g, m, v, n, b1, b2, (float)lr_t, (float)c2, eps);
+    hipLaunchKernelGGL(k_optim<1>, grid, dim3(256), 0, st, p, g, m, v, n, b1, b2, (float)lr_t, (float)c2, eps, factor);
   // p, g, m, v read; p, m, v written
   ps.done_bytes(kind == 0 ? "k_optim<adam>" : "k_optim<adabelief>", 28.0 * n);
   PG_LAUNCH_CHECK();

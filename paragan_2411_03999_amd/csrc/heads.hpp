@@ -49,7 +49,8 @@ void shared_grad(hipStream_t st, const float* dcond, int dc, const int32_t* y, i
                  float* dshared);
 
 // One optimiser step t (>= 1) over n fp32 parameters: kind 0 Adam, 1 AdaBelief.
+// The gradient is multiplied by *factor (device) where there is one.
 void optim_step(hipStream_t st, int kind, float* p, const float* g, float* m, float* v, int64_t n, float b1,
-                float b2, float lr, float eps, int64_t t);
+                float b2, float lr, float eps, int64_t t, const float* factor = nullptr);
 
 }  // namespace pg

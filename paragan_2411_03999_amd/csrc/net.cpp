@@ -12,6 +12,7 @@
 //              gradient only, G backward, Adam on G.
 // Only one host synchronisation per call: the losses at the end.
 #include "net.hpp"
+#include "token.hpp"
 
 #include <cstdio>
 
@@ -533,6 +534,20 @@ namespace {
 // The pieces of a training iteration over one workspace: the generator
 // (batch B), the discriminator on the 2B batch of a D step and on the B
 // images of a G step (their saved buffers share one region).
+// One optimiser step on the gradient just computed, with clipping on by the
+// factor of its norm (the gradient itself stays as it is).
+void optimise(paragan_ctx* ctx, hipStream_t st, const paragan_optim& o, paragan_net_state* N, int64_t n, bool is_d) {
+  const float most = is_d ? ctx->clip_d : ctx->clip_g;
+  float* norm = nullptr;
+  if (most > 0.f) {
+    norm = (float*)ctx->clip_buf + (is_d ? 2 : 0);
+    clip_flat(st, N->grads, n, most, norm, (double*)((char*)ctx->clip_buf + 256) + (is_d ? kClipFlatBlocks : 0));
+  }
+  N->opt_t += 1;
+  optim_step(st, o.kind, N->params, N->grads, N->opt_m, N->opt_v, n, o.beta1, o.beta2, o.lr, o.eps, N->opt_t,
+             norm ? norm + 1 : nullptr);
+}
+
 struct StepRun {
   Arch a;
   int B;
@@ -545,7 +560,7 @@ struct StepRun {
   Params PG, PD;
   int64_t pix;
   StepRun(paragan_ctx* ctx, const paragan_biggan_desc* d, paragan_net_state* G, paragan_net_state* D, void* ws)
-      : a(arch_from(d)), B(d->B), st(ctx->stream), g(a, B), d2(a, 2 * B), d1(a, B) {
+      : a(arch_from(d)), B(d->B), st(ctx->stream), g(a, B), d2(a, 2 * B), d1(a, B), ctx(ctx) {
     Arena w(ws);
     r = step_carve(a, B, w, g, d2, d1, ctx->n_cu);
     ex = Exec{st, ctx->n_cu, r.net, r.net_bytes};
@@ -564,17 +579,14 @@ struct StepRun {
     PD = Params{&LD, "", D ? D->params : nullptr, D ? D->u : nullptr, D ? D->grads : nullptr};
     pix = (int64_t)a.img * a.img;
   }
-  static void optimise(hipStream_t st, const paragan_optim& o, paragan_net_state* N, int64_t n) {
-    N->opt_t += 1;
-    optim_step(st, o.kind, N->params, N->grads, N->opt_m, N->opt_v, n, o.beta1, o.beta2, o.lr, o.eps, N->opt_t);
-  }
+  paragan_ctx* ctx;
   // D step on the batch already in r.ximg / r.ylab: forward, hinge (L_D to
   // *loss), backward with weight gradients, D's optimiser
   void d_update(const paragan_biggan_desc* d, paragan_net_state* D, float* loss) {
     d2.fwd(ex, PD, r.ximg, r.ylab, r.logits);
     hinge(st, r.logits, B, B, false, r.dout, loss);
     d2.bwd(ex, PD, r.ylab, r.dout, nullptr, true);
-    optimise(st, d->opt_d, D, LD.n_params);
+    optimise(ctx, st, d->opt_d, D, LD.n_params, true);
   }
   void stage_real(const float* x_real, const int32_t* y_real, const int32_t* y_fake) {
     PG_HIP(hipMemcpyAsync(r.ximg, x_real, (size_t)B * pix * 3 * 4, hipMemcpyDeviceToDevice, st));
@@ -595,7 +607,7 @@ struct StepRun {
     hinge(st, r.logits, 0, B, true, r.dout, loss);
     d1.bwd(ex, PD, y, r.dout, r.dimg, false);
     g.bwd(ex, PG, z, y, r.dimg, 4);
-    optimise(st, d->opt_g, G, LG.n_params);
+    optimise(ctx, st, d->opt_g, G, LG.n_params, false);
   }
   void losses_to_host(float* host, int n) {
     PG_HIP(hipMemcpyAsync(host, r.dloss, (size_t)n * 4, hipMemcpyDeviceToHost, st));
@@ -781,9 +793,7 @@ void async_step(paragan_ctx* ctx, const paragan_biggan_desc* d, paragan_net_stat
     hinge(sg, r.glog, 0, BG, true, r.gdout, r.gloss);
     ds.bwd(eg, PS, in->y, r.gdout, r.gdimg, false);
     g.bwd(eg, PG, in->z, in->y, r.gdimg, 4);
-    G->opt_t += 1;
-    optim_step(sg, d->opt_g.kind, G->params, G->grads, G->opt_m, G->opt_v, LG.n_params, d->opt_g.beta1,
-               d->opt_g.beta2, d->opt_g.lr, d->opt_g.eps, G->opt_t);
+    optimise(ctx, sg, d->opt_g, G, LG.n_params, false);
     PG_HIP(hipEventRecord(ctx->ev[1], sg));
     // discriminator side: step k on B real images and the k-th B of the
     // previous iteration's samples
@@ -797,9 +807,7 @@ void async_step(paragan_ctx* ctx, const paragan_biggan_desc* d, paragan_net_stat
       d2.fwd(ed, PD, r.dimg, r.dlab, r.dlog);
       hinge(st, r.dlog, B, B, false, r.ddout, r.dloss + k);
       d2.bwd(ed, PD, r.dlab, r.ddout, nullptr, true);
-      D->opt_t += 1;
-      optim_step(st, d->opt_d.kind, D->params, D->grads, D->opt_m, D->opt_v, LD.n_params, d->opt_d.beta1,
-                 d->opt_d.beta2, d->opt_d.lr, d->opt_d.eps, D->opt_t);
+      optimise(ctx, st, d->opt_d, D, LD.n_params, true);
     }
     // join, then this iteration's samples become the next one's img_buff
     PG_HIP(hipStreamWaitEvent(st, ctx->ev[1], 0));

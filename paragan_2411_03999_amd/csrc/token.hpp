@@ -77,5 +77,9 @@ struct ClipPiece {                             // one entry of a plan
 size_t clip_ws_bytes();
 void clip(hipStream_t st, int64_t n_pieces, double bytes, bool in_place, const void* plan, float max_norm,
           float grad_scale, float* norm, void* ws);
+// Norm and factor of one flat fp32 gradient, for an optimiser that takes the factor along: norm [2], part
+// kClipFlatBlocks doubles
+constexpr int kClipFlatBlocks = 1024;
+void clip_flat(hipStream_t st, const float* g, int64_t n, float max_norm, float* norm, double* part);
 
 }  // namespace pg

@@ -154,6 +154,8 @@ _SIGS = {
     "paragan_last_error": (C.c_char_p, [_P]),
     "paragan_sync": (C.c_int, [_P]),
     "paragan_set_overlap_wgrad": (C.c_int, [_P, C.c_int]),
+    "paragan_grad_clip_size": (C.c_int, [C.POINTER(C.c_size_t)]),
+    "paragan_set_grad_clip": (C.c_int, [_P, C.c_float, C.c_float, _P]),
     "paragan_cpad": (C.c_int64, [C.c_int64]),
     "paragan_sn_ws_size": (C.c_int, [C.c_int64, C.c_int64, C.POINTER(C.c_size_t)]),
     "paragan_sn_power_iter": (C.c_int, [_P, _P, C.c_int64, C.c_int64, _P, _P, _P, C.c_int, C.c_float, _P]),
@@ -328,6 +330,21 @@ class Context:
         """Run the block backwards' weight gradients of the step calls on a
         further stream beside their data gradients (bit-identical results)."""
         return self.check(load().paragan_set_overlap_wgrad(self.h, int(on)))
+
+    def set_grad_clip(self, max_norm_g, max_norm_d):
+        """Clip the gradients of the step calls' optimisers by their norms (0: off, infinity: norms alone).  Returns a float32
+        tensor of the generator's last norm and factor, then the discriminator's, or None when both are off."""
+        n = C.c_size_t()
+        _check_static(load().paragan_grad_clip_size(C.byref(n)))
+        buf = workspace(n.value) if max_norm_g > 0 or max_norm_d > 0 else None
+        self.check(load().paragan_set_grad_clip(self.h, max_norm_g, max_norm_d, _ptr(buf)))
+        self._clip_buf = buf                                  # the library writes there while clipping is on
+        if buf is None:
+            return None
+        import torch
+        buf[:16].zero_()
+        torch.cuda.current_stream().synchronize()             # ahead of steps on any stream
+        return buf[:16].view(torch.float32)
 
     def close(self):
         if self.h:

@@ -1,0 +1,146 @@
+"""Clipping inside the step calls: the optimisers take the gradient that the
+step leaves in `grads` times the factor of its norm, everything else is as
+without it."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from paragan_2411_03999_amd import lib
+
+from .parity import context, need_gpu
+from .test_gpu_train_step import ARCHS, hparams, make_nets, minimal_arch, run_train_step, step_inputs
+
+pytestmark = pytest.mark.gpu
+
+U32 = 2.0 ** -24
+
+
+def moved(opt, p, m, v, g, t):
+    """float64 parameters after one update, and what fp32 arithmetic may be off by."""
+    b1, b2, lr, eps = (float(np.float32(x)) for x in (opt.beta1, opt.beta2, opt.lr, opt.eps))
+    m1 = b1 * m + (1 - b1) * g
+    d = g - m1 if opt.kind == lib.ADABELIEF else g
+    v1 = b2 * v + (1 - b2) * d * d + (eps if opt.kind == lib.ADABELIEF else 0.0)
+    step = lr / (1 - b1 ** t) * m1 / (np.sqrt(v1 / (1 - b2 ** t)) + eps)
+    # m1 and d are off by the rounding of their terms, v1 by that of d twice; the step's quotient by half of v1's
+    em = 4 * U32 * (np.abs(b1 * m) + (1 - b1) * np.abs(g))
+    ed = em + 2 * U32 * np.abs(g)
+    ev = (1 - b2) * 2 * np.abs(d) * ed + 8 * U32 * v1
+    root = np.sqrt(v1 / (1 - b2 ** t))
+    es = lr / (1 - b1 ** t) * em / (root + eps) + np.abs(step) * (0.5 * ev / np.maximum(v1, 1e-300) * root / (root + eps) + 16 * U32)
+    return p - step, es + 2 * U32 * np.abs(p)
+
+
+def num(t):
+    return t.detach().double().cpu().numpy()
+
+
+def test_steps_take_the_clipped_gradient():
+    torch = need_gpu()
+    a, B = minimal_arch(), 8
+    hp = hparams()
+    d, s, _, _, G0, D0 = make_nets(torch, a, B, 811, hp, smooth_opt=True)
+    inp, keep = step_inputs(torch, s, a, B, 1)
+    ws = lib.workspace(lib.paragan_train_step_ws_size(d))
+    loss = (C.c_float * 1)()
+    img = torch.rand(B, a.img, a.img, 3, device="cuda") * 2 - 1
+
+    def step(which, limit):
+        ctx = context()
+        G, D = G0.clone(torch), D0.clone(torch)
+        said = ctx.set_grad_clip(*((0.0, limit) if which else (limit, 0.0))) if limit is not None else None
+        if which:
+            ctx.check(lib.paragan_d_step(ctx, d, D.state, keep[0], keep[1], img, keep[1], ws, loss))
+        else:
+            ctx.check(lib.paragan_g_step(ctx, d, G.state, D.state, keep[4], keep[5], ws, loss))
+        torch.cuda.synchronize()
+        return (D if which else G), None if said is None else said.cpu().tolist(), loss[0]
+
+    for which, opt, first in ((0, d.opt_g, G0), (1, d.opt_d, D0)):
+        free, _, l0 = step(which, None)
+        norm = math.sqrt((num(free.G) ** 2).sum())
+        loose, said, l1 = step(which, math.inf)
+        assert l0 == l1 and all(torch.equal(x, y) for x, y in zip(free.tensors(), loose.tensors()))
+        assert abs(said[2 * which] - norm) <= 2 * U32 * norm and said[2 * which + 1] == 1.0 and said[2 - 2 * which] == 0.0
+        limit = float(np.float32(0.25 * norm))
+        tight, said, l2 = step(which, limit)
+        assert l0 == l2 and torch.equal(free.G, tight.G) and torch.equal(free.U, tight.U) and not torch.equal(free.P, tight.P)
+        assert abs(said[2 * which + 1] - limit / norm) <= 2 * U32 * limit / norm
+        k = said[2 * which + 1]
+        want, tol = moved(opt, num(first.P), num(first.M), num(first.V), num(free.G) * k, first.state.opt_t + 1)
+        err = np.abs(num(tight.P) - want)
+        print("  network", which, "norm", norm, "largest share of the bound", (err / tol).max(), flush=True)
+        assert np.all(err <= tol)
+
+
+@pytest.mark.parametrize("arch", ["minimal", "small"])
+def test_fused_and_overlapped_steps_clip_alike(arch):
+    torch = need_gpu()
+    a, B, n_D = ARCHS[arch](), 4, 2
+    d, s, _, _, G0, D0 = make_nets(torch, a, B, 823, hparams())
+    inp, keep = step_inputs(torch, s, a, B, n_D)
+    ws = lib.workspace(lib.paragan_train_step_ws_size(d))
+    runs = []
+    for limit, overlap in ((None, 0), (math.inf, 0), (1e-2, 0), (1e-2, 1)):
+        ctx = context()
+        ctx.set_overlap_wgrad(overlap)
+        said = ctx.set_grad_clip(limit, limit) if limit else None
+        G, D = G0.clone(torch), D0.clone(torch)
+        run_train_step(torch, d, G, D, inp, n_D, ws, ctx)
+        torch.cuda.synchronize()
+        if said is not None:
+            v = said.cpu().tolist()
+            gn = [math.sqrt((num(N.G) ** 2).sum()) for N in (G, D)]
+            assert abs(v[0] - gn[0]) <= 2 * U32 * gn[0] and abs(v[2] - gn[1]) <= 2 * U32 * gn[1], (v, gn)
+        ctx.set_grad_clip(0.0, 0.0)
+        runs.append((G, D))
+    for X, Y in zip(runs[0] + runs[2], runs[1] + runs[3]):
+        assert all(torch.equal(t0, t1) for t0, t1 in zip(X.tensors(), Y.tensors()))
+    assert not torch.equal(runs[0][1].P, runs[2][1].P)
+
+
+def test_async_step_clips_both_networks():
+    torch = need_gpu()
+    a, B, n_D = minimal_arch(), 4, 2
+    d, s, _, _, G0, D0 = make_nets(torch, a, B, 829, hparams())
+    ws = lib.workspace(lib.paragan_async_ws_size(d, n_D))
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    real = [torch.rand(B, a.img, a.img, 3, device="cuda", generator=gen) * 2 - 1 for _ in range(n_D)]
+    lab = [torch.randint(0, a.n_classes, (B,), device="cuda", dtype=torch.int32, generator=gen) for _ in range(n_D)]
+    z = torch.randn(n_D * B, a.dz, device="cuda", generator=gen)
+    y = torch.randint(0, a.n_classes, (n_D * B,), device="cuda", dtype=torch.int32, generator=gen)
+    runs = []
+    for limit in (None, math.inf, 1e-3):
+        ctx = context()
+        said = ctx.set_grad_clip(limit, limit) if limit else None
+        G, D = G0.clone(torch), D0.clone(torch)
+        img = torch.zeros(n_D * B, a.img, a.img, 3, device="cuda")
+        labels, pred = torch.zeros(n_D * B, dtype=torch.int32, device="cuda"), torch.zeros(n_D * B, device="cuda")
+        arr = lambda t: (C.c_void_p * n_D)(*[x.data_ptr() for x in t])  # noqa: E731
+        inp = lib.AsyncInputs(arr(real), arr(lab), z.data_ptr(), y.data_ptr(), img.data_ptr(), labels.data_ptr(), pred.data_ptr())
+        losses = (C.c_float * (n_D + 1))()
+        torch.cuda.synchronize()
+        ctx.check(lib.paragan_async_step(ctx, d, G.state, D.state, inp, n_D, ws, losses))
+        torch.cuda.synchronize()
+        if said is not None:
+            v = said.cpu().tolist()
+            gn = [math.sqrt((num(N.G) ** 2).sum()) for N in (G, D)]
+            assert abs(v[0] - gn[0]) <= 2 * U32 * gn[0] and abs(v[2] - gn[1]) <= 2 * U32 * gn[1], (v, gn)
+        runs.append((G, D))
+    for X, Y in zip(runs[0], runs[1]):
+        assert all(torch.equal(t0, t1) for t0, t1 in zip(X.tensors(), Y.tensors()))
+    assert not torch.equal(runs[0][0].P, runs[2][0].P) and not torch.equal(runs[0][1].P, runs[2][1].P)
+
+
+def test_clip_settings_are_checked():
+    need_gpu()
+    ctx = lib.Context()
+    for g, d in ((-1.0, 0.0), (0.0, float("nan")), (-math.inf, 1.0)):
+        with pytest.raises(lib.ParaganError):
+            ctx.set_grad_clip(g, d)
+    buf = lib.workspace(1 << 16)
+    for bad in (None, buf[1:]):
+        assert lib.load().paragan_set_grad_clip(ctx.h, 1.0, 0.0, None if bad is None else C.c_void_p(bad.data_ptr())) == lib.EINVAL
+    assert ctx.set_grad_clip(0.0, 0.0) is None

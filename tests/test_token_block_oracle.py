@@ -204,6 +204,12 @@ def test_clip_refusals(L):
     assert L.paragan_clip(None, None, None, 1.0, 1.0, None, None) == lib.EINVAL
 
 
+def test_step_clip_refusals(L):
+    n = C.c_size_t()
+    assert L.paragan_grad_clip_size(C.byref(n)) == lib.OK and n.value >= 16 and L.paragan_grad_clip_size(None) == lib.EINVAL
+    assert L.paragan_set_grad_clip(None, 1.0, 1.0, C.c_void_p(256)) == lib.EINVAL
+
+
 def test_binding_refuses_before_the_library():
     torch = pytest.importorskip("torch")
     z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)  # noqa: E731
