@@ -444,7 +444,7 @@ int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
  * fp32 [D], finite.  h0: the states before the first token taken, fp32
  * [B][D], or NULL for zeros; ht: those after the last, or NULL.  A sequence
  * of no tokens has ht = h0.  ht may be h0: with S = 1 that is the step of one
- * new token.  States and sums are fp32; the backward divides by a root no
+ * new token.  Outputs must not overlap inputs otherwise.  States and sums are fp32; the backward divides by a root no
  * smaller than 1.1e-19.  A NaN or infinity in a token reaches the tokens
  * after it (in the backward those before it too) of its sequence and channel,
  * and the channel's ddecay.  A stride between tokens is below 2^20. */

@@ -23,7 +23,7 @@ struct ScArgs {
   float* ht;                       // backward: dh0
   void *y, *dr, *dg;               // y; backward: dx in y
   float* saved;                    // [B][ceil(S / kStep or kKeep)][D]: the state ahead of that many tokens
-  float* maps;                     // [B][chunks][D][2]: A, H of every chunk
+  float* maps;                     // [B][chunks][D][2]: A, H of every chunk; in the one nobody needs, the state from outside
   double* part;                    // [B][chunks][D]: sums of dla s
   int64_t xs[2], rs[2], gs[2], ys[2];
   int B, S, D, reverse;
@@ -320,12 +320,15 @@ struct Tokens {
       if (p.ok) st2f((T*)(const_cast<char*>(base) + t * st) + p.c, 0.f, 0.f);
   }
 };
-// tokens from m on (of this lane) past the length never come in
+// tokens from m on (of this lane) past the length never come in (x: where tokens repeat, it was read all the same)
 template <typename F>
-PG_DEV void past(Two<typename F::T>* r, int m, int len, int reverse) {
+PG_DEV void past(Two<typename F::T>* r, Two<typename F::T>* x, int m, int len, int reverse) {
 #pragma unroll
   for (int j = 0; j < F::TOK; ++j)
-    if (m + (reverse ? F::TOK - 1 - j : j) >= len) r[j] = never<typename F::T>();
+    if (m + (reverse ? F::TOK - 1 - j : j) >= len) {
+      r[j] = never<typename F::T>();
+      x[j] = Two<typename F::T>{};
+    }
 }
 
 // (A, H) of what lies ahead of this lane's segment in its wave (ahead), and of
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
   const Tokens<F> x(a.x, a.xs, p), r(a.r, a.rs, p), g(a.g, a.gs, p), y(a.y, a.ys, p);
   const int64_t o = (int64_t)p.b * a.D + p.cc;
   const float2 k = rates(a, p.cc);
-  float2 h = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
+  float2 h = !SPLIT && a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
   Two<T> X[TOK], R[TOK], G[TOK];
   auto load = [&](int m) {
     r.load(R, m, p.len, a.reverse);
@@ -385,6 +388,8 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
   if (p.n) load(p.tile(0, a.reverse));
   if constexpr (SPLIT) {
     const float* m = a.maps + ((int64_t)p.b * a.nc * a.D + p.cc) * 2;
+    const float4 first = *reinterpret_cast<const float4*>(m + (int64_t)(a.nc - 1) * a.D * 2);
+    h = make_float2(first.y, first.w);
 #pragma unroll 8
     for (int j = 0; j < p.chunk; ++j) {
       const float4 q = *reinterpret_cast<const float4*>(m + (int64_t)j * a.D * 2);
@@ -394,7 +399,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
   int turn = 0;
   for (int t = 0; t < p.n; ++t, turn ^= 1) {
     const int m0 = p.tile(t, a.reverse), mine = m0 + p.mseg * TOK;
-    if (m0 + F::TT > p.len) past<F>(R, mine, p.len, a.reverse);
+    if (m0 + F::TT > p.len) past<F>(R, X, mine, p.len, a.reverse);
     float2 av[TOK], uv[TOK], A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < TOK; ++j) {
@@ -436,7 +441,13 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
   typedef typename F::T T;
   __shared__ float4 sh[NW][CL];
   const Place<F> p(a);
-  if (p.b >= a.B || p.chunk == a.nc - 1) return;   // nobody comes after the last one
+  if (p.b >= a.B) return;
+  if (p.chunk == a.nc - 1) {       // nobody comes after the last one: its place hands on h0, which ht may overwrite
+    const float2 h = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + (int64_t)p.b * a.D + p.cc) : make_float2(0.f, 0.f);
+    if (p.seg == 0 && p.ok)
+      *reinterpret_cast<float4*>(a.maps + (((int64_t)p.b * a.nc + p.chunk) * a.D + p.c) * 2) = make_float4(0.f, h.x, 0.f, h.y);
+    return;
+  }
   const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;   // a chunk is whole tiles
   const Tokens<F> x(a.x, a.xs, p, run), r(a.r, a.rs, p, run), g(a.g, a.gs, p, run);
   const float2 k = rates(a, p.cc);
@@ -452,7 +463,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
     load(0);
     for (int i = 0; i < run; i += TOK) {
       float2 av[TOK], uv[TOK];
-      if (p.lo + a.chunk > p.len) past<F>(R, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
+      if (p.lo + a.chunk > p.len) past<F>(R, X, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
 #pragma unroll
       for (int j = 0; j < TOK; ++j) {
         const float2 xx = X[j].get(), rr = R[j].get(), gg = G[j].get();
@@ -501,7 +512,8 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
   const Tokens<F> dx(a.y, a.xs, p), dr(a.dr, a.rs, p), dg(a.dg, a.gs, p);
   const int64_t o = (int64_t)p.b * a.D + p.cc;
   const float2 k = rates(a, p.cc);
-  float2 c = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);   // flows back into the tile
+  // what flows back into the tile
+  float2 c = !SPLIT && a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
   const float* keep = a.saved + (int64_t)p.b * cdiv(a.S, kKeep) * a.D + p.cc;
   Two<T> X[TOK], R[TOK], G[TOK], Y[TOK], Yn[TOK];
   float2 hn = make_float2(0.f, 0.f);
@@ -517,6 +529,8 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
   if (p.n) load(p.tile(p.n - 1, a.reverse));
   if constexpr (SPLIT) {
     const float* m = a.maps + ((int64_t)p.b * a.nc * a.D + p.cc) * 2;
+    const float4 outer = *reinterpret_cast<const float4*>(m);
+    c = make_float2(outer.y, outer.w);
 #pragma unroll 8
     for (int j = a.nc - 1; j > p.chunk; --j) {
       const float4 q = *reinterpret_cast<const float4*>(m + (int64_t)j * a.D * 2);
@@ -529,7 +543,7 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
   double sum0 = 0.0, sum1 = 0.0;
   for (int t = p.n - 1; t >= 0; --t, turn ^= 1) {
     const int m0 = p.tile(t, a.reverse);
-    if (m0 + F::TT > p.len) past<F>(R, m0 + p.mseg * TOK, p.len, a.reverse);
+    if (m0 + F::TT > p.len) past<F>(R, X, m0 + p.mseg * TOK, p.len, a.reverse);
     Grad e0[TOK], e1[TOK];
     float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f), C = make_float2(0.f, 0.f);
 #pragma unroll
@@ -622,7 +636,13 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
   typedef typename F::T T;
   __shared__ float4 sh[NW][CL];
   const Place<F> p(a);
-  if (p.b >= a.B || p.chunk == 0) return;
+  if (p.b >= a.B) return;
+  if (p.chunk == 0) {              // nobody comes before the first one: its place hands on dht, which dh0 may overwrite
+    const float2 h = a.h0 ? *reinterpret_cast<const float2*>(a.h0 + (int64_t)p.b * a.D + p.cc) : make_float2(0.f, 0.f);
+    if (p.seg == 0 && p.ok)
+      *reinterpret_cast<float4*>(a.maps + ((int64_t)p.b * a.nc * a.D + p.c) * 2) = make_float4(0.f, h.x, 0.f, h.y);
+    return;
+  }
   const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;
   const Tokens<F> r(a.r, a.rs, p, run), dy(a.dy, a.ys, p, run);
   const float2 k = rates(a, p.cc);
@@ -637,7 +657,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
     load(run - TOK);
     for (int i = run - TOK; i >= 0; i -= TOK) {
       float2 av[TOK], d[TOK];
-      if (p.lo + a.chunk > p.len) past<F>(R, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
+      if (p.lo + a.chunk > p.len) past<F>(R, Y, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
 #pragma unroll
       for (int j = 0; j < TOK; ++j) {
         const float2 rr = R[j].get();

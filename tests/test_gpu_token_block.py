@@ -268,6 +268,27 @@ def test_scan_state_in_place_and_steps_follow_the_whole():
     held("state", h, want["ht"], want["tol.ht"])
 
 
+@pytest.mark.parametrize("dims", [(2, 40, 72), (3, 300, 520), (1, 9000, 264), (2, 5000, 1000)])
+def test_scan_states_in_place(dims):
+    """ht over h0 and dh0 over dht, whole and in chunks: the bits of separate ones."""
+    torch = need_gpu()
+    B, S, D = dims
+    x, r, g, dy = (torch.randn(B, S, D, device="cuda").bfloat16() for _ in range(4))
+    dec, h0, dht = torch.rand(D, device="cuda") * 5 - 8, torch.randn(B, D, device="cuda"), torch.randn(B, D, device="cuda")
+    y, grads, ddec, ctx = torch.empty_like(x), [torch.empty_like(x) for _ in range(3)], torch.empty(D, device="cuda"), lib.Context()
+    d = lib.scan_desc(x, r, g, y, sharp=8.0)
+    sb, wb = lib.paragan_scan_sizes(d)
+    saved, ws, outs = lib.workspace(sb), lib.workspace(wb), []
+    for rep in range(4):
+        a, b = h0.clone(), dht.clone()
+        ht, dh0 = (a, b) if rep else (torch.empty_like(a), torch.empty_like(b))
+        lib.paragan_scan_fwd(ctx, d, x, r, g, dec, None, a, y, ht, saved, ws)
+        lib.paragan_scan_bwd(ctx, d, x, r, g, dec, None, saved, dy, b, *grads, ddec, dh0, ws)
+        torch.cuda.synchronize()
+        outs.append([t.clone() for t in (y, ht, *grads, ddec, dh0)])
+    assert all(torch.equal(u, v) for o in outs[1:] for u, v in zip(outs[0], o))
+
+
 def test_scan_nan_reaches_the_tokens_after_it_alone():
     torch = need_gpu()
     for S in (50, 3000):
