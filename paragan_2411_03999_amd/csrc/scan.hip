@@ -46,7 +46,7 @@ template <> struct Two<float> {
 PG_DEV void st2f(bf16_t* p, float a, float b) { *reinterpret_cast<uint32_t*>(p) = f2bf2(a, b); }
 PG_DEV void st2f(float* p, float a, float b) { *reinterpret_cast<float2*>(p) = make_float2(a, b); }
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // sigmoid(v) and 1 - sigmoid(v), both to the last digits (e^-v may be infinite)
 PG_DEV void sigmoid(float v, float& s, float& c) {
@@ -57,30 +57,30 @@ PG_DEV void sigmoid(float v, float& s, float& c) {
 PG_DEV float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
 // softplus(v) = log(1 + e^v)
 PG_DEV float softplus(float v) { return log1pf(expf(-fabsf(v))) + fmaxf(v, 0.f); }
-// -sharp softplus(decay) of two channels
+// -sharp softplus(decay) / ln 2 of two channels
 PG_DEV float2 rates(const ScArgs& a, int c) {
   const float2 d = *reinterpret_cast<const float2*>(a.decay + c);
-  return make_float2(-a.sharp * softplus(d.x), -a.sharp * softplus(d.y));
+  return make_float2(-a.sharp * softplus(d.x) * kLog2e, -a.sharp * softplus(d.y) * kLog2e);
 }
 
-// a = e^la and p = 1 - a^2 for la <= 0.  Where the difference would cancel, p
-// is -la Q(la) with a polynomial Q of degree 4 for (e^(2 la) - 1) / la on
-// [-0.2, 0] (least largest relative error, 6.3e-8 with rounded coefficients).
-// p is held above zero, so that w = p p^-1/2 and 1 / p are finite.
-PG_DEV void decay_of(float la, float& a, float& p) {
-  a = __builtin_amdgcn_exp2f(la * kLog2e);
-  float q = fmaf(la, 0.2258301079273224f, 0.6596707105636597f);
-  q = fmaf(la, q, 1.3328346014022827f);
-  q = fmaf(la, q, 1.9999873638153076f);
-  q = fmaf(la, q, 2.f);
-  p = fmaxf(la > -0.2f ? -la * q : fmaf(-a, a, 1.f), 1.17549435e-38f);
+// a = 2^l and p = 1 - a^2 for l = la / ln 2 <= 0.  Where the difference would
+// cancel, p is -l Q(l) with a polynomial Q of degree 4 for (4^l - 1) / l on
+// la in [-0.2, 0] (least largest relative error, 6.9e-8 with rounded
+// coefficients).
+PG_DEV void decay_of(float l, float& a, float& p) {
+  a = __builtin_amdgcn_exp2f(l);
+  float q = fmaf(l, 0.036133427172899246f, 0.15227515995502472f);
+  q = fmaf(l, q, 0.4438667893409729f);
+  q = fmaf(l, q, 0.9608999490737915f);
+  q = fmaf(l, q, 1.3862943649291992f);
+  p = l > -0.2f * kLog2e ? -l * q : fmaf(-a, a, 1.f);
 }
 
 // a and u of one element
 PG_DEV void gate(float x, float r, float g, float k, float& a, float& u) {
   float p;
   decay_of(k * sigmoid(r), a, p);
-  u = p * __builtin_amdgcn_rsqf(p) * sigmoid(g) * x;
+  u = __builtin_amdgcn_sqrtf(p) * sigmoid(g) * x;
 }
 // What one element needs after its gates are known: dx = E fx, dg = E fg,
 // dr = E M fr, ddecay += E M s, with M = a h_{t-1} - v.
@@ -91,14 +91,15 @@ PG_DEV void grad_gate(float x, float r, float g, float k, Grad& e) {
   float cs, sg, cg, p;
   sigmoid(r, e.s, cs);
   sigmoid(g, sg, cg);
-  const float la = k * e.s;
-  decay_of(la, e.a, p);
+  const float l = k * e.s;
+  decay_of(l, e.a, p);
+  p = fmaxf(p, 1.17549435e-38f);   // so that w = p p^-1/2 and 1 / p are finite
   const float q = __builtin_amdgcn_rsqf(p), aq = e.a * q;
   e.fx = p * q * sg;
   e.u = e.fx * x;
   e.v = e.u * aq * aq;
   e.fg = e.u * cg;
-  e.fr = la * cs;
+  e.fr = l * kLn2 * cs;
 }
 
 // One thread takes two channels of one sequence through all its tokens.
@@ -661,8 +662,8 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
 #pragma unroll
       for (int j = 0; j < TOK; ++j) {
         const float2 rr = R[j].get();
-        av[j].x = __builtin_amdgcn_exp2f(k.x * sigmoid(rr.x) * kLog2e);
-        av[j].y = __builtin_amdgcn_exp2f(k.y * sigmoid(rr.y) * kLog2e);
+        av[j].x = __builtin_amdgcn_exp2f(k.x * sigmoid(rr.x));
+        av[j].y = __builtin_amdgcn_exp2f(k.y * sigmoid(rr.y));
         d[j] = Y[j].get();
       }
       if (i > 0) load(i - TOK);
