@@ -738,10 +738,10 @@ Plan plan_of(const Scan& a, bool bwd) {
   // forward, 50 backward, in tiles 30 and 60; 64 x 64 x 4096 30 and 63, 32 and 62; 32 x 24 x 1024 8 and 17, 7 and 14)
   if (a.S <= kStep || (a.S <= 3 * kStep && rows >= 2048)) return Plan{0, 0, 0, 1, a.S};
   const bool split = split_pays(a, bwd, rows);
-  // blocks of four waves where there are many of them (64 x 256 x 1024 backward 53 us, of eight 64), for
-  // sequences of one tile, and side by side; of eight (a whole CU) where there are few (8 x 4096 x 2048: 213, of
-  // four 242).  A float tile of four would be shorter than kKeep.
-  p.nw = !a.f32 && (split || rows >= 512 || a.S <= kKeep) ? 4 : 8;
+  // blocks of four waves side by side, for sequences of one tile, and where many have only a few tiles (64 x 256 x
+  // 1024 backward 53 us, of eight 64); of eight otherwise (8 x 4096 x 2048 212, of four 241; 16 x 4096 x 2048 402,
+  // 451).  A float tile of four would be shorter than kKeep.
+  p.nw = !a.f32 && (split || a.S <= kKeep || (rows >= 512 && a.S <= 512)) ? 4 : 8;
   const int tt = p.nw * (64 / p.cl) * (a.f32 ? 4 : 8);
   // two to three blocks of four waves a CU (one of eight); each folds the chunks ahead of it, so no more than 96
   int64_t nc = 1;
