@@ -324,19 +324,22 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
   const double g1 = a.w.gain_post ? a.w.gain_post[cc] : 1.0, g2 = a.w.gain_pre ? a.w.gain_pre[cc] : 1.0;
   const double rs = a.res_scale;
   double t[5] = {0.0, 0.0, 0.0, 0.0, 0.0};   // over the sequences: e, q, p, (1 + scale) q, gate p
-  auto done = [&](int b, double e, double q, double p) {
+  auto weight = [&](const float* w, int b, double none) { return w ? (double)w[b * a.mod + cc] : none; };
+  auto done = [&](int b, double e, double q, double p, double scale, double gate) {
     const int64_t o = b * a.mod + cc;
     t[0] += e; t[1] += q; t[2] += p;
-    t[3] += (1.0 + (a.w.scale ? a.w.scale[o] : 0.0)) * q;
-    t[4] += (a.w.gate ? a.w.gate[o] : 1.0) * p;
+    t[3] += (1.0 + scale) * q;
+    t[4] += gate * p;
     if (a.mod && c < a.D) {
       if (a.g.shift) a.g.shift[o] = (float)e;
       if (a.g.scale) a.g.scale[o] = (float)(g2 * q);
       if (a.g.gate) a.g.gate[o] = (float)(rs * g1 * p);
     }
   };
-  double s[3] = {0.0, 0.0, 0.0};
+  double s[3] = {0.0, 0.0, 0.0}, scale = 0.0, gate = 0.0;
   for (int b = grp; b < a.B; b += ng) {
+    scale = weight(a.w.scale, b, 0.0);
+    gate = weight(a.w.gate, b, 1.0);
     const float* p = a.part + (int64_t)b * a.nc * 3 * a.D + cc;
     s[0] = s[1] = s[2] = 0.0;
     for (int i0 = li; i0 < a.nc; i0 += kAhead * a.gs) {
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
 #pragma unroll
         for (int w = 0; w < 3; ++w) s[w] += i0 + u * a.gs < a.nc ? v[u][w] : 0.f;
     }
-    if (a.gs == 1) done(b, s[0], s[1], s[2]);
+    if (a.gs == 1) done(b, s[0], s[1], s[2], scale, gate);
   }
   if (a.gs > 1) {                  // then a group of lanes has one sequence or none
 #pragma unroll
@@ -362,17 +365,19 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
         s[w] = 0.0;
         for (int i = 0; i < a.gs; ++i) s[w] += sh[w][l + i][j];
       }
-      done(grp, s[0], s[1], s[2]);
+      done(grp, s[0], s[1], s[2], scale, gate);
     }
     __syncthreads();
   }
+  if (li == 0) {
 #pragma unroll
-  for (int w = 0; w < 5; ++w) sh[w][l][j] = t[w];
+    for (int w = 0; w < 5; ++w) sh[w][grp][j] = t[w];
+  }
   __syncthreads();
   if (l >= 5 || c >= a.D) return;
   double v = 0.0;
 #pragma unroll 8
-  for (int i = 0; i < 64; ++i) v += sh[l][i][j];
+  for (int i = 0; i < min(ng, a.B); ++i) v += sh[l][i][j];
   if (l == 3 && a.g.gain_pre) a.g.gain_pre[c] = (float)v;
   if (l == 4 && a.g.gain_post) a.g.gain_post[c] = (float)(rs * v);
   if (a.mod) return;
