@@ -17,9 +17,9 @@
 // 16-byte access in bf16), a row lies over 8 to 64 lanes of a wave or over
 // the waves of a block, whose columns' rows (k, m, shift) stay in registers
 // over the tokens of one sequence that the block takes.  The backward's
-// blocks fill a CU with rows side by side (1024 threads, 128 registers a
-// lane), so that few blocks have column sums to be joined, and a row's loads
-// are under way while the one before it is summed.
+// blocks fill a CU with rows side by side, so that few blocks have column sums
+// to be joined, and a row's loads are under way while the one before it is
+// summed.
 #include "rows.hpp"
 #include "token.hpp"
 #include <type_traits>
@@ -169,8 +169,8 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
   }
 }
 
-template <typename TX, typename TH, int P, bool POST>
-__global__ __launch_bounds__(1024) void k_blocknorm_bwd(BnArgs a) {
+template <typename TX, typename TH, int P, bool POST, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_blocknorm_bwd(BnArgs a) {
   __shared__ float2 sh[2][16];
   // lanes of a row, rows a block takes side by side
   const int tid = threadIdx.x, W = P ? P : (a.D + 511) / 512 * 64, NG = (int)blockDim.x / W;
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(1024) void k_blocknorm_bwd(BnArgs a) {
     }
     return;
   }
-  __shared__ float cols[3][1024 * 8];
+  __shared__ float cols[3][THREADS * 8];
   st8f<float>(cols[0] + tid * 8, se);
   st8f<float>(cols[1] + tid * 8, sq);
   st8f<float>(cols[2] + tid * 8, sp);
@@ -395,7 +395,14 @@ int row_lanes(int D) {
 
 // Threads of a block, and rows it takes side by side
 int row_threads(int D) { return row_lanes(D) ? row_lanes(D) : (int)cdiv(D, 512) * 64; }
-int bwd_threads(int D) { return 1024 / row_threads(D) * row_threads(D); }
+// A backward's block: rows side by side on up to 12 waves, three a SIMD with
+// the registers that takes, or where a row has more than six waves on up to
+// 16 with 128 registers and a few of them in memory (8 x 4096 x 1152 post 172
+// us against 179 on 16, 8 x 2000 x 1024 fp32 142 against 155).
+int bwd_threads(int D) {
+  const int t = row_threads(D);
+  return (t <= 384 ? 768 : 1024) / t * t;
+}
 
 // Items: tokens of one sequence a block takes; enough of them to fill the
 // card (`want` blocks) and at most kMaxRows a thread, whole rounds of groups.
@@ -422,8 +429,9 @@ void launch2(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
   const dim3 grid((unsigned)((int64_t)a.B * g.nc)), blk(BWD ? bwd_threads(a.D) : p ? 256 : row_threads(a.D));
 #define PG_BN(P)                                                                              \
   case P:                                                                                     \
-    if (BWD) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, P, POST>), grid, blk, 0, st, g);     \
-    else hipLaunchKernelGGL((k_blocknorm_fwd<TX, TH, P, POST>), grid, blk, 0, st, g);         \
+    if (!BWD) hipLaunchKernelGGL((k_blocknorm_fwd<TX, TH, P, POST>), grid, blk, 0, st, g);    \
+    else if (blk.x <= 768) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, P, POST, 768>), grid, blk, 0, st, g); \
+    else if (P == 0) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, 0, POST, 1024>), grid, blk, 0, st, g);      \
     break;
   switch (p) { PG_BN(8) PG_BN(16) PG_BN(32) PG_BN(64) PG_BN(0) }
 #undef PG_BN
