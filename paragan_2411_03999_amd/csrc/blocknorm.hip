@@ -39,7 +39,7 @@ struct BnArgs {
   float* part;                     // [items][3][D]: e, q, p
   int64_t xs[2], hs[2], zs[2], ys[2], mod;
   int S, D, R, nc;                 // tokens of an item, items of a sequence
-  int layer, branch, pre;
+  int branch, pre;
   float eps, res_scale, inv_d;
 };
 
@@ -57,7 +57,7 @@ PG_DEV T* place(T* p, int64_t row, int c) {
   return reinterpret_cast<T*>(reinterpret_cast<B*>(p + row) + (uint32_t)(c * (int)sizeof(T)));
 }
 
-// Sums of two values over the lanes of a row.  P = 0: over the waves of the
+// Sums of one or two values over the lanes of a row.  P = 0: over the waves of the
 // block, through sh[2][16] float2, whose halves are used in turn so that one
 // barrier a sum is enough: who writes a half again has passed the barrier
 // that everybody reached after reading it.
@@ -65,6 +65,18 @@ template <int P>
 struct RowSum {
   float2 (*sh)[16];
   int turn, wave, first, waves;    // this wave; the row's first and how many
+  PG_DEV float operator()(float a) {
+    if constexpr (P > 0) {
+      return group_sum<P>(a);
+    } else {
+      a = group_sum<64>(a);
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) sh[turn][wave].x = a;
+      __syncthreads();
+      const int i = threadIdx.x & 15;
+      return group_sum<16>(i < waves ? sh[turn][first + i].x : 0.f);
+    }
+  }
   PG_DEV float2 operator()(float a, float b) {
     if constexpr (P > 0) {
       return make_float2(group_sum<P>(a), group_sum<P>(b));
@@ -83,27 +95,27 @@ struct RowSum {
 };
 
 // mean and factor of v over the row; v becomes the normed row (zeros outside)
-template <int P>
-PG_DEV float2 normalise(RowSum<P>& sum, bool layer, bool act, float inv_d, float eps, float* v) {
+template <int P, bool LAYER>
+PG_DEV float2 normalise(RowSum<P>& sum, bool act, float inv_d, float eps, float* v) {
   float mean = 0.f;
-  if (layer) {
+  if constexpr (LAYER) {
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s += v[e];
-    mean = sum(s, 0.f).x * inv_d;
+    mean = sum(s) * inv_d;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = act ? v[e] - mean : 0.f;
   }
   float s = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) s = fmaf(v[e], v[e], s);
-  const float r = __builtin_amdgcn_rsqf(fmaf(sum(s, 0.f).x, inv_d, eps));
+  const float r = __builtin_amdgcn_rsqf(fmaf(sum(s), inv_d, eps));
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] *= r;
   return make_float2(mean, r);
 }
 
-template <typename TX, typename TH, int P, bool POST>
+template <typename TX, typename TH, int P, bool POST, bool LAYER>
 __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
   __shared__ float2 sh[2][16];
   constexpr int NG = P ? 256 / P : 1;
@@ -150,14 +162,14 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
       }
     }
     float2 sth = make_float2(0.f, 1.f);
-    if constexpr (POST) sth = normalise<P>(sum, a.layer, act, a.inv_d, a.eps, hv);
+    if constexpr (POST) sth = normalise<P, LAYER>(sum, act, a.inv_d, a.eps, hv);
     if (a.branch) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) xv[e] = real ? fmaf(k[e], POST ? hv[e] * g1[e] : hv[e], xv[e]) : 0.f;
       if (ok) st8f<TX>(place(z, r * a.zs[1], c8), xv);
     }
     if (a.pre) {
-      const float2 stz = normalise<P>(sum, a.layer, act, a.inv_d, a.eps, xv);
+      const float2 stz = normalise<P, LAYER>(sum, act, a.inv_d, a.eps, xv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) xv[e] = real ? fmaf(xv[e], m[e], f[e]) : 0.f;
       if (ok) st8f<TH>(place(y, r * a.ys[1], c8), xv);
@@ -169,7 +181,7 @@ __global__ __launch_bounds__(P ? 256 : 1024) void k_blocknorm_fwd(BnArgs a) {
   }
 }
 
-template <typename TX, typename TH, int P, bool POST, int THREADS>
+template <typename TX, typename TH, int P, bool POST, bool LAYER, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_blocknorm_bwd(BnArgs a) {
   __shared__ float2 sh[2][16];
   // lanes of a row, rows a block takes side by side
@@ -222,39 +234,61 @@ __global__ __launch_bounds__(THREADS) void k_blocknorm_bwd(BnArgs a) {
     }
   };
   fetch(r0 + grp);
+  // lanes past the row's end take part with rows of zeros
+  if (!act) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[e] = m[e] = 0.f;
+  }
+  const int rl = min(r1, len);
+  // mean of t and of t n, and r (t - [mean t] - n mean(t n))
+  auto back = [&](const float* t, const float* n, float& c1, float& c2) {
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if constexpr (LAYER) s1 += t[e];
+      s2 = fmaf(t[e], n[e], s2);
+    }
+    if constexpr (LAYER) {
+      const float2 s = sum(s1, s2);
+      c1 = s.x * a.inv_d;
+      c2 = s.y * a.inv_d;
+    } else {
+      c1 = 0.f;
+      c2 = sum(s2) * a.inv_d;
+    }
+  };
   for (int rr = r0; rr < r1; rr += NG) {
     const int r = rr + grp;
-    const bool ok = act && r < r1, real = ok && r < len;
+    const bool ok = act && r < r1;
     float n[8], hn[8], dZ[8], dv[8];
-    const float4 st = sr;
+    float4 st = sr;
     xr.get(n);
     hr.get(hn);
     zr.get(dZ);
     yr.get(dv);
     if (rr + NG < r1) fetch(rr + NG + grp);
+    if (r >= rl) {                 // no token: zeros throughout
+      st = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) n[e] = hn[e] = dZ[e] = dv[e] = 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if (POST) hn[e] = (hn[e] - st.x) * st.y;
+      if constexpr (POST) hn[e] = (LAYER ? hn[e] - st.x : hn[e]) * st.y;
       if (a.branch) n[e] = fmaf(k[e], hn[e], n[e]);
-      n[e] = real ? (n[e] - st.z) * st.w : 0.f;
-      hn[e] = real ? hn[e] : 0.f;
-      dZ[e] = real ? dZ[e] : 0.f;
-      dv[e] = real ? dv[e] : 0.f;
+      n[e] = (LAYER ? n[e] - st.z : n[e]) * st.w;
     }
     if (a.pre) {
-      float s1 = 0.f, s2 = 0.f;
+      float c1, c2;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         se[e] += dv[e];
         sq[e] = fmaf(dv[e], n[e], sq[e]);
         dv[e] *= m[e];
-        s1 += dv[e];
-        s2 = fmaf(dv[e], n[e], s2);
       }
-      const float2 s = sum(s1, s2);
-      const float c1 = a.layer ? s.x * a.inv_d : 0.f, c2 = s.y * a.inv_d;
+      back(dv, n, c1, c2);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dZ[e] = real ? fmaf(st.w, dv[e] - c1 - n[e] * c2, dZ[e]) : 0.f;
+      for (int e = 0; e < 8; ++e) dZ[e] = fmaf(st.w, fmaf(-n[e], c2, LAYER ? dv[e] - c1 : dv[e]), dZ[e]);
     }
     if (ok) st8f<TX>(place(dx, r * a.xs[1], c8), dZ);
     if (a.branch) {
@@ -264,16 +298,10 @@ __global__ __launch_bounds__(THREADS) void k_blocknorm_bwd(BnArgs a) {
         dv[e] = dZ[e] * k[e];
       }
       if constexpr (POST) {
-        float s1 = 0.f, s2 = 0.f;
+        float c1, c2;
+        back(dv, hn, c1, c2);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          s1 += dv[e];
-          s2 = fmaf(dv[e], hn[e], s2);
-        }
-        const float2 s = sum(s1, s2);
-        const float c1 = a.layer ? s.x * a.inv_d : 0.f, c2 = s.y * a.inv_d;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dv[e] = real ? st.y * (dv[e] - c1 - hn[e] * c2) : 0.f;
+        for (int e = 0; e < 8; ++e) dv[e] = st.y * fmaf(-hn[e], c2, LAYER ? dv[e] - c1 : dv[e]);
       }
       if (ok) st8f<TH>(place(dh, r * a.hs[1], c8), dv);
     }
@@ -418,33 +446,35 @@ BnArgs make_args(const BlockNorm& a, const BlockNormRows& w, const int32_t* len,
   BnArgs g{};
   g.w = w; g.len = len; g.x = x; g.h = h;
   for (int i = 0; i < 2; ++i) { g.xs[i] = a.xs[i]; g.hs[i] = a.hs[i]; g.zs[i] = a.zs[i]; g.ys[i] = a.ys[i]; }
-  g.mod = a.mod; g.S = a.S; g.D = a.D; g.layer = a.layer; g.branch = a.branch; g.pre = a.pre;
+  g.mod = a.mod; g.S = a.S; g.D = a.D; g.branch = a.branch; g.pre = a.pre;
   g.eps = a.eps; g.res_scale = a.res_scale; g.inv_d = 1.f / (float)a.D;
   return g;
 }
 
-template <bool BWD, typename TX, typename TH, bool POST>
-void launch2(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
+template <bool BWD, typename TX, typename TH, bool POST, bool LAYER>
+void launch3(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
   const int p = row_lanes(a.D);
   const dim3 grid((unsigned)((int64_t)a.B * g.nc)), blk(BWD ? bwd_threads(a.D) : p ? 256 : row_threads(a.D));
-#define PG_BN(P)                                                                              \
-  case P:                                                                                     \
-    if (!BWD) hipLaunchKernelGGL((k_blocknorm_fwd<TX, TH, P, POST>), grid, blk, 0, st, g);    \
-    else if (blk.x <= 768) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, P, POST, 768>), grid, blk, 0, st, g); \
-    else if (P == 0) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, 0, POST, 1024>), grid, blk, 0, st, g);      \
+#define PG_BN(P)                                                                                                      \
+  case P:                                                                                                             \
+    if (!BWD) hipLaunchKernelGGL((k_blocknorm_fwd<TX, TH, P, POST, LAYER>), grid, blk, 0, st, g);                     \
+    else if (blk.x <= 768) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, P, POST, LAYER, 768>), grid, blk, 0, st, g);   \
+    else if (P == 0) hipLaunchKernelGGL((k_blocknorm_bwd<TX, TH, 0, POST, LAYER, 1024>), grid, blk, 0, st, g);        \
     break;
   switch (p) { PG_BN(8) PG_BN(16) PG_BN(32) PG_BN(64) PG_BN(0) }
 #undef PG_BN
   PG_LAUNCH_CHECK();
 }
+template <bool BWD, typename TX, typename TH>
+void launch2(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
+  if (a.post) a.layer ? launch3<BWD, TX, TH, true, true>(st, a, g) : launch3<BWD, TX, TH, true, false>(st, a, g);
+  else a.layer ? launch3<BWD, TX, TH, false, true>(st, a, g) : launch3<BWD, TX, TH, false, false>(st, a, g);
+}
 template <bool BWD>
 void launch(hipStream_t st, const BlockNorm& a, const BnArgs& g) {
-#define PG_BN(TX, TH)                                              \
-  (a.post ? launch2<BWD, TX, TH, true>(st, a, g) : launch2<BWD, TX, TH, false>(st, a, g))
-  if (a.f32) PG_BN(float, float);
-  else if (a.res32) PG_BN(float, bf16_t);
-  else PG_BN(bf16_t, bf16_t);
-#undef PG_BN
+  if (a.f32) launch2<BWD, float, float>(st, a, g);
+  else if (a.res32) launch2<BWD, float, bf16_t>(st, a, g);
+  else launch2<BWD, bf16_t, bf16_t>(st, a, g);
 }
 
 constexpr int64_t kFwdItems = 4096, kBwdItems = 256;
