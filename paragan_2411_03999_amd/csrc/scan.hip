@@ -7,6 +7,20 @@
 //   dla = E (a h_{t-1} - u a^2 / w^2);  dr = dla la (1 - s);
 //   dg = E u (1 - sg);  dx = E w sg;
 //   ddecay = -sharp sigmoid(decay) sum dla s;  dh0 = a_1 E_1.
+//
+// Bound by memory with the vector units close behind: forward 8 bytes and
+// about 35 vector instructions an element in bf16 (five of them
+// transcendental), backward 14 bytes and 60.  Every input is read once: a tile
+// of tokens lies in a block's registers while its tokens' maps of the state
+// are joined, so the sequence is not walked token after token, and only a
+// state every 64 tokens is kept for the backward.  Few sequences of few
+// channels leave the card idle; then chunks of them go side by side and the
+// inputs are read twice.
+// Measured, bf16: forward of 8 x 4096 x 2048 121 us (4.4 TB/s; a copy reaches
+// 5.2), of 16 x 4096 x 1536 218 us (3.7: 384 blocks on 256 CUs), of 1 x 32768
+// x 1280 in chunks 126 us (4.6 over both passes), backward of 8 x 4096 x 2048
+// 205 us (4.6).  Slabs of 32 channels (64-byte rows) were slower, forward 156
+// and backward 402 us where these took 121 and 265.
 #include "token.hpp"
 
 namespace pg {
