@@ -399,7 +399,7 @@ int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d,
 enum { PARAGAN_NORM_RMS = 0, PARAGAN_NORM_LAYER = 1 };
 
 typedef struct {
-  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S < 2^31 */
+  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S <= 2^30 */
   int32_t D;                       /* width, a multiple of 8 up to 8192 */
   int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: h, y and their gradients */
   int32_t stream_dtype;            /* x, z and their gradients: dtype, or PARAGAN_F32 */
@@ -449,7 +449,7 @@ int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
  * after it (in the backward those before it too) of its sequence and channel,
  * and the channel's ddecay.  A stride between tokens is below 2^20. */
 typedef struct {
-  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S < 2^31 */
+  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S <= 2^30 */
   int32_t D;                       /* channels, a multiple of 8, up to 2^20; B * D < 2^31 */
   int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: x, r, g, y and their gradients */
   int32_t reverse;                 /* 0 or 1 */

@@ -660,7 +660,7 @@ static bool rows_distinct(const int64_t* st, int64_t B, int64_t S, int64_t D) {
 
 static BlockNorm make_bn(const paragan_blocknorm_desc* d) {
   if (!d) throw Error{PARAGAN_EINVAL, "blocknorm: desc is NULL"};
-  PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S < (1LL << 31), "blocknorm: B, S must be >= 1 and B * S below 2^31");
+  PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S <= (1LL << 30), "blocknorm: B, S must be >= 1 and B * S at most 2^30");
   PG_CHECK(d->D >= 8 && d->D <= 8192 && d->D % 8 == 0, "blocknorm: D must be a multiple of 8 up to 8192");
   PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "blocknorm: dtype must be PARAGAN_BF16 or PARAGAN_F32");
   PG_CHECK(d->stream_dtype == PARAGAN_F32 || d->stream_dtype == d->dtype,
@@ -753,7 +753,7 @@ extern "C" int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_d
 
 static Scan make_scan(const paragan_scan_desc* d) {
   if (!d) throw Error{PARAGAN_EINVAL, "scan: desc is NULL"};
-  PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S < (1LL << 31), "scan: B, S must be >= 1 and B * S below 2^31");
+  PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S <= (1LL << 30), "scan: B, S must be >= 1 and B * S at most 2^30");
   PG_CHECK(d->D >= 8 && d->D <= (1 << 20) && d->D % 8 == 0 && (int64_t)d->B * d->D < (1LL << 31),
            "scan: D must be a multiple of 8 up to 2^20 and B * D below 2^31");
   PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "scan: dtype must be PARAGAN_BF16 or PARAGAN_F32");
