@@ -313,21 +313,25 @@ struct Tokens {
     st = s[1] * (int64_t)sizeof(T);
     lane = q.ok ? (uint32_t)q.mseg * (uint32_t)run * (uint32_t)st + (uint32_t)q.c * (uint32_t)sizeof(T) : kOOB;
   }
-  // descriptor from token m on; all of one row where tokens repeat
-  PG_DEV __amdgpu_buffer_rsrc_t at(int m, int len) const {
+  // bytes from token m on, all of one row where tokens repeat
+  PG_DEV uint32_t bytes(int m, int len) const {
     const int64_t n = (int64_t)(len - m) * st;
-    return make_rsrc(base + m * st, st == 0 || n > kBufMax ? kBufMax : n < 0 ? 0 : n);
+    return (uint32_t)(st == 0 || n > kBufMax ? kBufMax : n < 0 ? 0 : n);
   }
   PG_DEV uint32_t place(int j, int reverse) const { return (uint32_t)(reverse ? F::TOK - 1 - j : j) * (uint32_t)st; }
+  // The range check takes the uniform offset from the descriptor's bytes, so
+  // that offset stops there: past the length no lane's is below what is left.
   PG_DEV void load(Two<T>* v, int m, int len, int reverse, uint32_t so = 0) const {
-    const __amdgpu_buffer_rsrc_t r = at(m, len);
+    const uint32_t n = bytes(m, len);
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base + m * st, n);
 #pragma unroll
-    for (int j = 0; j < F::TOK; ++j) buf_load(v[j], r, lane, so + place(j, reverse));
+    for (int j = 0; j < F::TOK; ++j) buf_load(v[j], r, lane, min(so + place(j, reverse), n));
   }
   template <typename G> PG_DEV void store(int m, int len, int reverse, G&& get) const {
-    const __amdgpu_buffer_rsrc_t r = at(m, len);
+    const uint32_t n = bytes(m, len);
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base + m * st, n);
 #pragma unroll
-    for (int j = 0; j < F::TOK; ++j) buf_store<T>(r, lane, place(j, reverse), get(j));
+    for (int j = 0; j < F::TOK; ++j) buf_store<T>(r, lane, min(place(j, reverse), n), get(j));
   }
   // rows [max(lo, len), hi) become zeros
   PG_DEV void zero(const Place<F>& p) const {

@@ -228,6 +228,15 @@ def test_scan_ragged(lens, reverse):
     scan_case(4, 700, 136, lens=[n * 17 for n in lens], reverse=reverse)
 
 
+@pytest.mark.parametrize("reverse", [0, 1])
+@pytest.mark.parametrize("f32", [0, 1])
+def test_scan_lengths_that_cut_chunks(f32, reverse):
+    """Lengths that end on, just before and just after a tile, a chunk and a run inside one."""
+    for S in (3000, 4096):
+        scan_case(6, S, 72, lens=[S, S - 1, 2049, 65, 1, 1537], reverse=reverse, f32=f32, pad=0)
+    scan_case(3, 1000, 520, lens=[513, 1000, 129], reverse=reverse, f32=f32, pad=0)
+
+
 @pytest.mark.parametrize("shape", [(1, 4099, 64), (2, 2500, 264), (1, 8200, 8), (40, 130, 256), (3, 600, 2048)])
 def test_scan_long(shape):
     scan_case(*shape, reverse=shape[0] % 2, f32=shape[0] % 2)
