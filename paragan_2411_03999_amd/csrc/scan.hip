@@ -738,14 +738,16 @@ struct Plan {
 // at the price of a pass over the inputs ahead and its launch.  Split where
 // the modelled time says so, in us: a block walks its sequence at a rate of
 // its own, the split form moves bytes at the card's.  Measured against both
-// forms of 26 shapes the choice costs at most 5 %: forward of 5 x 3000 x 1320
-// 75 whole, 64 split, of 6 x 4096 x 1536 108 and 107, of 2 x 600 x 5000 19 and
-// 29; backward of 3 x 5000 x 1000 200 and 66, of 2 x 600 x 5000 33 and 36.
+// forms of 18 shapes in each type and direction the choice costs at most 5 %.
+// Whole and split, bf16: forward of 5 x 3000 x 1320 80 and 71, of 6 x 4096 x
+// 1536 106 and 117, of 2 x 600 x 5000 19 and 30, of 1 x 20000 x 2048 483 and
+// 123; with the backward 215 and 170, 286 and 272, 55 and 68, 1296 and 283.
+// fp32, with the backward, of 6 x 4096 x 1536 417 and 602.
 bool split_pays(const Scan& a, bool bwd, int64_t rows) {
   const double n = (double)a.B * a.S * a.D;
   const double whole = 5.0 + a.S * (bwd ? a.f32 ? 0.061 : 0.045 : a.f32 ? 0.033 : 0.026);
   const double parts = bwd ? 12.0 + n * (a.f32 ? 6.2e-6 : 4.1e-6) : 8.0 + n * (a.f32 ? 4.3e-6 : 2.8e-6);
-  return rows < 256 && whole > parts;
+  return rows <= (a.f32 ? 128 : 255) && whole > parts;   // a float block of eight waves has a CU to itself
 }
 Plan plan_of(const Scan& a, bool bwd) {
   Plan p{0, 0, 0, 1, a.S};
