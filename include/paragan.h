@@ -102,8 +102,9 @@ int paragan_set_overlap_wgrad(paragan_ctx* ctx, int on);
  * the call leaves in `grads` are not clipped.  0 (the default): off, with the
  * results of before; infinity: only the norms are taken.  buf: device buffer
  * of paragan_grad_clip_size() bytes, 256-byte aligned, kept by the caller
- * while clipping is on (NULL when both are off): its first four floats are the
- * generator's last norm and factor, then the discriminator's. */
+ * until the last step called with it has run (NULL when both are off): its
+ * first four floats are the generator's last norm and factor, then the
+ * discriminator's.  A NaN in a gradient makes both of its floats NaN. */
 int paragan_grad_clip_size(size_t* bytes);
 int paragan_set_grad_clip(paragan_ctx* ctx, float max_norm_g, float max_norm_d,
                           void* buf);
@@ -399,7 +400,7 @@ int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d,
 enum { PARAGAN_NORM_RMS = 0, PARAGAN_NORM_LAYER = 1 };
 
 typedef struct {
-  int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S <= 2^30 */
+  int32_t B, S;                    /* sequences, tokens of each, >= 1; B <= 2^20, B * S <= 2^30 */
   int32_t D;                       /* width, a multiple of 8 up to 8192 */
   int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: h, y and their gradients */
   int32_t stream_dtype;            /* x, z and their gradients: dtype, or PARAGAN_F32 */
@@ -424,9 +425,9 @@ int paragan_blocknorm_fwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
 /* From the forward's inputs and saved, dz (NULL: zero; z's strides, or x's
  * without a branch) and dy (y's strides; with pre): dx (x's strides), dh
  * (h's strides; with branch) and the gradients of the rows, fp32,
- * overwritten: dgain_post, dgain_pre [D]; dgate, dscale, dshift as gate, scale and shift lie (with mod_stride 0
- * one row, the sum over all sequences).  Each of these five may be NULL: not
- * wanted. */
+ * overwritten: dgain_post, dgain_pre [D]; dgate, dscale, dshift as gate, scale
+ * and shift lie (with mod_stride 0 one row, the sum over all sequences).  Each
+ * of these five may be NULL: not wanted. */
 int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
                           const void* x, const void* h, const float* gain_post,
                           const float* gate, const float* gain_pre,
@@ -444,13 +445,13 @@ int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
  * fp32 [D], finite.  h0: the states before the first token taken, fp32
  * [B][D], or NULL for zeros; ht: those after the last, or NULL.  A sequence
  * of no tokens has ht = h0.  ht may be h0: with S = 1 that is the step of one
- * new token.  Outputs must not overlap inputs otherwise.  States and sums are fp32; the backward divides by a root no
- * smaller than 1.1e-19.  A NaN or infinity in a token reaches the tokens
+ * new token.  Outputs must not overlap inputs otherwise.  States and sums are
+ * fp32; the backward divides by a root no smaller than 1.1e-19.  A NaN or infinity in a token reaches the tokens
  * after it (in the backward those before it too) of its sequence and channel,
  * and the channel's ddecay.  A stride between tokens is below 2^20. */
 typedef struct {
   int32_t B, S;                    /* sequences, tokens of each, >= 1; B * S <= 2^30 */
-  int32_t D;                       /* channels, a multiple of 8, up to 2^20; B * D < 2^31 */
+  int32_t D;                       /* channels, a multiple of 8, up to 2^20; B * D < 2^31, B * ceil(D / 64) <= 2^22 */
   int32_t dtype;                   /* PARAGAN_BF16 or PARAGAN_F32: x, r, g, y and their gradients */
   int32_t reverse;                 /* 0 or 1 */
   float sharp;                     /* > 0, finite */

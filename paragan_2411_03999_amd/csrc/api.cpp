@@ -661,6 +661,7 @@ static bool rows_distinct(const int64_t* st, int64_t B, int64_t S, int64_t D) {
 static BlockNorm make_bn(const paragan_blocknorm_desc* d) {
   if (!d) throw Error{PARAGAN_EINVAL, "blocknorm: desc is NULL"};
   PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S <= (1LL << 30), "blocknorm: B, S must be >= 1 and B * S at most 2^30");
+  PG_CHECK(d->B <= (1 << 20), "blocknorm: B is more than 2^20");   // a block of up to 1024 threads each
   PG_CHECK(d->D >= 8 && d->D <= 8192 && d->D % 8 == 0, "blocknorm: D must be a multiple of 8 up to 8192");
   PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "blocknorm: dtype must be PARAGAN_BF16 or PARAGAN_F32");
   PG_CHECK(d->stream_dtype == PARAGAN_F32 || d->stream_dtype == d->dtype,
@@ -756,6 +757,7 @@ static Scan make_scan(const paragan_scan_desc* d) {
   PG_CHECK(d->B >= 1 && d->S >= 1 && (int64_t)d->B * d->S <= (1LL << 30), "scan: B, S must be >= 1 and B * S at most 2^30");
   PG_CHECK(d->D >= 8 && d->D <= (1 << 20) && d->D % 8 == 0 && (int64_t)d->B * d->D < (1LL << 31),
            "scan: D must be a multiple of 8 up to 2^20 and B * D below 2^31");
+  PG_CHECK(d->B * cdiv(d->D, 64) <= (1 << 22), "scan: more than 2^22 sequences of 64 channels");   // a block of up to 512 threads each
   PG_CHECK(d->dtype == PARAGAN_BF16 || d->dtype == PARAGAN_F32, "scan: dtype must be PARAGAN_BF16 or PARAGAN_F32");
   PG_CHECK(d->reverse == 0 || d->reverse == 1, "scan: reverse must be 0 or 1");
   PG_CHECK(d->sharp > 0.f && std::isfinite(d->sharp), "scan: sharp must be > 0 and finite");

@@ -108,7 +108,7 @@ def test_blocknorm_refusals(L):
     for kw in good:
         assert lib.paragan_blocknorm_check(bn(**kw)) == lib.OK, kw
     nan = float("nan")
-    bad = (dict(B=0), dict(S=0), dict(S=-1), dict(B=1 << 16, S=1 << 15), dict(B=1, S=2 ** 30 + 1), dict(D=0), dict(D=4), dict(D=60), dict(D=8200), dict(dtype=2),
+    bad = (dict(B=0), dict(S=0), dict(S=-1), dict(B=1 << 16, S=1 << 15), dict(B=1, S=2 ** 30 + 1), dict(B=2 ** 20 + 1, S=1), dict(D=0), dict(D=4), dict(D=60), dict(D=8200), dict(dtype=2),
            dict(dtype=lib.F32), dict(stream_dtype=7), dict(kind=2), dict(branch=2), dict(post=-1), dict(pre=3), dict(branch=0), dict(branch=0, post=0, pre=0),
            dict(eps=0.0), dict(eps=1e-39), dict(eps=nan), dict(eps=float("inf")), dict(res_scale=nan), dict(mod_stride=32), dict(mod_stride=100),
            dict(mod_stride=-192), dict(x_stride=(640, -64)), dict(x_stride=(640, 63)), dict(h_stride=(1 << 58, 64)), dict(z_stride=(0, 64)),
@@ -138,7 +138,7 @@ def test_scan_refusals(L):
     for kw in (dict(dtype=lib.F32), dict(reverse=1), dict(x_stride=(0, 192)), dict(r_stride=(0, 0)), dict(S=1, y_stride=(64, 0)), dict(sharp=1e-3)):
         assert lib.paragan_scan_check(sc(**kw)) == lib.OK, kw
     nan = float("nan")
-    for kw in (dict(B=0), dict(S=0), dict(B=1 << 16, S=1 << 15), dict(B=1, S=2 ** 30 + 1), dict(D=0), dict(D=12), dict(D=(1 << 20) + 8), dict(dtype=3), dict(reverse=2),
+    for kw in (dict(B=0), dict(S=0), dict(B=1 << 16, S=1 << 15), dict(B=1, S=2 ** 30 + 1), dict(B=2 ** 22 + 1, S=1), dict(D=0), dict(D=12), dict(D=(1 << 20) + 8), dict(dtype=3), dict(reverse=2),
                dict(sharp=0.0), dict(sharp=-1.0), dict(sharp=nan), dict(sharp=float("inf")), dict(y_stride=(0, 64)), dict(y_stride=(640, 56)),
                dict(x_stride=(1920, 100)), dict(g_stride=(-1920, 192)), dict(r_stride=(1 << 58, 192)), dict(B=1 << 14, D=1 << 17), dict(x_stride=(1 << 28, 1 << 20))):
         assert lib.paragan_scan_check(sc(**kw)) == lib.EINVAL, kw
@@ -217,7 +217,7 @@ def test_binding_refuses_before_the_library():
     kw = dict(kind=lib.NORM_RMS, eps=1e-6)
     for args in ((x, h, None, h, None), (x, None, None, None, None), (x, h, z(2, 5, 8), h, None), (x, h, x.float(), h, None),
                  (x, h, x, z(2, 5, 16, dt=torch.float16), None), (x, z(2, 16, 5).transpose(1, 2), x, h, None), (x, h, x, h, z(3, 16)),
-                 (x, h, x, h, z(2, 8))):
+                 (x, h, x, h, z(2, 8)), (x[0], h[0], x[0], h[0], None)):
         with pytest.raises(lib.ParaganError):
             lib.blocknorm_desc(*args, **kw)
     d = lib.blocknorm_desc(x, h, x, h, z(2, 48, dt=torch.float32)[:, 16:32], **kw)
