@@ -334,14 +334,16 @@ class Context:
     def set_grad_clip(self, max_norm_g, max_norm_d):
         """Clip the gradients of the step calls' optimisers by their norms (0: off, infinity: norms alone).  Returns a float32
         tensor of the generator's last norm and factor, then the discriminator's, or None when both are off."""
+        import torch
         n = C.c_size_t()
         _check_static(load().paragan_grad_clip_size(C.byref(n)))
         buf = workspace(n.value) if max_norm_g > 0 or max_norm_d > 0 else None
         self.check(load().paragan_set_grad_clip(self.h, max_norm_g, max_norm_d, _ptr(buf)))
+        if getattr(self, "_clip_buf", None) is not None:      # steps under way, on any stream, write to the one before
+            torch.cuda.synchronize()
         self._clip_buf = buf                                  # the library writes there while clipping is on
         if buf is None:
             return None
-        import torch
         buf[:16].zero_()
         torch.cuda.current_stream().synchronize()             # ahead of steps on any stream
         return buf[:16].view(torch.float32)
@@ -589,6 +591,8 @@ def blocknorm_desc(x, h, z, y, mod=None, *, kind, post=0, eps, res_scale=1.0):
     """BlockNormDesc of x, z (the stream) and h, y (a block's output, the next one's input), [B][S][D] tensors or views of any
     strides (the last dimension contiguous); h and z None: no branch; y None: no norm after it.  mod: any of gate, scale and
     shift, which lie alike: [B][D], rows of any stride, or [1][D] or [D] for one row that all sequences share (also None)."""
+    if x.dim() != 3:
+        raise ParaganError(EINVAL, "blocknorm: x must be [B][S][D]")
     B, S, D = x.shape
     if (h is None) != (z is None):
         raise ParaganError(EINVAL, "blocknorm: h and z belong together")
@@ -652,7 +656,7 @@ def paragan_blocknorm_bwd(ctx, desc, x, h, gain_post, gate, gain_pre, scale, shi
 def scan_desc(x, r, g, y, *, sharp, reverse=0):
     """ScanDesc of x, r, g, y [B][S][D], tensors or views of any strides (the last dimension contiguous)."""
     for t in (x, r, g, y):
-        if tuple(t.shape) != tuple(x.shape) or t.dtype != x.dtype or t.dim() != 3 or t.stride(2) != 1:
+        if tuple(t.shape) != tuple(x.shape) or t.dtype != x.dtype or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
             raise ParaganError(EINVAL, "scan: x, r, g and y differ in shape or type, or the last dimension is not contiguous")
     return ScanDesc(*x.shape, _token_dtype("scan", x), int(reverse), sharp, *(_token_stride(t) for t in (x, r, g, y)))
 

@@ -144,3 +144,6 @@ def test_clip_settings_are_checked():
     for bad in (None, buf[1:]):
         assert lib.load().paragan_set_grad_clip(ctx.h, 1.0, 0.0, None if bad is None else C.c_void_p(bad.data_ptr())) == lib.EINVAL
     assert ctx.set_grad_clip(0.0, 0.0) is None
+    first, second = ctx.set_grad_clip(1.0, 0.0), ctx.set_grad_clip(2.0, math.inf)
+    assert first.data_ptr() != second.data_ptr() and not second.any()
+    assert ctx.set_grad_clip(0.0, 0.0) is None

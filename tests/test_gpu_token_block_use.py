@@ -358,6 +358,9 @@ def test_refused_calls_touch_nothing():
         args[i] = bad
         with pytest.raises(lib.ParaganError):
             lib.paragan_blocknorm_bwd(ctx, d, *args)
+    shared = lib.blocknorm_desc(x, h, zo, y, rows[:1].expand(2, 32), kind=lib.NORM_RMS, eps=EPS)   # one row: given as one
+    with pytest.raises(lib.ParaganError):
+        lib.paragan_blocknorm_fwd(ctx, shared, x, h, None, rows[:1].expand(2, 32), None, None, None, None, zo, y, None)
     d0 = lib.blocknorm_desc(x, None, None, y, kind=lib.NORM_RMS, eps=EPS)
     for args in ([x, None, None, None, None, None, None, None, saved, None, None, grads[0]] + [None] * 6 + [ws],
                  [x, None, None, None, None, None, None, None, saved, None, y, grads[0], None, grads[2]] + [None] * 4 + [ws]):
