@@ -461,9 +461,9 @@ typedef struct {
 int paragan_scan_check(const paragan_scan_desc* d);
 /* saved: kept from a forward to its backward; ws: scratch of either call. */
 int paragan_scan_sizes(const paragan_scan_desc* d, size_t* saved_bytes, size_t* ws_bytes);
-/* saved may be NULL when no backward follows.  x, r, g may repeat through
- * zero strides in the forward; y, and in the backward x, r and g (whose
- * strides dx, dr and dg share), must not overlap themselves. */
+/* saved may be NULL when no backward follows.  Rows of x, r, g may overlap or
+ * repeat (strides from 0 up) in the forward; y, and in the backward x, r and g
+ * (whose strides dx, dr and dg share), must not overlap themselves. */
 int paragan_scan_fwd(paragan_ctx* ctx, const paragan_scan_desc* d, const void* x,
                      const void* r, const void* g, const float* decay,
                      const int32_t* len, const float* h0, void* y, float* ht,

@@ -301,26 +301,28 @@ PG_DEV void buf_store(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t so, float
   else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, (int)off, (int)so, 0);
 }
 
-// A tensor's tokens as a lane takes them: `run` tokens in memory from mseg * run on.
-template <typename F>
+// A tensor's tokens as a lane takes them: `run` tokens in memory from mseg * run on.  OVER: they may overlap or repeat (the
+// forward's inputs; where none may, the backward of 8 x 4096 x 2048 is 5 us faster without).
+template <typename F, bool OVER = false>
 struct Tokens {
   typedef typename F::T T;
   const char* base;                // the sequence
-  int64_t st;                      // bytes between tokens
+  int64_t st, over = 0;            // bytes between tokens; by how much a token reaches into the next one
   uint32_t lane;
-  PG_DEV Tokens(const void* p, const int64_t* s, const Place<F>& q, int run = F::TOK) {
+  PG_DEV Tokens(const void* p, const int64_t* s, const Place<F>& q, int D = 0, int run = F::TOK) {
     base = (const char*)p + q.b * s[0] * (int64_t)sizeof(T);
     st = s[1] * (int64_t)sizeof(T);
+    if constexpr (OVER) over = max((int64_t)0, D * (int64_t)sizeof(T) - st);
     lane = q.ok ? (uint32_t)q.mseg * (uint32_t)run * (uint32_t)st + (uint32_t)q.c * (uint32_t)sizeof(T) : kOOB;
   }
-  // bytes from token m on, all of one row where tokens repeat
+  // bytes from token m on, to the end of the last one's row where tokens overlap or repeat
   PG_DEV uint32_t bytes(int m, int len) const {
-    const int64_t n = (int64_t)(len - m) * st;
-    return (uint32_t)(st == 0 || n > kBufMax ? kBufMax : n < 0 ? 0 : n);
+    const int64_t n = (int64_t)(len - m) * st + (OVER && len > m ? over : 0);
+    return (uint32_t)(n > kBufMax ? kBufMax : n < 0 ? 0 : n);
   }
   PG_DEV uint32_t place(int j, int reverse) const { return (uint32_t)(reverse ? F::TOK - 1 - j : j) * (uint32_t)st; }
   // The range check takes the uniform offset from the descriptor's bytes, so
-  // that offset stops there: past the length no lane's is below what is left.
+  // that offset stops there: at them no lane's is below what is left.
   PG_DEV void load(Two<T>* v, int m, int len, int reverse, uint32_t so = 0) const {
     const uint32_t n = bytes(m, len);
     const __amdgpu_buffer_rsrc_t r = make_rsrc(base + m * st, n);
@@ -339,14 +341,15 @@ struct Tokens {
       if (p.ok) st2f((T*)(const_cast<char*>(base) + t * st) + p.c, 0.f, 0.f);
   }
 };
-// tokens from m on (of this lane) past the length never come in (x: where tokens repeat, it was read all the same)
-template <typename F>
-PG_DEV void past(Two<typename F::T>* r, Two<typename F::T>* x, int m, int len, int reverse) {
+// tokens from m on (of this lane) past the length never come in (the others: where tokens overlap or repeat, what real ones
+// own was read all the same)
+template <typename F, typename... Others>
+PG_DEV void past(int m, int len, int reverse, Two<typename F::T>* r, Others... others) {
 #pragma unroll
   for (int j = 0; j < F::TOK; ++j)
     if (m + (reverse ? F::TOK - 1 - j : j) >= len) {
       r[j] = never<typename F::T>();
-      x[j] = Two<typename F::T>{};
+      ((others[j] = Two<typename F::T>{}), ...);
     }
 }
 
@@ -394,7 +397,8 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
   __shared__ float4 sh[2][NW][CL];
   const Place<F> p(a);
   if (p.b >= a.B) return;
-  const Tokens<F> x(a.x, a.xs, p), r(a.r, a.rs, p), g(a.g, a.gs, p), y(a.y, a.ys, p);
+  const Tokens<F, true> x(a.x, a.xs, p, a.D), r(a.r, a.rs, p, a.D), g(a.g, a.gs, p, a.D);
+  const Tokens<F> y(a.y, a.ys, p);
   const int64_t o = (int64_t)p.b * a.D + p.cc;
   const float2 k = rates(a, p.cc);
   float2 h = !SPLIT && a.h0 ? *reinterpret_cast<const float2*>(a.h0 + o) : make_float2(0.f, 0.f);
@@ -418,7 +422,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_fwd(ScArgs a) {
   int turn = 0;
   for (int t = 0; t < p.n; ++t, turn ^= 1) {
     const int m0 = p.tile(t, a.reverse), mine = m0 + p.mseg * TOK;
-    if (m0 + F::TT > p.len) past<F>(R, X, mine, p.len, a.reverse);
+    if (m0 + F::TT > p.len) past<F>(mine, p.len, a.reverse, R, G, X);
     float2 av[TOK], uv[TOK], A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
 #pragma unroll
     for (int j = 0; j < TOK; ++j) {
@@ -468,7 +472,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
     return;
   }
   const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;   // a chunk is whole tiles
-  const Tokens<F> x(a.x, a.xs, p, run), r(a.r, a.rs, p, run), g(a.g, a.gs, p, run);
+  const Tokens<F, true> x(a.x, a.xs, p, a.D, run), r(a.r, a.rs, p, a.D, run), g(a.g, a.gs, p, a.D, run);
   const float2 k = rates(a, p.cc);
   float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
   Two<T> X[TOK], R[TOK], G[TOK];
@@ -482,7 +486,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_maps(ScArgs a) {
     load(0);
     for (int i = 0; i < run; i += TOK) {
       float2 av[TOK], uv[TOK];
-      if (p.lo + a.chunk > p.len) past<F>(R, X, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
+      if (p.lo + a.chunk > p.len) past<F>(m + (a.reverse ? run - TOK - i : i), p.len, a.reverse, R, G, X);
 #pragma unroll
       for (int j = 0; j < TOK; ++j) {
         const float2 xx = X[j].get(), rr = R[j].get(), gg = G[j].get();
@@ -562,7 +566,7 @@ __global__ __launch_bounds__(F::NW * 64, 2) void k_scan_bwd(ScArgs a) {
   double sum0 = 0.0, sum1 = 0.0;
   for (int t = p.n - 1; t >= 0; --t, turn ^= 1) {
     const int m0 = p.tile(t, a.reverse);
-    if (m0 + F::TT > p.len) past<F>(R, X, m0 + p.mseg * TOK, p.len, a.reverse);
+    if (m0 + F::TT > p.len) past<F>(m0 + p.mseg * TOK, p.len, a.reverse, R, X);
     Grad e0[TOK], e1[TOK];
     float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f), C = make_float2(0.f, 0.f);
 #pragma unroll
@@ -663,7 +667,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
     return;
   }
   const int run = a.chunk / F::NSEG, m = p.lo + p.mseg * run;
-  const Tokens<F> r(a.r, a.rs, p, run), dy(a.dy, a.ys, p, run);
+  const Tokens<F> r(a.r, a.rs, p, 0, run), dy(a.dy, a.ys, p, 0, run);
   const float2 k = rates(a, p.cc);
   float2 A = make_float2(1.f, 1.f), H = make_float2(0.f, 0.f);
   Two<T> R[TOK], Y[TOK];
@@ -676,7 +680,7 @@ __global__ __launch_bounds__(F::NW * 64, 4) void k_scan_back_maps(ScArgs a) {
     load(run - TOK);
     for (int i = run - TOK; i >= 0; i -= TOK) {
       float2 av[TOK], d[TOK];
-      if (p.lo + a.chunk > p.len) past<F>(R, Y, m + (a.reverse ? run - TOK - i : i), p.len, a.reverse);
+      if (p.lo + a.chunk > p.len) past<F>(m + (a.reverse ? run - TOK - i : i), p.len, a.reverse, R, Y);
 #pragma unroll
       for (int j = 0; j < TOK; ++j) {
         const float2 rr = R[j].get();
