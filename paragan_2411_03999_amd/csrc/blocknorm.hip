@@ -271,10 +271,10 @@ __global__ __launch_bounds__(THREADS) void k_blocknorm_bwd(BnArgs a) {
     zr.get(dZ);
     yr.get(dv);
     if (rr + NG < r1) fetch(rr + NG + grp);
-    if (r >= rl) {                 // no token: zeros throughout
+    if (r >= rl) {                 // no token, nor any after it: zeros throughout, the condition's rows (which may not be finite) too
       st = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) n[e] = hn[e] = dZ[e] = dv[e] = 0.f;
+      for (int e = 0; e < 8; ++e) n[e] = hn[e] = dZ[e] = dv[e] = k[e] = m[e] = 0.f;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -339,6 +339,7 @@ constexpr int kAhead = 16;         // items of a lane whose loads are under way 
 struct BnJoin {
   BlockNormRows w;
   BlockNormGrads g;
+  const int32_t* len;
   const float* part;
   int64_t mod;
   int B, D, nc, gs;                // gs: lanes that share a sequence's items, a power of two
@@ -348,7 +349,8 @@ struct BnJoin {
 // The rows' gradients from the items' sums, in 64 bits and in order: 16
 // columns x 64 lanes a block.  Lanes take sequences; where these are fewer, gs
 // lanes share the items of one.  What all sequences share is summed over the
-// lanes at the end.
+// lanes at the end.  A sequence of no tokens adds nothing, whatever its rows
+// hold: zero times what is not finite would be NaN.
 __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
   __shared__ double sh[5][64][17];
   const int j = threadIdx.x & 15, l = threadIdx.x >> 4, c = blockIdx.x * 16 + j, cc = min(c, a.D - 1);
@@ -359,13 +361,16 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
   auto weight = [&](const float* w, int b, double none) { return w ? (double)w[b * a.mod + cc] : none; };
   auto done = [&](int b, double e, double q, double p, double scale, double gate) {
     const int64_t o = b * a.mod + cc;
-    t[0] += e; t[1] += q; t[2] += p;
-    t[3] += (1.0 + scale) * q;
-    t[4] += gate * p;
+    const bool some = !a.len || a.len[b] > 0;
+    if (some) {
+      t[0] += e; t[1] += q; t[2] += p;
+      t[3] += (1.0 + scale) * q;
+      t[4] += gate * p;
+    }
     if (a.mod && c < a.D) {
-      if (a.g.shift) a.g.shift[o] = (float)e;
-      if (a.g.scale) a.g.scale[o] = (float)(g2 * q);
-      if (a.g.gate) a.g.gate[o] = (float)(rs * g1 * p);
+      if (a.g.shift) a.g.shift[o] = some ? (float)e : 0.f;
+      if (a.g.scale) a.g.scale[o] = some ? (float)(g2 * q) : 0.f;
+      if (a.g.gate) a.g.gate[o] = some ? (float)(rs * g1 * p) : 0.f;
     }
   };
   double s[3] = {0.0, 0.0, 0.0}, scale = 0.0, gate = 0.0;
@@ -516,7 +521,7 @@ void blocknorm_bwd(hipStream_t st, const BlockNorm& a, const BlockNormRows& w, c
     int gs = 64;
     while (gs > 1 && 64 / gs < a.B) gs /= 2;
     hipLaunchKernelGGL(k_blocknorm_join, dim3((unsigned)cdiv(a.D, 16)), dim3(1024), 0, st,
-                       BnJoin{w, gr, g.part, a.mod, a.B, a.D, g.nc, gs, a.res_scale});
+                       BnJoin{w, gr, len, g.part, a.mod, a.B, a.D, g.nc, gs, a.res_scale});
     PG_LAUNCH_CHECK();
   }
   const double one = (a.res32 ? 4.0 : 2.0) * (1 + (dz ? 1 : 0) + a.pre) + (a.f32 ? 4.0 : 2.0) * (2 * a.branch + a.pre);

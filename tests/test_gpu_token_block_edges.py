@@ -80,3 +80,76 @@ def test_scan_windows_keep_nan_in_their_channels(S, reverse):
         y, ht = run()
         assert np.array_equal(np.isnan(num(y.v)), want), (which, "y")
         assert np.array_equal(np.isnan(num(ht)), np.stack([after[-1], np.zeros(D, bool)])), (which, "ht")
+
+
+# ------------------------------------------------------------- block norm: rows that no token uses
+def norm_of(torch, B, S, D, lens, gate, sc, sh, *, layer, post, f32=0, gains=True, given_post=None, shared=0, seed=0):
+    """Backward of a block norm with every row given; its outputs and the definition's with rows of sequences without tokens as
+    zeros there.  given_post: gain_post goes in whether or not the descriptor uses it."""
+    gen = torch.Generator().manual_seed(seed + B + S + D)
+    dt = torch.float32 if f32 else torch.bfloat16
+    mk = lambda: Rows(torch, B, S, D, dt).set(torch.randn(B, S, D, generator=gen).to(dt), lens)  # noqa: E731
+    x, h, DZ, DY = (mk() for _ in range(4))
+    g1, g2 = (1 + 0.2 * torch.randn(D, generator=gen).cuda() for _ in range(2))
+    g1 = g1 if gains and (post if given_post is None else given_post) else None
+    g2 = g2 if gains else None
+    z, y, dx, dh = (Rows(torch, B, S, D, dt, fill=7.0) for _ in range(4))
+    desc = lib.blocknorm_desc(x.v, h.v, z.v, y.v, gate, kind=layer, post=post, eps=1e-5, res_scale=0.75)
+    sb, wb = lib.paragan_blocknorm_sizes(desc)
+    saved, ws = lib.workspace(sb), lib.workspace(wb)
+    saved.fill_(255), ws.fill_(255)
+    L = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ctx = lib.Context()
+    rows = (g1, gate, g2, sc, sh)
+    lib.paragan_blocknorm_fwd(ctx, desc, x.v, h.v, *rows, L, z.v, y.v, saved)
+    vec, dmod = torch.full((2, D), 7.0, device="cuda"), torch.full((gate.shape[0], 3 * D), 7.0, device="cuda")   # as the rows lie
+    grads = [vec[0] if post else None, dmod[:, :D], vec[1], dmod[:, D:2 * D], dmod[:, 2 * D:]]
+    lib.paragan_blocknorm_bwd(ctx, desc, x.v, h.v, *rows, L, saved, DZ.v, DY.v, dx.v, dh.v, *grads, ws)
+    torch.cuda.synchronize()
+    clean = lambda r: np.nan_to_num(num(r.v))  # noqa: E731
+    some = np.ones((1, 1), bool) if shared else (np.asarray(lens) > 0)[:, None]
+    row = lambda t: np.where(some, num(t), 0.0)  # noqa: E731
+    un = lambda t: None if t is None else num(t)  # noqa: E731
+    want = T.blocknorm(clean(x), clean(h), un(g1) if post else None, row(gate), un(g2), row(sc), row(sh), lens, layer=layer, branch=1,
+                       post=post, pre=1, eps=float(np.float32(1e-5)), res_scale=0.75, shared=shared, dz=clean(DZ), dy=clean(DY),
+                       uz=U32 if f32 else U16, uy=U32 if f32 else U16)
+    got = dict(z=z.v, y=y.v, dx=dx.v, dh=dh.v, dgain_post=grads[0], dgate=grads[1], dgain_pre=grads[2], dscale=grads[3], dshift=grads[4])
+    return got, want
+
+
+def hold_all(got, want):
+    for name, t in got.items():
+        if t is not None:
+            held(name, t, want[name], want["tol." + name] + 1e-30)
+
+
+@pytest.mark.parametrize("D", [8, 72, 264, 520, 1152, 4104])
+@pytest.mark.parametrize("layer,post", [(0, 0), (1, 0), (0, 1), (1, 1)])
+def test_blocknorm_rows_of_empty_sequences(layer, post, D):
+    """Rows of the condition of sequences without tokens are not finite: zeros there, and nothing of them in any sum."""
+    torch = need_gpu()
+    for lens in ([7, 0, 3, 0], [0, 0], [5, 0] * 40):
+        B = len(lens)
+        gen = torch.Generator().manual_seed(D + B)
+        mod = 0.5 * torch.randn(B, 3 * D, generator=gen).cuda()
+        for b, n in enumerate(lens):
+            if n == 0:
+                mod[b] = (float("nan"), float("inf"), -float("inf"))[b % 3]
+        hold_all(*norm_of(torch, B, 7, D, lens, mod[:, :D], mod[:, D:2 * D], mod[:, 2 * D:], layer=layer, post=post))
+
+
+@pytest.mark.parametrize("D", [72, 520, 4104])
+@pytest.mark.parametrize("layer,post", [(0, 0), (1, 1)])
+def test_blocknorm_padding_stays_zero(layer, post, D):
+    """Rows past a length are zeros in every output where a row of the condition is not finite."""
+    torch = need_gpu()
+    lens = [3, 7, 1]
+    for bad in (float("nan"), float("inf")):
+        for at in range(3):
+            mod = torch.ones(3, 3 * D, device="cuda")
+            mod[:, at * D + D // 2] = bad
+            with np.errstate(invalid="ignore", over="ignore"):     # the definition's are not compared
+                got, _ = norm_of(torch, 3, 7, D, lens, mod[:, :D], mod[:, D:2 * D], mod[:, 2 * D:], layer=layer, post=post)
+            for name in ("z", "y", "dx", "dh"):
+                for b, n in enumerate(lens):
+                    assert bool((got[name][b, n:] == 0).all()), (name, b, at, bad)
