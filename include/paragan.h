@@ -391,8 +391,9 @@ int paragan_mha_bwd(paragan_ctx* ctx, const paragan_mha_desc* d,
  * rows of D, mod_stride elements from one sequence's to the next one's (views
  * of one projection of the condition, for instance), or 0 for one row that
  * all sequences share (a norm's bias, a learned gate).  Each may be NULL: a
- * gain or gate of ones, a scale or shift of zeros.  Statistics and sums are
- * fp32 (sums over tokens are joined in 64 bits).
+ * gain or gate of ones, a scale or shift of zeros; those of a part that the
+ * descriptor leaves out (gain_post without post, for instance) are not used.
+ * Statistics and sums are fp32 (sums over tokens are joined in 64 bits).
  * Element (b, s, c) of a tensor is at b * stride[0] + s * stride[1] + c.
  * z may be x and y may be h (same pointer and strides) where no backward
  * follows, which reads x and h; outputs must not overlap inputs otherwise.

@@ -687,13 +687,15 @@ static BlockNorm make_bn(const paragan_blocknorm_desc* d) {
   PG_CHECK(!a.pre || rows_distinct(a.ys, a.B, a.S, a.D), "blocknorm: y overlaps itself");
   return a;
 }
-static BlockNormRows bn_rows(const float* gain_post, const float* gate, const float* gain_pre, const float* scale,
-                             const float* shift) {
+// The rows that the descriptor uses: the others are not read, nor do they enter any gradient
+static BlockNormRows bn_rows(const BlockNorm& a, const float* gain_post, const float* gate, const float* gain_pre,
+                             const float* scale, const float* shift) {
   const float* p[5] = {gain_post, gate, gain_pre, scale, shift};
   const char* n[5] = {"gain_post", "gate", "gain_pre", "scale", "shift"};
   for (int i = 0; i < 5; ++i)
     if (p[i]) need16(p[i], n[i]);
-  return BlockNormRows{gain_post, gate, gain_pre, scale, shift};
+  return BlockNormRows{a.post ? gain_post : nullptr, a.branch ? gate : nullptr, a.pre ? gain_pre : nullptr,
+                       a.pre ? scale : nullptr, a.pre ? shift : nullptr};
 }
 
 extern "C" int paragan_blocknorm_check(const paragan_blocknorm_desc* d) { PG_TRY(nullptr, make_bn(d)) }
@@ -714,7 +716,7 @@ extern "C" int paragan_blocknorm_fwd(paragan_ctx* ctx, const paragan_blocknorm_d
   ProfBind pb(ctx);
   PG_TRY(ctx, {
     const BlockNorm a = make_bn(d);
-    const BlockNormRows w = bn_rows(gain_post, gate, gain_pre, scale, shift);
+    const BlockNormRows w = bn_rows(a, gain_post, gate, gain_pre, scale, shift);
     need16(x, "x");
     if (a.branch) { need16(h, "h"); need16(z, "z"); }
     if (a.pre) need16(y, "y");
@@ -733,7 +735,7 @@ extern "C" int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_d
   ProfBind pb(ctx);
   PG_TRY(ctx, {
     const BlockNorm a = make_bn(d);
-    const BlockNormRows w = bn_rows(gain_post, gate, gain_pre, scale, shift);
+    const BlockNormRows w = bn_rows(a, gain_post, gate, gain_pre, scale, shift);
     PG_CHECK(rows_distinct(a.xs, a.B, a.S, a.D) && (!a.branch || rows_distinct(a.hs, a.B, a.S, a.D)),
              "blocknorm_bwd: x or h overlaps itself (dx and dh share their strides)");
     need16(x, "x"); need16(dx, "dx");

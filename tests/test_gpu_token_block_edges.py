@@ -153,3 +153,19 @@ def test_blocknorm_padding_stays_zero(layer, post, D):
             for name in ("z", "y", "dx", "dh"):
                 for b, n in enumerate(lens):
                     assert bool((got[name][b, n:] == 0).all()), (name, b, at, bad)
+
+
+@pytest.mark.parametrize("shared", [0, 1])
+@pytest.mark.parametrize("D", [72, 1152])
+def test_blocknorm_gain_that_is_not_used(D, shared):
+    """gain_post given without post changes nothing."""
+    torch = need_gpu()
+    lens = [6, 2, 7]
+    mod = 0.5 * torch.randn(1 if shared else 3, 3 * D, generator=torch.Generator().manual_seed(D)).cuda()
+    part = [mod[:, i * D:(i + 1) * D] for i in range(3)]
+    runs = []
+    for given in (1, 0):
+        got, want = norm_of(torch, 3, 7, D, lens, *part, layer=0, post=0, given_post=given, shared=shared)
+        hold_all(got, want)
+        runs.append(got)
+    assert all(torch.equal(runs[0][k], runs[1][k]) for k in got if got[k] is not None)
