@@ -443,7 +443,8 @@ int paragan_blocknorm_bwd(paragan_ctx* ctx, const paragan_blocknorm_desc* d,
  *   h_t = a_t h_{t-1} + (1 - a_t^2)^(1/2) * sigmoid(g_t) * x_t,   y_t = h_t,
  * over the tokens of a sequence from the first to the last, or with reverse
  * from the last to the first.  x, r, g are the program's projections; decay:
- * fp32 [D], finite.  h0: the states before the first token taken, fp32
+ * fp32 [D], finite (where sharp * softplus(decay) is past 2.3e38 it counts as
+ * that).  h0: the states before the first token taken, fp32
  * [B][D], or NULL for zeros; ht: those after the last, or NULL.  A sequence
  * of no tokens has ht = h0.  ht may be h0: with S = 1 that is the step of one
  * new token.  Outputs must not overlap inputs otherwise.  States and sums are

@@ -23,6 +23,8 @@
 // and backward 402 us where these took 121 and 265.
 #include "token.hpp"
 
+#include <cfloat>
+
 namespace pg {
 
 namespace {
@@ -71,10 +73,15 @@ PG_DEV void sigmoid(float v, float& s, float& c) {
 PG_DEV float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -kLog2e)); }
 // softplus(v) = log(1 + e^v)
 PG_DEV float softplus(float v) { return log1pf(expf(-fabsf(v))) + fmaxf(v, 0.f); }
-// -sharp softplus(decay) / ln 2 of two channels
+// -sharp softplus(decay) / ln 2 of two channels; past the largest float that
+// one, since an infinity times a closed gate's zero would be NaN (a NaN stays)
+PG_DEV float rate(float sharp, float decay) {
+  const float k = -sharp * softplus(decay) * kLog2e;
+  return k < -FLT_MAX ? -FLT_MAX : k;
+}
 PG_DEV float2 rates(const ScArgs& a, int c) {
   const float2 d = *reinterpret_cast<const float2*>(a.decay + c);
-  return make_float2(-a.sharp * softplus(d.x) * kLog2e, -a.sharp * softplus(d.y) * kLog2e);
+  return make_float2(rate(a.sharp, d.x), rate(a.sharp, d.y));
 }
 
 // a = 2^l and p = 1 - a^2 for l = la / ln 2 <= 0.  Where the difference would

@@ -169,3 +169,63 @@ def test_blocknorm_gain_that_is_not_used(D, shared):
         hold_all(got, want)
         runs.append(got)
     assert all(torch.equal(runs[0][k], runs[1][k]) for k in got if got[k] is not None)
+
+
+# ------------------------------------------------------------- recurrence: rates past the largest float
+@pytest.mark.parametrize("reverse", [0, 1])
+@pytest.mark.parametrize("S,f32", [(12, 0), (40, 0), (40, 1), (300, 0), (1000, 0), (1000, 1)])
+def test_scan_rates_past_the_largest_float(S, f32, reverse):
+    """sharp times softplus(decay) overflows: every token forgets what was before it, a token whose gate is closed to the last
+    bit keeps it, and what is past a length does neither."""
+    torch = need_gpu()
+    B, D, closed = 3, 72, 4
+    lens = [S, 0, S - 7]
+    gen = torch.Generator().manual_seed(S)
+    dt, uo = (torch.float32, U32) if f32 else (torch.bfloat16, U16)
+    x, r, g, dy = (torch.randn(B, S, D, generator=gen).to(dt).cuda() for _ in range(4))
+    r[:, closed] = -200.0                                 # its sigmoid is zero in fp32
+    dec, h0, dht = torch.full((D,), 1e38, device="cuda"), torch.randn(B, D, generator=gen).cuda(), torch.randn(B, D, generator=gen).cuda()
+    for b, n in enumerate(lens):
+        for t in (x, r, g, dy):
+            t[b, n:] = float("nan")
+    y, (dx, dr, dg) = torch.full_like(x, 7.0), (torch.full_like(x, 7.0) for _ in range(3))
+    ht, dh0, ddec = torch.empty(B, D, device="cuda"), torch.empty(B, D, device="cuda"), torch.empty(D, device="cuda")
+    d = lib.scan_desc(x, r, g, y, sharp=8.0, reverse=reverse)
+    saved, ws = (lib.workspace(n) for n in lib.paragan_scan_sizes(d))
+    L = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ctx = lib.Context()
+    lib.paragan_scan_fwd(ctx, d, x, r, g, dec, L, h0, y, ht, saved, ws)
+    lib.paragan_scan_bwd(ctx, d, x, r, g, dec, L, saved, dy, dht, dx, dr, dg, ddec, dh0, ws)
+    torch.cuda.synchronize()
+    # decays are zero and roots one, or the other way round: y = sigmoid(g) x, or the y before
+    wy, wdx, wdg, wht, wdh0 = (np.zeros(s) for s in ((B, S, D),) * 3 + ((B, D),) * 2)
+    ey, edx, edg = (np.zeros((B, S, D)) for _ in range(3))
+    for b, n in enumerate(lens):
+        at = list(range(n))[::-1] if reverse else list(range(n))
+        sg = 1 / (1 + np.exp(-np.nan_to_num(num(g[b]))))
+        rel = U32 * (2 * np.abs(np.nan_to_num(num(g[b]))) + 20)     # of the sigmoid, the root and the products
+        X, dY, cur = num(x[b]), num(dy[b]), num(h0[b])
+        back, mag = num(dht[b]), np.abs(num(dht[b]))
+        for t in at:
+            if t != closed:
+                cur = sg[t] * X[t]
+            wy[b, t] = cur
+            ey[b, t] = np.abs(cur) * (uo + rel[t] + rel[at[at.index(t) - 1]])
+        for t in at[::-1]:
+            E, mag = dY[t] + back, np.abs(dY[t]) + mag
+            if t == closed:
+                back = E
+                continue
+            wdx[b, t], wdg[b, t] = E * sg[t], E * sg[t] * X[t] * (1 - sg[t])
+            edx[b, t] = uo * np.abs(wdx[b, t]) + sg[t] * (np.abs(E) * rel[t] + 8 * U32 * mag)
+            edg[b, t] = uo * np.abs(wdg[b, t]) + np.abs(X[t]) * sg[t] * (1 - sg[t]) * (np.abs(E) * 2 * rel[t] + 8 * U32 * mag)
+            back, mag = np.zeros(D), np.zeros(D)
+        wht[b], wdh0[b] = cur, back
+    # a closed token's root: 1.1e-19 at most where the backward divides by it
+    held("y", y, wy, ey + 1e-18)
+    held("ht", ht, wht, np.abs(wht) * 64 * U32 + 1e-18)
+    held("dx", dx, wdx, edx + 1e-17)
+    held("dg", dg, wdg, edg + 1e-17)
+    held("dh0", dh0, wdh0, np.abs(wdh0) * 4 * U32 + 1e-30)
+    held("dr", dr, np.zeros((B, S, D)), np.full((B, S, D), 1e-30))
+    held("ddecay", ddec, np.zeros(D), np.full(D, 1e-30))
