@@ -1,4 +1,5 @@
-"""Calls at the edges of what the token block's operators accept."""
+"""Calls at the edges of what the token block's operators accept, and the
+forms that large batches and large gradients take."""
 import numpy as np
 import pytest
 
@@ -7,7 +8,7 @@ from paragan_2411_03999_amd import lib
 
 from .parity import need_gpu
 from .test_gpu_token import held
-from .test_gpu_token_block import Rows, num
+from .test_gpu_token_block import Rows, num, scan_case
 
 pytestmark = pytest.mark.gpu
 
@@ -229,3 +230,75 @@ def test_scan_rates_past_the_largest_float(S, f32, reverse):
     held("dh0", dh0, wdh0, np.abs(wdh0) * 4 * U32 + 1e-30)
     held("dr", dr, np.zeros((B, S, D)), np.full((B, S, D), 1e-30))
     held("ddecay", ddec, np.zeros(D), np.full(D, 1e-30))
+
+
+# ------------------------------------------------------------- recurrence: the forms that large batches take
+def form_of(B, S, D, f32, reverse):
+    """(tokens between kept states, chunks of the backward) of contiguous tensors, by the sizes that the library asks for."""
+    two = lib.C.c_int64 * 2
+    d = lib.ScanDesc(B, S, D, lib.F32 if f32 else lib.BF16, reverse, 8.0, two(S * 3 * D, 3 * D), two(S * 3 * D, 3 * D), two(S * 3 * D, 3 * D),
+                     two(S * D, D))
+    sb, wb = lib.paragan_scan_sizes(d)
+    step = next(s for s in (16, 64) if sb == -(-B * -(-S // s) * D * 4 // 256) * 256)
+    return step, wb // (16 * B * D)               # 8 bytes of maps and 8 of sums a chunk, sequence and channel
+
+
+SEQ = [(2060, 40, 64), (70, 33, 2048), (33, 48, 4096)]
+WHOLE = [(5, 400, 3336, 0), (3, 400, 2824, 1), (260, 257, 64, 0), (8, 200, 4104, 0), (520, 130, 40, 0)]
+
+
+@pytest.mark.parametrize("reverse", [0, 1])
+@pytest.mark.parametrize("shape", SEQ)
+def test_scan_a_thread_a_sequence_of_many_tokens(shape, reverse):
+    """Several kept states a sequence, the last group of tokens not full."""
+    need_gpu()
+    B, S, D = shape
+    assert form_of(B, S, D, 0, reverse) == (16, 1)
+    lens = [(S, 0, 1, 16, 17, S - 1, 32)[b % 7] for b in range(B)]
+    scan_case(B, S, D, reverse=reverse, lens=lens)
+    if B < 100:
+        scan_case(B, S, D, reverse=reverse, f32=1)
+
+
+@pytest.mark.parametrize("reverse", [0, 1])
+@pytest.mark.parametrize("shape", WHOLE)
+def test_scan_undivided_of_several_tiles(shape, reverse):
+    """Sequences of three and more tiles that are not split, lengths on and beside the tiles' ends."""
+    need_gpu()
+    B, S, D, f32 = shape
+    assert form_of(B, S, D, f32, reverse) == (64, 1)
+    scan_case(B, S, D, f32=f32, reverse=reverse)
+    scan_case(B, S, D, f32=f32, reverse=reverse, lens=[(S, 0, 129, 128, S - 1, 64, 63, 1)[b % 8] for b in range(B)], state=0, pad=0)
+
+
+@pytest.mark.parametrize("reverse", [0, 1])
+@pytest.mark.parametrize("B,S", [(2, 900), (1, 1000)])   # undivided, the second sequence past 4 GB; two chunks, for their bytes alone
+def test_scan_far_tokens_of_many_channels(B, S, reverse):
+    """fp32 tokens 4 MB apart where the slabs alone would not be split."""
+    torch = need_gpu()
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    D, ts = 8200, (1 << 20) - 8
+    gen = torch.Generator().manual_seed(9)
+    small = [torch.randn(B, S, D, generator=gen) for _ in range(4)]
+    big, out = (torch.zeros(B * S * ts, device="cuda") for _ in range(2))
+    view = lambda t, i: t.as_strided((B, S, D), (S * ts, ts, 1), i * 8200)  # noqa: E731
+    x, r, g, dy = (view(big, i) for i in range(4))
+    for v, t in zip((x, r, g, dy), small):
+        v.copy_(t)
+    y, dx, dr, dg = (view(out, i) for i in range(4))
+    dec = (torch.rand(D, generator=gen) * 5 - 8).cuda()
+    d = lib.scan_desc(x, r, g, y, sharp=8.0, reverse=reverse)
+    sb, wb = lib.paragan_scan_sizes(d)
+    assert wb // (16 * B * D) == (2 if S > 960 else 1)
+    saved, ws, ddec = lib.workspace(sb), lib.workspace(wb), torch.empty(D, device="cuda")
+    lens = [S, S - 70][:B]
+    L = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    ctx = lib.Context()
+    lib.paragan_scan_fwd(ctx, d, x, r, g, dec, L, None, y, None, saved, ws)
+    lib.paragan_scan_bwd(ctx, d, x, r, g, dec, L, saved, dy, None, dx, dr, dg, ddec, None, ws)
+    torch.cuda.synchronize()
+    want = T.scan(*(num(t) for t in small[:3]), num(dec), lens, sharp=8.0, reverse=reverse, dy=num(small[3]), uo=U32)
+    for name, t in (("y", y), ("dx", dx), ("dr", dr), ("dg", dg), ("ddecay", ddec)):
+        held(name, t.contiguous(), want[name], want["tol." + name] + 1e-30)
+    assert int(torch.count_nonzero(out[4 * 8200:ts])) == 0
