@@ -147,3 +147,23 @@ def test_clip_settings_are_checked():
     first, second = ctx.set_grad_clip(1.0, 0.0), ctx.set_grad_clip(2.0, math.inf)
     assert first.data_ptr() != second.data_ptr() and not second.any()
     assert ctx.set_grad_clip(0.0, 0.0) is None
+
+
+def test_norms_of_gradients_that_many_blocks_share():
+    """A network of more floats than one round of the norm's blocks takes: its norm is that of all of its gradient."""
+    torch = need_gpu()
+    a, B = ARCHS["biggan128"](), 2
+    d, s, _, _, G0, D0 = make_nets(torch, a, B, 839, hparams())
+    inp, keep = step_inputs(torch, s, a, B, 1)
+    ws = lib.workspace(lib.paragan_train_step_ws_size(d))
+    ctx = context()
+    said = ctx.set_grad_clip(math.inf, math.inf)
+    G, D = G0.clone(torch), D0.clone(torch)
+    run_train_step(torch, d, G, D, inp, 1, ws, ctx)
+    torch.cuda.synchronize()
+    v = said.cpu().tolist()
+    ctx.set_grad_clip(0.0, 0.0)
+    for N, norm, factor in ((G, v[0], v[1]), (D, v[2], v[3])):
+        assert N.G.numel() > 3 * 1024 * 4096
+        want = math.sqrt((N.G.double() ** 2).sum().item())
+        assert abs(norm - want) <= 2 * U32 * want and factor == 1.0, (norm, want)

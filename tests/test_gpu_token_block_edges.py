@@ -1,5 +1,7 @@
 """Calls at the edges of what the token block's operators accept, and the
 forms that large batches and large gradients take."""
+import math
+
 import numpy as np
 import pytest
 
@@ -302,3 +304,34 @@ def test_scan_far_tokens_of_many_channels(B, S, reverse):
     for name, t in (("y", y), ("dx", dx), ("dr", dr), ("dg", dg), ("ddecay", ddec)):
         held(name, t.contiguous(), want[name], want["tol." + name] + 1e-30)
     assert int(torch.count_nonzero(out[4 * 8200:ts])) == 0
+
+
+# ------------------------------------------------------------- clipping of more than the caches hold
+@pytest.mark.parametrize("in_place", [0, 1])
+def test_clip_of_more_than_the_caches_hold(in_place):
+    """More than 256 MB in both types at odd places, every element; fp32 out of place and in place."""
+    torch = need_gpu()
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    sizes = [(50_000_003, 0), (30_000_001, 1), (20_000_000, 0), (7, 1), (16_384 * 9 + 5, 0), (9_000_001, 1)]
+    grads, outs = [], []
+    for i, (n, bf) in enumerate(sizes):
+        dt = torch.bfloat16 if bf else torch.float32
+        grads.append(torch.randn(n + 8, device="cuda", generator=gen).to(dt)[i:i + n])
+        o = 2 * i + 1 if i in (1, 3) else i           # both alike, or not: by vectors, or one at a time
+        outs.append(torch.full((n + 16,), 7.0, dtype=dt, device="cuda")[o:o + n])
+    before = [g.clone() for g in grads]
+    wn = math.sqrt(sum((g.double() ** 2).sum().item() for g in grads))
+    most = float(np.float32(0.37 * wn))
+    plan = lib.ClipPlan(grads, None if in_place else outs)
+    assert plan.desc.bytes > 256e6
+    norm, ws = torch.zeros(2, device="cuda"), lib.workspace(plan.ws_bytes)
+    lib.paragan_clip(lib.Context(), plan, most, 1.0, norm, ws)
+    torch.cuda.synchronize()
+    # (the sum of the squares itself is taken in 64 bits, in another order)
+    assert abs(norm[0].item() - wn) <= 2 * U32 * wn and abs(norm[1].item() - most / wn) <= 2 * U32 * most / wn
+    for (n, bf), g, o, b in zip(sizes, grads, outs, before):
+        w = b.double() * (most / wn)
+        off = ((g if in_place else o).double() - w).abs()
+        assert bool((off <= ((U16 if bf else 0.0) + 3 * U32) * w.abs() + 2.0 ** -133).all()), (n, bf)
+        if not in_place:
+            assert torch.equal(g, b)
