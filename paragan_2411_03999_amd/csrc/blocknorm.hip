@@ -351,6 +351,7 @@ struct BnJoin {
 // lanes share the items of one.  What all sequences share is summed over the
 // lanes at the end.  A sequence of no tokens adds nothing, whatever its rows
 // hold: zero times what is not finite would be NaN.
+template <bool LEN>
 __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
   __shared__ double sh[5][64][17];
   const int j = threadIdx.x & 15, l = threadIdx.x >> 4, c = blockIdx.x * 16 + j, cc = min(c, a.D - 1);
@@ -359,22 +360,23 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
   const double rs = a.res_scale;
   double t[5] = {0.0, 0.0, 0.0, 0.0, 0.0};   // over the sequences: e, q, p, (1 + scale) q, gate p
   auto weight = [&](const float* w, int b, double none) { return w ? (double)w[b * a.mod + cc] : none; };
-  auto done = [&](int b, double e, double q, double p, double scale, double gate) {
+  // (without tokens, n <= 0, the sums are zeros)
+  auto done = [&](int b, int n, double e, double q, double p, double scale, double gate) {
     const int64_t o = b * a.mod + cc;
-    const bool some = !a.len || a.len[b] > 0;
-    if (some) {
-      t[0] += e; t[1] += q; t[2] += p;
-      t[3] += (1.0 + scale) * q;
-      t[4] += gate * p;
-    }
+    const bool some = !LEN || n > 0;
+    t[0] += e; t[1] += q; t[2] += p;
+    t[3] += some ? (1.0 + scale) * q : 0.0;
+    t[4] += some ? gate * p : 0.0;
     if (a.mod && c < a.D) {
-      if (a.g.shift) a.g.shift[o] = some ? (float)e : 0.f;
+      if (a.g.shift) a.g.shift[o] = (float)e;
       if (a.g.scale) a.g.scale[o] = some ? (float)(g2 * q) : 0.f;
       if (a.g.gate) a.g.gate[o] = some ? (float)(rs * g1 * p) : 0.f;
     }
   };
   double s[3] = {0.0, 0.0, 0.0}, scale = 0.0, gate = 0.0;
+  int n = 1;
   for (int b = grp; b < a.B; b += ng) {
+    if (LEN) n = a.len[b];
     scale = weight(a.w.scale, b, 0.0);
     gate = weight(a.w.gate, b, 1.0);
     const float* p = a.part + (int64_t)b * a.nc * 3 * a.D + cc;
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
 #pragma unroll
         for (int w = 0; w < 3; ++w) s[w] += i0 + u * a.gs < a.nc ? v[u][w] : 0.f;
     }
-    if (a.gs == 1) done(b, s[0], s[1], s[2], scale, gate);
+    if (a.gs == 1) done(b, n, s[0], s[1], s[2], scale, gate);
   }
   if (a.gs > 1) {                  // then a group of lanes has one sequence or none
 #pragma unroll
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(1024) void k_blocknorm_join(BnJoin a) {
         s[w] = 0.0;
         for (int i = 0; i < a.gs; ++i) s[w] += sh[w][l + i][j];
       }
-      done(grp, s[0], s[1], s[2], scale, gate);
+      done(grp, n, s[0], s[1], s[2], scale, gate);
     }
     __syncthreads();
   }
@@ -520,7 +522,7 @@ void blocknorm_bwd(hipStream_t st, const BlockNorm& a, const BlockNormRows& w, c
   if (gr.gain_pre || gr.gain_post || gr.gate || gr.scale || gr.shift) {
     int gs = 64;
     while (gs > 1 && 64 / gs < a.B) gs /= 2;
-    hipLaunchKernelGGL(k_blocknorm_join, dim3((unsigned)cdiv(a.D, 16)), dim3(1024), 0, st,
+    hipLaunchKernelGGL(len ? k_blocknorm_join<true> : k_blocknorm_join<false>, dim3((unsigned)cdiv(a.D, 16)), dim3(1024), 0, st,
                        BnJoin{w, gr, len, g.part, a.mod, a.B, a.D, g.nc, gs, a.res_scale});
     PG_LAUNCH_CHECK();
   }
