@@ -769,7 +769,7 @@ static Scan make_scan(const paragan_scan_desc* d) {
   token_strides(d->r_stride, a.rs, a.B, a.S, "scan: r");
   token_strides(d->g_stride, a.gs, a.B, a.S, "scan: g");
   token_strides(d->y_stride, a.ys, a.B, a.S, "scan: y");
-  for (int64_t t : {a.xs[1], a.rs[1], a.gs[1], a.ys[1]})   // a tile of 512 tokens is addressed in 32 bits
+  for (int64_t t : {a.xs[1], a.rs[1], a.gs[1], a.ys[1]})   // a tile of up to 128 tokens is addressed in 32 bits
     PG_CHECK(t < (1LL << 20), "scan: a token stride is 2^20 or more");
   PG_CHECK(rows_distinct(a.ys, a.B, a.S, a.D), "scan: y overlaps itself");
   return a;

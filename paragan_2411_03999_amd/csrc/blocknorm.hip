@@ -20,9 +20,9 @@
 // blocks fill a CU with rows side by side, so that few blocks have column sums
 // to be joined, and a row's loads are under way while the one before it is
 // summed.
-// Measured, bf16: forward of 8 x 4096 x 1152 with a normed branch 57 us (5.3
-// TB/s; a copy reaches 5.2), backward 92 us (4.9) and 8 us to join the column
-// sums; fp32 stream, 3 x 1365 x 1480 padded, 13.8 and 26 + 7 us.  Before the
+// Measured, bf16: forward of 8 x 4096 x 1152 with a normed branch 59 us (5.1
+// TB/s; a copy reaches 5.2), backward 92 us (4.9) and 9 us to join the column
+// sums; fp32 stream, 3 x 1365 x 1480 padded, 13 and 27 + 8 us.  Before the
 // loads ahead and the rows side by side that backward took 165 us.
 #include "rows.hpp"
 #include "token.hpp"
@@ -445,6 +445,11 @@ int bwd_threads(int D) {
 
 // Items: tokens of one sequence a block takes; enough of them to fill the
 // card (`want` blocks) and at most kMaxRows a thread, whole rounds of groups.
+// An item does not reach into another sequence, so a few more than `want` may
+// come out, which leave CUs idle in a second round (7 x 585 x 1536, 259 items
+// of the backward: 24.7 us where the bytes take 15), and many short sequences
+// are many small items with a row of column sums each (4096 x 1 x 768 backward
+// 80 and join 247 us, 16384 x 4 x 64 185 and 937).
 void split(const BlockNorm& a, int threads, int64_t want, int& R, int& nc) {
   const int ng = threads / row_threads(a.D);
   int64_t r = cdiv((int64_t)a.B * a.S, want);

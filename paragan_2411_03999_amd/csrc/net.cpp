@@ -531,9 +531,6 @@ size_t train_step_ws(const paragan_biggan_desc* d, int n_cu) {
 }
 
 namespace {
-// The pieces of a training iteration over one workspace: the generator
-// (batch B), the discriminator on the 2B batch of a D step and on the B
-// images of a G step (their saved buffers share one region).
 // One optimiser step on the gradient just computed, with clipping on by the
 // factor of its norm (the gradient itself stays as it is).
 void optimise(paragan_ctx* ctx, hipStream_t st, const paragan_optim& o, paragan_net_state* N, int64_t n, bool is_d) {
@@ -548,6 +545,9 @@ void optimise(paragan_ctx* ctx, hipStream_t st, const paragan_optim& o, paragan_
              norm ? norm + 1 : nullptr);
 }
 
+// The pieces of a training iteration over one workspace: the generator
+// (batch B), the discriminator on the 2B batch of a D step and on the B
+// images of a G step (their saved buffers share one region).
 struct StepRun {
   Arch a;
   int B;

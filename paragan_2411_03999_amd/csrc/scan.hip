@@ -16,11 +16,11 @@
 // state every 64 tokens is kept for the backward.  Few sequences of few
 // channels leave the card idle; then chunks of them go side by side and the
 // inputs are read twice.
-// Measured, bf16: forward of 8 x 4096 x 2048 121 us (4.4 TB/s; a copy reaches
-// 5.2), of 16 x 4096 x 1536 218 us (3.7: 384 blocks on 256 CUs), of 1 x 32768
-// x 1280 in chunks 126 us (4.6 over both passes), backward of 8 x 4096 x 2048
-// 205 us (4.6).  Slabs of 32 channels (64-byte rows) were slower, forward 156
-// and backward 402 us where these took 121 and 265.
+// Measured, bf16: forward of 8 x 4096 x 2048 that keeps states 131 us (4.1
+// TB/s; a copy reaches 5.2), of 16 x 4096 x 1536 219 us (3.7: 384 blocks on
+// 256 CUs), of 1 x 32768 x 1280 in chunks 53 and 73 us (4.8 and 4.6), backward
+// of 8 x 4096 x 2048 202 us (4.7).  Slabs of 32 channels (64-byte rows) were
+// slower when the backward of 64 took 265 us: 402, and the forward 156 for 121.
 #include "token.hpp"
 
 #include <cfloat>
@@ -748,8 +748,11 @@ struct Plan {
 // Few slabs leave the card idle: then chunks of the sequences go side by side,
 // at the price of a pass over the inputs ahead and its launch.  Split where
 // the modelled time says so, in us: a block walks its sequence at a rate of
-// its own, the split form moves bytes at the card's.  Measured against both
-// forms of 18 shapes in each type and direction the choice costs at most 5 %.
+// its own, the split form moves bytes at the card's.  Of 18 shapes of up to
+// 255 slabs (fp32: 128), each timed in both forms, types and directions, the
+// choice costs at most 5 %.  More slabs are not split, whatever that costs: a
+// block of eight waves of the backward has a CU to itself, so that 288 slabs
+// (9 x 4096 x 2048) take two rounds and 349 us where 256 take 202.
 // Whole and split, bf16: forward of 5 x 3000 x 1320 80 and 71, of 6 x 4096 x
 // 1536 106 and 117, of 2 x 600 x 5000 19 and 30, of 1 x 20000 x 2048 483 and
 // 123; with the backward 215 and 170, 286 and 272, 55 and 68, 1296 and 283.
