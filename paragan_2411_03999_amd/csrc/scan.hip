@@ -780,7 +780,7 @@ Plan plan_of(const Scan& a, bool bwd) {
   // two to three blocks of four waves a CU (one of eight); each folds the chunks ahead of it, so no more than 96
   int64_t nc = 1;
   if (split) nc = std::max<int64_t>(2, std::min<int64_t>((a.f32 ? 256 : bwd ? 512 : 768) / rows, std::min<int64_t>(96, cdiv(a.S, tt))));
-  // a chunk is addressed in 32 bits
+  // a chunk is addressed in 32 bits (y's stride covers a row, so this holds for inputs whose rows reach into the next ones too)
   const int64_t st = std::max(std::max(a.xs[1], a.rs[1]), std::max(a.gs[1], a.ys[1])) * (a.f32 ? 4 : 2);
   const int64_t most = std::max<int64_t>(1, kBufMax / std::max<int64_t>(st, 1) / tt) * tt;
   p.chunk = (int)std::min(cdiv(cdiv(a.S, nc), tt) * tt, most);
